@@ -61,7 +61,8 @@ typedef enum {
     NACHO_ERR_TOO_LARGE = -6    /* nacho_spmv_static: the call needs more than the built-in scratch */
 } nacho_status;
 
-typedef enum { NACHO_F32 = 0, NACHO_F64 = 1 } nacho_dtype;
+/* F32 and F64: sparse algebra.  F32, BF16 and F16: the operators that train models (nacho_distill and below). */
+typedef enum { NACHO_F32 = 0, NACHO_F64 = 1, NACHO_BF16 = 2, NACHO_F16 = 3 } nacho_dtype;
 typedef enum { NACHO_DENSE = 0, NACHO_COMPRESSED = 1, NACHO_NONUNIQUE = 2, NACHO_SINGLETON = 3 } nacho_level_kind;
 typedef enum {
     NACHO_OP_PARTITION = 0, NACHO_OP_SPMV = 1, NACHO_OP_SPMM = 2, NACHO_OP_SPADD = 3, NACHO_OP_SPMUL = 4
@@ -394,6 +395,45 @@ int32_t nacho_spadd_k(const nacho_tensor *ops, int32_t k, int32_t dtype, int64_t
  */
 int32_t nacho_spmul_k(const nacho_tensor *ops, int32_t k, int32_t dtype, int64_t P,
                       const nacho_sparse_out *out, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Operators that train models, around the sparse matrices which training makes:
+ * a teacher's top logits, the routing of tokens to experts.  Dense arrays are
+ * row-major with a leading dimension in elements, of F32, BF16 or F16, aligned to
+ * their elements (16 bytes and leading dimensions that are multiples of 16 bytes
+ * are fastest); sums, softmax statistics and losses are held in 32 bits, results of
+ * 16 bits are rounded once.  Matrices may have up to 2^31 - 1 rows and more than
+ * 2^31 elements.  Outputs must not overlap inputs.
+ *
+ * nacho_distill: the distillation loss of every row against a teacher's top logits.
+ *   teacher     CSR [n_rows x vocabulary], values F32: the logits stored for a row,
+ *               columns as in every CSR operand; a row may store none
+ *   logits      the student's, [n_rows x vocabulary], leading dimension ldl
+ *   weight      device float[n_rows], a factor of every row, or NULL for ones
+ *   temperature tau, 1e-30 .. 1e30
+ * With p the softmax of a row's stored teacher logits / tau (the others have no
+ * share) and q the softmax of all its student logits / tau,
+ *   loss[i] = weight[i] tau^2 sum_j p_j (log p_j - log q_j)
+ *   lse[i]  = log sum_v exp(z_v / tau)
+ *   grad    = weight[i] tau (q - p), the gradient of the sum of all losses, leading
+ *             dimension ldg; NULL: not wanted
+ * Rows of weight 0 and rows without a teacher's logit above -inf have loss, lse and
+ * gradient 0, and their logits are not read.  Student logits of -inf have q = 0
+ * (a loss of +inf where the teacher gives them a share).  A row with nothing but
+ * -inf, or with a NaN, has no distribution: NaN.
+ * Workspace: nacho_distill_workspace_bytes (may be 0: then ws may be NULL).
+ *
+ * nacho_distill_grad: grad alone, from the logits and the lse of an earlier
+ * nacho_distill on the same operands and temperature; weight then is the factor of
+ * the loss times the gradient that arrives at it.
+ */
+int32_t nacho_distill_workspace_bytes(int64_t n_rows, int64_t n_cols, int32_t dtype, size_t *bytes);
+int32_t nacho_distill(const nacho_tensor *teacher, const void *logits, int64_t ldl, int32_t dtype,
+                      const float *weight, float temperature, float *loss, float *lse, void *grad, int64_t ldg,
+                      void *ws, size_t ws_bytes, void *hip_stream);
+int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int64_t ldl, int32_t dtype,
+                           const float *weight, float temperature, const float *lse, void *grad, int64_t ldg,
+                           void *hip_stream);
 
 /*
  * Debug aid, not part of the hot path: checks on the device the preconditions

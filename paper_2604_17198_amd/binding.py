@@ -17,7 +17,7 @@ import torch
 
 from . import build as _build
 
-F32, F64 = 0, 1
+F32, F64, BF16, F16 = 0, 1, 2, 3
 DENSE, COMPRESSED, NONUNIQUE, SINGLETON = 0, 1, 2, 3
 OP_PARTITION, OP_SPMV, OP_SPMM, OP_SPADD, OP_SPMUL = 0, 1, 2, 3, 4
 MAX_OPERANDS, MAX_LEVELS = 8, 3
@@ -29,6 +29,7 @@ EXPORTS = [
     "nacho_static_scratch_bytes", "nacho_instrument", "nacho_instrument_record_bytes", "nacho_instrument_wait",
     "nacho_probe", "nacho_merge_wavefronts", "nacho_rowcost_partitions", "nacho_partition_rowcost",
     "nacho_spmv_rowcost", "nacho_partition_csr64", "nacho_spmv_fused", "nacho_spadd_fused",
+    "nacho_distill_workspace_bytes", "nacho_distill", "nacho_distill_grad",
 ]
 
 
@@ -116,6 +117,11 @@ def lib():
         L.nacho_spmv_rowcost.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64,
                                          C.c_void_p, C.c_size_t, C.c_void_p]
         L.nacho_probe.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int64, C.c_void_p]
+        L.nacho_distill_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]
+        L.nacho_distill.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_float, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.nacho_distill_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_float, C.c_void_p,
+                                         C.c_void_p, C.c_int64, C.c_void_p]
         _libs[_instrumented] = L
         _lib = L
     return _lib
@@ -459,6 +465,86 @@ def nacho_spmul_k(ops, out: SparseOut, P=0, ws=None):
     _check(lib().nacho_spmul_k(arr, len(ops), dt, P, C.byref(out.c), _ptr(ws),
                                ws.numel(), _stream()), "nacho_spmul_k")
     return out
+
+
+# --------------------------------------------------------------------------- #
+# operators that train models
+# --------------------------------------------------------------------------- #
+_MODEL_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def model_dtype_code(dt) -> int:
+    code = _MODEL_TYPES.get(dt)
+    if code is None:
+        raise TypeError(f"unsupported value type {dt}")
+    return code
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _matrix(t, what, shape=None, dtype=None, device=None):
+    """A matrix whose rows are contiguous; returns its leading dimension."""
+    _need(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{what}: a matrix with contiguous rows is needed")
+    _need(shape is None or tuple(t.shape) == tuple(shape), f"{what}: shape {tuple(t.shape)}, expected {shape}")
+    _need(dtype is None or t.dtype is dtype, f"{what}: type {t.dtype}, expected {dtype}")
+    _need(device is None or t.device == device, f"{what}: on {t.device}, expected {device}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _vector_of(t, what, n, dtype, device):
+    """A contiguous array of n elements, or None."""
+    _need(t is None or (t.numel() == n and t.is_contiguous()), f"{what}: {n} contiguous elements are needed")
+    _need(t is None or t.dtype is dtype, f"{what}: expected {dtype}")
+    _need(t is None or t.device == device, f"{what}: expected on {device}")
+    return t
+
+
+def _check_teacher(teacher, logits, weight):
+    if teacher.nlevels != 2 or teacher.c.lvl[0].kind != DENSE or teacher.c.lvl[1].kind != COMPRESSED:
+        raise NachoError(-2, "teacher: a CSR operand is needed")
+    _need(teacher.val is not None and teacher.val.dtype is torch.float32, "teacher: values of float32 are needed")
+    _need(teacher.val.numel() == teacher.nnz and teacher.val.is_contiguous(), "teacher: a value for every stored column is needed")
+    rows, cols = teacher.c.lvl[0].extent, teacher.c.lvl[1].extent
+    _need(teacher.keep[0].numel() == rows + 1, "teacher: rows + 1 positions are needed")
+    _need(teacher.val.device == logits.device, "teacher: expected on the logits' device")
+    ld = _matrix(logits, "logits", (rows, cols))
+    _vector_of(weight, "weight", rows, torch.float32, logits.device)
+    return rows, cols, ld
+
+
+def nacho_distill(teacher: Operand, logits, temperature=1.0, weight=None, grad=None, loss=None, lse=None, ws=None):
+    """Distillation loss of every row of `logits` against the teacher's stored logits (a CSR operand of
+    float32 values).  Returns (loss[rows], lse[rows]); `grad`, when given, receives the logits' gradient."""
+    dt = model_dtype_code(logits.dtype)
+    rows, cols, ld = _check_teacher(teacher, logits, weight)
+    dev = logits.device
+    ldg = _matrix(grad, "grad", (rows, cols), logits.dtype, dev) if grad is not None else 0
+    loss = _vector_of(loss, "loss", rows, torch.float32, dev) if loss is not None else torch.empty(rows, device=dev)
+    lse = _vector_of(lse, "lse", rows, torch.float32, dev) if lse is not None else torch.empty(rows, device=dev)
+    if ws is None:
+        n = C.c_size_t(0)
+        _check(lib().nacho_distill_workspace_bytes(rows, cols, dt, C.byref(n)), "nacho_distill_workspace_bytes")
+        ws = _workspace(n.value, dev) if n.value else None
+    _check(lib().nacho_distill(_pack([teacher]), _ptr(logits), ld, dt, _ptr(weight), temperature, _ptr(loss), _ptr(lse),
+                               _ptr(grad), ldg, _ptr(ws), ws.numel() if ws is not None else 0, _stream()), "nacho_distill")
+    return loss, lse
+
+
+def nacho_distill_grad(teacher: Operand, logits, lse, temperature=1.0, weight=None, grad=None):
+    """Gradient of the logits from the lse of an earlier nacho_distill; `weight` is the factor of each row's loss times
+    the gradient that arrives at it."""
+    dt = model_dtype_code(logits.dtype)
+    rows, cols, ld = _check_teacher(teacher, logits, weight)
+    _vector_of(lse, "lse", rows, torch.float32, logits.device)
+    if grad is None:
+        grad = torch.empty((rows, cols), dtype=logits.dtype, device=logits.device)
+    ldg = _matrix(grad, "grad", (rows, cols), logits.dtype, logits.device)
+    _check(lib().nacho_distill_grad(_pack([teacher]), _ptr(logits), ld, dt, _ptr(weight), temperature, _ptr(lse), _ptr(grad),
+                                    ldg, _stream()), "nacho_distill_grad")
+    return grad
 
 
 def nacho_validate(ops):

@@ -1,0 +1,98 @@
+// C-ABI entry points of the operators that train models: argument checks, workspace carving, kernel sequencing.
+#include "kernels.hpp"
+#include "model.hpp"
+
+using namespace nacho;
+using namespace nacho_host;
+
+namespace {
+
+bool value_type(int32_t dtype) { return dtype == NACHO_F32 || dtype == NACHO_BF16 || dtype == NACHO_F16; }
+int64_t value_bytes(int32_t dtype) { return dtype == NACHO_F32 ? 4 : 2; }
+bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+constexpr int64_t kMostRows = 0x7fffffffLL, kMostStride = (int64_t)1 << 40;
+
+// A dense matrix of `rows` rows of `cols` elements, `ld` apart.
+bool matrix(const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t elem)
+{
+    if (ld < cols || ld > kMostStride) return false;
+    return rows == 0 || cols == 0 || (p && aligned(p, (uintptr_t)elem));
+}
+
+// Whether two such matrices share a byte of the stretches they span.
+bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a_bytes > 0 && b_bytes > 0 && x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+int64_t span(int64_t rows, int64_t cols, int64_t ld, int64_t elem) { return rows > 0 ? ((rows - 1) * ld + cols) * elem : 0; }
+
+// The teacher: one CSR operand of floats.
+int32_t check_distill(const nacho_tensor *teacher, const void *logits, int64_t ldl, int32_t dtype, const float *weight,
+                      float temperature, void *grad, int64_t ldg, DistillArgs *a)
+{
+    if (!teacher || !value_type(dtype)) return NACHO_ERR_INVALID_ARG;
+    if (teacher->nlevels != 2 || teacher->lvl[0].kind != NACHO_DENSE || teacher->lvl[1].kind != NACHO_COMPRESSED)
+        return NACHO_ERR_UNSUPPORTED;
+    const int64_t rows = teacher->lvl[0].extent, cols = teacher->lvl[1].extent, stored = teacher->lvl[1].count;
+    if (rows < 0 || rows > kMostRows || cols < 0 || cols > kMostRows || stored < 0 || stored > kMostRows)
+        return NACHO_ERR_INVALID_ARG;
+    if (!teacher->lvl[1].pos || (stored > 0 && (!teacher->lvl[1].crd || !teacher->val))) return NACHO_ERR_INVALID_ARG;
+    if (!aligned(teacher->lvl[1].crd, 16) || !aligned(teacher->val, 16)) return NACHO_ERR_INVALID_ARG;
+    const int64_t elem = value_bytes(dtype);
+    if (!matrix(logits, rows, cols, ldl, elem) || !(temperature >= 1e-30f && temperature <= 1e30f)) return NACHO_ERR_INVALID_ARG;
+    if (grad && (!matrix(grad, rows, cols, ldg, elem) ||
+                 overlap(logits, span(rows, cols, ldl, elem), grad, span(rows, cols, ldg, elem))))
+        return NACHO_ERR_INVALID_ARG;
+    *a = DistillArgs{teacher->lvl[1].pos, teacher->lvl[1].crd, static_cast<const float *>(teacher->val), logits, ldl, weight,
+                     temperature, nullptr, nullptr, nullptr, grad, ldg, rows, (int32_t)cols};
+    return NACHO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t nacho_distill(const nacho_tensor *teacher, const void *logits, int64_t ldl, int32_t dtype, const float *weight,
+                      float temperature, float *loss, float *lse, void *grad, int64_t ldg, void *ws, size_t ws_bytes,
+                      void *hip_stream)
+{
+    DistillArgs a;
+    const int32_t rc = check_distill(teacher, logits, ldl, dtype, weight, temperature, grad, ldg, &a);
+    if (rc != NACHO_OK) return rc;
+    if (a.rows > 0 && (!loss || !lse)) return NACHO_ERR_INVALID_ARG;
+    (void)ws;
+    (void)ws_bytes;
+    a.loss = loss;
+    a.lse = lse;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (launch_distill(dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+    profile_mark("distill");
+    return NACHO_OK;
+}
+
+int32_t nacho_distill_workspace_bytes(int64_t n_rows, int64_t n_cols, int32_t dtype, size_t *bytes)
+{
+    if (!bytes || !value_type(dtype) || n_rows < 0 || n_rows > kMostRows || n_cols < 0 || n_cols > kMostRows)
+        return NACHO_ERR_INVALID_ARG;
+    *bytes = 0;
+    return NACHO_OK;
+}
+
+int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int64_t ldl, int32_t dtype, const float *weight,
+                           float temperature, const float *lse, void *grad, int64_t ldg, void *hip_stream)
+{
+    DistillArgs a;
+    const int32_t rc = check_distill(teacher, logits, ldl, dtype, weight, temperature, grad, ldg, &a);
+    if (rc != NACHO_OK) return rc;
+    if (a.rows > 0 && a.cols > 0 && (!lse || !grad)) return NACHO_ERR_INVALID_ARG;
+    a.lse_in = lse;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (launch_distill_grad(dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+    profile_mark("distill_grad");
+    return NACHO_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,247 @@
+"""nacho_distill, nacho_distill_grad against the definition in 64 bits.
+
+Tolerances.  A loss is a sum of n products of 32-bit numbers of relative error a few 2^-24 (exponentials of arguments
+up to 2^7 add 2^-24 * 2^7), divided and added to logarithms of sums: within 2e-5 of the sum of the magnitudes of its
+terms, for the lengths here.  A gradient differs from the exact one by that relative error on q and p, and by one
+rounding to its type (2^-8 of a bf16, 2^-11 of an f16, and half the smallest f16 step, 2^-25)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_17198_amd import binding as nb
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+STEP = {torch.float32: 2.0 ** -23, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+def teacher_rows(rng, rows, cols, least, most):
+    held = np.minimum(rng.integers(least, most + 1, rows), cols)
+    pos = np.concatenate([[0], np.cumsum(held)]).astype(np.int32)
+    crd = np.concatenate([np.sort(rng.choice(cols, n, replace=False)) for n in held] + [np.zeros(0, int)]).astype(np.int32)
+    return pos, crd, rng.normal(0, 3, pos[-1]).astype(np.float32)
+
+
+def operand(pos, crd, val, rows, cols):
+    dev = lambda a: torch.from_numpy(a).to("cuda")
+    return nb.csr(dev(pos), dev(crd), rows, cols, dev(val))
+
+
+def definition(pos, crd, val, z, weight, tau):
+    """loss, lse, gradient and the magnitude of a loss's terms, in 64 bits."""
+    rows = z.shape[0]
+    loss, lse, size, grad = np.zeros(rows), np.zeros(rows), np.zeros(rows), np.zeros(z.shape)
+    for i in range(rows):
+        j, u = crd[pos[i]:pos[i + 1]], val[pos[i]:pos[i + 1]].astype(np.float64) / tau
+        if weight[i] == 0 or not (u > -np.inf).any():
+            continue
+        t = z[i].astype(np.float64) / tau
+        lse[i] = t.max() + np.log(np.exp(t - t.max()).sum())
+        lp = u - u.max() - np.log(np.exp(u - u.max()).sum())
+        p, has = np.exp(lp), u > -np.inf
+        lq = t[j] - lse[i]
+        loss[i] = weight[i] * tau * tau * (p[has] * (lp[has] - lq[has])).sum()
+        size[i] = weight[i] * tau * tau * (1 + np.abs(lse[i]) + (p[has] * (np.abs(lp[has]) + np.abs(t[j][has]))).sum())
+        grad[i] = np.exp(t - lse[i])
+        grad[i][j] -= p
+        grad[i] *= weight[i] * tau
+    return loss, lse, grad, size
+
+
+def check(got_loss, got_lse, got_grad, want, weight, tau, dtype):
+    loss, lse, grad, size = want
+    assert np.all(np.abs(got_loss.cpu().numpy() - loss) <= 2e-5 * size)
+    assert np.all(np.abs(got_lse.cpu().numpy() - lse) <= 1e-5 * np.maximum(1, np.abs(lse)))
+    if got_grad is not None:
+        g = got_grad.float().cpu().numpy().astype(np.float64)
+        scale = np.abs(weight)[:, None] * tau
+        assert np.all(np.abs(g - grad) <= STEP[dtype] * np.abs(grad) + 4e-5 * np.abs(grad) + 2.0 ** -25 * (dtype is torch.float16) + 3e-6 * scale)
+
+
+def case(rng, rows, cols, least, most, dtype, masked=0.0, scale=3.0, ld=None):
+    pos, crd, val = teacher_rows(rng, rows, cols, least, most)
+    z = torch.from_numpy(rng.normal(0, scale, (rows, ld or cols)).astype(np.float32)).to(dtype).cuda()[:, :cols]
+    weight = rng.uniform(0.5, 1.5, rows).astype(np.float32)
+    weight[rng.random(rows) < masked] = 0
+    return pos, crd, val, z, weight
+
+
+SHAPES = [(1, 1), (1, 2), (3, 7), (5, 15), (2, 16), (4, 17), (7, 63), (3, 257), (9, 1000), (2, 2048), (3, 4099), (2, 8192),
+          (5, 16384), (2, 16391), (3, 32768), (2, 33001), (2, 65536), (1, 65537), (2, 131072), (1, 131080), (1, 200003), (300, 509)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_loss_and_gradient(rows, cols, dtype):
+    rng = np.random.default_rng(rows * 1000003 + cols)
+    tau = float(rng.choice([0.7, 1.0, 2.0]))
+    pos, crd, val, z, weight = case(rng, rows, cols, 0, min(cols, 70), dtype, 0.1)
+    want = definition(pos, crd, val, z.float().cpu().numpy(), weight, tau)
+    T, w = operand(pos, crd, val, rows, cols), torch.from_numpy(weight).cuda()
+    grad = torch.full_like(z, float("nan"))
+    loss, lse = nb.nacho_distill(T, z, temperature=tau, weight=w, grad=grad)
+    check(loss, lse, grad, want, weight, tau, dtype)
+    loss, lse = nb.nacho_distill(T, z, temperature=tau, weight=w)
+    check(loss, lse, None, want, weight, tau, dtype)
+    again = nb.nacho_distill_grad(T, z, lse, temperature=tau, weight=w)
+    check(loss, lse, again, want, weight, tau, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("ld,ldg,shift", [(1000, 1000, 0), (1008, 1000, 1), (1003, 1007, 3), (1003, 1003, 5), (1001, 1024, 0)])
+def test_leading_dimensions_and_alignment(ld, ldg, shift, dtype):
+    rng = np.random.default_rng(ld + ldg + shift)
+    rows, cols = 7, 997
+    pos, crd, val = teacher_rows(rng, rows, cols, 1, 40)
+    store = torch.from_numpy(rng.normal(0, 2, rows * ld + shift).astype(np.float32)).to(dtype).cuda()
+    z = store[shift:].view(rows, ld)[:, :cols]
+    weight = np.ones(rows, np.float32)
+    out = torch.full((rows, ldg), 7.0, dtype=dtype, device="cuda")
+    loss, lse = nb.nacho_distill(operand(pos, crd, val, rows, cols), z, temperature=1.3, grad=out[:, :cols])
+    check(loss, lse, out[:, :cols], definition(pos, crd, val, z.float().cpu().numpy(), weight, 1.3), weight, 1.3, dtype)
+    assert bool((out[:, cols:] == 7.0).all()), "written outside the rows"
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 501), (2, 70001)])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_rows_that_are_masked_hold_anything(rows, cols, dtype):
+    rng = np.random.default_rng(5)
+    pos, crd, val, z, weight = case(rng, rows + 3, cols, 4, 9, dtype)
+    weight[1] = 0                                            # a masked row full of NaN
+    z[1] = float("nan")
+    pos[3:] -= pos[3] - pos[2]                               # row 2 stores nothing
+    crd, val = crd[:pos[-1]], val[:pos[-1]]
+    crd = np.concatenate([np.sort(rng.choice(cols, n, replace=False)) for n in np.diff(pos)]).astype(np.int32)
+    z[2] = float("inf")
+    val[pos[0]:pos[1]] = -np.inf                             # row 0: no logit above -inf
+    T, w = operand(pos, crd, val, rows + 3, cols), torch.from_numpy(weight).cuda()
+    grad = torch.full_like(z, float("nan"))
+    loss, lse = nb.nacho_distill(T, z, weight=w, grad=grad)
+    for t in (loss[:3], lse[:3], grad[:3], nb.nacho_distill_grad(T, z, lse, weight=w)[:3]):
+        assert bool((t == 0).all())
+    want = definition(pos, crd, val, z.float().cpu().numpy(), weight, 1.0)
+    check(loss[3:], lse[3:], grad[3:], [a[3:] for a in want], weight[3:], 1.0, dtype)
+
+
+@pytest.mark.parametrize("cols", [40, 3001, 140_001])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_masked_logits(cols, dtype):
+    """-inf and the type's lowest value among the student's logits, -inf among the teacher's, away from the other's share."""
+    rng = np.random.default_rng(cols)
+    rows = 4
+    pos, crd, val, z, weight = case(rng, rows, cols, 6, 20, dtype)
+    out = rng.random((rows, cols)) < 0.5
+    for i in range(rows):
+        out[i, crd[pos[i]:pos[i + 1]]] = False
+    mask = torch.from_numpy(out).cuda()
+    low = float("-inf")
+    z[:2] = torch.where(mask[:2], torch.full_like(z[:2], low), z[:2])
+    z[2:] = torch.where(mask[2:], torch.full_like(z[2:], torch.finfo(dtype).min), z[2:])
+    val[pos[:-1]] = -np.inf
+    T, w = operand(pos, crd, val, rows, cols), torch.from_numpy(weight).cuda()
+    grad = torch.empty_like(z)
+    loss, lse = nb.nacho_distill(T, z, weight=w, grad=grad)
+    check(loss, lse, grad, definition(pos, crd, val, z.float().cpu().numpy(), weight, 1.0), weight, 1.0, dtype)
+    assert bool((grad[mask] == 0).all())
+    z[0, int(crd[1])] = low                                  # a share of the teacher's where the student has none
+    loss, _ = nb.nacho_distill(T, z, weight=w, grad=grad)
+    assert math.isinf(loss[0].item()) and loss[0].item() > 0 and bool(torch.isfinite(grad[0].float()).all())
+    z[1, 3] = float("nan")
+    z[3] = low
+    loss, _ = nb.nacho_distill(T, z, weight=w, grad=grad)
+    assert torch.isnan(loss).tolist() == [False, True, False, True]
+    assert bool(torch.isnan(grad[1]).all()) and bool(torch.isnan(grad[3]).all())
+
+
+@pytest.mark.parametrize("rows,cols,held", [(3, 20011, 20011), (1, 65536, 30000), (40, 600, 600)])
+def test_rows_the_teacher_stores_much_of(rows, cols, held):
+    rng = np.random.default_rng(held)
+    pos, crd, val, z, weight = case(rng, rows, cols, held, held, torch.float32)
+    T = operand(pos, crd, val, rows, cols)
+    grad = torch.empty_like(z)
+    loss, lse = nb.nacho_distill(T, z, temperature=2.0, weight=torch.from_numpy(weight).cuda(), grad=grad)
+    check(loss, lse, grad, definition(pos, crd, val, z.cpu().numpy(), weight, 2.0), weight, 2.0, torch.float32)
+
+
+def test_no_rows():
+    T = operand(np.zeros(1, np.int32), np.zeros(0, np.int32), np.zeros(0, np.float32), 0, 100)
+    loss, lse = nb.nacho_distill(T, torch.empty((0, 100), device="cuda"))
+    assert loss.numel() == 0 and lse.numel() == 0
+
+
+def test_gradient_against_differences():
+    """Central differences of the loss in 64 bits at step h: error h^2 / 6 times a third derivative below 1."""
+    rng = np.random.default_rng(3)
+    pos, crd, val, z, weight = case(rng, 2, 37, 5, 9, torch.float32, scale=1.0)
+    z64 = z.cpu().numpy().astype(np.float64)
+    grad = torch.empty_like(z)
+    nb.nacho_distill(operand(pos, crd, val, 2, 37), z, temperature=1.5, weight=torch.from_numpy(weight).cuda(), grad=grad)
+    h, g = 1e-3, grad.cpu().numpy()
+    for i in range(2):
+        for j in range(37):
+            up, down = z64.copy(), z64.copy()
+            up[i, j] += h
+            down[i, j] -= h
+            d = (definition(pos, crd, val, up, weight, 1.5)[0].sum() - definition(pos, crd, val, down, weight, 1.5)[0].sum()) / (2 * h)
+            assert abs(d - g[i, j]) <= 2e-5
+
+
+def test_another_stream_and_the_same_bits_again():
+    rng = np.random.default_rng(11)
+    pos, crd, val, z, weight = case(rng, 6, 50_000, 10, 60, torch.bfloat16)
+    T, w = operand(pos, crd, val, 6, 50_000), torch.from_numpy(weight).cuda()
+    first = torch.empty_like(z)
+    loss, lse = nb.nacho_distill(T, z, weight=w, grad=first)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        grad = torch.empty_like(z)
+        loss2, lse2 = nb.nacho_distill(T, z, weight=w, grad=grad)
+    side.synchronize()
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2) and torch.equal(first, grad)
+
+
+def test_more_than_two_to_the_31_elements():
+    """Rows whose offset in the matrix passes 32 bits."""
+    rng = np.random.default_rng(2)
+    rows, cols = 33_000, 66_000                              # 2.18e9 elements, 4.4 GB
+    z = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    last = torch.from_numpy(rng.normal(0, 2, cols).astype(np.float32)).to(torch.bfloat16).cuda()
+    z[-1] = last
+    weight = np.zeros(rows, np.float32)
+    weight[-1] = 1
+    crd = np.sort(rng.choice(cols, 50, replace=False)).astype(np.int32)
+    pos = np.zeros(rows + 1, np.int32)
+    pos[-1] = 50
+    val = rng.normal(0, 2, 50).astype(np.float32)
+    grad = torch.empty_like(z)
+    loss, lse = nb.nacho_distill(operand(pos, crd, val, rows, cols), z, weight=torch.from_numpy(weight).cuda(), grad=grad)
+    want = definition(np.array([0, 50]), crd, val, last.float().cpu().numpy()[None], weight[-1:], 1.0)
+    check(loss[-1:], lse[-1:], grad[-1:], want, weight[-1:], 1.0, torch.bfloat16)
+    assert bool((loss[:-1] == 0).all()) and not bool(grad[:100].any())
+
+
+def test_refusals():
+    rng = np.random.default_rng(1)
+    pos, crd, val, z, weight = case(rng, 4, 64, 2, 5, torch.float32)
+    T = operand(pos, crd, val, 4, 64)
+    with pytest.raises(TypeError):
+        nb.nacho_distill(T, z.double())
+    with pytest.raises(ValueError):
+        nb.nacho_distill(T, z[:, :63])
+    with pytest.raises(ValueError):
+        nb.nacho_distill(T, z, weight=torch.ones(3, device="cuda"))
+    with pytest.raises(ValueError):
+        nb.nacho_distill(T, z, grad=torch.empty((4, 64), dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(ValueError):
+        nb.nacho_distill(T, z.t().contiguous().t())
+    for tau in (0.0, -1.0, float("nan"), float("inf")):
+        with pytest.raises(nb.NachoError):
+            nb.nacho_distill(T, z, temperature=tau)
+    with pytest.raises(nb.NachoError):
+        nb.nacho_distill(T, z, grad=z)
+    with pytest.raises(nb.NachoError):
+        nb.nacho_distill(nb.vector(T.keep[1], 64, T.val), z)
