@@ -436,6 +436,49 @@ int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int6
                            void *hip_stream);
 
 /*
+ * nacho_route: the routing matrix of a mixture of experts.  Every token goes to the
+ * top_k experts with the largest logits (ties: the lowest index; a logit of -inf or
+ * NaN is never chosen, so a token may store fewer), and the matrix comes in the two
+ * compressed forms its users read, all arrays on the device:
+ *   by tokens   CSR [n_tokens x n_experts]: pos[n_tokens+1], expert (columns,
+ *               ascending), gate (values)
+ *   by experts  its transpose's pattern: expert_pos[n_experts+1], token (ascending
+ *               for every expert); slot[i] is the place there of entry i
+ * expert, gate, slot and token have room for n_tokens * top_k entries; places behind
+ * the last entry get expert, slot and token -1 and gate 0.
+ *   gate     the softmax of all the token's logits at the chosen experts; `normalise`
+ *            divides them by their sum
+ *   counts   [n_experts] entries of every expert
+ *   lse      [n_tokens] log of the sum of exponentials of the token's logits
+ *   balance  [1] n_experts * sum_e f_e P_e, f_e the expert's share of all entries, P_e
+ *            the mean of its softmax over the tokens that store an entry
+ *   routed   [1] the number of these tokens
+ * Tokens whose byte in `keep` (device, may be NULL) is 0 store nothing and have lse 0;
+ * their logits are not read.  So has a token whose logits are all -inf.  A NaN among
+ * a token's logits makes its gates, its lse and the balance loss NaN.
+ * Limits: n_experts <= 1024, top_k <= min(32, n_experts), n_tokens * top_k < 2^31.
+ * Workspace: nacho_route_workspace_bytes.
+ *
+ * nacho_route_grad: the logits' gradient from that of the gates (grad_gate, by the
+ * entries' order; NULL: none) plus `balance` times that of the balance loss (in which
+ * the counts are constants), from the arrays that nacho_route left.
+ */
+typedef struct {
+    int32_t *pos, *expert;
+    float *gate;
+    int32_t *slot, *expert_pos, *token, *counts;
+    float *lse, *balance;
+    int32_t *routed;
+} nacho_routing;
+int32_t nacho_route_workspace_bytes(int64_t n_tokens, int64_t n_experts, int32_t top_k, size_t *bytes);
+int32_t nacho_route(const void *logits, int64_t ldl, int64_t n_tokens, int64_t n_experts, int32_t dtype,
+                    int32_t top_k, int32_t normalise, const uint8_t *keep, const nacho_routing *out,
+                    void *ws, size_t ws_bytes, void *hip_stream);
+int32_t nacho_route_grad(const void *logits, int64_t ldl, int64_t n_tokens, int64_t n_experts, int32_t dtype,
+                         int32_t top_k, int32_t normalise, const nacho_routing *routing, const float *grad_gate,
+                         float balance, void *grad, int64_t ldg, void *hip_stream);
+
+/*
  * Debug aid, not part of the hot path: checks on the device the preconditions
  * that the other entry points rely on without looking -- pos arrays start at 0,
  * never decrease and end at the level's count; coordinates lie inside the

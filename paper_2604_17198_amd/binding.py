@@ -30,6 +30,7 @@ EXPORTS = [
     "nacho_probe", "nacho_merge_wavefronts", "nacho_rowcost_partitions", "nacho_partition_rowcost",
     "nacho_spmv_rowcost", "nacho_partition_csr64", "nacho_spmv_fused", "nacho_spadd_fused",
     "nacho_distill_workspace_bytes", "nacho_distill", "nacho_distill_grad",
+    "nacho_route_workspace_bytes", "nacho_route", "nacho_route_grad",
 ]
 
 
@@ -58,6 +59,11 @@ class _SparseOut(C.Structure):
                 ("crd1", C.c_void_p), ("val", C.c_void_p), ("cap_rows", C.c_int64),
                 ("cap_nnz", C.c_int64), ("counts", C.c_void_p), ("status", C.c_void_p),
                 ("pos2", C.c_void_p), ("crd2", C.c_void_p), ("cap_fibres", C.c_int64)]
+
+
+class _Routing(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pos", "expert", "gate", "slot", "expert_pos", "token", "counts", "lse",
+                                          "balance", "routed")]
 
 
 _lib = None
@@ -122,6 +128,11 @@ def lib():
                                     C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
         L.nacho_distill_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_float, C.c_void_p,
                                          C.c_void_p, C.c_int64, C.c_void_p]
+        L.nacho_route_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]
+        L.nacho_route.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.nacho_route_grad.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+                                       C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]
         _libs[_instrumented] = L
         _lib = L
     return _lib
@@ -544,6 +555,65 @@ def nacho_distill_grad(teacher: Operand, logits, lse, temperature=1.0, weight=No
     ldg = _matrix(grad, "grad", (rows, cols), logits.dtype, logits.device)
     _check(lib().nacho_distill_grad(_pack([teacher]), _ptr(logits), ld, dt, _ptr(weight), temperature, _ptr(lse), _ptr(grad),
                                     ldg, _stream()), "nacho_distill_grad")
+    return grad
+
+
+class Routing:
+    """The arrays nacho_route fills: the routing matrix by tokens (pos, expert, gate), by experts (expert_pos, token; slot:
+    the place there of every entry), counts, lse, the balance loss and the number of tokens that store an entry."""
+
+    def __init__(self, n_tokens, n_experts, top_k, device, normalise=False):
+        self.n_tokens, self.n_experts, self.top_k, self.normalise = n_tokens, n_experts, top_k, normalise
+        room = n_tokens * top_k
+        i32 = dict(dtype=torch.int32, device=device)
+        self.pos, self.expert_pos = torch.empty(n_tokens + 1, **i32), torch.empty(n_experts + 1, **i32)
+        self.expert, self.slot, self.token = torch.empty(room, **i32), torch.empty(room, **i32), torch.empty(room, **i32)
+        self.gate, self.lse = torch.empty(room, device=device), torch.empty(n_tokens, device=device)
+        self.counts, self.routed = torch.empty(n_experts, **i32), torch.empty(1, **i32)
+        self.balance = torch.empty(1, device=device)
+        # (arrays without an element have no address, and are not written)
+        self.c = _Routing(*[t.data_ptr() or self.balance.data_ptr() for t in
+                            (self.pos, self.expert, self.gate, self.slot, self.expert_pos, self.token, self.counts,
+                             self.lse, self.balance, self.routed)])
+
+    def matrix(self):
+        """The gates as a CSR operand [tokens x experts] (of full rows: every place holds an entry)."""
+        return csr(self.pos, self.expert, self.n_tokens, self.n_experts, self.gate)
+
+
+def nacho_route(logits, top_k, normalise=False, keep=None, out=None, ws=None):
+    """Routes every token to its top_k experts; `keep` (bool or uint8 [tokens]): tokens that take part.  Enqueues only."""
+    dt, dev = model_dtype_code(logits.dtype), logits.device
+    ld = _matrix(logits, "logits")
+    tokens, experts = logits.shape
+    if out is None:
+        out = Routing(tokens, experts, top_k, dev)
+    _need((out.n_tokens, out.n_experts, out.top_k) == (tokens, experts, top_k) and out.pos.device == dev,
+          "out: made for other sizes or another device")
+    out.normalise = bool(normalise)
+    if keep is not None:
+        _vector_of(keep, "keep", tokens, torch.bool if keep.dtype is torch.bool else torch.uint8, dev)
+    if ws is None:
+        n = C.c_size_t(0)
+        _check(lib().nacho_route_workspace_bytes(tokens, experts, top_k, C.byref(n)), "nacho_route_workspace_bytes")
+        ws = _workspace(n.value, dev)
+    _check(lib().nacho_route(_ptr(logits), ld, tokens, experts, dt, top_k, out.normalise, _ptr(keep), C.byref(out.c),
+                             _ptr(ws), ws.numel(), _stream()), "nacho_route")
+    return out
+
+
+def nacho_route_grad(logits, routing: Routing, grad_gate=None, balance=0.0, keep=None, grad=None):
+    """Gradient of the logits from that of the gates (by entry) and `balance` times that of the balance loss.  `keep` may
+    be given as to nacho_route; tokens that it leaves out store nothing, which is how they are known."""
+    dt, dev = model_dtype_code(logits.dtype), logits.device
+    r = routing
+    ld = _matrix(logits, "logits", (r.n_tokens, r.n_experts))
+    _vector_of(grad_gate, "grad_gate", r.n_tokens * r.top_k, torch.float32, dev)
+    if grad is None:
+        grad = torch.empty((r.n_tokens, r.n_experts), dtype=logits.dtype, device=dev)
+    ldg = _matrix(grad, "grad", (r.n_tokens, r.n_experts), logits.dtype, dev)
+    _check(lib().nacho_route_grad(_ptr(logits), ld, r.n_tokens, r.n_experts, dt, r.top_k, r.normalise, C.byref(r.c),
+                                  _ptr(grad_gate), balance, _ptr(grad), ldg, _stream()), "nacho_route_grad")
     return grad
 
 

@@ -27,6 +27,54 @@ bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
 }
 int64_t span(int64_t rows, int64_t cols, int64_t ld, int64_t elem) { return rows > 0 ? ((rows - 1) * ld + cols) * elem : 0; }
 
+// Slices of a workspace, 256-byte aligned.
+struct Slices {
+    char *base;
+    size_t off = 0;
+    explicit Slices(void *p) : base(static_cast<char *>(p)) {}
+    template <typename T> T *take(int64_t n)
+    {
+        off = align_up(off, 256);
+        T *r = base ? reinterpret_cast<T *>(base + off) : nullptr;
+        off += (size_t)n * sizeof(T);
+        return r;
+    }
+};
+
+RouteScratch carve_route(void *ws, int64_t tokens, int32_t experts, int32_t top_k, size_t *bytes)
+{
+    Slices c(ws);
+    RouteScratch w;
+    route_plan(tokens, experts, &w.groups, &w.per_group);
+    w.hist = c.take<int32_t>(w.groups * experts);
+    w.share = c.take<float>(w.groups * experts);
+    w.entries = c.take<int32_t>(w.groups);
+    w.routed = c.take<int32_t>(w.groups);
+    w.choice = c.take<uint16_t>(tokens * top_k);
+    w.gate = c.take<float>(tokens * top_k);
+    w.held = c.take<uint8_t>(tokens);
+    *bytes = align_up(c.off, 256);
+    return w;
+}
+
+// Sizes of a routing call.
+int32_t check_route(int64_t tokens, int64_t experts, int32_t top_k)
+{
+    if (tokens < 0 || experts < 1 || top_k < 1 || top_k > experts) return NACHO_ERR_INVALID_ARG;
+    if (experts > kMostExperts || top_k > kMostChoices) return NACHO_ERR_UNSUPPORTED;
+    return tokens * top_k > kMostRows || tokens > kMostRows ? NACHO_ERR_INVALID_ARG : NACHO_OK;
+}
+bool check_routing(const nacho_routing *r)
+{
+    if (!r || !r->pos || !r->expert || !r->gate || !r->slot || !r->expert_pos || !r->token || !r->counts || !r->lse ||
+        !r->balance || !r->routed)
+        return false;
+    const void *all[] = {r->pos, r->expert, r->gate, r->slot, r->expert_pos, r->token, r->counts, r->lse, r->balance, r->routed};
+    for (const void *p : all)
+        if (!aligned(p, 4)) return false;
+    return true;
+}
+
 // The teacher: one CSR operand of floats.
 int32_t check_distill(const nacho_tensor *teacher, const void *logits, int64_t ldl, int32_t dtype, const float *weight,
                       float temperature, void *grad, int64_t ldg, DistillArgs *a)
@@ -92,6 +140,50 @@ int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int6
     profile_begin(s);
     if (launch_distill_grad(dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
     profile_mark("distill_grad");
+    return NACHO_OK;
+}
+
+int32_t nacho_route_workspace_bytes(int64_t n_tokens, int64_t n_experts, int32_t top_k, size_t *bytes)
+{
+    if (!bytes) return NACHO_ERR_INVALID_ARG;
+    const int32_t rc = check_route(n_tokens, n_experts, top_k);
+    if (rc == NACHO_OK) carve_route(nullptr, n_tokens, (int32_t)n_experts, top_k, bytes);
+    return rc;
+}
+
+int32_t nacho_route(const void *logits, int64_t ldl, int64_t n_tokens, int64_t n_experts, int32_t dtype, int32_t top_k,
+                    int32_t normalise, const uint8_t *keep, const nacho_routing *out, void *ws, size_t ws_bytes,
+                    void *hip_stream)
+{
+    int32_t rc = check_route(n_tokens, n_experts, top_k);
+    if (rc != NACHO_OK) return rc;
+    if (!value_type(dtype) || !matrix(logits, n_tokens, n_experts, ldl, value_bytes(dtype)) || !check_routing(out))
+        return NACHO_ERR_INVALID_ARG;
+    size_t need = 0;
+    const RouteScratch w = carve_route(ws, n_tokens, (int32_t)n_experts, top_k, &need);
+    if (!ws || ws_bytes < need || !aligned(ws, 16)) return NACHO_ERR_WORKSPACE;
+    const RouteArgs a{logits, ldl, keep, n_tokens, (int32_t)n_experts, top_k, normalise != 0, *out};
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    return launch_route(dtype, a, w, s) == hipSuccess ? NACHO_OK : NACHO_ERR_HIP;
+}
+
+int32_t nacho_route_grad(const void *logits, int64_t ldl, int64_t n_tokens, int64_t n_experts, int32_t dtype, int32_t top_k,
+                         int32_t normalise, const nacho_routing *routing, const float *grad_gate, float balance,
+                         void *grad, int64_t ldg, void *hip_stream)
+{
+    const int32_t rc = check_route(n_tokens, n_experts, top_k);
+    if (rc != NACHO_OK) return rc;
+    if (!value_type(dtype) || !check_routing(routing) || !aligned(grad_gate, 4)) return NACHO_ERR_INVALID_ARG;
+    const int64_t elem = value_bytes(dtype);
+    if (!matrix(logits, n_tokens, n_experts, ldl, elem) || !matrix(grad, n_tokens, n_experts, ldg, elem) ||
+        overlap(logits, span(n_tokens, n_experts, ldl, elem), grad, span(n_tokens, n_experts, ldg, elem)))
+        return NACHO_ERR_INVALID_ARG;
+    const RouteGradArgs a{logits, ldl, n_tokens, (int32_t)n_experts, normalise != 0, *routing, grad_gate, balance, grad, ldg};
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (launch_route_grad(dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+    profile_mark("route_grad");
     return NACHO_OK;
 }
 

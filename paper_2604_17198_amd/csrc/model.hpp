@@ -22,4 +22,39 @@ struct DistillArgs {
 hipError_t launch_distill(int dtype, const DistillArgs &a, hipStream_t s);
 hipError_t launch_distill_grad(int dtype, const DistillArgs &a, hipStream_t s);
 
+// ---- routing ------------------------------------------------------------------
+constexpr int kMostExperts = 1024, kMostChoices = 32;
+struct RouteArgs {
+    const void *logits;            // [tokens] rows of `ldl` elements
+    int64_t ldl;
+    const uint8_t *keep;           // may be NULL: every token
+    int64_t tokens;
+    int32_t experts, top_k, normalise;
+    nacho_routing out;
+};
+// Scratch of a routing call: `groups` workgroups work on `per_group` consecutive tokens each.
+struct RouteScratch {
+    int64_t groups, per_group;
+    int32_t *hist;                 // [groups][experts]: entries; after the scan those of the groups before
+    float *share;                  // [groups][experts]: sums of probabilities; after the scan row 0 holds the total
+    int32_t *entries, *routed;     // [groups] entries and tokens that store one
+    uint16_t *choice;              // [tokens * top_k]
+    float *gate;                   // [tokens * top_k]
+    uint8_t *held;                 // [tokens] entries of a token
+};
+void route_plan(int64_t tokens, int32_t experts, int64_t *groups, int64_t *per_group);
+hipError_t launch_route(int dtype, const RouteArgs &a, const RouteScratch &w, hipStream_t s);
+struct RouteGradArgs {
+    const void *logits;
+    int64_t ldl;
+    int64_t tokens;
+    int32_t experts, normalise;
+    nacho_routing routing;         // (a token that is not kept stores nothing)
+    const float *grad_gate;
+    float balance;
+    void *grad;
+    int64_t ldg;
+};
+hipError_t launch_route_grad(int dtype, const RouteGradArgs &a, hipStream_t s);
+
 }  // namespace nacho

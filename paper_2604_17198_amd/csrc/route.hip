@@ -1,0 +1,470 @@
+// The routing matrix of a mixture of experts: top-k of every token's logits, gates, the transposed order, counts and the
+// balance loss; and the gradient of the logits.
+//
+// L lanes hold a token's logits, I consecutive experts a lane, so that an expert's running sums stay in one lane's
+// registers over all tokens of a group of lanes.  Three kernels: every workgroup chooses for a stretch of consecutive
+// tokens and leaves its counts by expert; one wavefront an expert turns these into the entries before every workgroup;
+// every workgroup then knows where its entries lie in both orders.  All sums are in a fixed order.
+#include "kernels.hpp"
+#include "model.hpp"
+
+namespace nacho {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChunk = 64;             // tokens whose entries are placed at a time
+
+// A float as an unsigned number of the same order; 0 for what is never chosen (-inf, not a number).
+__device__ inline unsigned order_of(float v)
+{
+    const unsigned u = __float_as_uint(v + 0.0f);              // (-0 counts as 0)
+    return v > -kInfinity ? ((int)u < 0 ? ~u : u | 0x80000000u) : 0u;
+}
+
+template <int L, typename Op> __device__ inline float group_reduce(float v, Op op)
+{
+#pragma unroll
+    for (int off = L / 2; off > 0; off >>= 1) v = op(v, __shfl_xor(v, off, NACHO_WAVE));
+    return v;
+}
+
+// I consecutive elements of a row from element `at`, those behind `n` are -inf.
+template <typename T, int I> __device__ inline void row_part(const T *row, int at, int n, bool words, float (&v)[I])
+{
+    constexpr int kBytes = I * (int)sizeof(T) < 16 ? I * (int)sizeof(T) : 16, kEach = kBytes / (int)sizeof(T);
+    typedef T part __attribute__((ext_vector_type(kEach)));
+    if (words && at + I <= n) {
+#pragma unroll
+        for (int i = 0; i < I; i += kEach) {
+            const part p = *reinterpret_cast<const part *>(row + at + i);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) v[i + e] = wide((T)p[e]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < I; ++i) v[i] = at + i < n ? wide(row[at + i]) : -kInfinity;
+    }
+}
+template <typename T, int I> __device__ inline void put_row_part(T *row, int at, int n, bool words, const float (&v)[I])
+{
+    constexpr int kBytes = I * (int)sizeof(T) < 16 ? I * (int)sizeof(T) : 16, kEach = kBytes / (int)sizeof(T);
+    typedef T part __attribute__((ext_vector_type(kEach)));
+    if (words && at + I <= n) {
+#pragma unroll
+        for (int i = 0; i < I; i += kEach) {
+            part p;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) p[e] = (T)v[i + e];
+            *reinterpret_cast<part *>(row + at + i) = p;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (at + i < n) row[at + i] = (T)v[i];
+    }
+}
+
+// Whether rows `ld` apart can be read in words of 16 bytes (or of a lane's I elements, if these are fewer).
+template <typename T, int I> __host__ __device__ inline bool in_words(const void *base, int64_t ld)
+{
+    constexpr int kBytes = I * (int)sizeof(T) < 16 ? I * (int)sizeof(T) : 16;
+    return ((uintptr_t)base & (kBytes - 1)) == 0 && (ld * (int64_t)sizeof(T)) % kBytes == 0;
+}
+
+// The softmax of a token's logits: exp(v - top) of a lane's experts, and their sum over the group.
+template <int L, int I> __device__ inline void exponentials(const float (&v)[I], float (&e)[I], float &top, float &sum)
+{
+    top = v[0];
+#pragma unroll
+    for (int i = 1; i < I; ++i) top = fmaxf(top, v[i]);
+    top = group_reduce<L>(top, MaxOf());
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        e[i] = v[i] == -kInfinity ? 0.0f : exp2_of((v[i] - top) * kLog2e);
+        sum += e[i];
+    }
+    sum = group_reduce<L>(sum, SumOf());
+}
+
+// The k largest of a group's experts, as bits of the lanes' own.
+template <int L, int I> __device__ inline unsigned choose(const float (&v)[I], int first, int k)
+{
+    unsigned key[I], taken = 0;
+#pragma unroll
+    for (int i = 0; i < I; ++i) key[i] = order_of(v[i]);
+    for (int r = 0; r < k; ++r) {
+        unsigned best = key[0];
+        int at = first;
+#pragma unroll
+        for (int i = 1; i < I; ++i)
+            if (key[i] > best) {
+                best = key[i];
+                at = first + i;
+            }
+#pragma unroll
+        for (int off = L / 2; off > 0; off >>= 1) {
+            const unsigned other = (unsigned)__shfl_xor((int)best, off, NACHO_WAVE);
+            const int there = __shfl_xor(at, off, NACHO_WAVE);
+            if (other > best || (other == best && there < at)) {
+                best = other;
+                at = there;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (best != 0 && at == first + i) {
+                key[i] = 0;
+                taken |= 1u << i;
+            }
+    }
+    return taken;
+}
+
+template <typename T, int L, int I>
+__global__ void __launch_bounds__(kThreads) route_choose_kernel(RouteArgs a, RouteScratch w)
+{
+    constexpr int kGroups = kThreads / L, kSlots = L * I;
+    __shared__ int hist[kSlots];
+    __shared__ float shares[kGroups][kSlots + 1];
+    __shared__ int totals[2];
+    const int tid = (int)threadIdx.x, group = tid / L, lane = tid % L, first = lane * I, n = a.experts, k = a.top_k;
+    for (int i = tid; i < kSlots; i += kThreads) hist[i] = 0;
+    if (tid < 2) totals[tid] = 0;
+    __syncthreads();
+    const int64_t begin = (int64_t)blockIdx.x * w.per_group;
+    const int64_t end = begin + w.per_group < a.tokens ? begin + w.per_group : a.tokens;
+    const T *logits = static_cast<const T *>(a.logits);
+    const bool words = in_words<T, I>(logits, a.ldl);
+    float share[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) share[i] = 0.0f;
+    int entries = 0, routed = 0;
+    // (every lane of a wavefront stays in the loop: the lanes of a group ask each other)
+    for (int64_t t0 = begin; t0 < end; t0 += kGroups) {
+        const int64_t t = t0 + group;
+        const bool live = t < end && (!a.keep || a.keep[t] != 0);
+        float v[I], e[I], top, sum;
+        if (live) row_part<T, I>(logits + t * a.ldl, first, n, words, v);
+        else {
+#pragma unroll
+            for (int i = 0; i < I; ++i) v[i] = -kInfinity;
+        }
+        exponentials<L, I>(v, e, top, sum);
+        const unsigned taken = choose<L, I>(v, first, k);
+        // places of the lane's entries among the token's: those of the lanes before it come first
+        const int own = __popc(taken);
+        int before = own;
+#pragma unroll
+        for (int off = 1; off < L; off <<= 1) {
+            const int left = __shfl_up(before, off, L);
+            if (lane >= off) before += left;
+        }
+        const int held = __shfl(before, L - 1, L);
+        before -= own;
+        float whole = 0.0f;
+#pragma unroll
+        for (int i = 0; i < I; ++i) whole += taken >> i & 1 ? e[i] : 0.0f;
+        whole = group_reduce<L>(whole, SumOf());
+        if (a.normalise) whole = sum != sum ? sum : whole;     // (a NaN among the logits)
+        const float by = 1.0f / (a.normalise ? whole : sum), part = 1.0f / sum;
+        int place = before;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if (live && sum != 0.0f) share[i] += e[i] * part;
+            if (taken >> i & 1) {
+                w.choice[t * k + place] = (uint16_t)(first + i);
+                w.gate[t * k + place] = e[i] * by;
+                atomicAdd(&hist[first + i], 1);
+                ++place;
+            }
+        }
+        if (t < end && lane == 0) {
+            w.held[t] = (uint8_t)held;
+            a.out.lse[t] = !live || sum == 0.0f ? 0.0f : top + logf(sum);
+            entries += held;
+            routed += held > 0;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < I; ++i) shares[group][first + i] = share[i];
+    if (lane == 0) {
+        atomicAdd(&totals[0], entries);
+        atomicAdd(&totals[1], routed);
+    }
+    __syncthreads();
+    for (int e = tid; e < n; e += kThreads) {
+        float total = 0.0f;
+        for (int g = 0; g < kGroups; ++g) total += shares[g][e];
+        w.share[(int64_t)blockIdx.x * n + e] = total;
+        w.hist[(int64_t)blockIdx.x * n + e] = hist[e];
+    }
+    if (tid == 0) {
+        w.entries[blockIdx.x] = totals[0];
+        w.routed[blockIdx.x] = totals[1];
+    }
+}
+
+// One wavefront an expert, and one for the tokens: what the workgroups left becomes what lies before each of them; the
+// totals go to counts, expert_pos[0] (entries) and routed.
+__global__ void __launch_bounds__(NACHO_WAVE) route_scan_kernel(RouteArgs a, RouteScratch w)
+{
+    const int e = (int)blockIdx.x, n = a.experts, lane = lane_id();
+    const int groups = (int)w.groups;
+    int running = 0, routed = 0;
+    float share = 0.0f;
+    for (int g0 = 0; g0 < groups; g0 += NACHO_WAVE) {
+        const int g = g0 + lane;
+        int v = 0;
+        if (g < groups) {
+            if (e < n) {
+                v = w.hist[(int64_t)g * n + e];
+                share += w.share[(int64_t)g * n + e];
+            } else {
+                v = w.entries[g];
+                routed += w.routed[g];
+            }
+        }
+        const int upto = wave_inclusive_scan(v);
+        if (g < groups) {
+            if (e < n) w.hist[(int64_t)g * n + e] = running + upto - v;
+            else w.entries[g] = running + upto - v;
+        }
+        running += __shfl(upto, NACHO_WAVE - 1, NACHO_WAVE);
+    }
+    share = wave_sum(share);
+    routed = wave_sum(routed);
+    if (lane == 0) {
+        if (e < n) {
+            a.out.counts[e] = running;
+            w.share[e] = share;
+        } else {
+            a.out.pos[a.tokens] = running;
+            a.out.routed[0] = routed;
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) route_place_kernel(RouteArgs a, RouteScratch w)
+{
+    __shared__ int base[kMostExperts];                 // where the workgroup's next entry of an expert goes
+    __shared__ unsigned bits[kMostExperts][kChunk / 32];
+    __shared__ int scan[kThreads / NACHO_WAVE];
+    __shared__ int before[kChunk + 1];
+    __shared__ float sums[kThreads / NACHO_WAVE];
+    const int tid = (int)threadIdx.x, n = a.experts, k = a.top_k, lane = lane_id(), wave = tid / NACHO_WAVE;
+    const int64_t begin = (int64_t)blockIdx.x * w.per_group;
+    const int64_t end = begin + w.per_group < a.tokens ? begin + w.per_group : a.tokens;
+    const int entries = a.out.pos[a.tokens];
+    // expert_pos: prefix sums of the counts, a thread 4 consecutive experts
+    constexpr int kEach = kMostExperts / kThreads;
+    int c[kEach], own = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        c[i] = tid * kEach + i < n ? a.out.counts[tid * kEach + i] : 0;
+        own += c[i];
+    }
+    const int upto = wave_inclusive_scan(own);
+    if (lane == NACHO_WAVE - 1) scan[wave] = upto;
+    __syncthreads();
+    int at = upto - own;
+    for (int i = 0; i < wave; ++i) at += scan[i];
+    float balance = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int e = tid * kEach + i;
+        if (e < n) {
+            base[e] = at + w.hist[(int64_t)blockIdx.x * n + e];
+            if (blockIdx.x == 0) {
+                a.out.expert_pos[e] = at;
+                balance += (float)c[i] * w.share[e];
+            }
+        }
+        at += c[i];
+    }
+    if (blockIdx.x == 0) {
+        balance = wave_sum(balance);
+        if (lane == 0) sums[wave] = balance;
+        __syncthreads();
+        if (tid == 0) {
+            float total = 0.0f;
+            for (int i = 0; i < kThreads / NACHO_WAVE; ++i) total += sums[i];
+            const int routed = a.out.routed[0];
+            a.out.expert_pos[n] = entries;
+            a.out.balance[0] = total * ((float)n / ((float)(entries > 0 ? entries : 1) * (float)(routed > 0 ? routed : 1)));
+        }
+    }
+    int first = w.entries[blockIdx.x];                 // the workgroup's next entry
+    for (int64_t t0 = begin; t0 < end; t0 += kChunk) {
+        const int many = (int)(end - t0 < kChunk ? end - t0 : kChunk);
+        for (int i = tid; i < n * (kChunk / 32); i += kThreads) (&bits[0][0])[i] = 0;
+        if (wave == 0) {
+            const int held = lane < many ? w.held[t0 + lane] : 0;
+            const int sum = wave_inclusive_scan(held);
+            before[lane + 1] = sum;
+            if (lane == 0) before[0] = 0;
+            if (lane < many) a.out.pos[t0 + lane] = first + sum - held;
+        }
+        __syncthreads();
+        for (int i = tid; i < many * k; i += kThreads) {
+            const int t = i / k, r = i - t * k;
+            if (r < before[t + 1] - before[t]) atomicOr(&bits[w.choice[t0 * k + i]][t / 32], 1u << (t % 32));
+        }
+        __syncthreads();
+        for (int i = tid; i < many * k; i += kThreads) {
+            const int t = i / k, r = i - t * k;
+            if (r < before[t + 1] - before[t]) {
+                const int e = w.choice[t0 * k + i], entry = first + before[t] + r;
+                int place = base[e];
+                if (t >= 32) place += __popc(bits[e][0]);
+                place += __popc(bits[e][t / 32] & ((1u << (t % 32)) - 1u));
+                a.out.expert[entry] = e;
+                a.out.gate[entry] = w.gate[t0 * k + i];
+                a.out.slot[entry] = place;
+                a.out.token[place] = (int32_t)(t0 + t);
+            }
+        }
+        first += before[many];
+        __syncthreads();
+        for (int e = tid; e < n; e += kThreads) base[e] += __popc(bits[e][0]) + __popc(bits[e][1]);
+        __syncthreads();
+    }
+    // the places behind the last entry, shared out
+    const int64_t room = a.tokens * k;
+    for (int64_t i = entries + (int64_t)blockIdx.x * kThreads + tid; i < room; i += (int64_t)gridDim.x * kThreads) {
+        a.out.expert[i] = -1;
+        a.out.gate[i] = 0.0f;
+        a.out.slot[i] = -1;
+        a.out.token[i] = -1;
+    }
+}
+
+template <typename T, int L, int I>
+__global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteGradArgs a)
+{
+    constexpr int kGroups = kThreads / L;
+    const int tid = (int)threadIdx.x, group = tid / L, lane = tid % L, first = lane * I, n = a.experts;
+    const T *logits = static_cast<const T *>(a.logits);
+    T *grad = static_cast<T *>(a.grad);
+    const bool words = in_words<T, I>(logits, a.ldl), words_out = in_words<T, I>(grad, a.ldg);
+    // the balance loss by an expert's probability
+    const int entries = a.routing.pos[a.tokens], routed = a.routing.routed[0];
+    const float unit = a.balance * ((float)n / ((float)(entries > 0 ? entries : 1) * (float)(routed > 0 ? routed : 1)));
+    float c[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) c[i] = first + i < n ? unit * (float)a.routing.counts[first + i] : 0.0f;
+    for (int64_t t0 = (int64_t)blockIdx.x * kGroups; t0 < a.tokens; t0 += (int64_t)gridDim.x * kGroups) {
+        const int64_t t = t0 + group;
+        int at = 0, held = 0;
+        if (t < a.tokens) {
+            at = a.routing.pos[t];
+            held = a.routing.pos[t + 1] - at;
+        }
+        float d[I];
+#pragma unroll
+        for (int i = 0; i < I; ++i) d[i] = 0.0f;
+        float v[I], p[I], top, sum, inner = 0.0f, mean = 0.0f;
+        if (held > 0) row_part<T, I>(logits + t * a.ldl, first, n, words, v);
+        else {
+#pragma unroll
+            for (int i = 0; i < I; ++i) v[i] = -kInfinity;
+        }
+        // (not by the lse of the forward call: next to large logits it has no room for the sum)
+        exponentials<L, I>(v, p, top, sum);
+        if (held > 0) {
+            const float part = 1.0f / sum;
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                p[i] *= part;
+                mean += p[i] * c[i];
+            }
+            if (a.grad_gate) {
+                for (int j = 0; j < held; ++j) inner += a.routing.gate[at + j] * a.grad_gate[at + j];
+                for (int j = 0; j < held; ++j) {
+                    const int e = a.routing.expert[at + j] - first;
+                    if (e >= 0 && e < I) {
+                        const float g = a.routing.gate[at + j], dg = a.grad_gate[at + j];
+                        const float add = g * (a.normalise ? dg - inner : dg);
+#pragma unroll
+                        for (int i = 0; i < I; ++i) d[i] += e == i ? add : 0.0f;
+                    }
+                }
+            }
+        }
+        mean = group_reduce<L>(mean, SumOf());
+        if (held > 0) {
+            const float less = mean + (a.normalise ? 0.0f : inner);
+#pragma unroll
+            for (int i = 0; i < I; ++i) d[i] += p[i] * (c[i] - less);
+        }
+        if (t < a.tokens) put_row_part<T, I>(grad + t * a.ldg, first, n, words_out, d);
+    }
+}
+
+// Lanes and experts a lane for n experts, as a call of f(L, I).
+template <typename F> void by_experts(int n, F f)
+{
+    using std::integral_constant;
+    if (n <= 16) f(integral_constant<int, 4>(), integral_constant<int, 4>());
+    else if (n <= 32) f(integral_constant<int, 4>(), integral_constant<int, 8>());
+    else if (n <= 64) f(integral_constant<int, 8>(), integral_constant<int, 8>());
+    else if (n <= 128) f(integral_constant<int, 16>(), integral_constant<int, 8>());
+    else if (n <= 256) f(integral_constant<int, 32>(), integral_constant<int, 8>());
+    else if (n <= 512) f(integral_constant<int, 64>(), integral_constant<int, 8>());
+    else f(integral_constant<int, 64>(), integral_constant<int, 16>());
+}
+template <typename F> void by_type(int dtype, F f)
+{
+    if (dtype == NACHO_F32) f((float)0);
+    else if (dtype == NACHO_BF16) f((bf16_t)0.0f);
+    else f((f16_t)0.0f);
+}
+
+}  // namespace
+
+void route_plan(int64_t tokens, int32_t, int64_t *groups, int64_t *per_group)
+{
+    // up to 1024 workgroups (four a compute unit), whole chunks of tokens each
+    const int64_t chunks = (tokens + kChunk - 1) / kChunk, each = (chunks + 1023) / 1024;
+    *per_group = (each > 0 ? each : 1) * kChunk;
+    *groups = (tokens + *per_group - 1) / *per_group;
+    if (*groups < 1) *groups = 1;
+}
+
+hipError_t launch_route(int dtype, const RouteArgs &a, const RouteScratch &w, hipStream_t s)
+{
+    by_type(dtype, [&](auto zero) {
+        by_experts(a.experts, [&](auto lanes, auto items) {
+            route_choose_kernel<decltype(zero), decltype(lanes)::value, decltype(items)::value>
+                <<<dim3((unsigned)w.groups), kThreads, 0, s>>>(a, w);
+        });
+    });
+    hipError_t rc = hipGetLastError();
+    if (rc != hipSuccess) return rc;
+    nacho_host::profile_mark("route_choose");
+    route_scan_kernel<<<dim3((unsigned)a.experts + 1), NACHO_WAVE, 0, s>>>(a, w);
+    rc = hipGetLastError();
+    if (rc != hipSuccess) return rc;
+    nacho_host::profile_mark("route_scan");
+    route_place_kernel<<<dim3((unsigned)w.groups), kThreads, 0, s>>>(a, w);
+    rc = hipGetLastError();
+    if (rc == hipSuccess) nacho_host::profile_mark("route_place");
+    return rc;
+}
+
+hipError_t launch_route_grad(int dtype, const RouteGradArgs &a, hipStream_t s)
+{
+    if (a.tokens == 0) return hipSuccess;
+    by_type(dtype, [&](auto zero) {
+        by_experts(a.experts, [&](auto lanes, auto items) {
+            constexpr int L = decltype(lanes)::value;
+            const int64_t tiles = (a.tokens + kThreads / L - 1) / (kThreads / L);
+            route_grad_kernel<decltype(zero), L, decltype(items)::value>
+                <<<dim3((unsigned)(tiles < 2048 ? tiles : 2048)), kThreads, 0, s>>>(a);
+        });
+    });
+    return hipGetLastError();
+}
+
+}  // namespace nacho

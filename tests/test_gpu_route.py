@@ -1,0 +1,244 @@
+"""nacho_route, nacho_route_grad against the definition in 64 bits.
+
+Indices, counts and places have to be equal: the choice depends on comparisons of the stored logits alone.  Tolerances:
+gates, lse and the balance loss come from exponentials of arguments up to 2^6 in 32 bits (relative error 2^-24 * 2^6 at
+most), sums of up to 1024 of them and a division: within 1e-5.  Gradients are differences of products of these, within 2e-5
+of the largest term, and rounded once to their type."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_17198_amd import binding as nb
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+STEP = {torch.float32: 2.0 ** -23, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+def definition(z, k, normalise, keep, grad_gate=None, coef=0.0):
+    z = z.astype(np.float64)
+    tokens, experts = z.shape
+    member = np.zeros(z.shape, bool)
+    p, lse = np.zeros(z.shape), np.zeros(tokens)
+    for t in range(tokens):
+        if not keep[t] or not (z[t] > -np.inf).any():
+            continue
+        best = sorted(range(experts), key=lambda e: (-z[t, e], e))[:k]
+        for e in best:
+            member[t, e] = z[t, e] > -np.inf
+        m = z[t].max()
+        e = np.exp(z[t] - m)                                 # (not by lse: next to 1e38 it has no room for the sum)
+        lse[t], p[t] = m + math.log(e.sum()), e / e.sum()
+    gate = np.where(member, p, 0)
+    if normalise:
+        gate = gate / np.maximum(gate.sum(1, keepdims=True), 1e-300)
+    t, e = np.nonzero(member)
+    te = np.nonzero(member.T)
+    number = np.zeros(z.shape, np.int64)
+    number[te[1], te[0]] = np.arange(len(te[0]))
+    counts, entries, routed = member.sum(0), int(member.sum()), int(member.any(1).sum())
+    c = experts * counts / max(1, entries) / max(1, routed)
+    out = dict(pos=np.concatenate([[0], np.cumsum(member.sum(1))]), expert=e, gate=gate[member], slot=number[member],
+               expert_pos=np.concatenate([[0], np.cumsum(counts)]), token=te[1], counts=counts, lse=lse,
+               balance=(c * p.sum(0)).sum(), routed=routed)
+    dg = np.zeros(z.shape)
+    if grad_gate is not None:
+        dg[member] = grad_gate[:entries]
+    inner = (gate * dg).sum(1, keepdims=True)
+    grad = gate * (dg - inner) if normalise else gate * dg - p * inner
+    out["grad"] = grad + p * coef * (c - (p * c).sum(1, keepdims=True))
+    out["size"] = gate * (np.abs(dg) + np.abs(inner)) + p * (np.abs(inner) + coef * (c + (p * c).sum(1, keepdims=True)))
+    return out
+
+
+def compare(r, want, tokens, top_k):
+    entries = len(want["expert"])
+    get = lambda x: x.cpu().numpy()
+    for name in ("pos", "expert_pos", "counts"):
+        assert np.array_equal(get(getattr(r, name)), want[name]), name
+    for name in ("expert", "slot", "token"):
+        a = get(getattr(r, name))
+        assert np.array_equal(a[:entries], want[name]), name
+        assert np.all(a[entries:] == -1), name
+    gate = get(r.gate)
+    assert np.all(np.abs(gate[:entries] - want["gate"]) <= 1e-5 * want["gate"] + 1e-37) and np.all(gate[entries:] == 0)
+    assert np.all(np.abs(get(r.lse) - want["lse"]) <= 1e-5 * np.maximum(1, np.abs(want["lse"])))
+    assert abs(r.balance.item() - want["balance"]) <= 1e-5 * max(1e-30, want["balance"]) and r.routed.item() == want["routed"]
+
+
+def compare_grad(grad, want, dtype):
+    g = grad.float().cpu().numpy().astype(np.float64)
+    assert np.all(np.abs(g - want["grad"]) <= STEP[dtype] * np.abs(want["grad"]) + 2e-5 * want["size"] + 2.0 ** -25 * (dtype is torch.float16))
+
+
+def logits_of(rng, tokens, experts, dtype, closed=0.0, coarse=False, ld=None):
+    z = rng.normal(0, 1.5, (tokens, ld or experts)).astype(np.float32)
+    if coarse:
+        z = np.round(z)                                      # ties, and both zeros
+    z[rng.random(z.shape) < closed] = -np.inf
+    return torch.from_numpy(z).to(dtype).cuda()[:, :experts]
+
+
+SHAPES = [(1, 1, 1), (1, 2, 2), (3, 5, 2), (16, 8, 2), (63, 16, 3), (64, 17, 1), (65, 32, 4), (5, 60, 3), (130, 64, 8),
+          (257, 65, 5), (100, 128, 8), (33, 200, 2), (70, 256, 32), (40, 300, 7), (20, 512, 8), (9, 1000, 10), (3, 1024, 32), (2000, 12, 3)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("tokens,experts,top_k", SHAPES)
+@pytest.mark.parametrize("kind", ["plain", "ties", "masked"])
+def test_routing_and_gradient(tokens, experts, top_k, kind, dtype):
+    rng = np.random.default_rng(tokens * 7 + experts * 1009 + top_k)
+    normalise = bool((tokens + top_k) % 2)
+    z = logits_of(rng, tokens, experts, dtype, 0.4 if kind == "masked" else 0.0, kind == "ties")
+    keep = rng.random(tokens) < (0.7 if kind == "masked" else 2.0)
+    grad_gate = rng.normal(0, 1, tokens * top_k).astype(np.float32)
+    want = definition(z.float().cpu().numpy(), top_k, normalise, keep, grad_gate, 0.5)
+    given = torch.from_numpy(keep).cuda() if kind == "masked" else None
+    r = nb.nacho_route(z, top_k, normalise=normalise, keep=given)
+    compare(r, want, tokens, top_k)
+    compare_grad(nb.nacho_route_grad(z, r, torch.from_numpy(grad_gate).cuda(), balance=0.5), want, dtype)
+    only = definition(z.float().cpu().numpy(), top_k, normalise, keep, None, 2.0)
+    compare_grad(nb.nacho_route_grad(z, r, balance=2.0), only, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_many_tokens(dtype):
+    """More tokens than the workgroups of a launch take in one go each: several stretches a workgroup."""
+    rng = np.random.default_rng(9)
+    tokens, experts, k = 140_000, 6, 2
+    z = logits_of(rng, tokens, experts, dtype, 0.3)
+    keep = rng.random(tokens) < 0.8
+    r = nb.nacho_route(z, k, normalise=True, keep=torch.from_numpy(keep).cuda())
+    want = definition(z.float().cpu().numpy(), k, True, keep)
+    compare(r, want, tokens, k)
+
+
+@pytest.mark.parametrize("ld,shift", [(64, 0), (72, 0), (67, 0), (64, 1), (60, 4)])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_leading_dimensions_and_alignment(ld, shift, dtype):
+    rng = np.random.default_rng(ld + shift)
+    tokens, experts, k = 37, 59, 4
+    store = torch.from_numpy(rng.normal(0, 1, tokens * ld + shift).astype(np.float32)).to(dtype).cuda()
+    z = store[shift:].view(tokens, ld)[:, :experts]
+    grad_gate = rng.normal(0, 1, tokens * k).astype(np.float32)
+    r = nb.nacho_route(z, k)
+    want = definition(z.float().cpu().numpy(), k, False, np.ones(tokens, bool), grad_gate, 0.1)
+    compare(r, want, tokens, k)
+    out = torch.full((tokens * ld + shift,), 7.0, dtype=dtype, device="cuda")
+    grad = out[shift:].view(tokens, ld)
+    compare_grad(nb.nacho_route_grad(z, r, torch.from_numpy(grad_gate).cuda(), balance=0.1, grad=grad[:, :experts]), want, dtype)
+    assert bool((grad[:, experts:] == 7.0).all()) and bool((out[:shift] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_values_that_are_no_logits(dtype):
+    rng = np.random.default_rng(4)
+    z = logits_of(rng, 8, 10, dtype)
+    z[0] = float("nan")                                      # not kept: never read
+    z[1] = float("-inf")                                     # no expert open
+    z[2, 3:] = float("-inf")                                 # three open, four wanted
+    z[3] = torch.finfo(dtype).min
+    z[4, 5] = torch.finfo(dtype).max
+    keep = np.array([0, 1, 1, 1, 1, 1, 1, 1], bool)
+    grad_gate = rng.normal(0, 1, 32).astype(np.float32)
+    r = nb.nacho_route(z, 4, normalise=True, keep=torch.from_numpy(keep).cuda().to(torch.uint8))
+    clean = z.float().cpu().numpy()
+    clean[0] = 0
+    want = definition(clean, 4, True, keep, grad_gate, 0.3)
+    compare(r, want, 8, 4)
+    grad = nb.nacho_route_grad(z, r, torch.from_numpy(grad_gate).cuda(), balance=0.3)
+    compare_grad(grad, want, dtype)
+    assert not bool(grad[:2].any())
+    # a NaN in a row that is read: never chosen, and felt in what depends on the row
+    z[5, 2] = float("nan")
+    r = nb.nacho_route(z, 4, keep=torch.from_numpy(keep).cuda())
+    pos, expert = r.pos.tolist(), r.expert.tolist()
+    assert pos[6] - pos[5] == 4 and 2 not in expert[pos[5]:pos[6]] and r.counts.sum().item() == pos[-1]
+    assert all(math.isnan(g) for g in r.gate[pos[5]:pos[6]].tolist()) and math.isnan(r.lse[5].item()) and math.isnan(r.balance.item())
+    assert bool(torch.isfinite(r.gate[pos[6]:pos[8]]).all())
+
+
+def test_no_tokens_and_none_kept():
+    r = nb.nacho_route(torch.empty((0, 6), device="cuda"), 2)
+    assert r.pos.tolist() == [0] and r.expert_pos.tolist() == [0] * 7 and r.counts.tolist() == [0] * 6 and r.balance.item() == 0
+    z = torch.full((70, 6), float("nan"), device="cuda")
+    r = nb.nacho_route(z, 2, keep=torch.zeros(70, dtype=torch.bool, device="cuda"))
+    assert not any(r.pos.tolist()) and not any(r.expert_pos.tolist()) and r.balance.item() == 0 and r.routed.item() == 0
+    assert bool((r.token == -1).all()) and bool((r.lse == 0).all())
+    assert not bool(nb.nacho_route_grad(z, r, torch.ones(140, device="cuda"), balance=1.0).any())
+
+
+def test_gradient_against_differences():
+    """Central differences of sum(gate * h) + 0.7 balance in 64 bits, away from ties; the counts stay as they are."""
+    rng = np.random.default_rng(6)
+    for normalise in (False, True):
+        z = logits_of(rng, 6, 9, torch.float32)
+        h = rng.normal(0, 1, 18).astype(np.float32)
+        r = nb.nacho_route(z, 3, normalise=normalise)
+        grad = nb.nacho_route_grad(z, r, torch.from_numpy(h).cuda(), balance=0.7).cpu().numpy()
+        z64, every = z.cpu().numpy().astype(np.float64), np.ones(6, bool)
+        base = definition(z64, 3, normalise, every)
+        step = 1e-4
+
+        def objective(a):
+            d = definition(a, 3, normalise, every)
+            assert np.array_equal(d["expert"], base["expert"])
+            return (d["gate"] * h).sum() + 0.7 * d["balance"]
+
+        for t in range(6):
+            for e in range(9):
+                up, down = z64.copy(), z64.copy()
+                up[t, e] += step
+                down[t, e] -= step
+                assert abs((objective(up) - objective(down)) / (2 * step) - grad[t, e]) <= 2e-5
+
+
+def test_matrix_is_an_operand_of_the_library():
+    """The routing matrix through the library's own calls: preconditions, and its product with a vector of ones."""
+    rng = np.random.default_rng(8)
+    z = logits_of(rng, 500, 40, torch.float32)
+    r = nb.nacho_route(z, 4, normalise=True)
+    A = r.matrix()
+    assert nb.nacho_validate([A])[0] == 0
+    y = nb.nacho_spmv(A, torch.ones(40, device="cuda"))
+    assert bool((y - 1).abs().max() <= 1e-5)
+
+
+def test_another_stream_and_the_same_bits_again():
+    rng = np.random.default_rng(12)
+    z = logits_of(rng, 5000, 96, torch.bfloat16)
+    first = nb.nacho_route(z, 6)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        second = nb.nacho_route(z, 6)
+    side.synchronize()
+    for name in ("pos", "expert", "gate", "slot", "expert_pos", "token", "counts", "lse", "balance"):
+        assert torch.equal(getattr(first, name), getattr(second, name)), name
+
+
+def test_refusals():
+    z = torch.zeros((4, 8), device="cuda")
+    for k in (0, 9):
+        with pytest.raises(nb.NachoError):
+            nb.nacho_route(z, k, out=nb.Routing(4, 8, k, "cuda") if k else nb.Routing(4, 8, 0, z.device))
+    with pytest.raises(nb.NachoError):
+        nb.nacho_route(torch.zeros((1, 1025), device="cuda"), 2)
+    with pytest.raises(nb.NachoError):
+        nb.nacho_route(torch.zeros((1, 100), device="cuda"), 33)
+    with pytest.raises(TypeError):
+        nb.nacho_route(z.double(), 2)
+    with pytest.raises(ValueError):
+        nb.nacho_route(z, 2, keep=torch.ones(3, dtype=torch.bool, device="cuda"))
+    with pytest.raises(ValueError):
+        nb.nacho_route(z, 2, out=nb.Routing(5, 8, 2, z.device))
+    with pytest.raises(nb.NachoError):
+        nb.nacho_route(z, 2, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    r = nb.nacho_route(z, 2)
+    with pytest.raises(nb.NachoError):
+        nb.nacho_route_grad(z, r, grad=z)
+    with pytest.raises(ValueError):
+        nb.nacho_route_grad(z, r, torch.ones(7, device="cuda"))
