@@ -479,6 +479,28 @@ int32_t nacho_route_grad(const void *logits, int64_t ldl, int64_t n_tokens, int6
                          float balance, void *grad, int64_t ldg, void *hip_stream);
 
 /*
+ * nacho_combine: for every token the weighted sum of its experts' rows,
+ *   out[t] = residual[t] + sum_i val_i y[crd_i]   over the entries i of row t of
+ *   routing   CSR [n_tokens x n_slots]: crd the slots, values F32 the gates (val
+ *             NULL: ones); in the arrays of nacho_routing pos, slot and gate.  Its
+ *             count is an upper bound, as many as pos[n_tokens] are read
+ *   y         [n_slots x n], residual (may be NULL), out [n_tokens x n], row-major
+ * Tokens without an entry get their residual, or 0.  out may be residual itself
+ * (same leading dimension), for sums in place.
+ *
+ * nacho_combine_grad: from grad_out [n_tokens x n]
+ *   grad_y[crd_i] = val_i grad_out[t]        (NULL: not wanted; slots of no entry
+ *                                             are not written; no slot may be in two)
+ *   grad_val[i]   = sum_c grad_out[t, c] y[crd_i, c]   (float, NULL: not wanted,
+ *                                             then y may be NULL)
+ */
+int32_t nacho_combine(const nacho_tensor *routing, const void *y, int64_t ldy, int64_t n, int32_t dtype,
+                      const void *residual, int64_t ldr, void *out, int64_t ldo, void *hip_stream);
+int32_t nacho_combine_grad(const nacho_tensor *routing, const void *y, int64_t ldy, int64_t n, int32_t dtype,
+                           const void *grad_out, int64_t ldg, void *grad_y, int64_t ldgy, float *grad_val,
+                           void *hip_stream);
+
+/*
  * Debug aid, not part of the hot path: checks on the device the preconditions
  * that the other entry points rely on without looking -- pos arrays start at 0,
  * never decrease and end at the level's count; coordinates lie inside the

@@ -30,7 +30,8 @@ EXPORTS = [
     "nacho_probe", "nacho_merge_wavefronts", "nacho_rowcost_partitions", "nacho_partition_rowcost",
     "nacho_spmv_rowcost", "nacho_partition_csr64", "nacho_spmv_fused", "nacho_spadd_fused",
     "nacho_distill_workspace_bytes", "nacho_distill", "nacho_distill_grad",
-    "nacho_route_workspace_bytes", "nacho_route", "nacho_route_grad",
+    "nacho_route_workspace_bytes", "nacho_route", "nacho_route_grad", "nacho_combine",
+    "nacho_combine_grad",
 ]
 
 
@@ -133,6 +134,10 @@ def lib():
                                   C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.nacho_route_grad.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
                                        C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]
+        L.nacho_combine.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
+                                    C.c_void_p, C.c_int64, C.c_void_p]
+        L.nacho_combine_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
+                                         C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
         _libs[_instrumented] = L
         _lib = L
     return _lib
@@ -615,6 +620,55 @@ def nacho_route_grad(logits, routing: Routing, grad_gate=None, balance=0.0, keep
     _check(lib().nacho_route_grad(_ptr(logits), ld, r.n_tokens, r.n_experts, dt, r.top_k, r.normalise, C.byref(r.c),
                                   _ptr(grad_gate), balance, _ptr(grad), ldg, _stream()), "nacho_route_grad")
     return grad
+
+
+def _slots_of(pos, slot, gate, n_slots, device):
+    """The routing matrix tokens x slots as a descriptor."""
+    _need(pos.dtype is torch.int32 and pos.is_contiguous() and pos.numel() > 0 and pos.device == device,
+          "pos: tokens + 1 contiguous int32 positions are needed on the rows' device")
+    _vector_of(slot, "slot", slot.numel(), torch.int32, device)
+    _vector_of(gate, "gate", slot.numel(), torch.float32, device)
+    c = _Tensor()
+    c.nlevels = 2
+    c.lvl[0].kind, c.lvl[0].extent = DENSE, pos.numel() - 1
+    low = c.lvl[1]
+    low.kind, low.extent, low.pos, low.crd, low.count = COMPRESSED, n_slots, pos.data_ptr(), slot.data_ptr() or None, slot.numel()
+    c.val = None if gate is None else gate.data_ptr() or None
+    return c
+
+
+def nacho_combine(pos, slot, y, gate=None, residual=None, out=None):
+    """out[t] = residual[t] + sum over the entries of token t of gate * y[slot] (pos, slot, gate: a Routing's).  `out` may
+    be `residual` itself."""
+    dt, dev = model_dtype_code(y.dtype), y.device
+    tokens, n = pos.numel() - 1, int(y.shape[1])
+    ldy = _matrix(y, "y")
+    ldr = _matrix(residual, "residual", (tokens, n), y.dtype, dev) if residual is not None else 0
+    if out is None:
+        out = torch.empty((tokens, n), dtype=y.dtype, device=dev)
+    ldo = _matrix(out, "out", (tokens, n), y.dtype, dev)
+    c = _slots_of(pos, slot, gate, y.shape[0], dev)
+    _check(lib().nacho_combine(C.byref(c), _ptr(y), ldy, n, dt, _ptr(residual), ldr, _ptr(out), ldo, _stream()),
+           "nacho_combine")
+    return out
+
+
+def nacho_combine_grad(pos, slot, y, grad_out, gate=None, grad_y=None, grad_gate=None):
+    """Gradients of y's rows and of the gates; rows of y that no entry names are left as they are."""
+    dt, dev = model_dtype_code(y.dtype), y.device
+    tokens, n = pos.numel() - 1, int(y.shape[1])
+    ldy = _matrix(y, "y")
+    ldg = _matrix(grad_out, "grad_out", (tokens, n), y.dtype, dev)
+    if grad_y is None:
+        grad_y = torch.empty((y.shape[0], n), dtype=y.dtype, device=dev)
+    ldgy = _matrix(grad_y, "grad_y", (y.shape[0], n), y.dtype, dev)
+    if grad_gate is None:
+        grad_gate = torch.empty(slot.numel(), device=dev)
+    _vector_of(grad_gate, "grad_gate", slot.numel(), torch.float32, dev)
+    c = _slots_of(pos, slot, gate, y.shape[0], dev)
+    _check(lib().nacho_combine_grad(C.byref(c), _ptr(y), ldy, n, dt, _ptr(grad_out), ldg, _ptr(grad_y), ldgy,
+                                    _ptr(grad_gate), _stream()), "nacho_combine_grad")
+    return grad_y, grad_gate
 
 
 def nacho_validate(ops):

@@ -97,6 +97,26 @@ int32_t check_distill(const nacho_tensor *teacher, const void *logits, int64_t l
     return NACHO_OK;
 }
 
+// The routing matrix of a combine call: CSR, tokens x slots.
+int32_t check_combine(const nacho_tensor *m, int64_t n, int32_t dtype, CombineArgs *a)
+{
+    if (!m || !value_type(dtype) || n < 0 || n > kMostRows) return NACHO_ERR_INVALID_ARG;
+    if (m->nlevels != 2 || m->lvl[0].kind != NACHO_DENSE || m->lvl[1].kind != NACHO_COMPRESSED) return NACHO_ERR_UNSUPPORTED;
+    const int64_t tokens = m->lvl[0].extent, slots = m->lvl[1].extent, stored = m->lvl[1].count;
+    if (tokens < 0 || tokens > kMostRows || slots < 0 || slots > kMostRows || stored < 0 || stored > kMostRows)
+        return NACHO_ERR_INVALID_ARG;
+    if (!m->lvl[1].pos || !aligned(m->lvl[1].pos, 4) || (stored > 0 && !m->lvl[1].crd) || !aligned(m->lvl[1].crd, 4) ||
+        !aligned(m->val, 4))
+        return NACHO_ERR_INVALID_ARG;
+    *a = CombineArgs{};
+    a->pos = m->lvl[1].pos;
+    a->slot = m->lvl[1].crd;
+    a->gate = static_cast<const float *>(m->val);
+    a->tokens = tokens;
+    a->cols = (int32_t)n;
+    return NACHO_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -184,6 +204,58 @@ int32_t nacho_route_grad(const void *logits, int64_t ldl, int64_t n_tokens, int6
     profile_begin(s);
     if (launch_route_grad(dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
     profile_mark("route_grad");
+    return NACHO_OK;
+}
+
+int32_t nacho_combine(const nacho_tensor *routing, const void *y, int64_t ldy, int64_t n, int32_t dtype,
+                      const void *residual, int64_t ldr, void *out, int64_t ldo, void *hip_stream)
+{
+    CombineArgs a;
+    const int32_t rc = check_combine(routing, n, dtype, &a);
+    if (rc != NACHO_OK) return rc;
+    const int64_t elem = value_bytes(dtype), slots = routing->lvl[1].extent, bytes = span(a.tokens, n, ldo, elem);
+    if (!matrix(y, slots, n, ldy, elem) || !matrix(out, a.tokens, n, ldo, elem) ||
+        overlap(y, span(slots, n, ldy, elem), out, bytes))
+        return NACHO_ERR_INVALID_ARG;
+    if (residual && (!matrix(residual, a.tokens, n, ldr, elem) ||
+                     (!(residual == out && ldr == ldo) && overlap(residual, span(a.tokens, n, ldr, elem), out, bytes))))
+        return NACHO_ERR_INVALID_ARG;
+    a.y = y;
+    a.ldy = ldy;
+    a.residual = residual;
+    a.ldr = ldr;
+    a.out = out;
+    a.ldo = ldo;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (launch_combine(dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+    profile_mark("combine");
+    return NACHO_OK;
+}
+
+int32_t nacho_combine_grad(const nacho_tensor *routing, const void *y, int64_t ldy, int64_t n, int32_t dtype,
+                           const void *grad_out, int64_t ldg, void *grad_y, int64_t ldgy, float *grad_val, void *hip_stream)
+{
+    CombineArgs a;
+    const int32_t rc = check_combine(routing, n, dtype, &a);
+    if (rc != NACHO_OK) return rc;
+    const int64_t elem = value_bytes(dtype), slots = routing->lvl[1].extent, bytes = span(slots, n, ldgy, elem);
+    if (!aligned(grad_val, 4) || !matrix(grad_out, a.tokens, n, ldg, elem) || (grad_val && !matrix(y, slots, n, ldy, elem)))
+        return NACHO_ERR_INVALID_ARG;
+    if (grad_y && (!matrix(grad_y, slots, n, ldgy, elem) || overlap(grad_out, span(a.tokens, n, ldg, elem), grad_y, bytes) ||
+                   (grad_val && overlap(y, span(slots, n, ldy, elem), grad_y, bytes))))
+        return NACHO_ERR_INVALID_ARG;
+    a.y = y;
+    a.ldy = ldy;
+    a.grad_out = grad_out;
+    a.ldg = ldg;
+    a.grad_y = grad_y;
+    a.ldgy = ldgy;
+    a.grad_gate = grad_val;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (launch_combine_grad(dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+    profile_mark("combine_grad");
     return NACHO_OK;
 }
 

@@ -57,4 +57,25 @@ struct RouteGradArgs {
 };
 hipError_t launch_route_grad(int dtype, const RouteGradArgs &a, hipStream_t s);
 
+// ---- sums of the experts' rows for every token ---------------------------------
+struct CombineArgs {
+    const int32_t *pos, *slot;     // CSR, tokens x slots
+    const float *gate;             // may be NULL: ones
+    int64_t tokens;
+    const void *y;                 // [slots] rows of `ldy` elements
+    int64_t ldy;
+    int32_t cols;
+    const void *residual;          // forward: may be NULL
+    int64_t ldr;
+    void *out;
+    int64_t ldo;
+    const void *grad_out;          // backward
+    int64_t ldg;
+    void *grad_y;                  // may be NULL
+    int64_t ldgy;
+    float *grad_gate;              // may be NULL
+};
+hipError_t launch_combine(int dtype, const CombineArgs &a, hipStream_t s);
+hipError_t launch_combine_grad(int dtype, const CombineArgs &a, hipStream_t s);
+
 }  // namespace nacho
