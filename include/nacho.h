@@ -479,6 +479,53 @@ int32_t nacho_route_grad(const void *logits, int64_t ldl, int64_t n_tokens, int6
                          float balance, void *grad, int64_t ldg, void *hip_stream);
 
 /*
+ * nacho_experts: one dense layer of a mixture of experts.  The slots (rows) of expert
+ * e are expert_pos[e] .. expert_pos[e+1], of any number, as nacho_route leaves them:
+ *   y[s] = act(x[token[s]] w[e]^T + bias[e])   for every slot s of expert e
+ *   expert_pos  device int32[n_experts+1], from 0, never decreasing, at most n_slots
+ *   token       device int32[n_slots], rows of x; NULL: slot s reads row s
+ *   x           [n_tokens x inner], leading dimension ldx
+ *   w           [n_experts][outer x inner], leading dimension ldw, experts w_stride
+ *               elements apart
+ *   bias        [n_experts][outer], experts bias_stride apart, or NULL
+ *   act         nacho_act; gelu is x Phi(x) with the error function
+ *   y           [n_slots x outer]; slots from expert_pos[n_experts] on are not written
+ *   pre         [n_slots x outer] or NULL: the rows before the activation, which the
+ *               way back needs unless act is NACHO_ACT_NONE
+ * All of one type; products are summed in 32 bits and rounded once.
+ *
+ * nacho_experts_grad: from grad_y [n_slots x outer], with z the rows before the
+ * activation and g_s = grad_y[s] act'(z_s) (rounded to the type, which the products
+ * below take),
+ *   grad_x[s]    = g_s w[e]             [n_slots x inner], by slots: nacho_combine
+ *                                       without gates sums them by tokens
+ *   grad_w[e]    = sum_s g_s^T x[token[s]]
+ *   grad_bias[e] = sum_s g_s
+ * each NULL where it is not wanted (w, or x and token, may then be NULL); experts
+ * without a slot get 0.  pre may be NULL with NACHO_ACT_NONE.
+ * Workspace: nacho_experts_workspace_bytes (may be 0: then ws may be NULL).
+ * Limits: n_experts <= 65536; inner, outer < 2^24.
+ */
+typedef enum { NACHO_ACT_NONE = 0, NACHO_ACT_RELU = 1, NACHO_ACT_GELU = 2, NACHO_ACT_SILU = 3 } nacho_act;
+typedef struct {
+    const int32_t *expert_pos, *token;
+    int64_t n_experts, n_slots, n_tokens, inner, outer;
+    const void *x;
+    int64_t ldx;
+    const void *w;
+    int64_t ldw, w_stride;
+    const void *bias;
+    int64_t bias_stride;
+    int32_t act, dtype;
+} nacho_experts_layer;
+int32_t nacho_experts_workspace_bytes(const nacho_experts_layer *layer, size_t *bytes);
+int32_t nacho_experts(const nacho_experts_layer *layer, void *y, int64_t ldy, void *pre, int64_t ldpre,
+                      void *hip_stream);
+int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y, int64_t ldgy, const void *pre,
+                           int64_t ldpre, void *grad_x, int64_t ldgx, void *grad_w, int64_t ldgw, int64_t gw_stride,
+                           void *grad_bias, int64_t gb_stride, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
  * nacho_combine: for every token the weighted sum of its experts' rows,
  *   out[t] = residual[t] + sum_i val_i y[crd_i]   over the entries i of row t of
  *   routing   CSR [n_tokens x n_slots]: crd the slots, values F32 the gates (val

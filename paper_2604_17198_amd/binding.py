@@ -31,7 +31,7 @@ EXPORTS = [
     "nacho_spmv_rowcost", "nacho_partition_csr64", "nacho_spmv_fused", "nacho_spadd_fused",
     "nacho_distill_workspace_bytes", "nacho_distill", "nacho_distill_grad",
     "nacho_route_workspace_bytes", "nacho_route", "nacho_route_grad", "nacho_combine",
-    "nacho_combine_grad",
+    "nacho_combine_grad", "nacho_experts_workspace_bytes", "nacho_experts", "nacho_experts_grad",
 ]
 
 
@@ -65,6 +65,13 @@ class _SparseOut(C.Structure):
 class _Routing(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("pos", "expert", "gate", "slot", "expert_pos", "token", "counts", "lse",
                                           "balance", "routed")]
+
+
+class _ExpertsLayer(C.Structure):
+    _fields_ = [("expert_pos", C.c_void_p), ("token", C.c_void_p), ("n_experts", C.c_int64), ("n_slots", C.c_int64),
+                ("n_tokens", C.c_int64), ("inner", C.c_int64), ("outer", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("w", C.c_void_p), ("ldw", C.c_int64), ("w_stride", C.c_int64), ("bias", C.c_void_p),
+                ("bias_stride", C.c_int64), ("act", C.c_int32), ("dtype", C.c_int32)]
 
 
 _lib = None
@@ -138,6 +145,11 @@ def lib():
                                     C.c_void_p, C.c_int64, C.c_void_p]
         L.nacho_combine_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
                                          C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.nacho_experts_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+        L.nacho_experts.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+        L.nacho_experts_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                         C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t,
+                                         C.c_void_p]
         _libs[_instrumented] = L
         _lib = L
     return _lib
@@ -620,6 +632,77 @@ def nacho_route_grad(logits, routing: Routing, grad_gate=None, balance=0.0, keep
     _check(lib().nacho_route_grad(_ptr(logits), ld, r.n_tokens, r.n_experts, dt, r.top_k, r.normalise, C.byref(r.c),
                                   _ptr(grad_gate), balance, _ptr(grad), ldg, _stream()), "nacho_route_grad")
     return grad
+
+
+_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def _stack(t, what, shape, dtype, device):
+    """Matrices (or rows) of one size, each with contiguous rows: leading dimension and distance."""
+    _need(tuple(t.shape) == tuple(shape) and t.dtype is dtype and t.device == device,
+          f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {tuple(shape)} of {dtype} on {device}")
+    _need(t.stride(-1) == 1 or t.shape[-1] <= 1, f"{what}: contiguous rows are needed")
+    size = 1
+    for n in shape[1:]:
+        size *= n
+    ld = max(t.stride(1), t.shape[2]) if t.dim() == 3 and t.shape[1] > 1 else shape[-1]
+    return ld, t.stride(0) if t.shape[0] > 1 else max(size, t.stride(0))
+
+
+def _layer(x, weight, expert_pos, token, bias, act):
+    """The descriptor of a layer of experts, and its number of slots."""
+    dt, dev = model_dtype_code(x.dtype), x.device
+    _need(weight.dim() == 3, "weight: [experts, outer, inner] is needed")
+    experts, outer, inner = weight.shape
+    ldx = _matrix(x, "x", (x.shape[0], inner))
+    ldw, stride = _stack(weight, "weight", weight.shape, x.dtype, dev)
+    _vector_of(expert_pos, "expert_pos", experts + 1, torch.int32, dev)
+    slots = x.shape[0] if token is None else token.numel()
+    _vector_of(token, "token", slots, torch.int32, dev)
+    _need(act in _ACTS, f"act: one of {', '.join(_ACTS)}")
+    gap = _stack(bias, "bias", (experts, outer), x.dtype, dev)[1] if bias is not None else 0
+    # (an array without an element has no address)
+    return _ExpertsLayer(expert_pos.data_ptr(), _ptr(token) or (expert_pos.data_ptr() if token is not None else None), experts,
+                         slots, x.shape[0], inner, outer, _ptr(x), ldx, _ptr(weight), ldw, stride, _ptr(bias), gap,
+                         _ACTS[act], dt), slots
+
+
+def nacho_experts(x, weight, expert_pos, token=None, bias=None, act="none", y=None, pre=None):
+    """y[s] = act(x[token[s]] weight[e]^T + bias[e]) for the slots s = expert_pos[e] .. expert_pos[e+1] of every expert e
+    (expert_pos, token: a Routing's).  `pre`, when given, receives the rows before the activation."""
+    c, slots = _layer(x, weight, expert_pos, token, bias, act)
+    shape = (slots, weight.shape[1])
+    if y is None:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    ldy = _matrix(y, "y", shape, x.dtype, x.device)
+    ldpre = _matrix(pre, "pre", shape, x.dtype, x.device) if pre is not None else 0
+    _check(lib().nacho_experts(C.byref(c), _ptr(y), ldy, _ptr(pre), ldpre, _stream()), "nacho_experts")
+    return y
+
+
+def nacho_experts_grad(grad_y, x, weight, expert_pos, token=None, act="none", pre=None, grad_x=None, grad_weight=None,
+                       grad_bias=None, ws=None):
+    """(gradient of every slot's row of x, gradient of the weights); `grad_bias`, when given, receives the biases'."""
+    c, slots = _layer(x, weight, expert_pos, token, None, act)
+    experts, outer, inner = weight.shape
+    dev = x.device
+    ldgy = _matrix(grad_y, "grad_y", (slots, outer), x.dtype, dev)
+    ldpre = _matrix(pre, "pre", (slots, outer), x.dtype, dev) if pre is not None else 0
+    if grad_x is None:
+        grad_x = torch.empty((slots, inner), dtype=x.dtype, device=dev)
+    if grad_weight is None:
+        grad_weight = torch.empty((experts, outer, inner), dtype=x.dtype, device=dev)
+    ldgx = _matrix(grad_x, "grad_x", (slots, inner), x.dtype, dev)
+    ldgw, gap = _stack(grad_weight, "grad_weight", (experts, outer, inner), x.dtype, dev)
+    gb = _stack(grad_bias, "grad_bias", (experts, outer), x.dtype, dev)[1] if grad_bias is not None else 0
+    if ws is None:
+        n = C.c_size_t(0)
+        _check(lib().nacho_experts_workspace_bytes(C.byref(c), C.byref(n)), "nacho_experts_workspace_bytes")
+        ws = _workspace(n.value, dev) if n.value else None
+    _check(lib().nacho_experts_grad(C.byref(c), _ptr(grad_y), ldgy, _ptr(pre), ldpre, _ptr(grad_x), ldgx, _ptr(grad_weight),
+                                    ldgw, gap, _ptr(grad_bias), gb, _ptr(ws), ws.numel() if ws is not None else 0,
+                                    _stream()), "nacho_experts_grad")
+    return grad_x, grad_weight
 
 
 def _slots_of(pos, slot, gate, n_slots, device):

@@ -117,6 +117,45 @@ int32_t check_combine(const nacho_tensor *m, int64_t n, int32_t dtype, CombineAr
     return NACHO_OK;
 }
 
+// `count` matrices of rows x cols elements, `ld` and `stride` apart.
+bool matrices(const void *p, int64_t count, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int64_t elem)
+{
+    if (!matrix(p, count > 0 ? rows : 0, cols, ld, elem) || stride > kMostStride) return false;
+    return count <= 1 || rows == 0 || stride >= (rows - 1) * ld + cols;
+}
+int64_t span(int64_t count, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int64_t elem)
+{
+    return count > 0 ? (count - 1) * stride * elem + span(rows, cols, ld, elem) : 0;
+}
+
+int32_t check_layer(const nacho_experts_layer *l)
+{
+    if (!l || !value_type(l->dtype) || l->act < NACHO_ACT_NONE || l->act > NACHO_ACT_SILU) return NACHO_ERR_INVALID_ARG;
+    if (l->n_experts < 1 || l->n_slots < 0 || l->n_slots > kMostRows || l->n_tokens < 0 || l->n_tokens > kMostRows ||
+        l->inner < 1 || l->outer < 1)
+        return NACHO_ERR_INVALID_ARG;
+    if (l->n_experts > 65536 || l->inner >= 1 << 24 || l->outer >= 1 << 24) return NACHO_ERR_UNSUPPORTED;
+    if (!l->expert_pos || !aligned(l->expert_pos, 4) || !aligned(l->token, 4)) return NACHO_ERR_INVALID_ARG;
+    // (without a list of tokens a slot reads the row of its own number)
+    return !l->token && l->n_tokens < l->n_slots ? NACHO_ERR_INVALID_ARG : NACHO_OK;
+}
+bool check_x(const nacho_experts_layer *l, int64_t elem) { return matrix(l->x, l->n_tokens, l->inner, l->ldx, elem); }
+bool check_w(const nacho_experts_layer *l, int64_t elem)
+{
+    return matrices(l->w, l->n_experts, l->outer, l->inner, l->ldw, l->w_stride, elem);
+}
+bool overlaps_inputs(const nacho_experts_layer *l, const void *p, int64_t bytes, int64_t elem)
+{
+    return overlap(p, bytes, l->x, l->x ? span(l->n_tokens, l->inner, l->ldx, elem) : 0) ||
+           overlap(p, bytes, l->w, l->w ? span(l->n_experts, l->outer, l->inner, l->ldw, l->w_stride, elem) : 0);
+}
+
+// What a gradient call keeps: the gradient before the activation.
+int64_t grad_z_bytes(const nacho_experts_layer *l)
+{
+    return l->act == NACHO_ACT_NONE ? 0 : (int64_t)align_up((size_t)(l->n_slots * ((l->outer + 7) / 8 * 8) * value_bytes(l->dtype)), 256);
+}
+
 }  // namespace
 
 extern "C" {
@@ -256,6 +295,99 @@ int32_t nacho_combine_grad(const nacho_tensor *routing, const void *y, int64_t l
     profile_begin(s);
     if (launch_combine_grad(dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
     profile_mark("combine_grad");
+    return NACHO_OK;
+}
+
+int32_t nacho_experts_workspace_bytes(const nacho_experts_layer *layer, size_t *bytes)
+{
+    if (!bytes) return NACHO_ERR_INVALID_ARG;
+    const int32_t rc = check_layer(layer);
+    if (rc == NACHO_OK) *bytes = (size_t)grad_z_bytes(layer);
+    return rc;
+}
+
+int32_t nacho_experts(const nacho_experts_layer *layer, void *y, int64_t ldy, void *pre, int64_t ldpre, void *hip_stream)
+{
+    const int32_t rc = check_layer(layer);
+    if (rc != NACHO_OK) return rc;
+    const nacho_experts_layer &l = *layer;
+    const int64_t elem = value_bytes(l.dtype), bytes = span(l.n_slots, l.outer, ldy, elem);
+    if (!check_x(layer, elem) || !check_w(layer, elem) || !matrix(y, l.n_slots, l.outer, ldy, elem)) return NACHO_ERR_INVALID_ARG;
+    if (l.bias && !matrices(l.bias, l.n_experts, 1, l.outer, l.outer, l.bias_stride, elem)) return NACHO_ERR_INVALID_ARG;
+    if (overlaps_inputs(layer, y, bytes, elem)) return NACHO_ERR_INVALID_ARG;
+    if (pre) {
+        const int64_t pre_bytes = span(l.n_slots, l.outer, ldpre, elem);
+        if (!matrix(pre, l.n_slots, l.outer, ldpre, elem) || overlaps_inputs(layer, pre, pre_bytes, elem) ||
+            overlap(y, bytes, pre, pre_bytes))
+            return NACHO_ERR_INVALID_ARG;
+    }
+    const ProductArgs a{l.expert_pos, l.token, (int32_t)l.n_experts, 0, (int32_t)l.outer, (int32_t)l.inner, l.n_slots, l.x, l.w,
+                        l.ldx, l.ldw, l.w_stride, y, ldy, 0, l.bias, l.bias_stride, pre, ldpre, l.act};
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (launch_experts_forward(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+    profile_mark("experts");
+    return NACHO_OK;
+}
+
+int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y, int64_t ldgy, const void *pre, int64_t ldpre,
+                           void *grad_x, int64_t ldgx, void *grad_w, int64_t ldgw, int64_t gw_stride, void *grad_bias,
+                           int64_t gb_stride, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    const int32_t rc = check_layer(layer);
+    if (rc != NACHO_OK) return rc;
+    const nacho_experts_layer &l = *layer;
+    const int64_t elem = value_bytes(l.dtype), gy_bytes = span(l.n_slots, l.outer, ldgy, elem);
+    const bool slope = l.act != NACHO_ACT_NONE;
+    if (!matrix(grad_y, l.n_slots, l.outer, ldgy, elem) || (slope && !matrix(pre, l.n_slots, l.outer, ldpre, elem)) ||
+        (grad_x && !check_w(layer, elem)) || (grad_w && !check_x(layer, elem)))
+        return NACHO_ERR_INVALID_ARG;
+    const int64_t pre_bytes = slope ? span(l.n_slots, l.outer, ldpre, elem) : 0;
+    const int64_t gx_bytes = grad_x ? span(l.n_slots, l.inner, ldgx, elem) : 0;
+    const int64_t gw_bytes = grad_w ? span(l.n_experts, l.outer, l.inner, ldgw, gw_stride, elem) : 0;
+    const int64_t gb_bytes = grad_bias ? span(l.n_experts, 1, l.outer, l.outer, gb_stride, elem) : 0;
+    if ((grad_x && !matrix(grad_x, l.n_slots, l.inner, ldgx, elem)) ||
+        (grad_w && !matrices(grad_w, l.n_experts, l.outer, l.inner, ldgw, gw_stride, elem)) ||
+        (grad_bias && !matrices(grad_bias, l.n_experts, 1, l.outer, l.outer, gb_stride, elem)))
+        return NACHO_ERR_INVALID_ARG;
+    const void *outs[] = {grad_x, grad_w, grad_bias};
+    const int64_t sizes[] = {gx_bytes, gw_bytes, gb_bytes};
+    for (int i = 0; i < 3; ++i) {
+        if (overlaps_inputs(layer, outs[i], sizes[i], elem) || overlap(outs[i], sizes[i], grad_y, gy_bytes) ||
+            overlap(outs[i], sizes[i], pre, pre_bytes))
+            return NACHO_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlap(outs[i], sizes[i], outs[j], sizes[j])) return NACHO_ERR_INVALID_ARG;
+    }
+    const bool products = grad_x || grad_w;
+    const int64_t need = products ? grad_z_bytes(layer) : 0;
+    if (need > 0 && (!ws || (int64_t)ws_bytes < need || !aligned(ws, 16))) return NACHO_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    const void *gz = grad_y;
+    int64_t ldgz = ldgy;
+    if ((slope && products) || grad_bias) {
+        SlopeArgs a{l.expert_pos, (int32_t)l.n_experts, (int32_t)l.outer, l.act, l.n_slots, grad_y, pre, ldgy, ldpre, nullptr, 0,
+                    grad_bias, gb_stride};
+        if (slope && products) {
+            gz = a.grad_z = ws;
+            ldgz = a.ldgz = (l.outer + 7) / 8 * 8;
+        }
+        if (launch_experts_slope(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+        profile_mark("experts_slope");
+    }
+    if (grad_x) {
+        const ProductArgs a{l.expert_pos, nullptr, (int32_t)l.n_experts, 0, (int32_t)l.inner, (int32_t)l.outer, l.n_slots, gz, l.w,
+                            ldgz, l.ldw, l.w_stride, grad_x, ldgx, 0, nullptr, 0, nullptr, 0, NACHO_ACT_NONE};
+        if (launch_experts_rows(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+        profile_mark("experts_rows");
+    }
+    if (grad_w) {
+        const ProductArgs a{l.expert_pos, l.token, (int32_t)l.n_experts, (int32_t)l.outer, (int32_t)l.inner, 0, l.n_slots, gz, l.x,
+                            ldgz, l.ldx, 0, grad_w, ldgw, gw_stride, nullptr, 0, nullptr, 0, NACHO_ACT_NONE};
+        if (launch_experts_weights(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+        profile_mark("experts_weights");
+    }
     return NACHO_OK;
 }
 

@@ -78,4 +78,40 @@ struct CombineArgs {
 hipError_t launch_combine(int dtype, const CombineArgs &a, hipStream_t s);
 hipError_t launch_combine_grad(int dtype, const CombineArgs &a, hipStream_t s);
 
+// ---- the experts' products -----------------------------------------------------
+// out[m][n] = sum_k Q(m, k) P(n, k) for every expert, in one of three forms:
+//   forward   m: slots, n: outer, k: inner   Q = x[token], P = w[e]            + bias, activation
+//   rows      m: slots, n: inner, k: outer   Q = grad_z,   P = w[e] transposed
+//   weights   m: outer, n: inner, k: slots   Q = grad_z transposed, P = x[token] transposed
+struct ProductArgs {
+    const int32_t *bounds, *token; // token: may be NULL (forward, weights)
+    int32_t experts, m, n, k;      // sizes, but for the one that is the slots
+    int64_t slots;                 // at most
+    const void *q, *p;
+    int64_t ldq, ldp, p_stride;    // p_stride: from expert to expert
+    void *out;
+    int64_t ldo, out_stride;
+    const void *bias;              // may be NULL
+    int64_t bias_stride;
+    void *pre;                     // may be NULL
+    int64_t ldpre;
+    int32_t act;
+};
+hipError_t launch_experts_forward(int dtype, const ProductArgs &a, hipStream_t s);
+hipError_t launch_experts_rows(int dtype, const ProductArgs &a, hipStream_t s);
+hipError_t launch_experts_weights(int dtype, const ProductArgs &a, hipStream_t s);
+// grad_z = grad_y act'(pre), and the sums of its rows by expert (grad_bias, may be NULL).  grad_z may be NULL: not wanted.
+struct SlopeArgs {
+    const int32_t *bounds;
+    int32_t experts, cols, act;
+    int64_t slots;
+    const void *grad_y, *pre;
+    int64_t ldgy, ldpre;
+    void *grad_z;
+    int64_t ldgz;
+    void *grad_bias;
+    int64_t bias_stride;
+};
+hipError_t launch_experts_slope(int dtype, const SlopeArgs &a, hipStream_t s);
+
 }  // namespace nacho
