@@ -325,7 +325,7 @@ int32_t nacho_experts(const nacho_experts_layer *layer, void *y, int64_t ldy, vo
                         l.ldx, l.ldw, l.w_stride, y, ldy, 0, l.bias, l.bias_stride, pre, ldpre, l.act};
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     profile_begin(s);
-    if (launch_experts_forward(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+    if (const hipError_t e = launch_experts_forward(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
     profile_mark("experts");
     return NACHO_OK;
 }
@@ -379,13 +379,13 @@ int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y,
     if (grad_x) {
         const ProductArgs a{l.expert_pos, nullptr, (int32_t)l.n_experts, 0, (int32_t)l.inner, (int32_t)l.outer, l.n_slots, gz, l.w,
                             ldgz, l.ldw, l.w_stride, grad_x, ldgx, 0, nullptr, 0, nullptr, 0, NACHO_ACT_NONE};
-        if (launch_experts_rows(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+        if (const hipError_t e = launch_experts_rows(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
         profile_mark("experts_rows");
     }
     if (grad_w) {
         const ProductArgs a{l.expert_pos, l.token, (int32_t)l.n_experts, (int32_t)l.outer, (int32_t)l.inner, 0, l.n_slots, gz, l.x,
                             ldgz, l.ldx, 0, grad_w, ldgw, gw_stride, nullptr, 0, nullptr, 0, NACHO_ACT_NONE};
-        if (launch_experts_weights(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+        if (const hipError_t e = launch_experts_weights(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
         profile_mark("experts_weights");
     }
     return NACHO_OK;

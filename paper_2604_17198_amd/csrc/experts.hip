@@ -18,7 +18,7 @@ namespace nacho {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / NACHO_WAVE;
+constexpr int kThreads = 256;
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned int v4u __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
@@ -105,63 +105,115 @@ template <int kM> __device__ inline bool find_tile(const ProductArgs &a, int til
     return false;
 }
 
-// A side of the product: kRows rows (of Q or P), kStep bytes of k of each.
-constexpr int kStep = 128, kUnits = kStep / 16;        // 16-byte words of k a row
-template <typename T> constexpr int kDepth = kStep / (int)sizeof(T);
+// A side of the product: kRows rows (of Q or P), kStep bytes of k of each, loaded by kThreads threads.
+template <typename T, int kStep> constexpr int kDepth = kStep / (int)sizeof(T);
 
-// Rows that run along k.  A thread loads the words `unit` of the rows tid / kUnits + i * 32.
-template <typename T, int kRows, bool kWords> struct AlongK {
-    static constexpr int kLoads = kRows * kUnits / kThreads, kBytes = kRows * kStep;
-    const T *row[kLoads];
+// 16 bytes from every lane's own address to LDS, one lane's behind the other's from `to` on (the same for the whole
+// wavefront); not there before wait_loads has counted it.
+__device__ inline void load_to_lds(const void *from, char *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+// Waits until the wavefront's loads and LDS reads are there, then for the workgroup.  (The builtin: the compiler counts
+// the loads to LDS too, and waits again for those it does not see waited for.)
+__device__ inline void wait_loads()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x70);          // vmcnt 0, lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// The address of row `row` of rows `ld` < 2^31 elements apart: one instruction where it is needed (the compiler would
+// keep running addresses of every row in registers that the results need).
+template <typename T> __device__ inline const T *at_row(const T *base, int row, int64_t ld)
+{
+    asm volatile("" : "+v"(row));
+    return base + (uint64_t)(unsigned)row * (unsigned)ld;
+}
+
+// 16 bytes from any element's address, in one instruction (global memory takes any alignment); with `there` < n elements
+// left the others are zero.
+template <typename T> __device__ inline v4u load_anywhere(const T *from, int there)
+{
+    constexpr int n = Word<T>::n;
+    v4u word = {0, 0, 0, 0};
+    if (there >= n) __builtin_memcpy(&word, from, 16);
+    else if (there > 0) {
+        typename Word<T>::type v;
+#pragma unroll
+        for (int e = 0; e < n; ++e) v[e] = e < there ? from[e] : (T)0.0f;
+        word = __builtin_bit_cast(v4u, v);
+    }
+    return word;
+}
+
+// Rows that run along k.  A thread loads words of 16 bytes, the same one of several rows.
+template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct AlongK {
+    static constexpr int kUnits = kStep / 16, kApart = kThreads / kUnits;
+    static constexpr int kLoads = kRows / kApart, kBytes = kRows * kStep;
+    static_assert(kLoads * kApart == kRows, "a whole number of rows a thread");
+    const T *base;
+    int64_t ld;
+    int row[kLoads];
     v4u word[kLoads];
     int unit, at;
 
-    template <typename Row> __device__ void start(Row address)
+    // number(r): which row of the matrix is row r of the tile.
+    template <typename Row> __device__ void start(const T *matrix, int64_t apart, Row number)
     {
+        base = matrix;
+        ld = apart;
         unit = (int)threadIdx.x % kUnits;
         at = (int)threadIdx.x / kUnits;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) row[i] = address(at + i * (kThreads / kUnits));
+        for (int i = 0; i < kLoads; ++i) row[i] = number(at + i * kApart);
     }
     __device__ void load(int k0, int k)
     {
         constexpr int n = Word<T>::n;
         const int first = k0 + unit * n;
-        if constexpr (kWords) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) word[i] = first < k ? *reinterpret_cast<const v4u *>(row[i] + first) : v4u{0, 0, 0, 0};
-        } else {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                typename Word<T>::type v;
-#pragma unroll
-                for (int e = 0; e < n; ++e) v[e] = first + e < k ? row[i][first + e] : (T)0.0f;
-                word[i] = __builtin_bit_cast(v4u, v);
-            }
+        for (int i = 0; i < kLoads; ++i) {
+            const T *from = base + row[i] * ld + first;
+            if constexpr (kWords) word[i] = first < k ? *reinterpret_cast<const v4u *>(from) : v4u{0, 0, 0, 0};
+            else word[i] = load_anywhere(from, k - first);
         }
     }
-    // (8 rows' words of one column of the tile lie in all 8 columns: the 8 lanes that the LDS serves at a time read
-    // different banks)
+    // Asks for the words k0 .. of all rows (whole words).  What a lane loads lies behind what the lane before it loads,
+    // so the lanes share out the words of a row in the order in which they lie.
+    __device__ void ask(int k0, char *lds) const
+    {
+        static_assert(kApart % 8 == 0, "the same turn for all rows of a thread");
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / NACHO_WAVE);
+        const int first = k0 + (unit ^ turn(at)) * Word<T>::n;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load_to_lds(at_row(base, row[i], ld) + first, lds + (i * kThreads + wave * NACHO_WAVE) * 16);
+    }
+    // Where word u of row r lies: the same word of 8 consecutive rows, which the LDS serves at a time, in 8 different
+    // sixteens of bytes of 128.
+    static __device__ int turn(int r) { return kUnits == 8 ? r & 7 : r >> 1 & 3; }
+    static __device__ int place(int r, int u) { return r * kStep + ((u ^ turn(r)) << 4); }
     __device__ void store(char *lds) const
     {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int r = at + i * (kThreads / kUnits);
-            *reinterpret_cast<v4u *>(lds + r * kStep + ((unit ^ (r & 7)) << 4)) = word[i];
-        }
+        for (int i = 0; i < kLoads; ++i) *reinterpret_cast<v4u *>(lds + place(at + i * kApart, unit)) = word[i];
     }
-    // The lane's 16 bytes of rows r0 .. r0 + 15 in step `step` of 64 bytes.
-    static __device__ v4u fragment(const char *lds, int r0, int step)
+    // Where a lane's fragments of the rows from r0 on (a multiple of 16) start; and its 16 bytes of rows 16 number ..
+    // from there in step `step` of 64 bytes.
+    static __device__ int lane_base(int r0) { return r0 * kStep + lane_id() % 16 * kStep; }
+    static __device__ v4u fragment(const char *lds, int base, int number, int step)
     {
-        const int lane = lane_id(), r = r0 + lane % 16, u = step * 4 + lane / 16;
-        return *reinterpret_cast<const v4u *>(lds + r * kStep + ((u ^ (r & 7)) << 4));
+        const int u = (step * 4 + lane_id() / 16) ^ turn(lane_id() % 16);
+        return *reinterpret_cast<const v4u *>(lds + base + number * 16 * kStep + (u << 4));
     }
 };
 
 // Columns that run along k: for every k a row of kRows elements.
-template <typename T, int kRows, bool kWords> struct AcrossK {
+template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct AcrossK {
     static constexpr int kRowBytes = kRows * (int)sizeof(T), kRowWords = kRowBytes / 16;
-    static constexpr int kLoads = kDepth<T> * kRowWords / kThreads, kBytes = kDepth<T> * kRowBytes;
+    static constexpr int kLoads = kDepth<T, kStep> * kRowWords / kThreads, kBytes = kDepth<T, kStep> * kRowBytes;
+    static_assert(kRowWords >= 16 && kLoads * kThreads == kDepth<T, kStep> * kRowWords, "rows that the turns fit into");
     v4u word[kLoads];
 
     // address(k): the row of k; `most`: elements of it from the tile's first one on.
@@ -175,22 +227,28 @@ template <typename T, int kRows, bool kWords> struct AcrossK {
             if (kk < k && first < most) {
                 const T *from = address(kk) + first;
                 if constexpr (kWords) word[i] = *reinterpret_cast<const v4u *>(from);
-                else {
-                    typename Word<T>::type v;
-#pragma unroll
-                    for (int e = 0; e < n; ++e) v[e] = first + e < most ? from[e] : (T)0.0f;
-                    word[i] = __builtin_bit_cast(v4u, v);
-                }
+                else word[i] = load_anywhere(from, most - first);
             }
+        }
+    }
+    // Asks for the rows of k0 ..; address(i, kk): the row of kk, which is k0 or more by i threads' words.  (Words behind
+    // the last: the last one again, whose results are not stored.)
+    static __device__ int row_of_load(int i) { return (int)threadIdx.x / kRowWords + i * (kThreads / kRowWords); }
+    template <typename Row> __device__ void ask(Row address, int k0, int most, char *lds) const
+    {
+        constexpr int n = Word<T>::n;
+        constexpr bool kSame = kThreads / kRowWords % 16 == 0;           // (the same turn for all rows of a thread)
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / NACHO_WAVE);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int first = ((int)threadIdx.x % kRowWords ^ turn(row_of_load(kSame ? 0 : i))) * n;
+            load_to_lds(address(i, k0 + row_of_load(i)) + (first < most ? first : most - n), lds + (i * kThreads + wave * NACHO_WAVE) * 16);
         }
     }
     // Where word w of the row of k lies: rows that are read together by one instruction lie in different banks, 32
     // bytes (16-bit types: rows k .. k + 3 of two fours of eight) or 64 bytes (floats: rows 4 apart) of each.
-    static __device__ int place(int k, int w)
-    {
-        const int turn = sizeof(T) == 2 ? ((k & 3) | (k >> 1 & 4)) << 1 : (k >> 2 & 3) << 2;
-        return k * kRowBytes + ((w ^ turn) << 4);
-    }
+    static __device__ int turn(int k) { return sizeof(T) == 2 ? ((k & 3) | (k >> 1 & 4)) << 1 : (k >> 2 & 3) << 2; }
+    static __device__ int place(int k, int w) { return k * kRowBytes + ((w ^ turn(k)) << 4); }
     __device__ void store(char *lds) const
     {
 #pragma unroll
@@ -199,7 +257,8 @@ template <typename T, int kRows, bool kWords> struct AcrossK {
             *reinterpret_cast<v4u *>(lds + place(u / kRowWords, u % kRowWords)) = word[i];
         }
     }
-    static __device__ v4u fragment(const char *lds, int r0, int step)
+    static __device__ int lane_base(int r0) { return r0 * (int)sizeof(T); }
+    static __device__ v4u fragment(const char *lds, int base, int number, int step)
     {
         const int lane = lane_id(), four = lane / 16, i = lane % 16;
         if constexpr (sizeof(T) == 2) {
@@ -207,15 +266,15 @@ template <typename T, int kRows, bool kWords> struct AcrossK {
             v4s part[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int k = step * 32 + four * 8 + h * 4 + i / 4, byte = (r0 + (i % 4) * 4) * 2;
-                const char *at = lds + place(k, byte >> 4) + (byte & 15);
+                const int k = four * 8 + i / 4, byte = base + number * 32 + i % 4 * 8;       // (h and step turn nothing)
+                const char *at = lds + (step * 32 + h * 4) * kRowBytes + place(k, byte >> 4) + (byte & 15);
                 part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)at);
             }
             typedef short v8s __attribute__((ext_vector_type(8)));
             return __builtin_bit_cast(v4u, (v8s)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             v4u v;
-            const int byte = (r0 + i) * 4;
+            const int byte = base + number * 64 + i * 4;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int k = step * 16 + four * 4 + j;
@@ -226,16 +285,41 @@ template <typename T, int kRows, bool kWords> struct AcrossK {
     }
 };
 
-// One tile of kM x kN results; kWavesM x kWavesN wavefronts share it.
-template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, bool kWords>
-__global__ void __launch_bounds__(kThreads) experts_kernel(ProductArgs a, int tiles_n)
+template <typename F, int... i> __device__ inline void unrolled(F f, std::integer_sequence<int, i...>)
 {
-    static_assert(kWavesM * kWavesN == kWaves, "four wavefronts");
-    constexpr int kTileM = kM / kWavesM, kTileN = kN / kWavesN, kFragM = kTileM / 16, kFragN = kTileN / 16;
-    constexpr bool kAcrossQ = kForm == WEIGHTS, kAcrossP = kForm != FORWARD;
-    typedef std::conditional_t<kAcrossQ, AcrossK<T, kM, kWords>, AlongK<T, kM, kWords>> SideQ;
-    typedef std::conditional_t<kAcrossP, AcrossK<T, kN, kWords>, AlongK<T, kN, kWords>> SideP;
-    __shared__ __attribute__((aligned(16))) char lds[2][SideQ::kBytes + SideP::kBytes];
+    (f(std::integral_constant<int, i>()), ...);
+}
+template <int n, typename F> __device__ inline void unrolled(F f) { unrolled(f, std::make_integer_sequence<int, n>()); }
+
+// One tile of kM x kN results; kWavesM x kWavesN wavefronts share it.
+template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, bool kWords> struct Tile {
+    static constexpr int kThreads = kWavesM * kWavesN * NACHO_WAVE;
+    static constexpr int kTileM = kM / kWavesM, kTileN = kN / kWavesN, kFragM = kTileM / 16, kFragN = kTileN / 16;
+    static constexpr bool kAcrossQ = kForm == WEIGHTS, kAcrossP = kForm != FORWARD;
+    typedef std::conditional_t<kAcrossQ, AcrossK<T, kM, kStep, kThreads, kWords>, AlongK<T, kM, kStep, kThreads, kWords>> SideQ;
+    typedef std::conditional_t<kAcrossP, AcrossK<T, kN, kStep, kThreads, kWords>, AlongK<T, kN, kStep, kThreads, kWords>> SideP;
+    static constexpr int kBytes = SideQ::kBytes + SideP::kBytes;
+    // (The stages are arguments that do not overlap: so the compiler knows that reads of one do not wait for loads to the
+    // other, also those reads that transpose.)
+    static __device__ void compute(const ProductArgs &a, int tiles_n, char *__restrict stage0, char *__restrict stage1);
+};
+
+template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, bool kWords>
+__global__ void __launch_bounds__(kWavesM * kWavesN * NACHO_WAVE) experts_kernel(ProductArgs a, int tiles_n)
+{
+    typedef Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords> Work;
+    __shared__ __attribute__((aligned(16))) char stage0[Work::kBytes], stage1[Work::kBytes];
+    Work::compute(a, tiles_n, stage0, stage1);
+}
+
+template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, bool kWords>
+__device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::compute(const ProductArgs &a, int tiles_n,
+                                                                                        char *__restrict stage0, char *__restrict stage1)
+{
+    auto stage = [&](auto i) -> char * {
+        if constexpr (decltype(i)::value == 0) return stage0;
+        else return stage1;
+    };
     const int number = (int)(blockIdx.y * gridDim.x + blockIdx.x), tile = number / tiles_n, n0 = (number - tile * tiles_n) * kN;
     int expert, m0, m_end, k_begin = 0, k = a.k;
     if (kForm == WEIGHTS) {
@@ -253,11 +337,11 @@ __global__ void __launch_bounds__(kThreads) experts_kernel(ProductArgs a, int ti
     SideP side_p;
     // rows behind the last: the last one again, whose results are not stored
     if constexpr (!kAcrossQ)
-        side_q.start([&](int r) {
+        side_q.start(q, a.ldq, [&](int r) {
             const int row = m0 + r < m_end ? m0 + r : m_end - 1;
-            return q + (int64_t)(kForm == FORWARD && a.token ? a.token[row] : row) * a.ldq;
+            return kForm == FORWARD && a.token ? a.token[row] : row;
         });
-    if constexpr (!kAcrossP) side_p.start([&](int r) { return p + (int64_t)(n0 + r < a.n ? n0 + r : a.n - 1) * a.ldp; });
+    if constexpr (!kAcrossP) side_p.start(p, a.ldp, [&](int r) { return n0 + r < a.n ? n0 + r : a.n - 1; });
     auto load = [&](int k0) {
         if constexpr (kAcrossQ)
             side_q.load([&](int kk) { return q + (int64_t)(k_begin + kk) * a.ldq + m0; }, k0, k, a.m - m0);
@@ -277,73 +361,201 @@ __global__ void __launch_bounds__(kThreads) experts_kernel(ProductArgs a, int ti
     for (int i = 0; i < kFragM; ++i)
 #pragma unroll
         for (int j = 0; j < kFragN; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    if (k > 0) {
-        load(0);
-        side_q.store(lds[0]);
-        side_p.store(lds[0] + SideQ::kBytes);
-        __syncthreads();
-        int buffer = 0;
-        for (int k0 = 0; k0 < k; k0 += kDepth<T>) {
-            const bool more = k0 + kDepth<T> < k;
-            if (more) load(k0 + kDepth<T>);
+    int base_q = SideQ::lane_base(wm), base_p = SideP::lane_base(wn);
+    // A wavefront multiplies two of its rows of fragments at a time (or its only one); what the next ones need is read before.
+    constexpr int kPart = kFragM > 1 ? 2 : 1, kParts = kFragM / kPart, kSteps = kStep / 64;
+    static_assert(kFragM % kPart == 0 && kSteps % 2 == 0, "registers of P and of Q in turn");
+    v4u fp[2][kFragN], fq[2][kPart];
+    auto read_p = [&](const char *lds, auto step) {
+        constexpr int s = decltype(step)::value;
 #pragma unroll
-            for (int step = 0; step < kStep / 64; ++step) {
-                v4u fp[kFragN];
+        for (int j = 0; j < kFragN; ++j) fp[s % 2][j] = SideP::fragment(lds + SideQ::kBytes, base_p, j, s);
+    };
+    auto read_q = [&](const char *lds, auto step, auto part) {
+        constexpr int s = decltype(step)::value, h = decltype(part)::value;
 #pragma unroll
-                for (int j = 0; j < kFragN; ++j) fp[j] = SideP::fragment(lds[buffer] + SideQ::kBytes, wn + j * 16, step);
+        for (int i = 0; i < kPart; ++i) fq[(s * kParts + h) % 2][i] = SideQ::fragment(lds, base_q, h * kPart + i, s);
+    };
+    // (nothing moves across: what is read before it is on its way while it runs)
+    auto multiply = [&](auto step, auto part) {
+        constexpr int s = decltype(step)::value, h = decltype(part)::value;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < kFragM; ++i) {
-                    const v4u fq = SideQ::fragment(lds[buffer], wm + i * 16, step);
+        for (int i = 0; i < kPart; ++i)
 #pragma unroll
-                    for (int j = 0; j < kFragN; ++j) acc[i][j] = matrix_step<T>(fp[j], fq, acc[i][j]);
+            for (int j = 0; j < kFragN; ++j)
+                acc[h * kPart + i][j] = matrix_step<T>(fp[s % 2][j], fq[(s * kParts + h) % 2][i], acc[h * kPart + i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const std::integral_constant<int, 0> zero;
+    const std::integral_constant<int, 1> one;
+    // A step of k that is there, without one behind it.
+    auto multiply_all = [&](const char *lds) {
+        unrolled<kSteps>([&](auto step) {
+            read_p(lds, step);
+            unrolled<kParts>([&](auto part) {
+                read_q(lds, step, part);
+                multiply(step, part);
+            });
+        });
+    };
+    constexpr int kDeep = kDepth<T, kStep>;
+    int done = 0;
+    if constexpr (kWords) {
+        // Whole steps of k.  One is on its way to LDS while the one before it is multiplied; and while the matrix units
+        // have one half of a wavefront's tile, the registers of the next half are read.
+        const int steps = k / kDeep;
+        int slot[kForm == WEIGHTS ? SideP::kLoads : 1];       // rows of x that the words of the next step come from
+        auto look_up = [&](int t) {
+            if constexpr (kForm == WEIGHTS) {
+                const int s = k_begin + (t < steps ? t : steps - 1) * kDeep;
+#pragma unroll
+                for (int l = 0; l < SideP::kLoads; ++l) slot[l] = s + SideP::row_of_load(l);
+                if (a.token) {
+#pragma unroll
+                    for (int l = 0; l < SideP::kLoads; ++l) slot[l] = a.token[slot[l]];
                 }
             }
-            if (more) {
-                side_q.store(lds[buffer ^ 1]);
-                side_p.store(lds[buffer ^ 1] + SideQ::kBytes);
+        };
+        // (i: of stage t)
+        auto ask = [&](int t, auto i) {
+            char *lds = stage(i);
+            if constexpr (kAcrossQ) side_q.ask([&](int, int kk) { return at_row(q + m0, k_begin + kk, a.ldq); }, t * kDeep, a.m - m0, lds);
+            else side_q.ask(t * kDeep, lds);
+            if constexpr (kForm == WEIGHTS)
+                side_p.ask([&](int l, int) { return at_row(p + n0, slot[l], a.ldp); }, t * kDeep, a.n - n0, lds + SideQ::kBytes);
+            else if constexpr (kForm == ROWS)
+                side_p.ask([&](int, int kk) { return at_row(p + n0, kk, a.ldp); }, t * kDeep, a.n - n0, lds + SideQ::kBytes);
+            else side_p.ask(t * kDeep, lds + SideQ::kBytes);
+            look_up(t + 1);
+        };
+        // (Behind the last step the next one's registers are read all the same, and not used: a wait that is not there on
+        // every path would have the compiler wait for all loads before it reads.)
+        auto body = [&](int t, auto which) {
+            // (or the compiler keeps the address of every fragment in a register of its own)
+            asm volatile("" : "+v"(base_q), "+v"(base_p));
+            const std::integral_constant<int, 1 - decltype(which)::value> other;
+            unrolled<kSteps>([&](auto step) {
+                constexpr int s = decltype(step)::value;
+                unrolled<kParts>([&](auto part) {
+                    constexpr int h = decltype(part)::value;
+                    if constexpr (h + 1 < kParts) {
+                        read_q(stage(which), step, std::integral_constant<int, h + 1>());
+                    } else if constexpr (s + 1 < kSteps) {
+                        const std::integral_constant<int, s + 1> behind;
+                        read_p(stage(which), behind);
+                        read_q(stage(which), behind, zero);
+                    } else {
+                        wait_loads();
+                        if (t + 2 < steps) ask(t + 2, which);
+                        read_p(stage(other), zero);
+                        read_q(stage(other), zero, zero);
+                    }
+                    multiply(step, part);
+                });
+            });
+        };
+        if (steps > 0) {
+            look_up(0);
+            ask(0, zero);
+            wait_loads();
+            if (steps > 1) ask(1, one);
+            read_p(stage0, zero);
+            read_q(stage0, zero, zero);
+            int t = 0;
+            for (; t + 2 <= steps; t += 2) {
+                body(t, zero);
+                body(t + 1, one);
             }
-            __syncthreads();
-            buffer ^= 1;
+            if (t < steps) body(t, zero);
+        }
+        done = steps * kDeep;
+        __syncthreads();
+    }
+    if (done < k) {
+        load(done);
+        side_q.store(stage0);
+        side_p.store(stage0 + SideQ::kBytes);
+        __syncthreads();
+        for (; done < k; done += kDeep) {
+            const bool more = !kWords && done + kDeep < k;
+            if (more) load(done + kDeep);
+            multiply_all(stage0);
+            if (more) {
+                __syncthreads();
+                side_q.store(stage0);
+                side_p.store(stage0 + SideQ::kBytes);
+                __syncthreads();
+            }
         }
     }
-    // a lane has four consecutive columns of result row lane % 16 of every 16 x 16
+    // A lane has four consecutive columns of result row lane % 16 of every 16 x 16.  A wavefront takes its tile through its
+    // part of LDS, so that lanes that store side by side have neighbouring parts of a row, eight columns each.
+    __syncthreads();
+    constexpr int kRowBytes = kTileN * 4, kLanes = kTileN / 8, kPerWave = 2 * kBytes / (kThreads / NACHO_WAVE) / 1024 * 1024;
+    constexpr int kPhase = kPerWave / (16 * kRowBytes) < kFragM ? kPerWave / (16 * kRowBytes) : kFragM;
+    static_assert(kFragM % kPhase == 0 && kBytes % kPerWave == 0, "a wavefront's part lies in one stage");
+    char *const mine = (wave < kBytes / kPerWave ? stage0 : stage1) + wave % (kBytes / kPerWave) * kPerWave;
     T *const out = static_cast<T *>(a.out) + (kForm == WEIGHTS ? (int64_t)expert * a.out_stride : 0);
-    typedef T four __attribute__((ext_vector_type(4)));
+    const int n = n0 + wn + lane % kLanes * 8, width = a.n - n;
+    float bias[8];
 #pragma unroll
-    for (int i = 0; i < kFragM; ++i) {
-        const int m = m0 + wm + i * 16 + lane % 16;
-        if (m >= m_end) continue;
+    for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
+    if (kForm == FORWARD && a.bias) {
+        const T *b = static_cast<const T *>(a.bias) + (int64_t)expert * a.bias_stride + n;
 #pragma unroll
-        for (int j = 0; j < kFragN; ++j) {
-            const int n = n0 + wn + j * 16 + lane / 16 * 4;
-            v4f v = acc[i][j];
-            if (kForm == FORWARD && a.bias) {
-                const T *b = static_cast<const T *>(a.bias) + (int64_t)expert * a.bias_stride + n;
+        for (int e = 0; e < 8; ++e)
+            if (e < width) bias[e] = wide(b[e]);
+    }
+    auto put = [&](T *to, const float (&v)[8]) {
+        constexpr int kWord = Word<T>::n;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += n + e < a.n ? wide(b[e]) : 0.0f;
+        for (int h = 0; h < 8; h += kWord) {
+            if (h + kWord <= width) {
+                typename Word<T>::type w;
+#pragma unroll
+                for (int e = 0; e < kWord; ++e) w[e] = (T)v[h + e];
+                if constexpr (kWords) *reinterpret_cast<typename Word<T>::type *>(to + h) = w;
+                else __builtin_memcpy(to + h, &w, 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kWord; ++e)
+                    if (h + e < width) to[h + e] = (T)v[h + e];
             }
-            auto put = [&](T *to, const v4f &x) {
-                if (kWords && n + 4 <= a.n) {
-                    four w;
+        }
+    };
+    unrolled<kFragM / kPhase>([&](auto phase) {
+        constexpr int i0 = decltype(phase)::value * kPhase;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = (T)x[e];
-                    *reinterpret_cast<four *>(to) = w;
-                } else {
+        for (int i = 0; i < kPhase; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (n + e < a.n) to[e] = (T)x[e];
-                }
-            };
+            for (int j = 0; j < kFragN; ++j) {
+                const int r = lane % 16, unit = (j * 4 + lane / 16) ^ (r & 7);
+                *reinterpret_cast<v4f *>(mine + (i * 16 + r) * kRowBytes + unit * 16) = acc[i0 + i][j];
+            }
+        wave_sync();
+#pragma unroll 1
+        for (int r = lane / kLanes; r < kPhase * 16; r += NACHO_WAVE / kLanes) {
+            const int m = m0 + wm + i0 * 16 + r;
+            if (m >= m_end || width <= 0) break;
+            float v[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const v4f part = *reinterpret_cast<const v4f *>(mine + r * kRowBytes + (((lane % kLanes * 2 + h) ^ (r & 7)) << 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[h * 4 + e] = part[e] + bias[h * 4 + e];
+            }
             if (kForm == FORWARD) {
                 if (a.pre) put(static_cast<T *>(a.pre) + (int64_t)m * a.ldpre + n, v);
                 if (a.act != NACHO_ACT_NONE) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = activated(v[e], a.act);
+                    for (int e = 0; e < 8; ++e) v[e] = activated(v[e], a.act);
                 }
             }
             put(out + (int64_t)m * a.ldo + n, v);
         }
-    }
+        wave_sync();
+    });
 }
 
 // grad_z = grad_y act'(pre), a thread N consecutive elements at a time.
@@ -420,27 +632,63 @@ bool in_words(std::initializer_list<std::pair<const void *, int64_t>> all, int e
     return bits % 16 == 0;
 }
 
-template <Form kForm> hipError_t launch(int dtype, const ProductArgs &a, hipStream_t s)
+template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, bool kWords>
+hipError_t run(const ProductArgs &a, hipStream_t s)
 {
-    constexpr int kM = 128, kN = 128;
-    const int elem = dtype == NACHO_F32 ? 4 : 2;
     const int tiles_n = (a.n + kN - 1) / kN;
     // tiles of rows: as many as the slots fill, and a part of one for every expert that may have any
     const int64_t tiles_m = kForm == WEIGHTS ? (int64_t)a.experts * ((a.m + kM - 1) / kM)
                                              : a.slots / kM + (a.slots < a.experts ? a.slots : a.experts);
     if (tiles_m == 0) return hipSuccess;
     // (a launch holds 2^32 threads along its first dimension)
-    const int64_t tiles = tiles_m * tiles_n, wide_grid = tiles < (1 << 22) ? tiles : 1 << 22;
+    const int64_t tiles = tiles_m * tiles_n, row = tiles < (1 << 22) ? tiles : 1 << 22;
     if (tiles > 0x7fffffff - (1 << 22)) return hipErrorNotSupported;
-    const bool words = in_words({{a.q, a.ldq}, {a.p, a.ldp}, {a.p, a.p_stride}, {a.out, a.ldo}, {a.out, a.out_stride}, {a.pre, a.ldpre},
-                                 {a.q, kForm == WEIGHTS ? 0 : a.k}, {a.q, kForm == WEIGHTS ? a.m : 0}, {a.q, kForm == FORWARD ? 0 : a.n}}, elem);
-    const dim3 grid((unsigned)wide_grid, (unsigned)((tiles + wide_grid - 1) / wide_grid));
-    by_type(dtype, [&](auto zero) {
-        typedef decltype(zero) T;
-        if (words) experts_kernel<T, kForm, kM, kN, 2, 2, true><<<grid, kThreads, 0, s>>>(a, tiles_n);
-        else experts_kernel<T, kForm, kM, kN, 2, 2, false><<<grid, kThreads, 0, s>>>(a, tiles_n);
-    });
+    experts_kernel<T, kForm, kM, kN, kWavesM, kWavesN, 128, kWords>
+        <<<dim3((unsigned)row, (unsigned)((tiles + row - 1) / row)), kWavesM * kWavesN * NACHO_WAVE, 0, s>>>(a, tiles_n);
     return hipGetLastError();
+}
+
+constexpr int64_t kUnits = 256;        // compute units
+
+// Tiles of 256 x 256 need half the LDS reads of tiles of 128 x 128 for the same results, but leave more of a tile empty
+// and fill the chip only if there are many of them.  16384 slots bf16, us: 16 experts (1024 slots each), 2048 x 8192, forward
+// 579 and 900, rows 670 and 749, weights 702 and 793; 32 experts (512 each), 1024 x 4096, 217 and 209, 239 and 241, 236 and 309.
+// Tiles of 32 x 128 for few slots an expert, where the weights are what is read, and where larger ones would leave compute
+// units without one: 16 slots of 32 experts, 2048 x 4096, forward 26 (128 x 128: 37), rows 37 (47); 1200 of 24, 1024 x 4096, 36
+// (43), 41 (50).
+template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, bool words, hipStream_t s)
+{
+    const int64_t each = a.slots / a.experts, n128 = (a.n + 127) / 128;
+    if constexpr (kForm == WEIGHTS) {
+        const int64_t tiles = (int64_t)a.experts * ((a.m + 255) / 256) * ((a.n + 255) / 256);
+        if constexpr (sizeof(T) == 2) {
+            if (words && a.m >= 256 && a.n >= 256 && tiles >= kUnits) return run<T, kForm, 256, 256, 2, 4, true>(a, s);
+        } else if (tiles < kUnits) {
+            // (floats: four times as many matrix instructions for a load; 3000 slots of 7 experts, 777 x 499)
+            return words ? run<T, kForm, 64, 128, 1, 4, true>(a, s) : run<T, kForm, 64, 128, 1, 4, false>(a, s);
+        }
+        return words ? run<T, kForm, 128, 128, 2, 2, true>(a, s) : run<T, kForm, 128, 128, 2, 2, false>(a, s);
+    } else {
+        if constexpr (sizeof(T) == 2) {
+            if (words && each >= 512 && a.n >= 256 && a.slots / 256 * ((a.n + 255) / 256) >= kUnits)
+                return run<T, kForm, 256, 256, 2, 4, true>(a, s);
+        }
+        if (each <= 64 || a.slots / 128 * n128 < 2 * kUnits)
+            return words ? run<T, kForm, 32, 128, 1, 4, true>(a, s) : run<T, kForm, 32, 128, 1, 4, false>(a, s);
+        return words ? run<T, kForm, 128, 128, 2, 2, true>(a, s) : run<T, kForm, 128, 128, 2, 2, false>(a, s);
+    }
+}
+
+template <Form kForm> hipError_t launch(int dtype, const ProductArgs &a, hipStream_t s)
+{
+    const int elem = dtype == NACHO_F32 ? 4 : 2;
+    // (words of 16 bytes; addresses of rows are one product of 32 bits)
+    const bool words = a.ldq < 0x7fffffff && a.ldp < 0x7fffffff &&
+                       in_words({{a.q, a.ldq}, {a.p, a.ldp}, {a.p, a.p_stride}, {a.out, a.ldo}, {a.out, a.out_stride}, {a.pre, a.ldpre},
+                                 {a.q, kForm == WEIGHTS ? 0 : a.k}, {a.q, kForm == WEIGHTS ? a.m : 0}, {a.q, a.n}}, elem);
+    hipError_t rc = hipSuccess;
+    by_type(dtype, [&](auto zero) { rc = by_size<decltype(zero), kForm>(a, words, s); });
+    return rc;
 }
 
 }  // namespace
