@@ -150,10 +150,20 @@ bool overlaps_inputs(const nacho_experts_layer *l, const void *p, int64_t bytes,
            overlap(p, bytes, l->w, l->w ? span(l->n_experts, l->outer, l->inner, l->ldw, l->w_stride, elem) : 0);
 }
 
-// What a gradient call keeps: the gradient before the activation.
-int64_t grad_z_bytes(const nacho_experts_layer *l)
+// What a gradient call keeps: the gradient before the activation, and sums of its rows.
+struct GradWs {
+    void *grad_z;
+    float *sums;
+    size_t bytes;
+};
+GradWs carve_grad(void *ws, const nacho_experts_layer *l, bool grad_z, bool sums)
 {
-    return l->act == NACHO_ACT_NONE ? 0 : (int64_t)align_up((size_t)(l->n_slots * ((l->outer + 7) / 8 * 8) * value_bytes(l->dtype)), 256);
+    Slices c(ws);
+    GradWs w{};
+    if (grad_z) w.grad_z = c.take<char>(l->n_slots * ((l->outer + 7) / 8 * 8) * value_bytes(l->dtype));
+    if (sums) w.sums = c.take<float>(experts_slope_tiles(l->n_slots, l->n_experts) * l->outer);
+    w.bytes = align_up(c.off, 256);
+    return w;
 }
 
 }  // namespace
@@ -302,7 +312,7 @@ int32_t nacho_experts_workspace_bytes(const nacho_experts_layer *layer, size_t *
 {
     if (!bytes) return NACHO_ERR_INVALID_ARG;
     const int32_t rc = check_layer(layer);
-    if (rc == NACHO_OK) *bytes = (size_t)grad_z_bytes(layer);
+    if (rc == NACHO_OK) *bytes = carve_grad(nullptr, layer, layer->act != NACHO_ACT_NONE, true).bytes;
     return rc;
 }
 
@@ -360,20 +370,20 @@ int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y,
             if (overlap(outs[i], sizes[i], outs[j], sizes[j])) return NACHO_ERR_INVALID_ARG;
     }
     const bool products = grad_x || grad_w;
-    const int64_t need = products ? grad_z_bytes(layer) : 0;
-    if (need > 0 && (!ws || (int64_t)ws_bytes < need || !aligned(ws, 16))) return NACHO_ERR_WORKSPACE;
+    const GradWs w = carve_grad(ws, layer, slope && products, grad_bias != nullptr);
+    if (w.bytes > 0 && (!ws || ws_bytes < w.bytes || !aligned(ws, 16))) return NACHO_ERR_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     profile_begin(s);
     const void *gz = grad_y;
     int64_t ldgz = ldgy;
     if ((slope && products) || grad_bias) {
         SlopeArgs a{l.expert_pos, (int32_t)l.n_experts, (int32_t)l.outer, l.act, l.n_slots, grad_y, pre, ldgy, ldpre, nullptr, 0,
-                    grad_bias, gb_stride};
+                    grad_bias, gb_stride, w.sums};
         if (slope && products) {
-            gz = a.grad_z = ws;
+            gz = a.grad_z = w.grad_z;
             ldgz = a.ldgz = (l.outer + 7) / 8 * 8;
         }
-        if (launch_experts_slope(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+        if (const hipError_t e = launch_experts_slope(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
         profile_mark("experts_slope");
     }
     if (grad_x) {

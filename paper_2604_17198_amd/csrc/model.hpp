@@ -111,7 +111,9 @@ struct SlopeArgs {
     int64_t ldgz;
     void *grad_bias;
     int64_t bias_stride;
+    float *sums;                   // [experts_slope_tiles][cols], with grad_bias
 };
+int64_t experts_slope_tiles(int64_t slots, int64_t experts);
 hipError_t launch_experts_slope(int dtype, const SlopeArgs &a, hipStream_t s);
 
 }  // namespace nacho

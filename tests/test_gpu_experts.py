@@ -245,3 +245,17 @@ def test_refusals():
                               ws=torch.empty(64, dtype=torch.uint8, device="cuda"))
     with pytest.raises(nb.NachoError):
         nb.nacho_experts_grad(gy, d["x"], d["w"], d["bounds"], token=d["token"], grad_weight=d["w"])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("counts,inner,outer", [([1500, 700], 72, 8200), ([530, 513], 200, 16384), ([600, 900, 4], 8200, 264)])
+def test_the_largest_tiles(counts, inner, outer, dtype):
+    """Enough slots an expert, and enough of them, for tiles of 256 x 256 in every direction, with rows and columns left over."""
+    check(problem(20, counts, 300, inner, outer, dtype, True), "silu", dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("inner", [64, 128, 192, 256, 264, 320, 136])
+def test_steps_of_the_sum(inner, dtype):
+    """Even and odd numbers of whole steps of k, and parts of one behind them, in all three products."""
+    check(problem(21, [64 + inner, 130, inner // 2, 1], 90, inner, 384 - inner // 2, dtype, False), "none", dtype)
