@@ -93,7 +93,7 @@ int32_t check_distill(const nacho_tensor *teacher, const void *logits, int64_t l
                  overlap(logits, span(rows, cols, ldl, elem), grad, span(rows, cols, ldg, elem))))
         return NACHO_ERR_INVALID_ARG;
     *a = DistillArgs{teacher->lvl[1].pos, teacher->lvl[1].crd, static_cast<const float *>(teacher->val), logits, ldl, weight,
-                     temperature, nullptr, nullptr, nullptr, grad, ldg, rows, (int32_t)cols};
+                     temperature, nullptr, nullptr, nullptr, grad, ldg, rows, (int32_t)cols, nullptr};
     return NACHO_OK;
 }
 
@@ -178,8 +178,9 @@ int32_t nacho_distill(const nacho_tensor *teacher, const void *logits, int64_t l
     const int32_t rc = check_distill(teacher, logits, ldl, dtype, weight, temperature, grad, ldg, &a);
     if (rc != NACHO_OK) return rc;
     if (a.rows > 0 && (!loss || !lse)) return NACHO_ERR_INVALID_ARG;
-    (void)ws;
-    (void)ws_bytes;
+    const size_t need = align_up((size_t)distill_partials(dtype, a.rows, a.cols, grad != nullptr) * sizeof(float), 256);
+    if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return NACHO_ERR_WORKSPACE;
+    a.partial = static_cast<float *>(ws);
     a.loss = loss;
     a.lse = lse;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -193,7 +194,7 @@ int32_t nacho_distill_workspace_bytes(int64_t n_rows, int64_t n_cols, int32_t dt
 {
     if (!bytes || !value_type(dtype) || n_rows < 0 || n_rows > kMostRows || n_cols < 0 || n_cols > kMostRows)
         return NACHO_ERR_INVALID_ARG;
-    *bytes = 0;
+    *bytes = align_up((size_t)distill_partials(dtype, n_rows, n_cols, false) * sizeof(float), 256);
     return NACHO_OK;
 }
 

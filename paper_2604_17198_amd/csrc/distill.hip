@@ -6,6 +6,12 @@
 // With m the largest z and M the largest u of the row, e_j = exp((u_j - M) / tau), U = sum e_j, Z = sum exp((z_v - m) / tau):
 //   sum p (log p - log q) = sum_j e_j ((u_j - M) - (z_j - m)) / (tau U) - log U + log Z
 // so one pass over the row gives everything but the gradient.
+//
+// Bound by memory: the logits are read once and the gradient is written once.  A workgroup holds its words of 16 bytes in
+// registers from the maximum over the sums to the gradient, a row at a time where the registers of a workgroup hold one
+// (WHOLE, up to 1024 threads of 16 words: 131072 values of 16 bits, 65536 floats).  Longer rows, and few rows, which would
+// leave compute units idle, are cut into parts: one launch leaves every part's maximum and sum (STATS), the next one joins them
+// and writes its part of the gradient (APPLY).  The backward call knows the row's sum (GIVEN) and is cut likewise.
 #include "kernels.hpp"
 #include "model.hpp"
 
@@ -13,13 +19,7 @@ namespace nacho {
 
 namespace {
 
-constexpr int kThreads = 256;
-
-// What the threads of a workgroup know of a row's teacher.
-struct Teacher {
-    float top, total;      // M, U
-    bool held;             // an entry above -inf
-};
+enum Stage { WHOLE, STATS, APPLY, GIVEN };
 
 // Whether row `row` has something to do; its entries and factor.
 __device__ inline bool row_of(const DistillArgs &a, int64_t row, int &begin, int &end, float &w)
@@ -41,183 +41,237 @@ template <int kThreads> __device__ inline float largest_entry(const DistillArgs 
     return top;
 }
 
-template <typename T> __device__ inline void put_word(T *to, bool same, const typename Word<T>::type &v)
+// Between two uses the words stay as they were loaded (the compiler would keep every element in 32 bits, twice the registers
+// of 16-bit types: one workgroup a compute unit in place of two).
+template <typename W, int kEach> __device__ inline void keep(W (&v)[kEach])
 {
-    if (same) *reinterpret_cast<typename Word<T>::type *>(to) = v;
-    else {
 #pragma unroll
-        for (int e = 0; e < Word<T>::n; ++e) to[e] = v[e];
+    for (int i = 0; i < kEach; ++i) {
+        typedef unsigned int four __attribute__((ext_vector_type(4)));
+        four bits = __builtin_bit_cast(four, v[i]);
+        asm volatile("" : "+v"(bits));
+        v[i] = __builtin_bit_cast(W, bits);
     }
 }
 
-// The row of zeros of a row without loss.
-template <typename T, int kThreads> __device__ inline void zero_row(T *g, int cols)
-{
-    const RowSplit<T> split(g, cols);
-    const typename Word<T>::type none = (typename Word<T>::type)((T)0.0f);
-    for (int i = (int)threadIdx.x; i < split.words; i += kThreads)
-        reinterpret_cast<typename Word<T>::type *>(g + split.head)[i] = none;
-    const int edge = split.edge((int)threadIdx.x, cols);
-    if (edge >= 0) g[edge] = (T)0.0f;
-}
-
-// One workgroup a row: a pass over the logits with the running maximum and sum of every thread, then one that writes
-// the gradient.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) distill_row_kernel(DistillArgs a)
+template <typename T, int kThreads, int kEach, int kMore, Stage kStage>
+__global__ void __launch_bounds__(kThreads, kThreads == 512 && kMore < 16 ? 4 : 1) distill_kernel(DistillArgs a, int part, int parts, int many)
 {
     typedef typename Word<T>::type word;
-    __shared__ float share[3 * kThreads / NACHO_WAVE], share2[3 * kThreads / NACHO_WAVE];
-    const int tid = (int)threadIdx.x, cols = a.cols;
-    const float c = kLog2e / a.temperature;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        T *g = a.grad ? static_cast<T *>(a.grad) + row * a.ldg : nullptr;
-        int begin, end;
-        float w;
-        bool active = row_of(a, row, begin, end, w);
-        float top[2] = {-kInfinity, -kInfinity}, sum = 0.0f;
-        const T *z = static_cast<const T *>(a.logits) + row * a.ldl;
-        const RowSplit<T> split(z, cols);
-        const word *words = reinterpret_cast<const word *>(z + split.head);
-        const int edge = split.edge(tid, cols);
-        if (active) {
-            top[1] = largest_entry<kThreads>(a, begin, end);
-            for (int i = tid; i < split.words; i += kThreads) {
-                const word v = words[i];
-                float m = wide(v[0]);
+    constexpr int n = Word<T>::n, kWaves = kThreads / NACHO_WAVE;
+    __shared__ float share[2 * kWaves], share2[3 * kWaves];
+    __shared__ word more[kMore > 0 ? kMore * kThreads : 1];           // a thread's words that its registers do not hold
+    const int tid = (int)threadIdx.x;
+    const float tau = a.temperature, c = kLog2e / tau;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x)
+        for (int number = (int)blockIdx.y; number < many; number += (int)gridDim.y) {
+            const int c0 = number * part, cols = a.cols - c0 < part ? a.cols - c0 : part;
+            T *const g = kStage != STATS && a.grad ? static_cast<T *>(a.grad) + row * a.ldg + c0 : nullptr;
+            const T *const z = static_cast<const T *>(a.logits) + row * a.ldl + c0;
+            float *const left = a.partial + 2 * (row * parts + number);
+            int begin, end;
+            float w;
+            bool active = row_of(a, row, begin, end, w);
+            const RowSplit<T> split(z, cols);
+            // (the same offset for every thread's words behind a base that the whole workgroup shares: few registers)
+            const char *const words = reinterpret_cast<const char *>(z + split.head);
+            const unsigned own = (unsigned)tid * 16u;
+            auto word_at = [&](int i) -> const word & { return *reinterpret_cast<const word *>(words + (size_t)(i * kThreads) * 16 + own); };
+            const int edge = split.edge(tid, cols);
+            word v[kEach];
+            float beside = -kInfinity;
+            // (a row that has nothing to do is not read)
+            const int there = active && (kStage == WHOLE || kStage == STATS || g) ? split.words : 0;
 #pragma unroll
-                for (int e = 1; e < Word<T>::n; ++e) m = fmaxf(m, wide(v[e]));
-                if (m > top[0]) {
-                    sum = sum * exp2_of((top[0] - m) * c);
-                    top[0] = m;
-                }
-                if (top[0] == -kInfinity && m == -kInfinity) continue;
+            for (int i = 0; i < kEach; ++i) {
+                const int at = tid + i * kThreads;
+                v[i] = (word)((T)-kInfinity);
+                if (at < there) v[i] = word_at(i);
+            }
 #pragma unroll
-                for (int e = 0; e < Word<T>::n; ++e) sum += exp2_of((wide(v[e]) - top[0]) * c);
+            for (int i = 0; i < kMore; ++i) {
+                const int at = tid + (kEach + i) * kThreads;
+                more[i * kThreads + tid] = at < there ? word_at(kEach + i) : (word)((T)-kInfinity);
             }
-            if (edge >= 0) {
-                const float v = wide(z[edge]);
-                if (v > top[0]) {
-                    sum = sum * exp2_of((top[0] - v) * c);
-                    top[0] = v;
+            if (edge >= 0 && active) beside = wide(z[edge]);
+            // the largest logit (of the row, or of the part) and the largest stored one
+            float top[2] = {-kInfinity, -kInfinity};
+            if (active) {
+                if (kStage != STATS) top[1] = largest_entry<kThreads>(a, begin, end);
+                if (kStage == WHOLE || kStage == STATS) {
+                    top[0] = beside;
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i)
+#pragma unroll
+                        for (int e = 0; e < n; ++e) top[0] = fmaxf(top[0], wide((T)v[i][e]));
+#pragma unroll 2
+                    for (int i = 0; i < kMore; ++i) {
+                        const word x = more[i * kThreads + tid];
+#pragma unroll
+                        for (int e = 0; e < n; ++e) top[0] = fmaxf(top[0], wide((T)x[e]));
+                    }
+                } else if (kStage == APPLY)
+                    for (int i = tid; i < parts; i += kThreads) top[0] = fmaxf(top[0], a.partial[2 * (row * parts + i)]);
+                group_all<kThreads>(top, share, MaxOf(), MaxOf());
+                if (kStage == GIVEN) top[0] = a.lse_in[row] * tau;
+                if (kStage != STATS) active = top[1] > -kInfinity;
+            }
+            if (!active) {
+                if (kStage != STATS && kStage != GIVEN && tid == 0 && number == 0) a.loss[row] = a.lse[row] = 0.0f;
+                if (g) {
+                    const RowSplit<T> mine(g, cols);
+                    for (int i = tid; i < mine.words; i += kThreads) reinterpret_cast<word *>(g + mine.head)[i] = (word)((T)0.0f);
+                    const int last = mine.edge(tid, cols);
+                    if (last >= 0) g[last] = (T)0.0f;
                 }
-                if (v != -kInfinity) sum += exp2_of((v - top[0]) * c);
+                __syncthreads();
+                continue;
             }
-            const float own_top = top[0];
-            group_all<kThreads>(top, share, MaxOf(), MaxOf());
-            if (own_top != top[0]) sum *= exp2_of((own_top - top[0]) * c);
-            active = top[1] > -kInfinity;
-        }
-        if (!active) {
-            if (tid == 0 && a.loss) a.loss[row] = 0.0f;
-            if (tid == 0 && a.lse) a.lse[row] = 0.0f;
-            if (g) zero_row<T, kThreads>(g, cols);
+            keep(v);
+            // Z, U, and the sum over the entries
+            float s[3] = {0.0f, 0.0f, 0.0f};
+            if (kStage == WHOLE || kStage == STATS) {
+                // (a part of masked logits alone has nothing to add)
+                const float from = kStage == STATS && top[0] == -kInfinity ? 0.0f : top[0];
+                s[0] = edge >= 0 ? exp2_of((beside - from) * c) : 0.0f;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i)
+#pragma unroll
+                    for (int e = 0; e < n; ++e) s[0] += exp2_of((wide((T)v[i][e]) - from) * c);
+#pragma unroll 2
+                for (int i = 0; i < kMore; ++i) {
+                    const word x = more[i * kThreads + tid];
+#pragma unroll
+                    for (int e = 0; e < n; ++e) s[0] += exp2_of((wide((T)x[e]) - from) * c);
+                }
+            } else if (kStage == APPLY)
+                for (int i = tid; i < parts; i += kThreads) {
+                    const float m = a.partial[2 * (row * parts + i)], t = a.partial[2 * (row * parts + i) + 1];
+                    s[0] += m == top[0] ? t : t * exp2_of((m - top[0]) * c);
+                }
+            if (kStage != STATS)
+                for (int i = begin + tid; i < end; i += kThreads) {
+                    const float u = a.val[i] - top[1], e = exp2_of(u * c);
+                    s[1] += e;
+                    if (kStage != GIVEN && number == 0 && !(e == 0.0f)) s[2] += e * (u - (wide(z[a.crd[i]]) - top[0]));
+                }
+            group_all<kThreads>(s, share2, SumOf(), SumOf(), SumOf());
+            if (kStage == STATS) {
+                if (tid == 0) {
+                    left[0] = top[0];
+                    left[1] = s[0];
+                }
+                __syncthreads();
+                continue;
+            }
+            if (kStage != GIVEN && tid == 0 && number == 0) {
+                const float log_z = logf(s[0]);
+                a.loss[row] = w * tau * tau * (s[2] / (s[1] * tau) - logf(s[1]) + log_z);
+                a.lse[row] = top[0] / tau + log_z;
+            }
+            if (g) {
+                keep(v);
+                const float q = kStage == GIVEN ? w * tau : w * tau / s[0], p = w * tau / s[1];
+                const bool same = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
+                char *const grads = reinterpret_cast<char *>(g + split.head);
+                auto write = [&](int i, const word &from) {
+                    if (tid + i * kThreads >= split.words) return;
+                    word x;
+#pragma unroll
+                    for (int e = 0; e < n; ++e) x[e] = (T)(q * exp2_of((wide((T)from[e]) - top[0]) * c));
+                    char *to = grads + (size_t)(i * kThreads) * 16 + own;
+                    if (same) *reinterpret_cast<word *>(to) = x;
+                    else __builtin_memcpy(to, &x, sizeof(x));
+                };
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) write(i, v[i]);
+#pragma unroll 2
+                for (int i = 0; i < kMore; ++i) write(kEach + i, more[i * kThreads + tid]);
+                if (edge >= 0) g[edge] = (T)(q * exp2_of((beside - top[0]) * c));
+                __syncthreads();               // (the stored columns again, now with the teacher's part)
+                for (int i = begin + tid; i < end; i += kThreads) {
+                    const int j = a.crd[i] - c0;
+                    if (j >= 0 && j < cols)
+                        g[j] = (T)(q * exp2_of((wide(z[j]) - top[0]) * c) - p * exp2_of((a.val[i] - top[1]) * c));
+                }
+            }
             __syncthreads();
-            continue;
         }
-        float s[3] = {sum, 0.0f, 0.0f};
-        for (int i = begin + tid; i < end; i += kThreads) {
-            const float u = a.val[i] - top[1], e = exp2_of(u * c);
-            s[1] += e;
-            if (!(e == 0.0f)) s[2] += e * (u - (wide(z[a.crd[i]]) - top[0]));
-        }
-        group_all<kThreads>(s, share2, SumOf(), SumOf(), SumOf());
-        const float tau = a.temperature, log_z = logf(s[0]);
-        if (tid == 0) {
-            if (a.loss) a.loss[row] = w * tau * tau * (s[2] / (s[1] * tau) - logf(s[1]) + log_z);
-            if (a.lse) a.lse[row] = top[0] / tau + log_z;
-        }
-        if (g) {
-            const float q = w * tau / s[0], p = w * tau / s[1];
-            const bool same = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
-            for (int i = tid; i < split.words; i += kThreads) {
-                word v = words[i];
-#pragma unroll
-                for (int e = 0; e < Word<T>::n; ++e) v[e] = (T)(q * exp2_of((wide(v[e]) - top[0]) * c));
-                put_word(g + split.head + i * Word<T>::n, same, v);
-            }
-            if (edge >= 0) g[edge] = (T)(q * exp2_of((wide(z[edge]) - top[0]) * c));
-            __syncthreads();               // (the stored columns again, now with the teacher's part)
-            for (int i = begin + tid; i < end; i += kThreads) {
-                const int j = a.crd[i];
-                g[j] = (T)(q * exp2_of((wide(z[j]) - top[0]) * c) - p * exp2_of((a.val[i] - top[1]) * c));
-            }
-        }
-        __syncthreads();
-    }
 }
 
-// The gradient from what the forward call left.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) distill_grad_kernel(DistillArgs a)
+template <typename T, int kThreads, int kEach, int kMore, Stage kStage> hipError_t run(const DistillArgs &a, int part, int parts, hipStream_t s, int wanted = 0)
 {
-    typedef typename Word<T>::type word;
-    __shared__ float share[kThreads / NACHO_WAVE], share2[kThreads / NACHO_WAVE];
-    const int tid = (int)threadIdx.x, cols = a.cols;
-    const float c = kLog2e / a.temperature, tau = a.temperature;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        T *g = static_cast<T *>(a.grad) + row * a.ldg;
-        int begin, end;
-        float w;
-        bool active = row_of(a, row, begin, end, w);
-        float top[1] = {-kInfinity};
-        if (active) {
-            top[0] = largest_entry<kThreads>(a, begin, end);
-            group_all<kThreads>(top, share, MaxOf());
-            active = top[0] > -kInfinity;
-        }
-        if (!active) {
-            zero_row<T, kThreads>(g, cols);
-            __syncthreads();
-            continue;
-        }
-        float total[1] = {0.0f};
-        for (int i = begin + tid; i < end; i += kThreads) total[0] += exp2_of((a.val[i] - top[0]) * c);
-        group_all<kThreads>(total, share2, SumOf());
-        const T *z = static_cast<const T *>(a.logits) + row * a.ldl;
-        const RowSplit<T> split(z, cols);
-        const word *words = reinterpret_cast<const word *>(z + split.head);
-        const int edge = split.edge(tid, cols);
-        const float base = a.lse_in[row] * tau, q = w * tau, p = w * tau / total[0];
-        const bool same = (((uintptr_t)z ^ (uintptr_t)g) & 15u) == 0;
-        for (int i = tid; i < split.words; i += kThreads) {
-            word v = words[i];
-#pragma unroll
-            for (int e = 0; e < Word<T>::n; ++e) v[e] = (T)(q * exp2_of((wide(v[e]) - base) * c));
-            put_word(g + split.head + i * Word<T>::n, same, v);
-        }
-        if (edge >= 0) g[edge] = (T)(q * exp2_of((wide(z[edge]) - base) * c));
-        __syncthreads();
-        for (int i = begin + tid; i < end; i += kThreads) {
-            const int j = a.crd[i];
-            g[j] = (T)(q * exp2_of((wide(z[j]) - base) * c) - p * exp2_of((a.val[i] - top[0]) * c));
-        }
-        __syncthreads();
-    }
+    // (without a gradient the first part of a row, which writes its loss, is all that is wanted of the last launch)
+    const int many = wanted > 0 ? wanted : parts;
+    const dim3 grid((unsigned)(a.rows < (1 << 20) ? a.rows : 1 << 20), (unsigned)(many < 4096 ? many : 4096));
+    distill_kernel<T, kThreads, kEach, kMore, kStage><<<grid, kThreads, 0, s>>>(a, part, parts, many);
+    return hipGetLastError();
 }
 
-unsigned row_groups(int64_t rows) { return (unsigned)(rows < (1 << 20) ? rows : 1 << 20); }
+// Words that a workgroup of a part has: 256 threads of kPartEach words.
+constexpr int kPartEach = 4;
+template <typename T> constexpr int kPart = 256 * kPartEach * Word<T>::n;
+
+template <typename T> bool in_parts(int64_t rows, int64_t cols, bool grad)
+{
+    // rows that no workgroup holds, and long ones of which there are too few to fill the chip; without a gradient nothing
+    // has to be held
+    return cols / Word<T>::n > 512 * 32 || ((rows < 128 || !grad) && cols >= 4 * kPart<T>);
+}
+
+template <typename T> hipError_t forward(const DistillArgs &a, hipStream_t s)
+{
+    const int64_t words = a.cols / Word<T>::n;
+    if (in_parts<T>(a.rows, a.cols, a.grad != nullptr)) {
+        const int parts = (int)(((int64_t)a.cols + kPart<T> - 1) / kPart<T>);
+        const hipError_t rc = run<T, 256, kPartEach, 0, STATS>(a, kPart<T>, parts, s);
+        if (rc != hipSuccess) return rc;
+        nacho_host::profile_mark("distill_stats");
+        return run<T, 256, kPartEach, 0, APPLY>(a, kPart<T>, parts, s, a.grad ? parts : 1);
+    }
+    const int part = a.cols > 0 ? a.cols : 1;
+    if (words <= 64 * 4) return run<T, 64, 4, 0, WHOLE>(a, part, 1, s);
+    if (words <= 256 * 4) return run<T, 256, 4, 0, WHOLE>(a, part, 1, s);
+    if (words <= 256 * 8) return run<T, 256, 8, 0, WHOLE>(a, part, 1, s);
+    if (words <= 512 * 8) return run<T, 512, 8, 0, WHOLE>(a, part, 1, s);
+    if (words <= 512 * 16) return run<T, 512, 16, 0, WHOLE>(a, part, 1, s);
+    if (words <= 512 * 25) return run<T, 512, 16, 9, WHOLE>(a, part, 1, s);
+    return run<T, 512, 16, 16, WHOLE>(a, part, 1, s);
+}
+
+template <typename F> hipError_t by_type(int dtype, F f)
+{
+    if (dtype == NACHO_F32) return f((float)0);
+    return dtype == NACHO_BF16 ? f((bf16_t)0.0f) : f((f16_t)0.0f);
+}
 
 }  // namespace
+
+int64_t distill_partials(int dtype, int64_t rows, int64_t cols, bool grad)
+{
+    int64_t parts = 0;
+    (void)by_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        if (in_parts<T>(rows, cols, grad)) parts = (cols + kPart<T> - 1) / kPart<T>;
+        return hipSuccess;
+    });
+    return 2 * rows * parts;
+}
 
 hipError_t launch_distill(int dtype, const DistillArgs &a, hipStream_t s)
 {
     if (a.rows == 0) return hipSuccess;
-    const dim3 grid(row_groups(a.rows));
-    if (dtype == NACHO_F32) distill_row_kernel<float><<<grid, kThreads, 0, s>>>(a);
-    else if (dtype == NACHO_BF16) distill_row_kernel<bf16_t><<<grid, kThreads, 0, s>>>(a);
-    else distill_row_kernel<f16_t><<<grid, kThreads, 0, s>>>(a);
-    return hipGetLastError();
+    return by_type(dtype, [&](auto zero) { return forward<decltype(zero)>(a, s); });
 }
 
 hipError_t launch_distill_grad(int dtype, const DistillArgs &a, hipStream_t s)
 {
-    if (a.rows == 0) return hipSuccess;
-    const dim3 grid(row_groups(a.rows));
-    if (dtype == NACHO_F32) distill_grad_kernel<float><<<grid, kThreads, 0, s>>>(a);
-    else if (dtype == NACHO_BF16) distill_grad_kernel<bf16_t><<<grid, kThreads, 0, s>>>(a);
-    else distill_grad_kernel<f16_t><<<grid, kThreads, 0, s>>>(a);
-    return hipGetLastError();
+    if (a.rows == 0 || a.cols == 0) return hipSuccess;
+    return by_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        const int parts = (int)(((int64_t)a.cols + kPart<T> - 1) / kPart<T>);
+        return run<T, 256, kPartEach, 0, GIVEN>(a, kPart<T>, parts, s);
+    });
 }
 
 }  // namespace nacho

@@ -18,7 +18,10 @@ struct DistillArgs {
     int64_t ldg;
     int64_t rows;
     int32_t cols;
+    float *partial;                // distill_partials floats
 };
+// Floats that a call keeps of rows that are cut into parts.
+int64_t distill_partials(int dtype, int64_t rows, int64_t cols, bool grad);
 hipError_t launch_distill(int dtype, const DistillArgs &a, hipStream_t s);
 hipError_t launch_distill_grad(int dtype, const DistillArgs &a, hipStream_t s);
 
