@@ -508,37 +508,42 @@ def model_dtype_code(dt) -> int:
     return code
 
 
+# (What Python spends on a small call is most of its time: messages are put together only where something is wrong.)
 def _need(ok, what):
     if not ok:
         raise ValueError(what)
 
 
-def _matrix(t, what, shape=None, dtype=None, device=None):
-    """A matrix whose rows are contiguous; returns its leading dimension."""
-    _need(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{what}: a matrix with contiguous rows is needed")
-    _need(shape is None or tuple(t.shape) == tuple(shape), f"{what}: shape {tuple(t.shape)}, expected {shape}")
-    _need(dtype is None or t.dtype is dtype, f"{what}: type {t.dtype}, expected {dtype}")
-    _need(device is None or t.device == device, f"{what}: on {t.device}, expected {device}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _matrix(t, what, rows=None, cols=None, dtype=None, device=None):
+    """A matrix whose rows are contiguous, of the given sizes where they are given; returns its leading dimension."""
+    if t.dim() != 2:
+        raise ValueError(f"{what}: a matrix is needed, got {t.dim()} dimensions")
+    r, c = t.shape
+    ld, step = t.stride()
+    if step != 1 and c > 1:
+        raise ValueError(f"{what}: contiguous rows are needed")
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise ValueError(f"{what}: {r} x {c}, expected {rows} x {cols}")
+    if (dtype is not None and t.dtype is not dtype) or (device is not None and t.device != device):
+        raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype} on {device}")
+    return ld if r > 1 else (ld if ld > c else c)
 
 
 def _vector_of(t, what, n, dtype, device):
     """A contiguous array of n elements, or None."""
-    _need(t is None or (t.numel() == n and t.is_contiguous()), f"{what}: {n} contiguous elements are needed")
-    _need(t is None or t.dtype is dtype, f"{what}: expected {dtype}")
-    _need(t is None or t.device == device, f"{what}: expected on {device}")
+    if t is not None and (t.numel() != n or t.dtype is not dtype or not t.is_contiguous() or t.device != device):
+        raise ValueError(f"{what}: {n} contiguous elements of {dtype} on {device} are needed")
     return t
 
 
 def _check_teacher(teacher, logits, weight):
     if teacher.nlevels != 2 or teacher.c.lvl[0].kind != DENSE or teacher.c.lvl[1].kind != COMPRESSED:
         raise NachoError(-2, "teacher: a CSR operand is needed")
-    _need(teacher.val is not None and teacher.val.dtype is torch.float32, "teacher: values of float32 are needed")
-    _need(teacher.val.numel() == teacher.nnz and teacher.val.is_contiguous(), "teacher: a value for every stored column is needed")
+    _need(teacher.val is not None, "teacher: values are needed")
+    _vector_of(teacher.val, "teacher's values", teacher.nnz, torch.float32, logits.device)
     rows, cols = teacher.c.lvl[0].extent, teacher.c.lvl[1].extent
     _need(teacher.keep[0].numel() == rows + 1, "teacher: rows + 1 positions are needed")
-    _need(teacher.val.device == logits.device, "teacher: expected on the logits' device")
-    ld = _matrix(logits, "logits", (rows, cols))
+    ld = _matrix(logits, "logits", rows, cols)
     _vector_of(weight, "weight", rows, torch.float32, logits.device)
     return rows, cols, ld
 
@@ -549,7 +554,7 @@ def nacho_distill(teacher: Operand, logits, temperature=1.0, weight=None, grad=N
     dt = model_dtype_code(logits.dtype)
     rows, cols, ld = _check_teacher(teacher, logits, weight)
     dev = logits.device
-    ldg = _matrix(grad, "grad", (rows, cols), logits.dtype, dev) if grad is not None else 0
+    ldg = _matrix(grad, "grad", rows, cols, logits.dtype, dev) if grad is not None else 0
     loss = _vector_of(loss, "loss", rows, torch.float32, dev) if loss is not None else torch.empty(rows, device=dev)
     lse = _vector_of(lse, "lse", rows, torch.float32, dev) if lse is not None else torch.empty(rows, device=dev)
     if ws is None:
@@ -569,7 +574,7 @@ def nacho_distill_grad(teacher: Operand, logits, lse, temperature=1.0, weight=No
     _vector_of(lse, "lse", rows, torch.float32, logits.device)
     if grad is None:
         grad = torch.empty((rows, cols), dtype=logits.dtype, device=logits.device)
-    ldg = _matrix(grad, "grad", (rows, cols), logits.dtype, logits.device)
+    ldg = _matrix(grad, "grad", rows, cols, logits.dtype, logits.device)
     _check(lib().nacho_distill_grad(_pack([teacher]), _ptr(logits), ld, dt, _ptr(weight), temperature, _ptr(lse), _ptr(grad),
                                     ldg, _stream()), "nacho_distill_grad")
     return grad
@@ -581,17 +586,23 @@ class Routing:
 
     def __init__(self, n_tokens, n_experts, top_k, device, normalise=False):
         self.n_tokens, self.n_experts, self.top_k, self.normalise = n_tokens, n_experts, top_k, normalise
+        # one allocation for the whole numbers and one for the rest; the matrix's coordinates and values come first, where
+        # they start at a multiple of 16 bytes
         room = n_tokens * top_k
-        i32 = dict(dtype=torch.int32, device=device)
-        self.pos, self.expert_pos = torch.empty(n_tokens + 1, **i32), torch.empty(n_experts + 1, **i32)
-        self.expert, self.slot, self.token = torch.empty(room, **i32), torch.empty(room, **i32), torch.empty(room, **i32)
-        self.gate, self.lse = torch.empty(room, device=device), torch.empty(n_tokens, device=device)
-        self.counts, self.routed = torch.empty(n_experts, **i32), torch.empty(1, **i32)
-        self.balance = torch.empty(1, device=device)
-        # (arrays without an element have no address, and are not written)
-        self.c = _Routing(*[t.data_ptr() or self.balance.data_ptr() for t in
-                            (self.pos, self.expert, self.gate, self.slot, self.expert_pos, self.token, self.counts,
-                             self.lse, self.balance, self.routed)])
+        (self.expert, self.slot, self.token, self.pos, self.expert_pos, self.counts, self.routed), i = self._arrays(
+            (room, room, room, n_tokens + 1, n_experts + 1, n_experts, 1), torch.int32, device)
+        (self.gate, self.lse, self.balance), f = self._arrays((room, n_tokens, 1), torch.float32, device)
+        self.c = _Routing(i[3], i[0], f[0], i[1], i[4], i[2], i[5], f[1], f[2], i[6])
+
+    @staticmethod
+    def _arrays(sizes, dtype, device):
+        """Arrays of these numbers of 4-byte elements, and their addresses (one without an element has one too)."""
+        whole = torch.empty(sum(sizes), dtype=dtype, device=device)
+        at, starts = whole.data_ptr(), []
+        for n in sizes:
+            starts.append(at)
+            at += 4 * n
+        return torch.unsafe_split_with_sizes(whole, sizes), starts
 
     def matrix(self):
         """The gates as a CSR operand [tokens x experts] (of full rows: every place holds an entry)."""
@@ -624,11 +635,11 @@ def nacho_route_grad(logits, routing: Routing, grad_gate=None, balance=0.0, keep
     be given as to nacho_route; tokens that it leaves out store nothing, which is how they are known."""
     dt, dev = model_dtype_code(logits.dtype), logits.device
     r = routing
-    ld = _matrix(logits, "logits", (r.n_tokens, r.n_experts))
+    ld = _matrix(logits, "logits", r.n_tokens, r.n_experts)
     _vector_of(grad_gate, "grad_gate", r.n_tokens * r.top_k, torch.float32, dev)
     if grad is None:
         grad = torch.empty((r.n_tokens, r.n_experts), dtype=logits.dtype, device=dev)
-    ldg = _matrix(grad, "grad", (r.n_tokens, r.n_experts), logits.dtype, dev)
+    ldg = _matrix(grad, "grad", r.n_tokens, r.n_experts, logits.dtype, dev)
     _check(lib().nacho_route_grad(_ptr(logits), ld, r.n_tokens, r.n_experts, dt, r.top_k, r.normalise, C.byref(r.c),
                                   _ptr(grad_gate), balance, _ptr(grad), ldg, _stream()), "nacho_route_grad")
     return grad
@@ -639,43 +650,53 @@ _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 def _stack(t, what, shape, dtype, device):
     """Matrices (or rows) of one size, each with contiguous rows: leading dimension and distance."""
-    _need(tuple(t.shape) == tuple(shape) and t.dtype is dtype and t.device == device,
-          f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {tuple(shape)} of {dtype} on {device}")
-    _need(t.stride(-1) == 1 or t.shape[-1] <= 1, f"{what}: contiguous rows are needed")
-    size = 1
-    for n in shape[1:]:
-        size *= n
-    ld = max(t.stride(1), t.shape[2]) if t.dim() == 3 and t.shape[1] > 1 else shape[-1]
-    return ld, t.stride(0) if t.shape[0] > 1 else max(size, t.stride(0))
+    if tuple(t.shape) != shape or t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {shape} of {dtype} on {device}")
+    stride, cols = t.stride(), shape[-1]
+    if stride[-1] != 1 and cols > 1:
+        raise ValueError(f"{what}: contiguous rows are needed")
+    if len(shape) == 2:
+        return cols, stride[0] if shape[0] > 1 else max(cols, stride[0])
+    ld = max(stride[1], cols) if shape[1] > 1 else cols
+    return ld, stride[0] if shape[0] > 1 else max(shape[1] * ld, stride[0])
 
 
 def _layer(x, weight, expert_pos, token, bias, act):
     """The descriptor of a layer of experts, and its number of slots."""
-    dt, dev = model_dtype_code(x.dtype), x.device
-    _need(weight.dim() == 3, "weight: [experts, outer, inner] is needed")
-    experts, outer, inner = weight.shape
-    ldx = _matrix(x, "x", (x.shape[0], inner))
-    ldw, stride = _stack(weight, "weight", weight.shape, x.dtype, dev)
+    dtype, dev = x.dtype, x.device
+    dt = model_dtype_code(dtype)
+    if weight.dim() != 3:
+        raise ValueError("weight: [experts, outer, inner] is needed")
+    shape = tuple(weight.shape)
+    experts, outer, inner = shape
+    ldx = _matrix(x, "x", None, inner)
+    ldw, stride = _stack(weight, "weight", shape, dtype, dev)
     _vector_of(expert_pos, "expert_pos", experts + 1, torch.int32, dev)
-    slots = x.shape[0] if token is None else token.numel()
-    _vector_of(token, "token", slots, torch.int32, dev)
-    _need(act in _ACTS, f"act: one of {', '.join(_ACTS)}")
-    gap = _stack(bias, "bias", (experts, outer), x.dtype, dev)[1] if bias is not None else 0
-    # (an array without an element has no address)
-    return _ExpertsLayer(expert_pos.data_ptr(), _ptr(token) or (expert_pos.data_ptr() if token is not None else None), experts,
-                         slots, x.shape[0], inner, outer, _ptr(x), ldx, _ptr(weight), ldw, stride, _ptr(bias), gap,
-                         _ACTS[act], dt), slots
+    bounds, tokens = expert_pos.data_ptr(), x.shape[0]
+    if token is None:
+        slots, where = tokens, None
+    else:
+        slots = token.numel()
+        _vector_of(token, "token", slots, torch.int32, dev)
+        where = token.data_ptr() or bounds                   # (an array without an element has no address)
+    if act not in _ACTS:
+        raise ValueError(f"act: one of {', '.join(_ACTS)}")
+    gap = _stack(bias, "bias", (experts, outer), dtype, dev)[1] if bias is not None else 0
+    return _ExpertsLayer(bounds, where, experts, slots, tokens, inner, outer, x.data_ptr(), ldx, weight.data_ptr(), ldw, stride,
+                         _ptr(bias), gap, _ACTS[act], dt), slots
 
 
 def nacho_experts(x, weight, expert_pos, token=None, bias=None, act="none", y=None, pre=None):
     """y[s] = act(x[token[s]] weight[e]^T + bias[e]) for the slots s = expert_pos[e] .. expert_pos[e+1] of every expert e
     (expert_pos, token: a Routing's).  `pre`, when given, receives the rows before the activation."""
     c, slots = _layer(x, weight, expert_pos, token, bias, act)
-    shape = (slots, weight.shape[1])
+    outer = c.outer
     if y is None:
-        y = torch.empty(shape, dtype=x.dtype, device=x.device)
-    ldy = _matrix(y, "y", shape, x.dtype, x.device)
-    ldpre = _matrix(pre, "pre", shape, x.dtype, x.device) if pre is not None else 0
+        y = torch.empty((slots, outer), dtype=x.dtype, device=x.device)
+        ldy = outer
+    else:
+        ldy = _matrix(y, "y", slots, outer, x.dtype, x.device)
+    ldpre = _matrix(pre, "pre", slots, outer, x.dtype, x.device) if pre is not None else 0
     _check(lib().nacho_experts(C.byref(c), _ptr(y), ldy, _ptr(pre), ldpre, _stream()), "nacho_experts")
     return y
 
@@ -686,13 +707,13 @@ def nacho_experts_grad(grad_y, x, weight, expert_pos, token=None, act="none", pr
     c, slots = _layer(x, weight, expert_pos, token, None, act)
     experts, outer, inner = weight.shape
     dev = x.device
-    ldgy = _matrix(grad_y, "grad_y", (slots, outer), x.dtype, dev)
-    ldpre = _matrix(pre, "pre", (slots, outer), x.dtype, dev) if pre is not None else 0
+    ldgy = _matrix(grad_y, "grad_y", slots, outer, x.dtype, dev)
+    ldpre = _matrix(pre, "pre", slots, outer, x.dtype, dev) if pre is not None else 0
     if grad_x is None:
         grad_x = torch.empty((slots, inner), dtype=x.dtype, device=dev)
     if grad_weight is None:
         grad_weight = torch.empty((experts, outer, inner), dtype=x.dtype, device=dev)
-    ldgx = _matrix(grad_x, "grad_x", (slots, inner), x.dtype, dev)
+    ldgx = _matrix(grad_x, "grad_x", slots, inner, x.dtype, dev)
     ldgw, gap = _stack(grad_weight, "grad_weight", (experts, outer, inner), x.dtype, dev)
     gb = _stack(grad_bias, "grad_bias", (experts, outer), x.dtype, dev)[1] if grad_bias is not None else 0
     if ws is None:
@@ -726,10 +747,12 @@ def nacho_combine(pos, slot, y, gate=None, residual=None, out=None):
     dt, dev = model_dtype_code(y.dtype), y.device
     tokens, n = pos.numel() - 1, int(y.shape[1])
     ldy = _matrix(y, "y")
-    ldr = _matrix(residual, "residual", (tokens, n), y.dtype, dev) if residual is not None else 0
+    ldr = _matrix(residual, "residual", tokens, n, y.dtype, dev) if residual is not None else 0
     if out is None:
         out = torch.empty((tokens, n), dtype=y.dtype, device=dev)
-    ldo = _matrix(out, "out", (tokens, n), y.dtype, dev)
+        ldo = n
+    else:
+        ldo = _matrix(out, "out", tokens, n, y.dtype, dev)
     c = _slots_of(pos, slot, gate, y.shape[0], dev)
     _check(lib().nacho_combine(C.byref(c), _ptr(y), ldy, n, dt, _ptr(residual), ldr, _ptr(out), ldo, _stream()),
            "nacho_combine")
@@ -741,10 +764,10 @@ def nacho_combine_grad(pos, slot, y, grad_out, gate=None, grad_y=None, grad_gate
     dt, dev = model_dtype_code(y.dtype), y.device
     tokens, n = pos.numel() - 1, int(y.shape[1])
     ldy = _matrix(y, "y")
-    ldg = _matrix(grad_out, "grad_out", (tokens, n), y.dtype, dev)
+    ldg = _matrix(grad_out, "grad_out", tokens, n, y.dtype, dev)
     if grad_y is None:
         grad_y = torch.empty((y.shape[0], n), dtype=y.dtype, device=dev)
-    ldgy = _matrix(grad_y, "grad_y", (y.shape[0], n), y.dtype, dev)
+    ldgy = _matrix(grad_y, "grad_y", y.shape[0], n, y.dtype, dev)
     if grad_gate is None:
         grad_gate = torch.empty(slot.numel(), device=dev)
     _vector_of(grad_gate, "grad_gate", slot.numel(), torch.float32, dev)

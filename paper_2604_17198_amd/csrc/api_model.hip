@@ -93,7 +93,7 @@ int32_t check_distill(const nacho_tensor *teacher, const void *logits, int64_t l
                  overlap(logits, span(rows, cols, ldl, elem), grad, span(rows, cols, ldg, elem))))
         return NACHO_ERR_INVALID_ARG;
     *a = DistillArgs{teacher->lvl[1].pos, teacher->lvl[1].crd, static_cast<const float *>(teacher->val), logits, ldl, weight,
-                     temperature, nullptr, nullptr, nullptr, grad, ldg, rows, (int32_t)cols, nullptr};
+                     temperature, nullptr, nullptr, nullptr, grad, ldg, rows, (int32_t)cols, nullptr, false};
     return NACHO_OK;
 }
 

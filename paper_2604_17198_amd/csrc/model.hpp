@@ -19,6 +19,7 @@ struct DistillArgs {
     int64_t rows;
     int32_t cols;
     float *partial;                // distill_partials floats
+    bool stream;                   // the gradient is stored past the caches (set by the launch)
 };
 // Floats that a call keeps of rows that are cut into parts.
 int64_t distill_partials(int dtype, int64_t rows, int64_t cols, bool grad);
