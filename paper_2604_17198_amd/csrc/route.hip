@@ -22,11 +22,31 @@ __device__ inline unsigned order_of(float v)
     return v > -kInfinity ? ((int)u < 0 ? ~u : u | 0x80000000u) : 0u;
 }
 
+// One value over the L lanes of a group, the same bits in every lane.  (Moves inside 16 lanes are part of an instruction;
+// a shuffle is a round trip through the LDS unit.)
+template <int kCtrl> __device__ inline unsigned moved(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, 0xf, 0xf, true);
+}
+template <int L, typename Op> __device__ inline unsigned group_all_bits(unsigned v, Op op)
+{
+    if constexpr (L > 1) v = op(v, moved<0xb1>(v));            // lanes 1, 0, 3, 2
+    if constexpr (L > 2) v = op(v, moved<0x4e>(v));            // lanes 2, 3, 0, 1
+    if constexpr (L > 4) v = op(v, moved<0x141>(v));           // 8 lanes backwards
+    if constexpr (L > 8) v = op(v, moved<0x140>(v));           // 16 lanes backwards
+    if constexpr (L > 16) v = op(v, (unsigned)__shfl_xor((int)v, 16, NACHO_WAVE));
+    if constexpr (L > 32) v = op(v, (unsigned)__shfl_xor((int)v, 32, NACHO_WAVE));
+    return v;
+}
 template <int L, typename Op> __device__ inline float group_reduce(float v, Op op)
 {
-#pragma unroll
-    for (int off = L / 2; off > 0; off >>= 1) v = op(v, __shfl_xor(v, off, NACHO_WAVE));
-    return v;
+    return __uint_as_float(group_all_bits<L>(__float_as_uint(v), [&](unsigned x, unsigned y) {
+        return __float_as_uint(op(__uint_as_float(x), __uint_as_float(y)));
+    }));
+}
+template <int L> __device__ inline unsigned group_max(unsigned v)
+{
+    return group_all_bits<L>(v, [](unsigned x, unsigned y) { return x > y ? x : y; });
 }
 
 // I consecutive elements of a row from element `at`, those behind `n` are -inf.
@@ -88,38 +108,90 @@ template <int L, int I> __device__ inline void exponentials(const float (&v)[I],
     sum = group_reduce<L>(sum, SumOf());
 }
 
-// The k largest of a group's experts, as bits of the lanes' own.
-template <int L, int I> __device__ inline unsigned choose(const float (&v)[I], int first, int k)
+// Prefix sum over the lanes of a group, the lane's own included: inside 16 lanes, then with what the sixteens before hold.
+template <int L> __device__ inline int group_scan(int v)
 {
-    unsigned key[I], taken = 0;
-#pragma unroll
-    for (int i = 0; i < I; ++i) key[i] = order_of(v[i]);
-    for (int r = 0; r < k; ++r) {
-        unsigned best = key[0];
-        int at = first;
-#pragma unroll
-        for (int i = 1; i < I; ++i)
-            if (key[i] > best) {
-                best = key[i];
-                at = first + i;
-            }
-#pragma unroll
-        for (int off = L / 2; off > 0; off >>= 1) {
-            const unsigned other = (unsigned)__shfl_xor((int)best, off, NACHO_WAVE);
-            const int there = __shfl_xor(at, off, NACHO_WAVE);
-            if (other > best || (other == best && there < at)) {
-                best = other;
-                at = there;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < I; ++i)
-            if (best != 0 && at == first + i) {
-                key[i] = 0;
-                taken |= 1u << i;
-            }
+    const int lane = lane_id(), own = lane % (L < 16 ? L : 16);
+    auto add = [&](unsigned from, int off) { v += own >= off ? (int)from : 0; };
+    if constexpr (L > 1) add(moved<0x111>((unsigned)v), 1);              // from the lane 1, 2, 4, 8 before in 16 lanes
+    if constexpr (L > 2) add(moved<0x112>((unsigned)v), 2);
+    if constexpr (L > 4) add(moved<0x114>((unsigned)v), 4);
+    if constexpr (L > 8) add(moved<0x118>((unsigned)v), 8);
+    if constexpr (L > 16) {
+        const int before = __shfl(v, (lane & ~31) + 15, NACHO_WAVE);
+        v += lane & 16 ? before : 0;
     }
-    return taken;
+    if constexpr (L > 32) {
+        const int before = __shfl(v, 31, NACHO_WAVE);
+        v += lane & 32 ? before : 0;
+    }
+    return v;
+}
+// How many lanes of the group say yes.
+template <int L> __device__ inline int group_count(bool yes)
+{
+    const unsigned long long all = __ballot(yes);
+    if constexpr (L == NACHO_WAVE) return __popcll((long long)all);
+    else {
+        const int lane = lane_id();
+        unsigned low = (unsigned)all, high = (unsigned)(all >> 32);
+        asm volatile("" : "+s"(low), "+s"(high));      // (or the compiler makes one shift of 64 bits by a lane's own amount of it)
+        const unsigned half = (lane < 32 ? low : high) >> ((unsigned)(lane / L * L) & 31u);
+        return __popc(L == 32 ? half : half & ((1u << (L % 32)) - 1u));
+    }
+}
+
+// The k largest of a group's experts, as bits of the lanes' own.  Every lane sorts its keys (a network, two instructions a
+// pair); in a round the lanes whose first one is the group's largest drop it, until k are dropped: the last of them is the
+// threshold.  What lies above it is chosen, and of what equals it as many as are left, the lowest indices first.
+template <int L, int I> __device__ inline unsigned choose(const float (&v)[I], int k)
+{
+    unsigned key[I], sorted[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) sorted[i] = key[i] = order_of(v[i]);
+    // (Batcher's merges of odd and even places)
+#pragma unroll
+    for (int p = 1; p < I; p *= 2)
+#pragma unroll
+        for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+            for (int j = q % p; j + q < I; j += 2 * q)
+#pragma unroll
+                for (int i = 0; i < q; ++i)
+                    if (i + j + q < I && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+                        const unsigned x = sorted[i + j], y = sorted[i + j + q];
+                        sorted[i + j] = x > y ? x : y;
+                        sorted[i + j + q] = x > y ? y : x;
+                    }
+    unsigned threshold = 0;
+    int dropped = 0, left = 0;                 // left: of those at the threshold
+    for (int r = 0; r < k; ++r) {
+        const unsigned best = group_max<L>(sorted[0]);
+        const bool mine = sorted[0] == best;
+        if (dropped < k) {
+            if (best != threshold) left = k - dropped;
+            threshold = best;
+        }
+        dropped += group_count<L>(mine);
+#pragma unroll
+        for (int i = 0; i + 1 < I; ++i) {
+            unsigned next = sorted[i + 1];
+            asm volatile("" : "+v"(next));     // (or it becomes a choice of the place, and that a chain of choices)
+            sorted[i] = mine ? next : sorted[i];
+        }
+        sorted[I - 1] = mine ? 0u : sorted[I - 1];
+    }
+    unsigned above = 0, equal = 0;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        above |= key[i] > threshold ? 1u << i : 0u;
+        equal |= key[i] == threshold ? 1u << i : 0u;
+    }
+    if (threshold == 0) return above;          // (fewer than k may be chosen)
+    const int own = __popc(equal);
+    int room = left - (group_scan<L>(own) - own);
+    for (unsigned rest = equal; rest != 0 && room > 0; rest &= rest - 1, --room) above |= rest & (0u - rest);
+    return above;
 }
 
 template <typename T, int L, int I>
@@ -141,44 +213,51 @@ __global__ void __launch_bounds__(kThreads) route_choose_kernel(RouteArgs a, Rou
 #pragma unroll
     for (int i = 0; i < I; ++i) share[i] = 0.0f;
     int entries = 0, routed = 0;
-    // (every lane of a wavefront stays in the loop: the lanes of a group ask each other)
-    for (int64_t t0 = begin; t0 < end; t0 += kGroups) {
-        const int64_t t = t0 + group;
-        const bool live = t < end && (!a.keep || a.keep[t] != 0);
-        float v[I], e[I], top, sum;
-        if (live) row_part<T, I>(logits + t * a.ldl, first, n, words, v);
+    // (every lane of a wavefront stays in the loop: the lanes of a group ask each other; the next token is on its way)
+    auto fetch = [&](int64_t t, float (&to)[I]) {
+        const bool kept = t < end && (!a.keep || a.keep[t] != 0);
+        if (kept) row_part<T, I>(logits + t * a.ldl, first, n, words, to);
         else {
 #pragma unroll
-            for (int i = 0; i < I; ++i) v[i] = -kInfinity;
+            for (int i = 0; i < I; ++i) to[i] = -kInfinity;
         }
+        return kept;
+    };
+    float ahead[I];
+    bool kept_ahead = fetch(begin + group, ahead);
+    for (int64_t t0 = begin; t0 < end; t0 += kGroups) {
+        const int64_t t = t0 + group;
+        const bool live = kept_ahead;
+        float v[I], e[I], top, sum;
+#pragma unroll
+        for (int i = 0; i < I; ++i) v[i] = ahead[i];
+        kept_ahead = fetch(t + kGroups, ahead);
         exponentials<L, I>(v, e, top, sum);
-        const unsigned taken = choose<L, I>(v, first, k);
+        const unsigned taken = choose<L, I>(v, k);
         // places of the lane's entries among the token's: those of the lanes before it come first
         const int own = __popc(taken);
-        int before = own;
-#pragma unroll
-        for (int off = 1; off < L; off <<= 1) {
-            const int left = __shfl_up(before, off, L);
-            if (lane >= off) before += left;
-        }
-        const int held = __shfl(before, L - 1, L);
-        before -= own;
+        const int upto = group_scan<L>(own), before = upto - own;
+        const int held = __shfl(upto, L - 1, L);
         float whole = 0.0f;
 #pragma unroll
         for (int i = 0; i < I; ++i) whole += taken >> i & 1 ? e[i] : 0.0f;
         whole = group_reduce<L>(whole, SumOf());
         if (a.normalise) whole = sum != sum ? sum : whole;     // (a NaN among the logits)
         const float by = 1.0f / (a.normalise ? whole : sum), part = 1.0f / sum;
-        int place = before;
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
+        for (int i = 0; i < I; ++i)
             if (live && sum != 0.0f) share[i] += e[i] * part;
-            if (taken >> i & 1) {
-                w.choice[t * k + place] = (uint16_t)(first + i);
-                w.gate[t * k + place] = e[i] * by;
-                atomicAdd(&hist[first + i], 1);
-                ++place;
-            }
+        // (most lanes have no entry or one: a turn for every entry of the lane that has most)
+        int place = before;
+        for (unsigned rest = taken; rest != 0; rest &= rest - 1) {
+            const int at = __ffs((int)rest) - 1;
+            float mine = e[0];
+#pragma unroll
+            for (int i = 1; i < I; ++i) mine = at == i ? e[i] : mine;
+            w.choice[t * k + place] = (uint16_t)(first + at);
+            w.gate[t * k + place] = mine * by;
+            atomicAdd(&hist[first + at], 1);
+            ++place;
         }
         if (t < end && lane == 0) {
             w.held[t] = (uint8_t)held;
@@ -207,40 +286,50 @@ __global__ void __launch_bounds__(kThreads) route_choose_kernel(RouteArgs a, Rou
 }
 
 // One wavefront an expert, and one for the tokens: what the workgroups left becomes what lies before each of them; the
-// totals go to counts, expert_pos[0] (entries) and routed.
+// totals go to counts, pos and routed.  A lane has consecutive workgroups, all asked for at once.
+constexpr int kMostGroups = 1024;
 __global__ void __launch_bounds__(NACHO_WAVE) route_scan_kernel(RouteArgs a, RouteScratch w)
 {
-    const int e = (int)blockIdx.x, n = a.experts, lane = lane_id();
-    const int groups = (int)w.groups;
-    int running = 0, routed = 0;
-    float share = 0.0f;
-    for (int g0 = 0; g0 < groups; g0 += NACHO_WAVE) {
-        const int g = g0 + lane;
-        int v = 0;
-        if (g < groups) {
-            if (e < n) {
-                v = w.hist[(int64_t)g * n + e];
-                share += w.share[(int64_t)g * n + e];
-            } else {
-                v = w.entries[g];
-                routed += w.routed[g];
-            }
+    constexpr int kMost = kMostGroups / NACHO_WAVE;
+    const int e = (int)blockIdx.x, n = a.experts, lane = lane_id(), groups = (int)w.groups;
+    const int each = (groups + NACHO_WAVE - 1) / NACHO_WAVE, first = lane * each;
+    int32_t *const from = e < n ? w.hist + e : w.entries;
+    const int64_t step = e < n ? n : 1;
+    int v[kMost], routed = 0, own = 0;
+    float share = 0.0f, s[kMost];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const int g = first + i;
+        v[i] = 0;
+        s[i] = 0.0f;
+        if (i < each && g < groups) {
+            v[i] = from[g * step];
+            if (e < n) s[i] = w.share[(int64_t)g * n + e];
+            else routed += w.routed[g];
         }
-        const int upto = wave_inclusive_scan(v);
-        if (g < groups) {
-            if (e < n) w.hist[(int64_t)g * n + e] = running + upto - v;
-            else w.entries[g] = running + upto - v;
-        }
-        running += __shfl(upto, NACHO_WAVE - 1, NACHO_WAVE);
+    }
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        own += v[i];
+        share += s[i];
+    }
+    const int upto = wave_inclusive_scan(own);
+    int before = upto - own;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const int g = first + i;
+        if (i < each && g < groups) from[g * step] = before;
+        before += v[i];
     }
     share = wave_sum(share);
     routed = wave_sum(routed);
+    const int total = __shfl(upto, NACHO_WAVE - 1, NACHO_WAVE);
     if (lane == 0) {
         if (e < n) {
-            a.out.counts[e] = running;
+            a.out.counts[e] = total;
             w.share[e] = share;
         } else {
-            a.out.pos[a.tokens] = running;
+            a.out.pos[a.tokens] = total;
             a.out.routed[0] = routed;
         }
     }
@@ -344,6 +433,7 @@ template <typename T, int L, int I>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteGradArgs a)
 {
     constexpr int kGroups = kThreads / L;
+    __shared__ float added[kGroups][L * I];                    // what the gates add to every expert of a group's token
     const int tid = (int)threadIdx.x, group = tid / L, lane = tid % L, first = lane * I, n = a.experts;
     const T *logits = static_cast<const T *>(a.logits);
     T *grad = static_cast<T *>(a.grad);
@@ -354,51 +444,67 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(RouteGradArgs a)
     float c[I];
 #pragma unroll
     for (int i = 0; i < I; ++i) c[i] = first + i < n ? unit * (float)a.routing.counts[first + i] : 0.0f;
-    for (int64_t t0 = (int64_t)blockIdx.x * kGroups; t0 < a.tokens; t0 += (int64_t)gridDim.x * kGroups) {
-        const int64_t t = t0 + group;
-        int at = 0, held = 0;
+    // a token's logits and the place of its entries are on their way while the one before it is worked on (also of tokens
+    // that store nothing, whose result does not take them)
+    auto fetch = [&](int64_t t, float (&to)[I], int &at, int &held) {
+        at = held = 0;
         if (t < a.tokens) {
+            row_part<T, I>(logits + t * a.ldl, first, n, words, to);
             at = a.routing.pos[t];
             held = a.routing.pos[t + 1] - at;
-        }
-        float d[I];
+        } else {
 #pragma unroll
-        for (int i = 0; i < I; ++i) d[i] = 0.0f;
-        float v[I], p[I], top, sum, inner = 0.0f, mean = 0.0f;
-        if (held > 0) row_part<T, I>(logits + t * a.ldl, first, n, words, v);
-        else {
-#pragma unroll
-            for (int i = 0; i < I; ++i) v[i] = -kInfinity;
+            for (int i = 0; i < I; ++i) to[i] = -kInfinity;
         }
+    };
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    float ahead[I];
+    int at_ahead, held_ahead;
+    fetch((int64_t)blockIdx.x * kGroups + group, ahead, at_ahead, held_ahead);
+    for (int64_t t0 = (int64_t)blockIdx.x * kGroups; t0 < a.tokens; t0 += step) {
+        const int64_t t = t0 + group;
+        const int at = at_ahead, held = held_ahead;
+        float v[I], p[I], top, sum, mean = 0.0f, inner = 0.0f;
+#pragma unroll
+        for (int i = 0; i < I; ++i) v[i] = ahead[i];
+        // a lane has every L-th entry of the token, the first of them in registers
+        float g = 0.0f, dg = 0.0f;
+        int to = -1;
+        if (a.grad_gate && lane < held) {
+            g = a.routing.gate[at + lane];
+            dg = a.grad_gate[at + lane];
+            to = a.routing.expert[at + lane];
+        }
+        fetch(t + step, ahead, at_ahead, held_ahead);
+#pragma unroll
+        for (int i = 0; i < I; ++i) added[group][first + i] = 0.0f;
         // (not by the lse of the forward call: next to large logits it has no room for the sum)
         exponentials<L, I>(v, p, top, sum);
-        if (held > 0) {
-            const float part = 1.0f / sum;
+        const float part = sum != 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
-            for (int i = 0; i < I; ++i) {
-                p[i] *= part;
-                mean += p[i] * c[i];
-            }
-            if (a.grad_gate) {
-                for (int j = 0; j < held; ++j) inner += a.routing.gate[at + j] * a.grad_gate[at + j];
-                for (int j = 0; j < held; ++j) {
-                    const int e = a.routing.expert[at + j] - first;
-                    if (e >= 0 && e < I) {
-                        const float g = a.routing.gate[at + j], dg = a.grad_gate[at + j];
-                        const float add = g * (a.normalise ? dg - inner : dg);
-#pragma unroll
-                        for (int i = 0; i < I; ++i) d[i] += e == i ? add : 0.0f;
-                    }
-                }
-            }
+        for (int i = 0; i < I; ++i) {
+            p[i] *= part;
+            mean += p[i] * c[i];
         }
         mean = group_reduce<L>(mean, SumOf());
-        if (held > 0) {
-            const float less = mean + (a.normalise ? 0.0f : inner);
+        inner = g * dg;
+        if (a.grad_gate)
+            for (int j = lane + L; j < held; j += L) inner += a.routing.gate[at + j] * a.grad_gate[at + j];
+        inner = group_reduce<L>(inner, SumOf());
+        wave_sync();
+        if (to >= 0) added[group][to] = g * (a.normalise ? dg - inner : dg);
+        if (a.grad_gate)
+            for (int j = lane + L; j < held; j += L) {
+                const float more = a.routing.gate[at + j], by = a.grad_gate[at + j];
+                added[group][a.routing.expert[at + j]] = more * (a.normalise ? by - inner : by);
+            }
+        wave_sync();
+        const float less = mean + (a.normalise ? 0.0f : inner);
+        float d[I];
 #pragma unroll
-            for (int i = 0; i < I; ++i) d[i] += p[i] * (c[i] - less);
-        }
+        for (int i = 0; i < I; ++i) d[i] = held > 0 ? added[group][first + i] + p[i] * (c[i] - less) : 0.0f;
         if (t < a.tokens) put_row_part<T, I>(grad + t * a.ldg, first, n, words_out, d);
+        wave_sync();
     }
 }
 
@@ -426,7 +532,7 @@ template <typename F> void by_type(int dtype, F f)
 void route_plan(int64_t tokens, int32_t, int64_t *groups, int64_t *per_group)
 {
     // up to 1024 workgroups (four a compute unit), whole chunks of tokens each
-    const int64_t chunks = (tokens + kChunk - 1) / kChunk, each = (chunks + 1023) / 1024;
+    const int64_t chunks = (tokens + kChunk - 1) / kChunk, each = (chunks + kMostGroups - 1) / kMostGroups;
     *per_group = (each > 0 ? each : 1) * kChunk;
     *groups = (tokens + *per_group - 1) / *per_group;
     if (*groups < 1) *groups = 1;
