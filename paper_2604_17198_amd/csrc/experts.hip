@@ -160,21 +160,44 @@ template <typename T> __device__ inline const T *at_row(const T *base, int row, 
     return base + (uint64_t)(unsigned)row * (unsigned)ld;
 }
 
-// 16 bytes from any element's address, in one instruction (global memory takes any alignment); with `there` < n elements
-// left the others are zero.
-template <typename T> __device__ inline v4u load_anywhere(const T *from, int there)
-{
-    constexpr int n = Word<T>::n;
-    v4u word = {0, 0, 0, 0};
-    if (there >= n) __builtin_memcpy(&word, from, 16);
-    else if (there > 0) {
+// Words of rows that no 16-byte boundary fits: 16 bytes from any element's address, in one instruction (global memory takes
+// any alignment).  Of a row's last elements, fewer than a word, the word that ends with them is loaded and moved down by
+// `shift` elements when it is stored to LDS, so that nothing waits for it before.
+template <typename T> struct Ragged {
+    int there, shift;          // elements from the word's first one on; places that the word is moved down
+    bool single;               // rows too short for that: elements one by one
+    // `before`: elements of the row before the word.
+    __device__ Ragged(int left, int before)
+    {
+        constexpr int n = Word<T>::n;
+        there = left < n ? left : n;
+        shift = there > 0 ? n - there : 0;
+        single = shift > before;
+    }
+    __device__ v4u load(const T *from) const
+    {
+        constexpr int n = Word<T>::n;
+        v4u word = {0, 0, 0, 0};
+        if (there <= 0) return word;
+        if (!single) {
+            __builtin_memcpy(&word, from - shift, 16);
+            return word;
+        }
         typename Word<T>::type v;
 #pragma unroll
         for (int e = 0; e < n; ++e) v[e] = e < there ? from[e] : (T)0.0f;
-        word = __builtin_bit_cast(v4u, v);
+        return __builtin_bit_cast(v4u, v);
     }
-    return word;
-}
+    __device__ v4u placed(v4u w) const
+    {
+        if (shift == 0 || single) return w;
+        const int bytes = shift * (int)sizeof(T);
+        if (bytes & 8) w = v4u{w[2], w[3], 0, 0};
+        if (bytes & 4) w = v4u{w[1], w[2], w[3], 0};
+        if (bytes & 2) w = v4u{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+        return w;
+    }
+};
 
 // Rows that run along k.  A thread loads words of 16 bytes, the same one of several rows.
 template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct AlongK {
@@ -185,6 +208,7 @@ template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct Al
     int64_t ld;
     int row[kLoads];
     v4u word[kLoads];
+    Ragged<T> last = Ragged<T>(0, 0);
     int unit, at;
 
     // number(r): which row of the matrix is row r of the tile.
@@ -201,11 +225,12 @@ template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct Al
     {
         constexpr int n = Word<T>::n;
         const int first = k0 + unit * n;
+        if constexpr (!kWords) last = Ragged<T>(k - first, first);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const T *from = base + row[i] * ld + first;
             if constexpr (kWords) word[i] = first < k ? *reinterpret_cast<const v4u *>(from) : v4u{0, 0, 0, 0};
-            else word[i] = load_anywhere(from, k - first);
+            else word[i] = last.load(from);
         }
     }
     // Asks for the words k0 .. of all rows (whole words).  What a lane loads lies behind what the lane before it loads,
@@ -225,7 +250,7 @@ template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct Al
     __device__ void store(char *lds) const
     {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) *reinterpret_cast<v4u *>(lds + place(at + i * kApart, unit)) = word[i];
+        for (int i = 0; i < kLoads; ++i) *reinterpret_cast<v4u *>(lds + place(at + i * kApart, unit)) = kWords ? word[i] : last.placed(word[i]);
     }
     // Where a lane's fragments of the rows from r0 on (a multiple of 16) start; and its 16 bytes of rows 16 number ..
     // from there in step `step` of 64 bytes.
@@ -243,19 +268,22 @@ template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct Ac
     static constexpr int kLoads = kDepth<T, kStep> * kRowWords / kThreads, kBytes = kDepth<T, kStep> * kRowBytes;
     static_assert(kRowWords >= 16 && kLoads * kThreads == kDepth<T, kStep> * kRowWords, "rows that the turns fit into");
     v4u word[kLoads];
+    Ragged<T> last = Ragged<T>(0, 0);
 
-    // address(k): the row of k; `most`: elements of it from the tile's first one on.
-    template <typename Row> __device__ void load(Row address, int k0, int k, int most)
+    // address(i, k): the row of k (of the thread's i-th word), from the tile's first element on; `most`: elements of it from there on, `before`: those before.
+    template <typename Row> __device__ void load(Row address, int k0, int k, int most, int before)
     {
         constexpr int n = Word<T>::n;
+        static_assert(kThreads % kRowWords == 0, "the same word of all rows of a thread");
+        if constexpr (!kWords) last = Ragged<T>(most - (int)threadIdx.x % kRowWords * n, before + (int)threadIdx.x % kRowWords * n);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int u = (int)threadIdx.x + i * kThreads, kk = k0 + u / kRowWords, first = u % kRowWords * n;
             word[i] = v4u{0, 0, 0, 0};
             if (kk < k && first < most) {
-                const T *from = address(kk) + first;
+                const T *from = address(i, kk) + first;
                 if constexpr (kWords) word[i] = *reinterpret_cast<const v4u *>(from);
-                else word[i] = load_anywhere(from, most - first);
+                else word[i] = last.load(from);
             }
         }
     }
@@ -282,7 +310,7 @@ template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct Ac
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int u = (int)threadIdx.x + i * kThreads;
-            *reinterpret_cast<v4u *>(lds + place(u / kRowWords, u % kRowWords)) = word[i];
+            *reinterpret_cast<v4u *>(lds + place(u / kRowWords, u % kRowWords)) = kWords ? word[i] : last.placed(word[i]);
         }
     }
     static __device__ int lane_base(int r0) { return r0 * (int)sizeof(T); }
@@ -370,17 +398,31 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
             return kForm == FORWARD && a.token ? a.token[row] : row;
         });
     if constexpr (!kAcrossP) side_p.start(p, a.ldp, [&](int r) { return n0 + r < a.n ? n0 + r : a.n - 1; });
+    // Rows of x that the words of the next step of k come from: asked for a step ahead, or every step would wait for them
+    // before it can ask for the words.
+    int slot[kForm == WEIGHTS ? SideP::kLoads : 1];
+    auto look_up = [&](int k0) {
+        if constexpr (kForm == WEIGHTS) {
+#pragma unroll
+            for (int l = 0; l < SideP::kLoads; ++l) {
+                const int kk = k0 + SideP::row_of_load(l);
+                slot[l] = k_begin + (kk < k ? kk : k - 1);
+            }
+            if (a.token) {
+#pragma unroll
+                for (int l = 0; l < SideP::kLoads; ++l) slot[l] = a.token[slot[l]];
+            }
+        }
+    };
     auto load = [&](int k0) {
         if constexpr (kAcrossQ)
-            side_q.load([&](int kk) { return q + (int64_t)(k_begin + kk) * a.ldq + m0; }, k0, k, a.m - m0);
+            side_q.load([&](int, int kk) { return q + (int64_t)(k_begin + kk) * a.ldq + m0; }, k0, k, a.m - m0, m0);
         else side_q.load(k0, k);
-        if constexpr (kForm == ROWS) side_p.load([&](int kk) { return p + (int64_t)kk * a.ldp + n0; }, k0, k, a.n - n0);
-        else if constexpr (kForm == WEIGHTS)
-            side_p.load([&](int kk) {
-                const int s = k_begin + kk;
-                return p + (int64_t)(a.token ? a.token[s] : s) * a.ldp + n0;
-            }, k0, k, a.n - n0);
-        else side_p.load(k0, k);
+        if constexpr (kForm == ROWS) side_p.load([&](int, int kk) { return p + (int64_t)kk * a.ldp + n0; }, k0, k, a.n - n0, n0);
+        else if constexpr (kForm == WEIGHTS) {
+            side_p.load([&](int l, int) { return p + (int64_t)slot[l] * a.ldp + n0; }, k0, k, a.n - n0, n0);
+            look_up(k0 + kDepth<T, kStep> < k ? k0 + kDepth<T, kStep> : k0);
+        } else side_p.load(k0, k);
     };
     const int wave = (int)threadIdx.x / NACHO_WAVE, lane = lane_id();
     const int wm = wave / kWavesN * kTileM, wn = wave % kWavesN * kTileN;
@@ -429,22 +471,11 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
     };
     constexpr int kDeep = kDepth<T, kStep>;
     int done = 0;
+    if (k > 0) look_up(0);
     if constexpr (kWords) {
         // Whole steps of k.  One is on its way to LDS while the one before it is multiplied; and while the matrix units
         // have one half of a wavefront's tile, the registers of the next half are read.
         const int steps = k / kDeep;
-        int slot[kForm == WEIGHTS ? SideP::kLoads : 1];       // rows of x that the words of the next step come from
-        auto look_up = [&](int t) {
-            if constexpr (kForm == WEIGHTS) {
-                const int s = k_begin + (t < steps ? t : steps - 1) * kDeep;
-#pragma unroll
-                for (int l = 0; l < SideP::kLoads; ++l) slot[l] = s + SideP::row_of_load(l);
-                if (a.token) {
-#pragma unroll
-                    for (int l = 0; l < SideP::kLoads; ++l) slot[l] = a.token[slot[l]];
-                }
-            }
-        };
         // (i: of stage t)
         auto ask = [&](int t, auto i) {
             char *lds = stage(i);
@@ -455,7 +486,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
             else if constexpr (kForm == ROWS)
                 side_p.ask([&](int, int kk) { return at_row(p + n0, kk, a.ldp); }, t * kDeep, a.n - n0, lds + SideQ::kBytes);
             else side_p.ask(t * kDeep, lds + SideQ::kBytes);
-            look_up(t + 1);
+            look_up((t + 1) * kDeep);
         };
         // (Behind the last step the next one's registers are read all the same, and not used: a wait that is not there on
         // every path would have the compiler wait for all loads before it reads.)
@@ -484,7 +515,6 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
             });
         };
         if (steps > 0) {
-            look_up(0);
             ask(0, zero);
             wait_loads();
             if (steps > 1) ask(1, one);
@@ -505,15 +535,18 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
         side_q.store(stage0);
         side_p.store(stage0 + SideQ::kBytes);
         __syncthreads();
+        char *here = stage0, *there = stage1;
         for (; done < k; done += kDeep) {
             const bool more = !kWords && done + kDeep < k;
             if (more) load(done + kDeep);
-            multiply_all(stage0);
+            multiply_all(here);
             if (more) {
+                side_q.store(there);
+                side_p.store(there + SideQ::kBytes);
                 __syncthreads();
-                side_q.store(stage0);
-                side_p.store(stage0 + SideQ::kBytes);
-                __syncthreads();
+                char *const next = here;
+                here = there;
+                there = next;
             }
         }
     }
@@ -603,7 +636,10 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
     T *gz = static_cast<T *>(a.grad_z) + c;
     auto get = [&](const T *from) {
         if constexpr (kWords) return width > 0 ? *reinterpret_cast<const v4u *>(from) : v4u{0, 0, 0, 0};
-        else return load_anywhere(from, width);
+        else {
+            const Ragged<T> last(width, c);
+            return last.placed(last.load(from));
+        }
     };
     float sum[n];
 #pragma unroll
