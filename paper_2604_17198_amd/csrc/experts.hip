@@ -704,7 +704,14 @@ template <typename T> __global__ void __launch_bounds__(kThreads) experts_bias_k
     const int tiles = tiles_of(expert);
     if (c >= a.cols) return;
     float total = 0.0f;
-    for (int t = 0; t < tiles; ++t) total += a.sums[(int64_t)(first + t) * a.cols + c];
+    constexpr int kBatch = 8;
+    for (int t = 0; t < tiles; t += kBatch) {
+        float part[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) part[i] = a.sums[(int64_t)(first + (t + i < tiles ? t + i : tiles - 1)) * a.cols + c];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) total += t + i < tiles ? part[i] : 0.0f;
+    }
     (static_cast<T *>(a.grad_bias) + (int64_t)expert * a.bias_stride)[c] = (T)total;
 }
 
@@ -724,7 +731,7 @@ bool in_words(std::initializer_list<std::pair<const void *, int64_t>> all, int e
     return bits % 16 == 0;
 }
 
-template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, bool kWords>
+template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, bool kWords, int kStep = 128>
 hipError_t run(const ProductArgs &a, hipStream_t s)
 {
     const int tiles_n = (a.n + kN - 1) / kN;
@@ -735,7 +742,7 @@ hipError_t run(const ProductArgs &a, hipStream_t s)
     // (a launch holds 2^32 threads along its first dimension)
     const int64_t tiles = tiles_m * tiles_n, row = tiles < (1 << 22) ? tiles : 1 << 22;
     if (tiles > 0x7fffffff - (1 << 22)) return hipErrorNotSupported;
-    experts_kernel<T, kForm, kM, kN, kWavesM, kWavesN, 128, kWords>
+    experts_kernel<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>
         <<<dim3((unsigned)row, (unsigned)((tiles + row - 1) / row)), kWavesM * kWavesN * NACHO_WAVE, 0, s>>>(a, tiles_n);
     return hipGetLastError();
 }
@@ -766,7 +773,7 @@ template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, bool 
                 return run<T, kForm, 256, 256, 2, 4, true>(a, s);
         }
         if (each <= 64 || a.slots / 128 * n128 < 2 * kUnits)
-            return words ? run<T, kForm, 32, 128, 1, 4, true>(a, s) : run<T, kForm, 32, 128, 1, 4, false>(a, s);
+            return words ? run<T, kForm, 32, 128, 1, 4, true, 256>(a, s) : run<T, kForm, 32, 128, 1, 4, false>(a, s);
         return words ? run<T, kForm, 128, 128, 2, 2, true>(a, s) : run<T, kForm, 128, 128, 2, 2, false>(a, s);
     }
 }
