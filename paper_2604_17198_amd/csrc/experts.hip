@@ -133,6 +133,26 @@ template <int kM, typename Args> __device__ inline bool find_tile(const Args &a,
     return false;
 }
 
+// Which tile of rows (the experts' one after the other) and which columns a workgroup computes.  Workgroups are dealt out to
+// the chip's eight parts one by one, each of which has a cache; 32 of a part's that run at a time get 4 x 8 neighbouring
+// tiles, which need 12 stretches of Q and P between them.  (16384 slots, bf16, us, against tiles in the order of rows: 16
+// experts of 2048 x 8192, rows 663, weights 687.)
+template <int kN> __device__ inline void place_tile(int tiles_m, int tiles_n, int &tile, int &n0)
+{
+    constexpr int kRound = 256, kParts = 8, kTall = 4;
+    int number = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+    if ((number | (kRound - 1)) < tiles_m * tiles_n)
+        number = (number & ~(kRound - 1)) | (number % kParts) * (kRound / kParts) | (number % kRound) / kParts;
+    const int band = number / (kTall * tiles_n), in_band = number - band * kTall * tiles_n;
+    const int rows = tiles_m - band * kTall < kTall ? tiles_m - band * kTall : kTall;
+    tile = tiles_m;                    // (behind the last tile)
+    n0 = 0;
+    if (rows <= 0) return;
+    const int column = in_band / rows;
+    tile = band * kTall + in_band - column * rows;
+    n0 = column * kN;
+}
+
 // A side of the product: kRows rows (of Q or P), kStep bytes of k of each, loaded by kThreads threads.
 template <typename T, int kStep> constexpr int kDepth = kStep / (int)sizeof(T);
 
@@ -357,36 +377,37 @@ template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int 
     static constexpr int kBytes = SideQ::kBytes + SideP::kBytes;
     // (The stages are arguments that do not overlap: so the compiler knows that reads of one do not wait for loads to the
     // other, also those reads that transpose.)
-    static __device__ void compute(const ProductArgs &a, int tiles_n, char *__restrict stage0, char *__restrict stage1);
+    static __device__ void compute(const ProductArgs &a, int tiles_m, int tiles_n, char *__restrict stage0, char *__restrict stage1);
 };
 
 template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, bool kWords>
-__global__ void __launch_bounds__(kWavesM * kWavesN * NACHO_WAVE) experts_kernel(ProductArgs a, int tiles_n)
+__global__ void __launch_bounds__(kWavesM * kWavesN * NACHO_WAVE) experts_kernel(ProductArgs a, int tiles_m, int tiles_n)
 {
     typedef Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords> Work;
     __shared__ __attribute__((aligned(16))) char stage0[Work::kBytes], stage1[Work::kBytes];
-    Work::compute(a, tiles_n, stage0, stage1);
+    Work::compute(a, tiles_m, tiles_n, stage0, stage1);
 }
 
 template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, bool kWords>
-__device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::compute(const ProductArgs &a, int tiles_n,
+__device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::compute(const ProductArgs &a, int tiles_m, int tiles_n,
                                                                                         char *__restrict stage0, char *__restrict stage1)
 {
     auto stage = [&](auto i) -> char * {
         if constexpr (decltype(i)::value == 0) return stage0;
         else return stage1;
     };
-    const int number = (int)(blockIdx.y * gridDim.x + blockIdx.x), tile = number / tiles_n, n0 = (number - tile * tiles_n) * kN;
+    int tile, n0;
+    place_tile<kN>(tiles_m, tiles_n, tile, n0);
     int expert, m0, m_end, k_begin = 0, k = a.k;
     if (kForm == WEIGHTS) {
-        const int tiles_m = (a.m + kM - 1) / kM;
-        expert = tile / tiles_m;
+        const int tiles = (a.m + kM - 1) / kM;
+        expert = tile / tiles;
         if (expert >= a.experts) return;
-        m0 = (tile - expert * tiles_m) * kM;
+        m0 = (tile - expert * tiles) * kM;
         m_end = a.m;
         k_begin = bound_of(a, expert);
         k = bound_of(a, expert + 1) - k_begin;
-    } else if (!find_tile<kM>(a, tile, expert, m0, m_end)) return;
+    } else if (!find_tile<kM>(a, tile, expert, m0, m_end) || n0 >= a.n) return;
     const T *const q = static_cast<const T *>(a.q);
     const T *const p = static_cast<const T *>(a.p) + (int64_t)expert * a.p_stride;
     SideQ side_q;
@@ -426,6 +447,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
     };
     const int wave = (int)threadIdx.x / NACHO_WAVE, lane = lane_id();
     const int wm = wave / kWavesN * kTileM, wn = wave % kWavesN * kTileN;
+    const bool busy = __builtin_amdgcn_readfirstlane(m0 + wm < m_end && n0 + wn < a.n ? 1 : 0) != 0;
     v4f acc[kFragM][kFragN];
 #pragma unroll
     for (int i = 0; i < kFragM; ++i)
@@ -514,18 +536,32 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
                 });
             });
         };
+        // Wavefronts whose rows or columns all lie behind the last only load: the others of their SIMD then have the matrix unit
+        // for themselves.
         if (steps > 0) {
             ask(0, zero);
             wait_loads();
             if (steps > 1) ask(1, one);
-            read_p(stage0, zero);
-            read_q(stage0, zero, zero);
             int t = 0;
-            for (; t + 2 <= steps; t += 2) {
-                body(t, zero);
-                body(t + 1, one);
+            if (busy) {
+                read_p(stage0, zero);
+                read_q(stage0, zero, zero);
+                for (; t + 2 <= steps; t += 2) {
+                    body(t, zero);
+                    body(t + 1, one);
+                }
+                if (t < steps) body(t, zero);
+            } else {
+                auto pass = [&](int at, auto which) {
+                    wait_loads();
+                    if (at + 2 < steps) ask(at + 2, which);
+                };
+                for (; t + 2 <= steps; t += 2) {
+                    pass(t, zero);
+                    pass(t + 1, one);
+                }
+                if (t < steps) pass(t, zero);
             }
-            if (t < steps) body(t, zero);
         }
         done = steps * kDeep;
         __syncthreads();
@@ -539,7 +575,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
         for (; done < k; done += kDeep) {
             const bool more = !kWords && done + kDeep < k;
             if (more) load(done + kDeep);
-            multiply_all(here);
+            if (busy) multiply_all(here);
             if (more) {
                 side_q.store(there);
                 side_p.store(there + SideQ::kBytes);
@@ -743,7 +779,7 @@ hipError_t run(const ProductArgs &a, hipStream_t s)
     const int64_t tiles = tiles_m * tiles_n, row = tiles < (1 << 22) ? tiles : 1 << 22;
     if (tiles > 0x7fffffff - (1 << 22)) return hipErrorNotSupported;
     experts_kernel<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>
-        <<<dim3((unsigned)row, (unsigned)((tiles + row - 1) / row)), kWavesM * kWavesN * NACHO_WAVE, 0, s>>>(a, tiles_n);
+        <<<dim3((unsigned)row, (unsigned)((tiles + row - 1) / row)), kWavesM * kWavesN * NACHO_WAVE, 0, s>>>(a, (int)tiles_m, tiles_n);
     return hipGetLastError();
 }
 
@@ -764,7 +800,7 @@ template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, bool 
             if (words && a.m >= 256 && a.n >= 256 && tiles >= kUnits) return run<T, kForm, 256, 256, 2, 4, true>(a, s);
         } else if (tiles < kUnits) {
             // (floats: four times as many matrix instructions for a load; 3000 slots of 7 experts, 777 x 499)
-            return words ? run<T, kForm, 64, 128, 1, 4, true>(a, s) : run<T, kForm, 64, 128, 1, 4, false>(a, s);
+            return words ? run<T, kForm, 64, 64, 2, 2, true>(a, s) : run<T, kForm, 64, 64, 2, 2, false>(a, s);
         }
         return words ? run<T, kForm, 128, 128, 2, 2, true>(a, s) : run<T, kForm, 128, 128, 2, 2, false>(a, s);
     } else {
@@ -772,7 +808,11 @@ template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, bool 
             if (words && each >= 512 && a.n >= 256 && a.slots / 256 * ((a.n + 255) / 256) >= kUnits)
                 return run<T, kForm, 256, 256, 2, 4, true>(a, s);
         }
-        if (each <= 64 || a.slots / 128 * n128 < 2 * kUnits)
+        const bool small = each <= 64 || a.slots / 128 * n128 < 2 * kUnits;
+        if constexpr (sizeof(T) == 4) {
+            if (small && each > 64) return words ? run<T, kForm, 64, 64, 2, 2, true>(a, s) : run<T, kForm, 64, 64, 2, 2, false>(a, s);
+        }
+        if (small)
             return words ? run<T, kForm, 32, 128, 1, 4, true, 256>(a, s) : run<T, kForm, 32, 128, 1, 4, false>(a, s);
         return words ? run<T, kForm, 128, 128, 2, 2, true>(a, s) : run<T, kForm, 128, 128, 2, 2, false>(a, s);
     }
