@@ -528,11 +528,15 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
                         read_q(stage(which), behind, zero);
                     } else {
                         wait_loads();
-                        if (t + 2 < steps) ask(t + 2, which);
+                        if (kForm == WEIGHTS && t + 2 < steps) ask(t + 2, which);
                         read_p(stage(other), zero);
                         read_q(stage(other), zero, zero);
                     }
                     multiply(step, part);
+                    // (behind the part: its matrix instructions run while the loads are asked for; 16384 slots, 2048 x 8192, us:
+                    // forward 579 and 566, rows 661 and 616.  The weights' product has no registers left for that.)
+                    if constexpr (kForm != WEIGHTS && h + 1 == kParts && s + 1 == kSteps)
+                        if (t + 2 < steps) ask(t + 2, which);
                 });
             });
         };
