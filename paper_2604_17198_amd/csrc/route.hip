@@ -194,8 +194,8 @@ template <int L, int I> __device__ inline unsigned choose(const float (&v)[I], i
     return above;
 }
 
-template <typename T, int L, int I>
-__global__ void __launch_bounds__(kThreads) route_choose_kernel(RouteArgs a, RouteScratch w)
+// A workgroup's stretch of tokens: their experts and gates, and its counts and sums by expert.
+template <typename T, int L, int I> __device__ inline void choose_stretch(const RouteArgs &a, const RouteScratch &w)
 {
     constexpr int kGroups = kThreads / L, kSlots = L * I;
     __shared__ int hist[kSlots];
@@ -335,7 +335,8 @@ __global__ void __launch_bounds__(NACHO_WAVE) route_scan_kernel(RouteArgs a, Rou
     }
 }
 
-__global__ void __launch_bounds__(kThreads) route_place_kernel(RouteArgs a, RouteScratch w)
+// Where the entries of a workgroup's stretch lie, when the counts and what lies before the workgroup are known.
+__device__ inline void place_stretch(const RouteArgs &a, const RouteScratch &w)
 {
     __shared__ int base[kMostExperts];                 // where the workgroup's next entry of an expert goes
     __shared__ unsigned bits[kMostExperts][kChunk / 32];
@@ -427,6 +428,29 @@ __global__ void __launch_bounds__(kThreads) route_place_kernel(RouteArgs a, Rout
         a.out.slot[i] = -1;
         a.out.token[i] = -1;
     }
+}
+
+template <typename T, int L, int I>
+__global__ void __launch_bounds__(kThreads) route_choose_kernel(RouteArgs a, RouteScratch w) { choose_stretch<T, L, I>(a, w); }
+__global__ void __launch_bounds__(kThreads) route_place_kernel(RouteArgs a, RouteScratch w) { place_stretch(a, w); }
+
+// Tokens of one workgroup: nothing lies before it, and one launch does (16 tokens of 64 experts: 22 us a call with three).
+template <typename T, int L, int I>
+__global__ void __launch_bounds__(kThreads) route_few_kernel(RouteArgs a, RouteScratch w)
+{
+    choose_stretch<T, L, I>(a, w);
+    __syncthreads();
+    for (int e = (int)threadIdx.x; e < a.experts; e += kThreads) {
+        a.out.counts[e] = w.hist[e];
+        w.hist[e] = 0;
+    }
+    if (threadIdx.x == 0) {
+        a.out.pos[a.tokens] = w.entries[0];
+        a.out.routed[0] = w.routed[0];
+        w.entries[0] = 0;
+    }
+    __syncthreads();
+    place_stretch(a, w);
 }
 
 template <typename T, int L, int I>
@@ -540,6 +564,16 @@ void route_plan(int64_t tokens, int32_t, int64_t *groups, int64_t *per_group)
 
 hipError_t launch_route(int dtype, const RouteArgs &a, const RouteScratch &w, hipStream_t s)
 {
+    if (w.groups == 1) {
+        by_type(dtype, [&](auto zero) {
+            by_experts(a.experts, [&](auto lanes, auto items) {
+                route_few_kernel<decltype(zero), decltype(lanes)::value, decltype(items)::value><<<dim3(1), kThreads, 0, s>>>(a, w);
+            });
+        });
+        const hipError_t rc = hipGetLastError();
+        if (rc == hipSuccess) nacho_host::profile_mark("route");
+        return rc;
+    }
     by_type(dtype, [&](auto zero) {
         by_experts(a.experts, [&](auto lanes, auto items) {
             route_choose_kernel<decltype(zero), decltype(lanes)::value, decltype(items)::value>
