@@ -194,7 +194,8 @@ int32_t nacho_distill_workspace_bytes(int64_t n_rows, int64_t n_cols, int32_t dt
 {
     if (!bytes || !value_type(dtype) || n_rows < 0 || n_rows > kMostRows || n_cols < 0 || n_cols > kMostRows)
         return NACHO_ERR_INVALID_ARG;
-    *bytes = align_up((size_t)distill_partials(dtype, n_rows, n_cols, false) * sizeof(float), 256);
+    const int64_t with = distill_partials(dtype, n_rows, n_cols, true), without = distill_partials(dtype, n_rows, n_cols, false);
+    *bytes = align_up((size_t)(with > without ? with : without) * sizeof(float), 256);
     return NACHO_OK;
 }
 

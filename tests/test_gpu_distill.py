@@ -166,6 +166,24 @@ def test_rows_the_teacher_stores_much_of(rows, cols, held):
     check(loss, lse, grad, definition(pos, crd, val, z.cpu().numpy(), weight, 2.0), weight, 2.0, torch.float32)
 
 
+@pytest.mark.parametrize("rows,cols,dtype", [(130, 70_001, torch.bfloat16), (520, 66_003, torch.float16), (140, 40_005, torch.float32),
+                                             (513, 34_002, torch.float32)], ids=str)
+def test_long_rows_held_and_in_parts(rows, cols, dtype):
+    """Around the numbers of rows at which long ones are cut, with a gradient and without."""
+    rng = np.random.default_rng(rows + cols)
+    pos, crd, val, z, weight = case(rng, rows, cols, 1, 30, dtype, 0.1)
+    want = definition(pos, crd, val, z.float().cpu().numpy(), weight, 1.5)
+    T, w = operand(pos, crd, val, rows, cols), torch.from_numpy(weight).cuda()
+    for n in (rows, 100):
+        part = operand(pos[:n + 1], crd[:pos[n]], val[:pos[n]], n, cols)
+        some = tuple(v[:n] for v in want)
+        grad = torch.full_like(z[:n], float("nan"))
+        loss, lse = nb.nacho_distill(part, z[:n], temperature=1.5, weight=w[:n], grad=grad)
+        check(loss, lse, grad, some, weight[:n], 1.5, dtype)
+        loss, lse = nb.nacho_distill(part, z[:n], temperature=1.5, weight=w[:n])
+        check(loss, lse, None, some, weight[:n], 1.5, dtype)
+
+
 def test_no_rows():
     T = operand(np.zeros(1, np.int32), np.zeros(0, np.int32), np.zeros(0, np.float32), 0, 100)
     loss, lse = nb.nacho_distill(T, torch.empty((0, 100), device="cuda"))
