@@ -18,7 +18,10 @@
  *                       products (Section 2.1); DCSR operands intersect on the
  *                       outer level and take the recursive partitioning of
  *                       Section 3.3 (Algorithm 2);
- *   - nacho_validate  : debug aid, checks the preconditions below on the device.
+ *   - nacho_validate  : debug aid, checks the preconditions below on the device;
+ *   - nacho_distill, nacho_route, nacho_experts, nacho_combine, each with its
+ *                       gradient: operators that train models, around the sparse
+ *                       matrices which training makes (their own conventions below).
  *
  * Conventions that hold for every entry point
  *   * Descriptor structs (nacho_tensor, nacho_parts, nacho_sparse_out) live in
@@ -35,7 +38,8 @@
  *     checked): coordinates sorted and unique inside each segment, `pos`
  *     non-decreasing with pos[0] = 0, sum of the operands' nnz < 2^31, all
  *     operands of one call share the same level kinds and extents.
- *   * `crd`, `val` and dense operand arrays must be 16-byte aligned.
+ *   * `crd`, `val` and dense operand arrays must be 16-byte aligned (dense arrays of
+ *     the operators that train models: to their elements).
  *   * The return value is a status code.  Argument errors are detected on the
  *     host before anything is launched (nothing is written then); a failed HIP
  *     launch maps to NACHO_ERR_HIP.
@@ -418,14 +422,15 @@ int32_t nacho_spmul_k(const nacho_tensor *ops, int32_t k, int32_t dtype, int64_t
  *   grad    = weight[i] tau (q - p), the gradient of the sum of all losses, leading
  *             dimension ldg; NULL: not wanted
  * Rows of weight 0 and rows without a teacher's logit above -inf have loss, lse and
- * gradient 0, and their logits are not read.  Student logits of -inf have q = 0
+ * gradient 0, whatever their logits hold.  Student logits of -inf have q = 0
  * (a loss of +inf where the teacher gives them a share).  A row with nothing but
  * -inf, or with a NaN, has no distribution: NaN.
  * Workspace: nacho_distill_workspace_bytes (may be 0: then ws may be NULL).
  *
  * nacho_distill_grad: grad alone, from the logits and the lse of an earlier
  * nacho_distill on the same operands and temperature; weight then is the factor of
- * the loss times the gradient that arrives at it.
+ * the loss times the gradient that arrives at it.  lse has 32 bits: q is off by a
+ * factor of |lse| 2^-23, no matter for logits up to thousands.
  */
 int32_t nacho_distill_workspace_bytes(int64_t n_rows, int64_t n_cols, int32_t dtype, size_t *bytes);
 int32_t nacho_distill(const nacho_tensor *teacher, const void *logits, int64_t ldl, int32_t dtype,

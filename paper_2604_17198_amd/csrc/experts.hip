@@ -11,6 +11,10 @@
 //
 // Which expert a tile belongs to is found by its workgroup from expert_pos alone (a prefix sum of the experts' tiles
 // over the lanes), so nothing about the routing is read on the host.
+//
+// Bound by the matrix units for many slots an expert (16384 bf16 slots of 16 experts, 2048 x 8192: 636 us a call, 865 TFLOP/s
+// of the 1211 of a library's product of 8192^3), by the weights for few (16 of 32 experts, 2048 x 4096: 47 to 50 us a call for
+// 213 MB; 31 us a kernel where the last cache still has most of them).
 #include "kernels.hpp"
 #include "model.hpp"
 
@@ -135,8 +139,8 @@ template <int kM, typename Args> __device__ inline bool find_tile(const Args &a,
 
 // Which tile of rows (the experts' one after the other) and which columns a workgroup computes.  Workgroups are dealt out to
 // the chip's eight parts one by one, each of which has a cache; 32 of a part's that run at a time get 4 x 8 neighbouring
-// tiles, which need 12 stretches of Q and P between them.  (16384 slots, bf16, us, against tiles in the order of rows: 16
-// experts of 2048 x 8192, rows 663, weights 687.)
+// tiles, which need 12 stretches of Q and P between them.  (16384 slots of 16 experts, 2048 x 8192, bf16, us: weights 662, in
+// the order of rows 687; of 32 experts, 1024 x 4096, forward 205 and 217.)
 template <int kN> __device__ inline void place_tile(int tiles_m, int tiles_n, int &tile, int &n0)
 {
     constexpr int kRound = 256, kParts = 8, kTall = 4;
@@ -791,10 +795,12 @@ constexpr int64_t kUnits = 256;        // compute units
 
 // Tiles of 256 x 256 need half the LDS reads of tiles of 128 x 128 for the same results, but leave more of a tile empty
 // and fill the chip only if there are many of them.  16384 slots bf16, us: 16 experts (1024 slots each), 2048 x 8192, forward
-// 579 and 900, rows 670 and 749, weights 702 and 793; 32 experts (512 each), 1024 x 4096, 217 and 209, 239 and 241, 236 and 309.
+// 566 and 900, rows 616 and 749, weights 662 and 793; 32 experts (512 each), 1024 x 4096, 205 and 209, 219 and 241, 227 and 309.
 // Tiles of 32 x 128 for few slots an expert, where the weights are what is read, and where larger ones would leave compute
 // units without one: 16 slots of 32 experts, 2048 x 4096, forward 26 (128 x 128: 37), rows 37 (47); 1200 of 24, 1024 x 4096, 36
-// (43), 41 (50).
+// (43), 41 (50).  Their steps are of 256 bytes: 8 tokens, 2 of 32 experts, 49 us a call, with 128 bytes 53.
+// Floats need four times as many matrix instructions for what is loaded: tiles of 64 x 64, which are as many again.  3000 slots
+// of 7 experts, 777 x 499, us: weights 73 (64 x 128: 95), forward 42 (32 x 128: 45), rows 44 (50).
 template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, bool words, hipStream_t s)
 {
     const int64_t each = a.slots / a.experts, n128 = (a.n + 127) / 128;
@@ -803,7 +809,6 @@ template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, bool 
         if constexpr (sizeof(T) == 2) {
             if (words && a.m >= 256 && a.n >= 256 && tiles >= kUnits) return run<T, kForm, 256, 256, 2, 4, true>(a, s);
         } else if (tiles < kUnits) {
-            // (floats: four times as many matrix instructions for a load; 3000 slots of 7 experts, 777 x 499)
             return words ? run<T, kForm, 64, 64, 2, 2, true>(a, s) : run<T, kForm, 64, 64, 2, 2, false>(a, s);
         }
         return words ? run<T, kForm, 128, 128, 2, 2, true>(a, s) : run<T, kForm, 128, 128, 2, 2, false>(a, s);

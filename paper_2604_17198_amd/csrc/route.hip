@@ -4,7 +4,11 @@
 // L lanes hold a token's logits, I consecutive experts a lane, so that an expert's running sums stay in one lane's
 // registers over all tokens of a group of lanes.  Three kernels: every workgroup chooses for a stretch of consecutive
 // tokens and leaves its counts by expert; one wavefront an expert turns these into the entries before every workgroup;
-// every workgroup then knows where its entries lie in both orders.  All sums are in a fixed order.
+// every workgroup then knows where its entries lie in both orders.  Few tokens are one workgroup's, in one launch (16 x 64
+// bf16: 15.6 us a call, in three launches 22).  All sums are in a fixed order.
+//
+// Bound by instructions: 65536 x 128 floats, 8 each, 24 us to choose (the logits are 6 us of memory), 6 to 9 for
+// the scan, 6 to 9 to place, and 21 for the gradient, which waits for a token's entries before it can weigh them (11 us of memory).
 #include "kernels.hpp"
 #include "model.hpp"
 
