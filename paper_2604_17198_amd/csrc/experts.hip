@@ -12,8 +12,8 @@
 // Which expert a tile belongs to is found by its workgroup from expert_pos alone (a prefix sum of the experts' tiles
 // over the lanes), so nothing about the routing is read on the host.
 //
-// Bound by the matrix units for many slots an expert (16384 bf16 slots of 16 experts, 2048 x 8192: 636 us a call, 865 TFLOP/s
-// of the 1211 of a library's product of 8192^3), by the weights for few (16 of 32 experts, 2048 x 4096: 47 to 50 us a call for
+// Bound by the matrix units for many slots an expert (16384 bf16 slots of 16 experts, 2048 x 8192: 628 us a call, 875 TFLOP/s
+// of the 1211 of a library's product of 8192^3), by the weights for few (16 of 32 experts, 2048 x 4096: 47 to 58 us a call for
 // 213 MB; 31 us a kernel where the last cache still has most of them).
 #include "kernels.hpp"
 #include "model.hpp"
@@ -28,6 +28,7 @@ typedef unsigned int v4u __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
 enum Form { FORWARD, ROWS, WEIGHTS };
+enum Access { WORDS, ANYWHERE, TINY };  // rows of words of 16 bytes; rows that start and end anywhere; such rows shorter than a word
 
 // acc += (16 x 64 bytes of k) (64 bytes of k x 16); a lane's 16 bytes are consecutive k of row lane % 16, the lanes'
 // fours of 16 lie one after the other.  (The order of k inside a step does not matter as long as both sides agree.)
@@ -185,54 +186,60 @@ template <typename T> __device__ inline const T *at_row(const T *base, int row, 
 }
 
 // Words of rows that no 16-byte boundary fits: 16 bytes from any element's address, in one instruction (global memory takes
-// any alignment).  Of a row's last elements, fewer than a word, the word that ends with them is loaded and moved down by
-// `shift` elements when it is stored to LDS, so that nothing waits for it before.
-template <typename T> struct Ragged {
-    int there, shift;          // elements from the word's first one on; places that the word is moved down
-    bool single;               // rows too short for that: elements one by one
-    // `before`: elements of the row before the word.
-    __device__ Ragged(int left, int before)
+// any alignment).  Of a row's last elements, fewer than a word, and behind them, the word that ends with the row is loaded, and
+// moved down when it is stored to LDS, so that nothing waits for it before.  There is no branch on the way: behind one that loads
+// may be in, the next wait is for all loads (16384 bf16 slots of 16 experts, 1023 x 1025, both gradients: 441 us with branches,
+// 210 without).  Rows shorter than a word (kTiny): elements one by one.
+template <typename T, bool kTiny> struct Ragged {
+    int there, back;           // elements from the word's first one on; places that the loaded word lies before it
+    // `before`: elements of the row before the word; `length`: the row's, at least one.
+    __device__ Ragged(int length, int before)
     {
         constexpr int n = Word<T>::n;
-        there = left < n ? left : n;
-        shift = there > 0 ? n - there : 0;
-        single = shift > before;
+        there = length - before < n ? length - before : n;
+        back = n - there;
     }
     __device__ v4u load(const T *from) const
     {
         constexpr int n = Word<T>::n;
-        v4u word = {0, 0, 0, 0};
-        if (there <= 0) return word;
-        if (!single) {
-            __builtin_memcpy(&word, from - shift, 16);
-            return word;
-        }
-        typename Word<T>::type v;
+        v4u word;
+        if constexpr (!kTiny) __builtin_memcpy(&word, from - back, 16);
+        else {
+            typename Word<T>::type v;
 #pragma unroll
-        for (int e = 0; e < n; ++e) v[e] = e < there ? from[e] : (T)0.0f;
-        return __builtin_bit_cast(v4u, v);
+            for (int e = 0; e < n; ++e) v[e] = from[e < there ? e : there - 1];
+            word = __builtin_bit_cast(v4u, v);
+        }
+        return word;
     }
+    // The word with zeros behind the row.
     __device__ v4u placed(v4u w) const
     {
-        if (shift == 0 || single) return w;
-        const int bytes = shift * (int)sizeof(T);
+        constexpr int n = Word<T>::n;
+        if constexpr (kTiny) {
+            typename Word<T>::type v = __builtin_bit_cast(typename Word<T>::type, w);
+#pragma unroll
+            for (int e = 0; e < n; ++e) v[e] = e < there ? v[e] : (T)0.0f;
+            return __builtin_bit_cast(v4u, v);
+        }
+        const int bytes = back * (int)sizeof(T);
         if (bytes & 8) w = v4u{w[2], w[3], 0, 0};
         if (bytes & 4) w = v4u{w[1], w[2], w[3], 0};
         if (bytes & 2) w = v4u{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
-        return w;
+        return there > 0 ? w : v4u{0, 0, 0, 0};
     }
 };
 
 // Rows that run along k.  A thread loads words of 16 bytes, the same one of several rows.
-template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct AlongK {
+template <typename T, int kRows, int kStep, int kThreads, Access kAccess, int kSets> struct AlongK {
     static constexpr int kUnits = kStep / 16, kApart = kThreads / kUnits;
     static constexpr int kLoads = kRows / kApart, kBytes = kRows * kStep;
     static_assert(kLoads * kApart == kRows, "a whole number of rows a thread");
     const T *base;
     int64_t ld;
     int row[kLoads];
-    v4u word[kLoads];
-    Ragged<T> last = Ragged<T>(0, 0);
+    v4u word[kSets][kLoads];
+    int first[kSets], end;
     int unit, at;
 
     // number(r): which row of the matrix is row r of the tile.
@@ -245,16 +252,17 @@ template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct Al
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) row[i] = number(at + i * kApart);
     }
-    __device__ void load(int k0, int k)
+    template <typename Set> __device__ void load(Set set, int k0, int k)
     {
         constexpr int n = Word<T>::n;
-        const int first = k0 + unit * n;
-        if constexpr (!kWords) last = Ragged<T>(k - first, first);
+        const int from = k0 + unit * n;
+        first[set.value] = from;
+        end = k;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const T *from = base + row[i] * ld + first;
-            if constexpr (kWords) word[i] = first < k ? *reinterpret_cast<const v4u *>(from) : v4u{0, 0, 0, 0};
-            else word[i] = last.load(from);
+            const T *at = base + row[i] * ld + from;
+            if constexpr (kAccess == WORDS) word[set.value][i] = from < k ? *reinterpret_cast<const v4u *>(at) : v4u{0, 0, 0, 0};
+            else word[set.value][i] = Ragged<T, kAccess == TINY>(k, from).load(at);
         }
     }
     // Asks for the words k0 .. of all rows (whole words).  What a lane loads lies behind what the lane before it loads,
@@ -271,10 +279,14 @@ template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct Al
     // sixteens of bytes of 128.
     static __device__ int turn(int r) { return kUnits == 8 ? r & 7 : r >> 1 & 3; }
     static __device__ int place(int r, int u) { return r * kStep + ((u ^ turn(r)) << 4); }
-    __device__ void store(char *lds) const
+    template <typename Set> __device__ void store(Set set, char *lds) const
     {
+        const Ragged<T, kAccess == TINY> last(end, first[set.value]);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) *reinterpret_cast<v4u *>(lds + place(at + i * kApart, unit)) = kWords ? word[i] : last.placed(word[i]);
+        for (int i = 0; i < kLoads; ++i) {
+            const v4u w = word[set.value][i];
+            *reinterpret_cast<v4u *>(lds + place(at + i * kApart, unit)) = kAccess == WORDS ? w : last.placed(w);
+        }
     }
     // Where a lane's fragments of the rows from r0 on (a multiple of 16) start; and its 16 bytes of rows 16 number ..
     // from there in step `step` of 64 bytes.
@@ -287,28 +299,28 @@ template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct Al
 };
 
 // Columns that run along k: for every k a row of kRows elements.
-template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct AcrossK {
+template <typename T, int kRows, int kStep, int kThreads, Access kAccess, int kSets> struct AcrossK {
     static constexpr int kRowBytes = kRows * (int)sizeof(T), kRowWords = kRowBytes / 16;
     static constexpr int kLoads = kDepth<T, kStep> * kRowWords / kThreads, kBytes = kDepth<T, kStep> * kRowBytes;
     static_assert(kRowWords >= 16 && kLoads * kThreads == kDepth<T, kStep> * kRowWords, "rows that the turns fit into");
-    v4u word[kLoads];
-    Ragged<T> last = Ragged<T>(0, 0);
+    v4u word[kSets][kLoads];
+    Ragged<T, kAccess == TINY> last = Ragged<T, kAccess == TINY>(1, 0);
+    int rows[kSets];  // rows of k from the thread's first one on
 
-    // address(i, k): the row of k (of the thread's i-th word), from the tile's first element on; `most`: elements of it from there on, `before`: those before.
-    template <typename Row> __device__ void load(Row address, int k0, int k, int most, int before)
+    // address(i, k): the row of k (of the thread's i-th word); `length`: its elements, `before`: those before the tile's first.
+    template <typename Set, typename Row> __device__ void load(Set set, Row address, int k0, int k, int length, int before)
     {
         constexpr int n = Word<T>::n;
         static_assert(kThreads % kRowWords == 0, "the same word of all rows of a thread");
-        if constexpr (!kWords) last = Ragged<T>(most - (int)threadIdx.x % kRowWords * n, before + (int)threadIdx.x % kRowWords * n);
+        const int first = before + (int)threadIdx.x % kRowWords * n;
+        if constexpr (kAccess != WORDS) last = Ragged<T, kAccess == TINY>(length, first);
+        rows[set.value] = k - k0 - row_of_load(0);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int u = (int)threadIdx.x + i * kThreads, kk = k0 + u / kRowWords, first = u % kRowWords * n;
-            word[i] = v4u{0, 0, 0, 0};
-            if (kk < k && first < most) {
-                const T *from = address(i, kk) + first;
-                if constexpr (kWords) word[i] = *reinterpret_cast<const v4u *>(from);
-                else word[i] = last.load(from);
-            }
+            const int kk = k0 + row_of_load(i);
+            const T *from = address(i, kk < k ? kk : k - 1);
+            if constexpr (kAccess == WORDS) word[set.value][i] = *reinterpret_cast<const v4u *>(from + (first < length ? first : length - n));
+            else word[set.value][i] = last.load(from + first);
         }
     }
     // Asks for the rows of k0 ..; address(i, kk): the row of kk, which is k0 or more by i threads' words.  (Words behind
@@ -329,12 +341,13 @@ template <typename T, int kRows, int kStep, int kThreads, bool kWords> struct Ac
     // bytes (16-bit types: rows k .. k + 3 of two fours of eight) or 64 bytes (floats: rows 4 apart) of each.
     static __device__ int turn(int k) { return sizeof(T) == 2 ? ((k & 3) | (k >> 1 & 4)) << 1 : (k >> 2 & 3) << 2; }
     static __device__ int place(int k, int w) { return k * kRowBytes + ((w ^ turn(k)) << 4); }
-    __device__ void store(char *lds) const
+    template <typename Set> __device__ void store(Set set, char *lds) const
     {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int u = (int)threadIdx.x + i * kThreads;
-            *reinterpret_cast<v4u *>(lds + place(u / kRowWords, u % kRowWords)) = kWords ? word[i] : last.placed(word[i]);
+            const v4u w = kAccess == WORDS ? word[set.value][i] : last.placed(word[set.value][i]), zero = {0, 0, 0, 0};
+            *reinterpret_cast<v4u *>(lds + place(u / kRowWords, u % kRowWords)) = row_of_load(i) - row_of_load(0) < rows[set.value] ? w : zero;
         }
     }
     static __device__ int lane_base(int r0) { return r0 * (int)sizeof(T); }
@@ -372,28 +385,30 @@ template <typename F, int... i> __device__ inline void unrolled(F f, std::intege
 template <int n, typename F> __device__ inline void unrolled(F f) { unrolled(f, std::make_integer_sequence<int, n>()); }
 
 // One tile of kM x kN results; kWavesM x kWavesN wavefronts share it.
-template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, bool kWords> struct Tile {
+template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, Access kAccess> struct Tile {
     static constexpr int kThreads = kWavesM * kWavesN * NACHO_WAVE;
     static constexpr int kTileM = kM / kWavesM, kTileN = kN / kWavesN, kFragM = kTileM / 16, kFragN = kTileN / 16;
+    // steps of k that a thread has in registers on their way to LDS, where rows do not go there by themselves
+    static constexpr int kSets = kAccess == ANYWHERE && kM * kN <= 64 * 64 ? 2 : 1;
     static constexpr bool kAcrossQ = kForm == WEIGHTS, kAcrossP = kForm != FORWARD;
-    typedef std::conditional_t<kAcrossQ, AcrossK<T, kM, kStep, kThreads, kWords>, AlongK<T, kM, kStep, kThreads, kWords>> SideQ;
-    typedef std::conditional_t<kAcrossP, AcrossK<T, kN, kStep, kThreads, kWords>, AlongK<T, kN, kStep, kThreads, kWords>> SideP;
+    typedef std::conditional_t<kAcrossQ, AcrossK<T, kM, kStep, kThreads, kAccess, kSets>, AlongK<T, kM, kStep, kThreads, kAccess, kSets>> SideQ;
+    typedef std::conditional_t<kAcrossP, AcrossK<T, kN, kStep, kThreads, kAccess, kSets>, AlongK<T, kN, kStep, kThreads, kAccess, kSets>> SideP;
     static constexpr int kBytes = SideQ::kBytes + SideP::kBytes;
     // (The stages are arguments that do not overlap: so the compiler knows that reads of one do not wait for loads to the
     // other, also those reads that transpose.)
     static __device__ void compute(const ProductArgs &a, int tiles_m, int tiles_n, char *__restrict stage0, char *__restrict stage1);
 };
 
-template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, bool kWords>
+template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, Access kAccess>
 __global__ void __launch_bounds__(kWavesM * kWavesN * NACHO_WAVE) experts_kernel(ProductArgs a, int tiles_m, int tiles_n)
 {
-    typedef Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords> Work;
+    typedef Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess> Work;
     __shared__ __attribute__((aligned(16))) char stage0[Work::kBytes], stage1[Work::kBytes];
     Work::compute(a, tiles_m, tiles_n, stage0, stage1);
 }
 
-template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, bool kWords>
-__device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::compute(const ProductArgs &a, int tiles_m, int tiles_n,
+template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, int kStep, Access kAccess>
+__device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>::compute(const ProductArgs &a, int tiles_m, int tiles_n,
                                                                                         char *__restrict stage0, char *__restrict stage1)
 {
     auto stage = [&](auto i) -> char * {
@@ -425,7 +440,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
     if constexpr (!kAcrossP) side_p.start(p, a.ldp, [&](int r) { return n0 + r < a.n ? n0 + r : a.n - 1; });
     // Rows of x that the words of the next step of k come from: asked for a step ahead, or every step would wait for them
     // before it can ask for the words.
-    int slot[kForm == WEIGHTS ? SideP::kLoads : 1];
+    int slot[kForm == WEIGHTS ? SideP::kLoads : 1], found[kForm == WEIGHTS ? SideP::kLoads : 1];
     auto look_up = [&](int k0) {
         if constexpr (kForm == WEIGHTS) {
 #pragma unroll
@@ -433,21 +448,26 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
                 const int kk = k0 + SideP::row_of_load(l);
                 slot[l] = k_begin + (kk < k ? kk : k - 1);
             }
-            if (a.token) {
+            if constexpr (kAccess != WORDS) {
+                // (without a branch, see Ragged)
+                const int *list = a.token ? a.token : a.bounds;
+#pragma unroll
+                for (int l = 0; l < SideP::kLoads; ++l) found[l] = list[a.token ? slot[l] : 0];
+            } else if (a.token) {
 #pragma unroll
                 for (int l = 0; l < SideP::kLoads; ++l) slot[l] = a.token[slot[l]];
             }
         }
     };
-    auto load = [&](int k0) {
+    auto load = [&](auto set, int k0) {
         if constexpr (kAcrossQ)
-            side_q.load([&](int, int kk) { return q + (int64_t)(k_begin + kk) * a.ldq + m0; }, k0, k, a.m - m0, m0);
-        else side_q.load(k0, k);
-        if constexpr (kForm == ROWS) side_p.load([&](int, int kk) { return p + (int64_t)kk * a.ldp + n0; }, k0, k, a.n - n0, n0);
+            side_q.load(set, [&](int, int kk) { return q + (int64_t)(k_begin + kk) * a.ldq; }, k0, k, a.m, m0);
+        else side_q.load(set, k0, k);
+        if constexpr (kForm == ROWS) side_p.load(set, [&](int, int kk) { return p + (int64_t)kk * a.ldp; }, k0, k, a.n, n0);
         else if constexpr (kForm == WEIGHTS) {
-            side_p.load([&](int l, int) { return p + (int64_t)slot[l] * a.ldp + n0; }, k0, k, a.n - n0, n0);
+            side_p.load(set, [&](int l, int) { return p + (int64_t)(kAccess != WORDS && a.token ? found[l] : slot[l]) * a.ldp; }, k0, k, a.n, n0);
             look_up(k0 + kDepth<T, kStep> < k ? k0 + kDepth<T, kStep> : k0);
-        } else side_p.load(k0, k);
+        } else side_p.load(set, k0, k);
     };
     const int wave = (int)threadIdx.x / NACHO_WAVE, lane = lane_id();
     const int wm = wave / kWavesN * kTileM, wn = wave % kWavesN * kTileN;
@@ -498,7 +518,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
     constexpr int kDeep = kDepth<T, kStep>;
     int done = 0;
     if (k > 0) look_up(0);
-    if constexpr (kWords) {
+    if constexpr (kAccess == WORDS) {
         // Whole steps of k.  One is on its way to LDS while the one before it is multiplied; and while the matrix units
         // have one half of a wavefront's tile, the registers of the next half are read.
         const int steps = k / kDeep;
@@ -574,25 +594,43 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
         done = steps * kDeep;
         __syncthreads();
     }
-    if (done < k) {
-        load(done);
-        side_q.store(stage0);
-        side_p.store(stage0 + SideQ::kBytes);
-        __syncthreads();
-        char *here = stage0, *there = stage1;
-        for (; done < k; done += kDeep) {
-            const bool more = !kWords && done + kDeep < k;
-            if (more) load(done + kDeep);
-            if (busy) multiply_all(here);
-            if (more) {
-                side_q.store(there);
-                side_p.store(there + SideQ::kBytes);
-                __syncthreads();
-                char *const next = here;
-                here = there;
-                there = next;
-            }
+    auto store = [&](auto set, char *lds) {
+        side_q.store(set, lds);
+        side_p.store(set, lds + SideQ::kBytes);
+    };
+    if constexpr (kAccess == WORDS) {
+        // what is left of a step
+        if (done < k) {
+            load(zero, done);
+            store(zero, stage0);
+            __syncthreads();
+            // (a loop of one turn: with the product in line the tiles of 256 x 256 need two registers more than there are)
+            for (; done < k; done += kDeep)
+                if (busy) multiply_all(stage0);
         }
+    } else if (k > 0) {
+        // The next steps (two of them if there are registers) are on their way while one is multiplied.  (Behind the last step
+        // it is loaded again: a load that is not there on every path would have the compiler wait for all of them.)
+        const int steps = (k + kDeep - 1) / kDeep;
+        auto at = [&](int t) { return (t < steps ? t : steps - 1) * kDeep; };
+        load(zero, 0);
+        if constexpr (kSets == 2) load(one, at(1));
+        store(zero, stage0);
+        __syncthreads();
+        auto body = [&](int t, auto which) {
+            const std::integral_constant<int, (int)decltype(which)::value % kSets> set;
+            const std::integral_constant<int, 1 - (int)decltype(which)::value> other;
+            load(set, at(t + kSets));
+            if (busy) multiply_all(stage(which));
+            store(std::integral_constant<int, (int)decltype(other)::value % kSets>(), stage(other));
+            __syncthreads();
+        };
+        int t = 0;
+        for (; t + 2 <= steps; t += 2) {
+            body(t, zero);
+            body(t + 1, one);
+        }
+        if (t < steps) body(t, zero);
     }
     // A lane has four consecutive columns of result row lane % 16 of every 16 x 16.  A wavefront takes its tile through its
     // part of LDS, so that lanes that store side by side have neighbouring parts of a row, eight columns each.
@@ -620,7 +658,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
                 typename Word<T>::type w;
 #pragma unroll
                 for (int e = 0; e < kWord; ++e) w[e] = (T)v[h + e];
-                if constexpr (kWords) *reinterpret_cast<typename Word<T>::type *>(to + h) = w;
+                if constexpr (kAccess == WORDS) *reinterpret_cast<typename Word<T>::type *>(to + h) = w;
                 else __builtin_memcpy(to + h, &w, 16);
             } else {
 #pragma unroll
@@ -666,7 +704,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>::
 // grad_z = grad_y act'(pre), and the sums of its rows over tiles of kSlopeRows rows of an expert: a workgroup has a tile and
 // 16 words of 16 bytes of its columns, 16 threads along them and 16 along the rows.
 constexpr int kSlopeRows = 64;
-template <typename T, bool kWords>
+template <typename T, Access kAccess>
 __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, int tiles_n)
 {
     constexpr int n = Word<T>::n;
@@ -679,9 +717,9 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
     const T *gy = static_cast<const T *>(a.grad_y) + c, *pre = static_cast<const T *>(a.pre) + c;
     T *gz = static_cast<T *>(a.grad_z) + c;
     auto get = [&](const T *from) {
-        if constexpr (kWords) return width > 0 ? *reinterpret_cast<const v4u *>(from) : v4u{0, 0, 0, 0};
+        if constexpr (kAccess == WORDS) return width > 0 ? *reinterpret_cast<const v4u *>(from) : v4u{0, 0, 0, 0};
         else {
-            const Ragged<T> last(width, c);
+            const Ragged<T, kAccess == TINY> last(a.cols, c);
             return last.placed(last.load(from));
         }
     };
@@ -711,7 +749,7 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
         if (m < end && a.grad_z) {
             T *to = gz + (int64_t)m * a.ldgz;
             if (width >= n) {
-                if constexpr (kWords) *reinterpret_cast<word *>(to) = v;
+                if constexpr (kAccess == WORDS) *reinterpret_cast<word *>(to) = v;
                 else __builtin_memcpy(to, &v, 16);
             } else {
 #pragma unroll
@@ -775,7 +813,7 @@ bool in_words(std::initializer_list<std::pair<const void *, int64_t>> all, int e
     return bits % 16 == 0;
 }
 
-template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, bool kWords, int kStep = 128>
+template <typename T, Form kForm, int kM, int kN, int kWavesM, int kWavesN, Access kAccess, int kStep = 128>
 hipError_t run(const ProductArgs &a, hipStream_t s)
 {
     const int tiles_n = (a.n + kN - 1) / kN;
@@ -786,7 +824,7 @@ hipError_t run(const ProductArgs &a, hipStream_t s)
     // (a launch holds 2^32 threads along its first dimension)
     const int64_t tiles = tiles_m * tiles_n, row = tiles < (1 << 22) ? tiles : 1 << 22;
     if (tiles > 0x7fffffff - (1 << 22)) return hipErrorNotSupported;
-    experts_kernel<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kWords>
+    experts_kernel<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>
         <<<dim3((unsigned)row, (unsigned)((tiles + row - 1) / row)), kWavesM * kWavesN * NACHO_WAVE, 0, s>>>(a, (int)tiles_m, tiles_n);
     return hipGetLastError();
 }
@@ -800,30 +838,33 @@ constexpr int64_t kUnits = 256;        // compute units
 // units without one: 16 slots of 32 experts, 2048 x 4096, forward 26 (128 x 128: 37), rows 37 (47); 1200 of 24, 1024 x 4096, 36
 // (43), 41 (50).  Their steps are of 256 bytes: 8 tokens, 2 of 32 experts, 49 us a call, with 128 bytes 53.
 // Floats need four times as many matrix instructions for what is loaded: tiles of 64 x 64, which are as many again.  3000 slots
-// of 7 experts, 777 x 499, us: weights 73 (64 x 128: 95), forward 42 (32 x 128: 45), rows 44 (50).
-template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, bool words, hipStream_t s)
+// of 7 experts, 777 x 499, us: weights 73 (64 x 128: 95), forward 42 (32 x 128: 45), rows 44 (50); with two steps on their way
+// in registers 54, 43 and 42.
+template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, Access access, hipStream_t s)
 {
     const int64_t each = a.slots / a.experts, n128 = (a.n + 127) / 128;
+    const bool words = access == WORDS;
+    if (access == TINY) return run<T, kForm, kForm == WEIGHTS ? 128 : 32, 128, kForm == WEIGHTS ? 2 : 1, kForm == WEIGHTS ? 2 : 4, TINY>(a, s);
     if constexpr (kForm == WEIGHTS) {
         const int64_t tiles = (int64_t)a.experts * ((a.m + 255) / 256) * ((a.n + 255) / 256);
         if constexpr (sizeof(T) == 2) {
-            if (words && a.m >= 256 && a.n >= 256 && tiles >= kUnits) return run<T, kForm, 256, 256, 2, 4, true>(a, s);
+            if (words && a.m >= 256 && a.n >= 256 && tiles >= kUnits) return run<T, kForm, 256, 256, 2, 4, WORDS>(a, s);
         } else if (tiles < kUnits) {
-            return words ? run<T, kForm, 64, 64, 2, 2, true>(a, s) : run<T, kForm, 64, 64, 2, 2, false>(a, s);
+            return words ? run<T, kForm, 64, 64, 2, 2, WORDS>(a, s) : run<T, kForm, 64, 64, 2, 2, ANYWHERE>(a, s);
         }
-        return words ? run<T, kForm, 128, 128, 2, 2, true>(a, s) : run<T, kForm, 128, 128, 2, 2, false>(a, s);
+        return words ? run<T, kForm, 128, 128, 2, 2, WORDS>(a, s) : run<T, kForm, 128, 128, 2, 2, ANYWHERE>(a, s);
     } else {
         if constexpr (sizeof(T) == 2) {
             if (words && each >= 512 && a.n >= 256 && a.slots / 256 * ((a.n + 255) / 256) >= kUnits)
-                return run<T, kForm, 256, 256, 2, 4, true>(a, s);
+                return run<T, kForm, 256, 256, 2, 4, WORDS>(a, s);
         }
         const bool small = each <= 64 || a.slots / 128 * n128 < 2 * kUnits;
         if constexpr (sizeof(T) == 4) {
-            if (small && each > 64) return words ? run<T, kForm, 64, 64, 2, 2, true>(a, s) : run<T, kForm, 64, 64, 2, 2, false>(a, s);
+            if (small && each > 64) return words ? run<T, kForm, 64, 64, 2, 2, WORDS>(a, s) : run<T, kForm, 64, 64, 2, 2, ANYWHERE>(a, s);
         }
         if (small)
-            return words ? run<T, kForm, 32, 128, 1, 4, true, 256>(a, s) : run<T, kForm, 32, 128, 1, 4, false>(a, s);
-        return words ? run<T, kForm, 128, 128, 2, 2, true>(a, s) : run<T, kForm, 128, 128, 2, 2, false>(a, s);
+            return words ? run<T, kForm, 32, 128, 1, 4, WORDS, 256>(a, s) : run<T, kForm, 32, 128, 1, 4, ANYWHERE>(a, s);
+        return words ? run<T, kForm, 128, 128, 2, 2, WORDS>(a, s) : run<T, kForm, 128, 128, 2, 2, ANYWHERE>(a, s);
     }
 }
 
@@ -834,8 +875,11 @@ template <Form kForm> hipError_t launch(int dtype, const ProductArgs &a, hipStre
     const bool words = a.ldq < 0x7fffffff && a.ldp < 0x7fffffff &&
                        in_words({{a.q, a.ldq}, {a.p, a.ldp}, {a.p, a.p_stride}, {a.out, a.ldo}, {a.out, a.out_stride}, {a.pre, a.ldpre},
                                  {a.q, kForm == WEIGHTS ? 0 : a.k}, {a.q, kForm == WEIGHTS ? a.m : 0}, {a.q, a.n}}, elem);
+    // the shorter rows that are read
+    const int64_t along = kForm == WEIGHTS ? a.m : a.k, other = kForm == FORWARD ? a.k : a.n, least = along < other ? along : other;
+    const Access access = words ? WORDS : least * elem < 16 ? TINY : ANYWHERE;
     hipError_t rc = hipSuccess;
-    by_type(dtype, [&](auto zero) { rc = by_size<decltype(zero), kForm>(a, words, s); });
+    by_type(dtype, [&](auto zero) { rc = by_size<decltype(zero), kForm>(a, access, s); });
     return rc;
 }
 
@@ -864,8 +908,9 @@ hipError_t launch_experts_slope(int dtype, const SlopeArgs &a, hipStream_t s)
         }
         if (tiles > 0) {
             const dim3 grid((unsigned)row, (unsigned)((tiles + row - 1) / row));
-            if (words) experts_slope_kernel<T, true><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
-            else experts_slope_kernel<T, false><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
+            if (words) experts_slope_kernel<T, WORDS><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
+            else if (a.cols >= Word<T>::n) experts_slope_kernel<T, ANYWHERE><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
+            else experts_slope_kernel<T, TINY><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
             rc = hipGetLastError();
         }
         if (rc == hipSuccess && a.grad_bias) {

@@ -129,6 +129,18 @@ def test_layer_and_gradients(counts, tokens, inner, outer, dtype):
     check(problem(at, counts, tokens, inner, outer, dtype, at % 2 == 0), ACTS[at % 4], dtype)
 
 
+ODD = [([300, 0, 90], 200, 5, 7), ([40, 3], 30, 3, 300), ([70, 129], 90, 301, 6), ([700, 260, 1], 400, 131, 261),
+       ([2100, 1500, 0, 900], 1000, 67, 2051), ([33, 64, 65, 31, 32], 50, 129, 515)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("counts,tokens,inner,outer", ODD)
+def test_rows_that_no_word_fits(counts, tokens, inner, outer, dtype):
+    """Rows shorter than 16 bytes, and longer ones of odd lengths: one step of the sum, a few and many, ended early or not."""
+    at = ODD.index((counts, tokens, inner, outer))
+    check(problem(40 + at, counts, tokens, inner, outer, dtype, at % 2 == 0), ACTS[at % 4], dtype)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("pad", [0, 8, 5])
