@@ -3,8 +3,10 @@
 //
 // Bound by memory: every row of y is read (or written) once.  kLanes lanes have a token (8 to 64 of a wavefront where its
 // rows are short, else a workgroup), a lane words of 16 bytes; it keeps its columns of the token's row in registers while it
-// goes over the entries, four at a time.  Rows that start anywhere are read and written in words too (global memory takes any
-// alignment), their last elements one by one.  16384 x 4 x 4096 bf16: sums 167 us, gradients 227 us, 5.1 TB/s.
+// goes over the entries, four at a time: their slots first, then the rows, so that four rows are on their way at once.  Rows
+// that start anywhere are read and written in words too (global memory takes any alignment).  16384 x 4 x 4096 bf16: sums
+// 155 us, gradients 244, 5.1 TB/s (a row asked for before the next one's slot is known: 160 and 250); 16384 x 4 x 4095 168 and
+// 266 (with a branch around each load 184 and 291).
 #include "kernels.hpp"
 #include "model.hpp"
 
@@ -14,29 +16,46 @@ namespace {
 
 constexpr int kBatch = 4;              // entries whose rows are asked for together
 
-// A word of a row; `left` elements are there from its first one on.
-template <typename T, bool kAligned> __device__ inline void get(const T *at, int left, float (&v)[Word<T>::n])
+enum Access { WORDS, ANYWHERE, TINY };  // rows of words of 16 bytes; rows that start and end anywhere; such rows shorter than a word
+
+// A word of a row, `left` elements of which are there from its first one on.  The word that ends with the row is loaded where
+// fewer are there, and moved down when it is used: no branch lies around a load, as behind one that loads may be in, the next
+// wait is for all of them.  (Rows shorter than a word: elements one by one.)
+template <typename T, Access kAccess> __device__ inline typename Word<T>::type load(const T *at, int left)
 {
     constexpr int n = Word<T>::n;
     typename Word<T>::type w;
-    if (left >= n) {
-        if constexpr (kAligned) w = *reinterpret_cast<const typename Word<T>::type *>(at);
-        else __builtin_memcpy(&w, at, 16);
-    } else {
+    if constexpr (kAccess == WORDS) w = *reinterpret_cast<const typename Word<T>::type *>(at);
+    else if constexpr (kAccess == ANYWHERE) __builtin_memcpy(&w, at - (left < n ? n - left : 0), 16);
+    else {
 #pragma unroll
-        for (int e = 0; e < n; ++e) w[e] = e < left ? at[e] : (T)0.0f;
+        for (int e = 0; e < n; ++e) w[e] = at[e < left ? e : left - 1];
     }
-#pragma unroll
-    for (int e = 0; e < n; ++e) v[e] = wide((T)w[e]);
+    return w;
 }
-template <typename T, bool kAligned> __device__ inline void put(T *at, int left, const float (&v)[Word<T>::n])
+template <typename T, Access kAccess> __device__ inline void widen(typename Word<T>::type w, int left, float (&v)[Word<T>::n])
 {
     constexpr int n = Word<T>::n;
-    if (left >= n) {
+    if constexpr (kAccess == ANYWHERE) {
+        typedef unsigned int four __attribute__((ext_vector_type(4)));
+        four u = __builtin_bit_cast(four, w);
+        const int bytes = left < n ? (n - left) * (int)sizeof(T) : 0;
+        if (bytes & 8) u = four{u[2], u[3], 0, 0};
+        if (bytes & 4) u = four{u[1], u[2], u[3], 0};
+        if (bytes & 2) u = four{u[0] >> 16 | u[1] << 16, u[1] >> 16 | u[2] << 16, u[2] >> 16 | u[3] << 16, u[3] >> 16};
+        w = __builtin_bit_cast(typename Word<T>::type, u);
+    }
+#pragma unroll
+    for (int e = 0; e < n; ++e) v[e] = kAccess == TINY && e >= left ? 0.0f : wide((T)w[e]);
+}
+template <typename T, Access kAccess> __device__ inline void put(T *at, int left, const float (&v)[Word<T>::n])
+{
+    constexpr int n = Word<T>::n;
+    if (kAccess == WORDS || left >= n) {
         typename Word<T>::type w;
 #pragma unroll
         for (int e = 0; e < n; ++e) w[e] = (T)v[e];
-        if constexpr (kAligned) *reinterpret_cast<typename Word<T>::type *>(at) = w;
+        if constexpr (kAccess == WORDS) *reinterpret_cast<typename Word<T>::type *>(at) = w;
         else __builtin_memcpy(at, &w, 16);
     } else {
 #pragma unroll
@@ -45,9 +64,27 @@ template <typename T, bool kAligned> __device__ inline void put(T *at, int left,
     }
 }
 
+// The rows and factors of the entries from i on (behind the last: the last one again).
+struct Entries {
+    int64_t slot[kBatch];
+    float gate[kBatch];
+    __device__ Entries(const CombineArgs &a, int i, int end)
+    {
+        const float *gates = a.gate ? a.gate : reinterpret_cast<const float *>(a.slot);
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int at = i + b < end ? i + b : end - 1;
+            slot[b] = a.slot[at];
+            gate[b] = gates[at];
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) gate[b] = a.gate ? gate[b] : 1.0f;
+    }
+};
+
 template <int kLanes> constexpr int kThreads = kLanes <= 64 ? 64 : kLanes;
 
-template <typename T, bool kAligned, int kLanes>
+template <typename T, Access kAccess, int kLanes>
 __global__ void __launch_bounds__(kThreads<kLanes>) combine_kernel(CombineArgs a)
 {
     constexpr int n = Word<T>::n, kTokens = kThreads<kLanes> / kLanes;
@@ -61,33 +98,34 @@ __global__ void __launch_bounds__(kThreads<kLanes>) combine_kernel(CombineArgs a
             float sum[n];
 #pragma unroll
             for (int e = 0; e < n; ++e) sum[e] = 0.0f;
+            typename Word<T>::type last = {};
+            if (residual) last = load<T, kAccess>(residual + t * a.ldr + c, left);
             for (int i = begin; i < end; i += kBatch) {
-                float v[kBatch][n], g[kBatch];
+                const Entries of(a, i, end);
+                typename Word<T>::type w[kBatch];
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) w[b] = load<T, kAccess>(y + of.slot[b] * a.ldy + c, left);
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b)
                     if (i + b < end) {
-                        get<T, kAligned>(y + (int64_t)a.slot[i + b] * a.ldy + c, left, v[b]);
-                        g[b] = a.gate ? a.gate[i + b] : 1.0f;
-                    }
+                        float v[n];
+                        widen<T, kAccess>(w[b], left, v);
 #pragma unroll
-                for (int b = 0; b < kBatch; ++b)
-                    if (i + b < end) {
-#pragma unroll
-                        for (int e = 0; e < n; ++e) sum[e] += g[b] * v[b][e];
+                        for (int e = 0; e < n; ++e) sum[e] += of.gate[b] * v[e];
                     }
             }
             if (residual) {
                 float r[n];
-                get<T, kAligned>(residual + t * a.ldr + c, left, r);
+                widen<T, kAccess>(last, left, r);
 #pragma unroll
                 for (int e = 0; e < n; ++e) sum[e] += r[e];
             }
-            put<T, kAligned>(out + t * a.ldo + c, left, sum);
+            put<T, kAccess>(out + t * a.ldo + c, left, sum);
         }
     }
 }
 
-template <typename T, bool kAligned, int kLanes>
+template <typename T, Access kAccess, int kLanes>
 __global__ void __launch_bounds__(kThreads<kLanes>) combine_grad_kernel(CombineArgs a)
 {
     constexpr int n = Word<T>::n, kTokens = kThreads<kLanes> / kLanes;
@@ -101,30 +139,37 @@ __global__ void __launch_bounds__(kThreads<kLanes>) combine_grad_kernel(CombineA
         // (the tokens of one wavefront go on together, as long as the longest has entries)
         for (int i = begin; kTokens == 1 ? i < end : __any(i < end); i += kBatch) {
             float dot[kBatch] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (i < end)
+            if (i < end) {
+                const Entries of(a, i, end);
                 for (int64_t c = lane * n; c < a.cols; c += kLanes * n) {
                     const int left = a.cols - (int)c;
+                    const typename Word<T>::type w = load<T, kAccess>(grad_out + t * a.ldg + c, left);
                     float go[n];
-                    get<T, kAligned>(grad_out + t * a.ldg + c, left, go);
+                    if (a.grad_gate) {
+                        typename Word<T>::type row[kBatch];
 #pragma unroll
-                    for (int b = 0; b < kBatch; ++b)
-                        if (i + b < end) {
-                            const int64_t slot = a.slot[i + b];
-                            if (a.grad_gate) {
-                                float v[n];
-                                get<T, kAligned>(y + slot * a.ldy + c, left, v);
+                        for (int b = 0; b < kBatch; ++b) row[b] = load<T, kAccess>(y + of.slot[b] * a.ldy + c, left);
+                        widen<T, kAccess>(w, left, go);
 #pragma unroll
-                                for (int e = 0; e < n; ++e) dot[b] += go[e] * v[e];
-                            }
-                            if (grad_y) {
-                                const float g = a.gate ? a.gate[i + b] : 1.0f;
-                                float v[n];
+                        for (int b = 0; b < kBatch; ++b) {
+                            float v[n];
+                            widen<T, kAccess>(row[b], left, v);
 #pragma unroll
-                                for (int e = 0; e < n; ++e) v[e] = g * go[e];
-                                put<T, kAligned>(grad_y + slot * a.ldgy + c, left, v);
-                            }
+                            for (int e = 0; e < n; ++e) dot[b] += go[e] * v[e];
                         }
+                    } else widen<T, kAccess>(w, left, go);
+                    if (grad_y) {
+#pragma unroll
+                        for (int b = 0; b < kBatch; ++b)
+                            if (i + b < end) {
+                                float v[n];
+#pragma unroll
+                                for (int e = 0; e < n; ++e) v[e] = of.gate[b] * go[e];
+                                put<T, kAccess>(grad_y + of.slot[b] * a.ldgy + c, left, v);
+                            }
+                    }
                 }
+            }
             if (a.grad_gate) {
                 if constexpr (kLanes <= NACHO_WAVE) {
 #pragma unroll
@@ -158,13 +203,15 @@ template <typename F> void by_shape(int dtype, int64_t cols, bool aligned, F f)
         const int64_t words = (cols + Word<decltype(zero)>::n - 1) / Word<decltype(zero)>::n;
         auto by_lanes = [&](auto whole) {
             if (words <= 8) f(zero, whole, integral_constant<int, 8>());
+            else if constexpr (whole.value == TINY) return;          // (a word)
             else if (words <= 16) f(zero, whole, integral_constant<int, 16>());
             else if (words <= 32) f(zero, whole, integral_constant<int, 32>());
             else if (words <= 128) f(zero, whole, integral_constant<int, 64>());
             else f(zero, whole, integral_constant<int, 256>());
         };
-        if (aligned) by_lanes(integral_constant<bool, true>());
-        else by_lanes(integral_constant<bool, false>());
+        if (aligned) by_lanes(integral_constant<Access, WORDS>());
+        else if (cols >= Word<decltype(zero)>::n) by_lanes(integral_constant<Access, ANYWHERE>());
+        else by_lanes(integral_constant<Access, TINY>());
     };
     if (dtype == NACHO_F32) by_type((float)0);
     else if (dtype == NACHO_BF16) by_type((bf16_t)0.0f);
