@@ -12,7 +12,7 @@
 // Which expert a tile belongs to is found by its workgroup from expert_pos alone (a prefix sum of the experts' tiles
 // over the lanes), so nothing about the routing is read on the host.
 //
-// Bound by the matrix units for many slots an expert (16384 bf16 slots of 16 experts, 2048 x 8192: 628 us a call, 875 TFLOP/s
+// Bound by the matrix units for many slots an expert (16384 bf16 slots of 16 experts, 2048 x 8192: 622 us a call, 885 TFLOP/s
 // of the 1211 of a library's product of 8192^3), by the weights for few (16 of 32 experts, 2048 x 4096: 47 to 58 us a call for
 // 213 MB; 31 us a kernel where the last cache still has most of them).
 #include "kernels.hpp"
