@@ -500,8 +500,9 @@ int32_t nacho_route_grad(const void *logits, int64_t ldl, int64_t n_tokens, int6
  * All of one type; products are summed in 32 bits and rounded once.
  *
  * nacho_experts_grad: from grad_y [n_slots x outer], with z the rows before the
- * activation and g_s = grad_y[s] act'(z_s) (rounded to the type, which the products
- * below take),
+ * activation (taken from pre, so rounded to the type) and g_s = grad_y[s] act'(z_s),
+ * rounded to the type for the products, which the matrix units take it in, and not
+ * for the sums of grad_bias,
  *   grad_x[s]    = g_s w[e]             [n_slots x inner], by slots: nacho_combine
  *                                       without gates sums them by tokens
  *   grad_w[e]    = sum_s g_s^T x[token[s]]

@@ -741,10 +741,18 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
     for (int i = 0; i < kRows; ++i) {
         const int m = row + ty + i * 16;
         word v = __builtin_bit_cast(word, g[i]);
+        // (what the sums take is not rounded to the type yet; behind the last row it is zero)
         if (a.act != NACHO_ACT_NONE) {
             const word at = __builtin_bit_cast(word, z[i]);
 #pragma unroll
-            for (int e = 0; e < n; ++e) v[e] = (T)(wide((T)v[e]) * slope_at<T>(wide((T)at[e]), a.act));
+            for (int e = 0; e < n; ++e) {
+                const float x = wide((T)v[e]) * slope_at<T>(wide((T)at[e]), a.act);
+                v[e] = (T)x;
+                sum[e] += x;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < n; ++e) sum[e] += wide((T)v[e]);
         }
         if (m < end && a.grad_z) {
             T *to = gz + (int64_t)m * a.ldgz;
@@ -756,10 +764,6 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
                 for (int e = 0; e < n; ++e)
                     if (e < width) to[e] = v[e];
             }
-        }
-        if (m < end) {
-#pragma unroll
-            for (int e = 0; e < n; ++e) sum[e] += wide((T)v[e]);
         }
     }
     if (!a.sums) return;

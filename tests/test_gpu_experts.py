@@ -271,3 +271,24 @@ def test_the_largest_tiles(counts, inner, outer, dtype):
 def test_steps_of_the_sum(inner, dtype):
     """Even and odd numbers of whole steps of k, and parts of one behind them, in all three products."""
     check(problem(21, [64 + inner, 130, inner // 2, 1], 90, inner, 384 - inner // 2, dtype, False), "none", dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+@pytest.mark.parametrize("outer", [96, 101, 3])
+def test_bias_gradients_are_rounded_once(outer, act, dtype):
+    """Sums of what the rows' gradients are before they are rounded to the type: a rounding of the sum, n 2^-24 of the terms for a
+    sum in 32 bits, and 2^-20 of a term's factor for slopes of 16-bit rows."""
+    g = torch.Generator().manual_seed(outer)
+    counts, inner = [900, 0, 70], 8
+    bounds = torch.tensor([0, 900, 900, 970], dtype=torch.int32)
+    pre, gy = ((torch.randn((970, outer), generator=g) * 1.5).to(dtype) for _ in range(2))
+    x, w = torch.zeros((970, inner), dtype=dtype, device="cuda"), torch.zeros((3, outer, inner), dtype=dtype, device="cuda")
+    gb = torch.full((3, outer), 7.0, dtype=dtype, device="cuda")
+    nb.nacho_experts_grad(gy.cuda(), x, w, bounds.cuda(), act=act, pre=pre.cuda(), grad_bias=gb)
+    for e in range(3):
+        a, b = bounds[e], bounds[e + 1]
+        term = gy[a:b].double() * slope64(pre[a:b].double(), act)
+        size = (gy[a:b].double().abs() * (slope64(pre[a:b].double(), act).abs() * (counts[e] + 8) * 2.0 ** -24 + 2.0 ** -20)).sum(0)
+        room = STEP[dtype] * term.sum(0).abs() + size + 2.0 ** -25 * (dtype is torch.float16)
+        assert bool(((gb[e].cpu().double() - term.sum(0)).abs() <= room).all()), e
