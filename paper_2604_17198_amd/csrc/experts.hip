@@ -81,25 +81,29 @@ template <typename T> __device__ inline float activated(float z, int act)
     }
     return z;
 }
+// (A row past its type's range is kept as an infinity: its slope is that of any number so far out, 0 or 1, where the formulas'
+// products of zero and infinity would make a NaN.)
 template <typename T> __device__ inline float slope_at(float z, int act)
 {
     if (act == NACHO_ACT_RELU) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
     if constexpr (sizeof(T) == 4) {
         const double v = z;
-        if (act == NACHO_ACT_GELU)
-            return (float)(0.5 * erfc(-0.70710678118654752440 * v) + v * 0.39894228040143267794 * exp(-0.5 * v * v));
+        if (act == NACHO_ACT_GELU) {
+            const double density = 0.39894228040143267794 * exp(-0.5 * v * v);
+            return (float)(0.5 * erfc(-0.70710678118654752440 * v) + (density == 0.0 ? 0.0 : v * density));
+        }
         if (act == NACHO_ACT_SILU) {
-            const double q = 1.0 / (1.0 + exp(-v));
-            return (float)(q * (1.0 + v * (1.0 - q)));
+            const double q = 1.0 / (1.0 + exp(-v)), both = q * (1.0 - q);
+            return (float)(both == 0.0 ? q : q + v * both);
         }
     } else {
         if (act == NACHO_ACT_GELU) {
             const Normal at(z);
-            return at.below + z * at.density;
+            return at.below + (at.density == 0.0f ? 0.0f : z * at.density);
         }
         if (act == NACHO_ACT_SILU) {
-            const float q = __builtin_amdgcn_rcpf(1.0f + exp2_of(-kLog2e * z));
-            return q * (1.0f + z * (1.0f - q));
+            const float q = __builtin_amdgcn_rcpf(1.0f + exp2_of(-kLog2e * z)), both = q * (1.0f - q);
+            return both == 0.0f ? q : q + z * both;
         }
     }
     return 1.0f;

@@ -292,3 +292,20 @@ def test_bias_gradients_are_rounded_once(outer, act, dtype):
         size = (gy[a:b].double().abs() * (slope64(pre[a:b].double(), act).abs() * (counts[e] + 8) * 2.0 ** -24 + 2.0 ** -20)).sum(0)
         room = STEP[dtype] * term.sum(0).abs() + size + 2.0 ** -25 * (dtype is torch.float16)
         assert bool(((gb[e].cpu().double() - term.sum(0)).abs() <= room).all()), e
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("act,outer", [("relu", 24), ("gelu", 24), ("silu", 24), ("gelu", 13), ("silu", 13)])
+def test_slopes_of_rows_past_the_types_range(act, outer, dtype):
+    """A row before the activation that left its type's range is kept as an infinity: slope 0 below and 1 above, as of any
+    number as far out; a NaN stays one."""
+    far = torch.tensor([float("-inf"), float("inf"), torch.finfo(dtype).min, torch.finfo(dtype).max], dtype=dtype)
+    pre = far[:, None].expand(4, outer).contiguous()
+    bounds = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    x, w = torch.ones((4, 8), dtype=dtype, device="cuda"), torch.ones((1, outer, 8), dtype=dtype, device="cuda")
+    gb = torch.empty((1, outer), dtype=dtype, device="cuda")
+    gx, gw = nb.nacho_experts_grad(torch.ones((4, outer), dtype=dtype, device="cuda"), x, w, bounds, act=act, pre=pre.cuda(), grad_bias=gb)
+    assert gx[:, 0].tolist() == [0, outer, 0, outer] and bool((gb == 2).all()) and bool((gw == 2).all())
+    pre[2, 1] = float("nan")
+    gx, gw = nb.nacho_experts_grad(torch.ones((4, outer), dtype=dtype, device="cuda"), x, w, bounds, act=act, pre=pre.cuda(), grad_bias=gb)
+    assert torch.isnan(gx[:, 0]).tolist() == [False, False, True, False] and bool(torch.isnan(gb[0, 1])) and bool((gb[0, 2:] == 2).all())
