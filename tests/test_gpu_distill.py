@@ -263,3 +263,20 @@ def test_refusals():
         nb.nacho_distill(T, z, grad=z)
     with pytest.raises(nb.NachoError):
         nb.nacho_distill(nb.vector(T.keep[1], 64, T.val), z)
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 500), (130, 70_001), (3, 70_001), (520, 70_001), (3, 140_001)])
+def test_rows_of_masked_logits_alone_have_no_lse(rows, cols):
+    """Rows with nothing but -inf, held by a workgroup and in parts, with a gradient and without: NaN throughout."""
+    rng = np.random.default_rng(rows)
+    pos, crd, val, z, weight = case(rng, rows, cols, 2, 6, torch.bfloat16)
+    z[1] = float("-inf")
+    T, w = operand(pos, crd, val, rows, cols), torch.from_numpy(weight).cuda()
+    grad = torch.empty_like(z)
+    for more in (dict(grad=grad), {}):
+        loss, lse = nb.nacho_distill(T, z, weight=w, **more)
+        for t in (loss, lse):
+            assert torch.isnan(t).tolist() == [i == 1 for i in range(rows)]
+    assert bool(torch.isnan(grad[1]).all()) and not bool(torch.isnan(grad[0]).any())
+    grad = nb.nacho_distill_grad(T, z, lse, weight=w)
+    assert bool(torch.isnan(grad[1]).all()) and not bool(torch.isnan(grad[0]).any())
