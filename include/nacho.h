@@ -414,7 +414,7 @@ int32_t nacho_spmul_k(const nacho_tensor *ops, int32_t k, int32_t dtype, int64_t
  *               columns as in every CSR operand; a row may store none
  *   logits      the student's, [n_rows x vocabulary], leading dimension ldl
  *   weight      device float[n_rows], a factor of every row, or NULL for ones
- *   temperature tau, 1e-30 .. 1e30
+ *   temperature tau, 1e-30 .. 1e18 (of higher ones the square is no 32-bit number)
  * With p the softmax of a row's stored teacher logits / tau (the others have no
  * share) and q the softmax of all its student logits / tau,
  *   loss[i] = weight[i] tau^2 sum_j p_j (log p_j - log q_j)
@@ -425,12 +425,18 @@ int32_t nacho_spmul_k(const nacho_tensor *ops, int32_t k, int32_t dtype, int64_t
  * gradient 0, whatever their logits hold.  Student logits of -inf have q = 0
  * (a loss of +inf where the teacher gives them a share).  A row with nothing but
  * -inf, or with a NaN, has no distribution: NaN.
+ * The loss is a difference of sums held in 32 bits, right to about 2^-20 of their
+ * size, weight[i] tau^2 (1 + log n_cols + the logits' spread / tau): its last digits
+ * where a teacher stores a small part of the vocabulary.  Of one that stores nearly
+ * all of it, p and q are nearly alike at a high temperature and little of the loss is
+ * left (32000 columns, all stored: off by 1e-4 of it at tau = 20, 3e-3 at 100, a third
+ * at 1000).  grad has no difference but q - p itself.
  * Workspace: nacho_distill_workspace_bytes (may be 0: then ws may be NULL).
  *
  * nacho_distill_grad: grad alone, from the logits and the lse of an earlier
  * nacho_distill on the same operands and temperature; weight then is the factor of
  * the loss times the gradient that arrives at it.  lse has 32 bits: q is off by a
- * factor of |lse| 2^-23, no matter for logits up to thousands.
+ * factor of exp(|lse| 2^-23), no matter for logits / tau up to thousands.
  */
 int32_t nacho_distill_workspace_bytes(int64_t n_rows, int64_t n_cols, int32_t dtype, size_t *bytes);
 int32_t nacho_distill(const nacho_tensor *teacher, const void *logits, int64_t ldl, int32_t dtype,

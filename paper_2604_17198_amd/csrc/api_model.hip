@@ -88,7 +88,7 @@ int32_t check_distill(const nacho_tensor *teacher, const void *logits, int64_t l
     if (!teacher->lvl[1].pos || (stored > 0 && (!teacher->lvl[1].crd || !teacher->val))) return NACHO_ERR_INVALID_ARG;
     if (!aligned(teacher->lvl[1].crd, 16) || !aligned(teacher->val, 16)) return NACHO_ERR_INVALID_ARG;
     const int64_t elem = value_bytes(dtype);
-    if (!matrix(logits, rows, cols, ldl, elem) || !(temperature >= 1e-30f && temperature <= 1e30f)) return NACHO_ERR_INVALID_ARG;
+    if (!matrix(logits, rows, cols, ldl, elem) || !(temperature >= 1e-30f && temperature <= 1e18f)) return NACHO_ERR_INVALID_ARG;
     if (grad && (!matrix(grad, rows, cols, ldg, elem) ||
                  overlap(logits, span(rows, cols, ldl, elem), grad, span(rows, cols, ldg, elem))))
         return NACHO_ERR_INVALID_ARG;

@@ -168,7 +168,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 && kMore < 16 ? 4 : 
             }
             if (kStage != GIVEN && tid == 0 && number == 0) {
                 const float log_z = logf(s[0]);
-                a.loss[row] = w * tau * tau * (s[2] / (s[1] * tau) - logf(s[1]) + log_z);
+                // (one tau inside the sum: the square of a small one is zero)
+                a.loss[row] = w * tau * (s[2] / s[1] + tau * (log_z - logf(s[1])));
                 // (a row of masked logits alone has no distribution; joined parts have summed it to zero)
                 a.lse[row] = top[0] == -kInfinity ? __builtin_nanf("") : top[0] / tau + log_z;
             }

@@ -280,3 +280,32 @@ def test_rows_of_masked_logits_alone_have_no_lse(rows, cols):
     assert bool(torch.isnan(grad[1]).all()) and not bool(torch.isnan(grad[0]).any())
     grad = nb.nacho_distill_grad(T, z, lse, weight=w)
     assert bool(torch.isnan(grad[1]).all()) and not bool(torch.isnan(grad[0]).any())
+
+
+@pytest.mark.parametrize("cols", [700, 140_001])
+@pytest.mark.parametrize("tau", [1e-30, 1e-22, 1e18])
+def test_temperatures_at_the_ends_of_their_range(tau, cols):
+    """Where the square of a temperature is no 32-bit number, and next to the highest.  Terms and their sizes are those of the
+    definition, so the tolerance is that of all other tests."""
+    rng = np.random.default_rng(17)
+    pos, crd, val, z, weight = case(rng, 3, cols, 3, 20, torch.float32)
+    tau = float(np.float32(tau))
+    want = definition(pos, crd, val, z.cpu().numpy(), weight.astype(np.float64), tau)
+    T, w = operand(pos, crd, val, 3, cols), torch.from_numpy(weight).cuda()
+    grad = torch.empty_like(z)
+    loss, lse = nb.nacho_distill(T, z, temperature=tau, weight=w, grad=grad)
+    check(loss, lse, grad, want, weight, tau, torch.float32)
+    # (that tolerance is an absolute one next to a loss that is small: these are not, and are right to the fourth digit)
+    assert np.all(np.abs(loss.cpu().numpy() - want[0]) <= 1e-4 * want[0])
+
+
+def test_temperatures_whose_square_is_no_number_are_refused():
+    rng = np.random.default_rng(18)
+    pos, crd, val, z, _ = case(rng, 2, 64, 2, 5, torch.float32)
+    T = operand(pos, crd, val, 2, 64)
+    lse = torch.zeros(2, device="cuda")
+    for tau in (1.01e18, 1e19, 1e30):
+        with pytest.raises(nb.NachoError):
+            nb.nacho_distill(T, z, temperature=tau)
+        with pytest.raises(nb.NachoError):
+            nb.nacho_distill_grad(T, z, lse, temperature=tau)
