@@ -536,6 +536,11 @@ def _vector_of(t, what, n, dtype, device):
     return t
 
 
+def _floats(n, device):
+    """A new array of n results (whatever the program's default type is)."""
+    return torch.empty(n, dtype=torch.float32, device=device)
+
+
 def _check_teacher(teacher, logits, weight):
     if teacher.nlevels != 2 or teacher.c.lvl[0].kind != DENSE or teacher.c.lvl[1].kind != COMPRESSED:
         raise NachoError(-2, "teacher: a CSR operand is needed")
@@ -555,8 +560,8 @@ def nacho_distill(teacher: Operand, logits, temperature=1.0, weight=None, grad=N
     rows, cols, ld = _check_teacher(teacher, logits, weight)
     dev = logits.device
     ldg = _matrix(grad, "grad", rows, cols, logits.dtype, dev) if grad is not None else 0
-    loss = _vector_of(loss, "loss", rows, torch.float32, dev) if loss is not None else torch.empty(rows, device=dev)
-    lse = _vector_of(lse, "lse", rows, torch.float32, dev) if lse is not None else torch.empty(rows, device=dev)
+    loss = _vector_of(loss, "loss", rows, torch.float32, dev) if loss is not None else _floats(rows, dev)
+    lse = _vector_of(lse, "lse", rows, torch.float32, dev) if lse is not None else _floats(rows, dev)
     if ws is None:
         n = C.c_size_t(0)
         _check(lib().nacho_distill_workspace_bytes(rows, cols, dt, C.byref(n)), "nacho_distill_workspace_bytes")
@@ -769,7 +774,7 @@ def nacho_combine_grad(pos, slot, y, grad_out, gate=None, grad_y=None, grad_gate
         grad_y = torch.empty((y.shape[0], n), dtype=y.dtype, device=dev)
     ldgy = _matrix(grad_y, "grad_y", y.shape[0], n, y.dtype, dev)
     if grad_gate is None:
-        grad_gate = torch.empty(slot.numel(), device=dev)
+        grad_gate = _floats(slot.numel(), dev)
     _vector_of(grad_gate, "grad_gate", slot.numel(), torch.float32, dev)
     c = _slots_of(pos, slot, gate, y.shape[0], dev)
     _check(lib().nacho_combine_grad(C.byref(c), _ptr(y), ldy, n, dt, _ptr(grad_out), ldg, _ptr(grad_y), ldgy,

@@ -108,3 +108,30 @@ def test_under_a_captured_graph():
         torch.cuda.synchronize()
         for a, b in zip(captured, work()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float64])
+def test_whatever_the_default_type_is(default):
+    """The operators' results under another default type of torch, bit for bit."""
+    new = lambda *shape: torch.randn(shape, device="cuda", dtype=torch.float32)
+    z, x, w, logits = new(40, 6), new(40, 32), new(6, 24, 32), new(40, 300)
+    pos = torch.arange(41, dtype=torch.int32, device="cuda") * 5
+    crd = (torch.arange(200, device="cuda") % 5 * 50).to(torch.int32)
+    teacher = nb.csr(pos, crd, 40, 300, new(200))
+
+    def work():
+        r = nb.nacho_route(z, 2)
+        y = nb.nacho_experts(x, w, r.expert_pos, token=r.token)
+        loss, lse = nb.nacho_distill(teacher, logits)
+        return [r.gate, r.lse, r.balance, y, nb.nacho_combine(r.pos, r.slot, y, gate=r.gate), *nb.nacho_combine_grad(r.pos, r.slot, y, x[:, :24], gate=r.gate),
+                nb.nacho_route_grad(z, r, r.gate, balance=0.5), *nb.nacho_experts_grad(y, x, w, r.expert_pos, token=r.token), loss, lse,
+                nb.nacho_distill_grad(teacher, logits, lse)]
+
+    first, before = work(), torch.get_default_dtype()
+    try:
+        torch.set_default_dtype(default)
+        second = work()
+    finally:
+        torch.set_default_dtype(before)
+    for a, b in zip(first, second):
+        assert a.dtype is torch.float32 and torch.equal(a, b)

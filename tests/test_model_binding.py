@@ -1,0 +1,55 @@
+"""What the Python side of the training operators makes and refuses before the library is called (the library's calls are
+replaced, nothing is launched, no GPU)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2604_17198_amd import binding as nb
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Names of the library's calls, none of which is made; host tensors stand for those of a GPU."""
+    made = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                made.append(name)
+                if name.endswith("_workspace_bytes"):
+                    C.cast(args[-1], C.POINTER(C.c_size_t))[0] = 256
+                return 0
+            return call
+
+    monkeypatch.setattr(nb, "lib", lambda: Library())
+    monkeypatch.setattr(nb, "_stream", lambda: 0)
+    monkeypatch.setattr(nb, "_GPU", "cpu", raising=False)
+    return made
+
+
+def ints(*values):
+    return torch.tensor(values, dtype=torch.int32)
+
+
+def teacher(rows=3, cols=20):
+    return nb.csr(torch.arange(rows + 1, dtype=torch.int32) * 2, ints(*[1, 5] * rows), rows, cols, torch.zeros(2 * rows, dtype=torch.float32))
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float16, torch.float64])
+def test_results_do_not_take_the_default_type(calls, default):
+    """A program that sets torch's default type gets results of the types that the library writes."""
+    before = torch.get_default_dtype()
+    try:
+        torch.set_default_dtype(default)
+        z = torch.zeros((3, 20), dtype=torch.bfloat16)
+        loss, lse = nb.nacho_distill(teacher(), z)
+        r = nb.nacho_route(z, 2)
+        y = torch.zeros((6, 20), dtype=torch.float16)
+        _, grad_gate = nb.nacho_combine_grad(ints(0, 2, 4, 6), ints(0, 1, 2, 3, 4, 5), y, y[:3])
+        for t in (loss, lse, r.gate, r.lse, r.balance, grad_gate):
+            assert t.dtype is torch.float32
+        for t in (nb.nacho_distill_grad(teacher(), z, lse), nb.nacho_route_grad(z, r)):
+            assert t.dtype is z.dtype
+    finally:
+        torch.set_default_dtype(before)
