@@ -662,7 +662,9 @@ def _stack(t, what, shape, dtype, device):
         raise ValueError(f"{what}: contiguous rows are needed")
     if len(shape) == 2:
         return cols, stride[0] if shape[0] > 1 else max(cols, stride[0])
-    ld = max(stride[1], cols) if shape[1] > 1 else cols
+    ld = stride[1] if shape[1] > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{what}: rows that do not overlap are needed")
     return ld, stride[0] if shape[0] > 1 else max(shape[1] * ld, stride[0])
 
 

@@ -53,3 +53,22 @@ def test_results_do_not_take_the_default_type(calls, default):
             assert t.dtype is z.dtype
     finally:
         torch.set_default_dtype(before)
+
+
+def test_weights_whose_rows_lie_on_each_other_are_refused(calls):
+    """Expanded weights (distance 0 between rows) are not what a leading dimension of their length reads, past their end."""
+    x, bounds, token = torch.zeros((5, 16)), ints(0, 3, 7), ints(0, 1, 2, 3, 4, 0, 1)
+    row, flat, y = torch.zeros((2, 1, 16)), torch.zeros((1, 24, 16)), torch.zeros((7, 24))
+    whole = torch.zeros((2, 24, 16))
+    for weight in (row.expand(2, 24, 16), row[:1].expand(2, 24, 16), torch.zeros(16).expand(2, 24, 16)):
+        with pytest.raises(ValueError):
+            nb.nacho_experts(x, weight, bounds, token=token)
+        with pytest.raises(ValueError):
+            nb.nacho_experts_grad(y, x, weight, bounds, token=token)
+        with pytest.raises(ValueError):
+            nb.nacho_experts_grad(y, x, whole, bounds, token=token, grad_weight=weight)
+    assert "nacho_experts" not in calls and "nacho_experts_grad" not in calls
+    # (one row or one expert may have any distance; padded rows and experts have their own)
+    assert nb._stack(row.expand(2, 1, 16), "w", (2, 1, 16), torch.float32, row.device) == (16, 16)
+    assert nb._stack(flat, "w", (1, 24, 16), torch.float32, flat.device) == (16, 24 * 16)
+    assert nb._stack(torch.zeros((2, 30, 20))[:, :24, :16], "w", (2, 24, 16), torch.float32, flat.device) == (20, 600)
