@@ -179,8 +179,9 @@ def _raw_stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
-# (torch's raw getters are private names: without them the public call)
+# (torch's raw getters are private names: without them the public calls)
 _stream = _raw_stream if all(hasattr(torch._C, n) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice")) else _public_stream
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
 def dtype_code(dt) -> int:
@@ -514,8 +515,15 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _on_gpu(t, what):
+    """The call's first array: on the GPU whose stream the kernels go to (all others have to be where it is)."""
+    if not t.is_cuda or t.get_device() != _current_device():
+        raise ValueError(f"{what}: on {t.device}, and not on the current GPU")
+
+
 def _matrix(t, what, rows=None, cols=None, dtype=None, device=None):
-    """A matrix whose rows are contiguous, of the given sizes where they are given; returns its leading dimension."""
+    """A matrix whose rows are contiguous, of the given sizes where they are given; returns its leading dimension.  Without a
+    device to be on it has to be on the current GPU."""
     if t.dim() != 2:
         raise ValueError(f"{what}: a matrix is needed, got {t.dim()} dimensions")
     r, c = t.shape
@@ -524,7 +532,9 @@ def _matrix(t, what, rows=None, cols=None, dtype=None, device=None):
         raise ValueError(f"{what}: contiguous rows are needed")
     if (rows is not None and r != rows) or (cols is not None and c != cols):
         raise ValueError(f"{what}: {r} x {c}, expected {rows} x {cols}")
-    if (dtype is not None and t.dtype is not dtype) or (device is not None and t.device != device):
+    if device is None:
+        _on_gpu(t, what)
+    elif t.dtype is not dtype or t.device != device:
         raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype} on {device}")
     return ld if r > 1 else (ld if ld > c else c)
 
@@ -534,6 +544,15 @@ def _vector_of(t, what, n, dtype, device):
     if t is not None and (t.numel() != n or t.dtype is not dtype or not t.is_contiguous() or t.device != device):
         raise ValueError(f"{what}: {n} contiguous elements of {dtype} on {device} are needed")
     return t
+
+
+def _room(ws, device):
+    """The bytes of a workspace."""
+    if ws is None:
+        return 0
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"ws: contiguous memory on {device} is needed")
+    return ws.numel()
 
 
 def _floats(n, device):
@@ -567,7 +586,7 @@ def nacho_distill(teacher: Operand, logits, temperature=1.0, weight=None, grad=N
         _check(lib().nacho_distill_workspace_bytes(rows, cols, dt, C.byref(n)), "nacho_distill_workspace_bytes")
         ws = _workspace(n.value, dev) if n.value else None
     _check(lib().nacho_distill(_pack([teacher]), _ptr(logits), ld, dt, _ptr(weight), temperature, _ptr(loss), _ptr(lse),
-                               _ptr(grad), ldg, _ptr(ws), ws.numel() if ws is not None else 0, _stream()), "nacho_distill")
+                               _ptr(grad), ldg, _ptr(ws), _room(ws, dev), _stream()), "nacho_distill")
     return loss, lse
 
 
@@ -631,7 +650,7 @@ def nacho_route(logits, top_k, normalise=False, keep=None, out=None, ws=None):
         _check(lib().nacho_route_workspace_bytes(tokens, experts, top_k, C.byref(n)), "nacho_route_workspace_bytes")
         ws = _workspace(n.value, dev)
     _check(lib().nacho_route(_ptr(logits), ld, tokens, experts, dt, top_k, out.normalise, _ptr(keep), C.byref(out.c),
-                             _ptr(ws), ws.numel(), _stream()), "nacho_route")
+                             _ptr(ws), _room(ws, dev), _stream()), "nacho_route")
     return out
 
 
@@ -641,6 +660,7 @@ def nacho_route_grad(logits, routing: Routing, grad_gate=None, balance=0.0, keep
     dt, dev = model_dtype_code(logits.dtype), logits.device
     r = routing
     ld = _matrix(logits, "logits", r.n_tokens, r.n_experts)
+    _need(r.pos.device == dev, "routing: on another device than the logits")
     _vector_of(grad_gate, "grad_gate", r.n_tokens * r.top_k, torch.float32, dev)
     if grad is None:
         grad = torch.empty((r.n_tokens, r.n_experts), dtype=logits.dtype, device=dev)
@@ -728,8 +748,8 @@ def nacho_experts_grad(grad_y, x, weight, expert_pos, token=None, act="none", pr
         _check(lib().nacho_experts_workspace_bytes(C.byref(c), C.byref(n)), "nacho_experts_workspace_bytes")
         ws = _workspace(n.value, dev) if n.value else None
     _check(lib().nacho_experts_grad(C.byref(c), _ptr(grad_y), ldgy, _ptr(pre), ldpre, _ptr(grad_x), ldgx, _ptr(grad_weight),
-                                    ldgw, gap, _ptr(grad_bias), gb, _ptr(ws), ws.numel() if ws is not None else 0,
-                                    _stream()), "nacho_experts_grad")
+                                    ldgw, gap, _ptr(grad_bias), gb, _ptr(ws), _room(ws, dev), _stream()),
+           "nacho_experts_grad")
     return grad_x, grad_weight
 
 
@@ -752,8 +772,8 @@ def nacho_combine(pos, slot, y, gate=None, residual=None, out=None):
     """out[t] = residual[t] + sum over the entries of token t of gate * y[slot] (pos, slot, gate: a Routing's).  `out` may
     be `residual` itself."""
     dt, dev = model_dtype_code(y.dtype), y.device
-    tokens, n = pos.numel() - 1, int(y.shape[1])
     ldy = _matrix(y, "y")
+    tokens, n = pos.numel() - 1, y.shape[1]
     ldr = _matrix(residual, "residual", tokens, n, y.dtype, dev) if residual is not None else 0
     if out is None:
         out = torch.empty((tokens, n), dtype=y.dtype, device=dev)
@@ -769,8 +789,8 @@ def nacho_combine(pos, slot, y, gate=None, residual=None, out=None):
 def nacho_combine_grad(pos, slot, y, grad_out, gate=None, grad_y=None, grad_gate=None):
     """Gradients of y's rows and of the gates; rows of y that no entry names are left as they are."""
     dt, dev = model_dtype_code(y.dtype), y.device
-    tokens, n = pos.numel() - 1, int(y.shape[1])
     ldy = _matrix(y, "y")
+    tokens, n = pos.numel() - 1, y.shape[1]
     ldg = _matrix(grad_out, "grad_out", tokens, n, y.dtype, dev)
     if grad_y is None:
         grad_y = torch.empty((y.shape[0], n), dtype=y.dtype, device=dev)

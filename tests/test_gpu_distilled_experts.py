@@ -135,3 +135,13 @@ def test_whatever_the_default_type_is(default):
         torch.set_default_dtype(before)
     for a, b in zip(first, second):
         assert a.dtype is torch.float32 and torch.equal(a, b)
+
+
+def test_rows_of_another_gpu_are_refused(monkeypatch):
+    """Kernels go to the current GPU's stream; rows have to be there."""
+    z = torch.zeros((4, 8), device="cuda")
+    monkeypatch.setattr(nb, "_current_device", lambda: z.get_device() + 1)
+    for call in (lambda: nb.nacho_route(z, 2), lambda: nb.nacho_experts(z, torch.zeros((1, 8, 8), device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")),
+                 lambda: nb.nacho_combine(torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"), z)):
+        with pytest.raises(ValueError):
+            call()

@@ -24,7 +24,7 @@ def calls(monkeypatch):
 
     monkeypatch.setattr(nb, "lib", lambda: Library())
     monkeypatch.setattr(nb, "_stream", lambda: 0)
-    monkeypatch.setattr(nb, "_GPU", "cpu", raising=False)
+    monkeypatch.setattr(nb, "_on_gpu", lambda t, what: None)
     return made
 
 
@@ -72,3 +72,30 @@ def test_weights_whose_rows_lie_on_each_other_are_refused(calls):
     assert nb._stack(row.expand(2, 1, 16), "w", (2, 1, 16), torch.float32, row.device) == (16, 16)
     assert nb._stack(flat, "w", (1, 24, 16), torch.float32, flat.device) == (16, 24 * 16)
     assert nb._stack(torch.zeros((2, 30, 20))[:, :24, :16], "w", (2, 24, 16), torch.float32, flat.device) == (20, 600)
+
+
+def test_host_tensors_are_refused():
+    z, x, w, y = torch.zeros((3, 20)), torch.zeros((5, 16)), torch.zeros((2, 20, 16)), torch.zeros((6, 20))
+    bounds, token, pos, slot = ints(0, 3, 6), ints(0, 1, 2, 3, 4, 0), ints(0, 2, 4, 6), ints(0, 1, 2, 3, 4, 5)
+    floats, r = torch.zeros(3), nb.Routing(3, 20, 2, z.device)
+    for call in (lambda: nb.nacho_distill(teacher(), z), lambda: nb.nacho_distill(teacher(), z, grad=torch.zeros_like(z)),
+                 lambda: nb.nacho_distill_grad(teacher(), z, floats), lambda: nb.nacho_route(z, 2), lambda: nb.nacho_route(z, 2, out=r),
+                 lambda: nb.nacho_route_grad(z, r), lambda: nb.nacho_experts(x, w, bounds, token=token),
+                 lambda: nb.nacho_experts_grad(y, x, w, bounds, token=token), lambda: nb.nacho_combine(pos, slot, y),
+                 lambda: nb.nacho_combine_grad(pos, slot, y, z)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_workspaces_and_routings_elsewhere_are_refused(calls):
+    """(the device `meta` stands for another one than that of the rows)"""
+    z, other = torch.zeros((3, 20)), torch.empty(1 << 20, dtype=torch.uint8, device="meta")
+    x, w, bounds = torch.zeros((6, 16)), torch.zeros((2, 20, 16)), ints(0, 3, 6)
+    strange = nb.Routing(3, 20, 2, z.device)
+    strange.pos = strange.pos.to("meta")
+    for call in (lambda: nb.nacho_distill(teacher(), z, ws=other), lambda: nb.nacho_route(z, 2, ws=other),
+                 lambda: nb.nacho_route(z, 2, ws=torch.zeros(1 << 20, dtype=torch.uint8)[::2]), lambda: nb.nacho_route_grad(z, strange),
+                 lambda: nb.nacho_experts_grad(torch.zeros((6, 20)), x, w, bounds, ws=other)):
+        with pytest.raises(ValueError):
+            call()
+    assert not [c for c in calls if not c.endswith("_bytes")]
