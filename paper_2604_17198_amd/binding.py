@@ -228,6 +228,10 @@ class Operand:
         if val is not None:
             self.keep.append(val)
             c.val = val.data_ptr() if val.numel() else None
+        where = self.keep[0].device
+        for t in self.keep:
+            if t.device != where or not t.is_contiguous():
+                raise ValueError(f"an operand's arrays: contiguous ones on one device are needed (here {where})")
         self.c = c
         self.nlevels = len(levels)
         self.nnz = int(levels[-1]["crd"].numel())

@@ -99,3 +99,17 @@ def test_workspaces_and_routings_elsewhere_are_refused(calls):
         with pytest.raises(ValueError):
             call()
     assert not [c for c in calls if not c.endswith("_bytes")]
+
+
+def test_operands_arrays_lie_together():
+    """Arrays of one operand that have gaps, or that lie on several devices, make no descriptor."""
+    pos, crd, val = ints(0, 2, 4), ints(1, 5, 2, 3), torch.zeros(4)
+    gaps = lambda t: torch.stack([t, t], dim=1)[:, 0]
+    for p, c, v in ((gaps(pos), crd, val), (pos, gaps(crd), val), (pos, crd, gaps(val)), (pos.to("meta"), crd, val), (pos, crd.to("meta"), val),
+                    (pos, crd, val.to("meta"))):
+        with pytest.raises(ValueError):
+            nb.csr(p, c, 2, 9, v)
+    assert nb.csr(pos, crd, 2, 9, val).nnz == 4
+    rows = ints(0, 1, 1, 2)
+    with pytest.raises(ValueError):
+        nb.coo(gaps(rows), crd, 3, 9, val)
