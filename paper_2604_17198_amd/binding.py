@@ -734,18 +734,23 @@ def nacho_experts(x, weight, expert_pos, token=None, bias=None, act="none", y=No
 
 def nacho_experts_grad(grad_y, x, weight, expert_pos, token=None, act="none", pre=None, grad_x=None, grad_weight=None,
                        grad_bias=None, ws=None):
-    """(gradient of every slot's row of x, gradient of the weights); `grad_bias`, when given, receives the biases'."""
+    """(gradient of every slot's row of x, gradient of the weights); `grad_bias`, when given, receives the biases'.  A
+    `grad_x` or `grad_weight` that is False is not wanted: it is not computed, and None is returned."""
     c, slots = _layer(x, weight, expert_pos, token, None, act)
     experts, outer, inner = weight.shape
     dev = x.device
     ldgy = _matrix(grad_y, "grad_y", slots, outer, x.dtype, dev)
     ldpre = _matrix(pre, "pre", slots, outer, x.dtype, dev) if pre is not None else 0
-    if grad_x is None:
+    if grad_x is False:
+        grad_x = None
+    elif grad_x is None:
         grad_x = torch.empty((slots, inner), dtype=x.dtype, device=dev)
-    if grad_weight is None:
+    if grad_weight is False:
+        grad_weight = None
+    elif grad_weight is None:
         grad_weight = torch.empty((experts, outer, inner), dtype=x.dtype, device=dev)
-    ldgx = _matrix(grad_x, "grad_x", slots, inner, x.dtype, dev)
-    ldgw, gap = _stack(grad_weight, "grad_weight", (experts, outer, inner), x.dtype, dev)
+    ldgx = _matrix(grad_x, "grad_x", slots, inner, x.dtype, dev) if grad_x is not None else 0
+    ldgw, gap = _stack(grad_weight, "grad_weight", (experts, outer, inner), x.dtype, dev) if grad_weight is not None else (0, 0)
     gb = _stack(grad_bias, "grad_bias", (experts, outer), x.dtype, dev)[1] if grad_bias is not None else 0
     if ws is None:
         n = C.c_size_t(0)
@@ -791,15 +796,20 @@ def nacho_combine(pos, slot, y, gate=None, residual=None, out=None):
 
 
 def nacho_combine_grad(pos, slot, y, grad_out, gate=None, grad_y=None, grad_gate=None):
-    """Gradients of y's rows and of the gates; rows of y that no entry names are left as they are."""
+    """Gradients of y's rows and of the gates; rows of y that no entry names, and places of gates behind the last entry, are
+    left as they are.  One that is False is not wanted: it is not computed, and None is returned."""
     dt, dev = model_dtype_code(y.dtype), y.device
     ldy = _matrix(y, "y")
     tokens, n = pos.numel() - 1, y.shape[1]
     ldg = _matrix(grad_out, "grad_out", tokens, n, y.dtype, dev)
-    if grad_y is None:
+    if grad_y is False:
+        grad_y = None
+    elif grad_y is None:
         grad_y = torch.empty((y.shape[0], n), dtype=y.dtype, device=dev)
-    ldgy = _matrix(grad_y, "grad_y", y.shape[0], n, y.dtype, dev)
-    if grad_gate is None:
+    ldgy = _matrix(grad_y, "grad_y", y.shape[0], n, y.dtype, dev) if grad_y is not None else 0
+    if grad_gate is False:
+        grad_gate = None
+    elif grad_gate is None:
         grad_gate = _floats(slot.numel(), dev)
     _vector_of(grad_gate, "grad_gate", slot.numel(), torch.float32, dev)
     c = _slots_of(pos, slot, gate, y.shape[0], dev)

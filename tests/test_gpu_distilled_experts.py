@@ -145,3 +145,31 @@ def test_rows_of_another_gpu_are_refused(monkeypatch):
                  lambda: nb.nacho_combine(torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"), z)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_gradients_that_are_not_wanted(act):
+    """The others are the same bits, whichever are left out."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    new = lambda *shape: torch.randn(shape, generator=g, device="cuda")
+    bounds = torch.tensor([0, 30, 30, 77], dtype=torch.int32, device="cuda")
+    x, w, gy, pre = new(77, 48), new(3, 40, 48), new(77, 40), new(77, 40)
+
+    def run(wanted):
+        bias = new(3, 40) if wanted[2] else None
+        gx, gw = nb.nacho_experts_grad(gy, x, w, bounds, act=act, pre=pre, grad_x=None if wanted[0] else False,
+                                       grad_weight=None if wanted[1] else False, grad_bias=bias)
+        return gx, gw, bias
+
+    every = run((True, True, True))
+    for number in range(8):
+        wanted = tuple(bool(number >> i & 1) for i in range(3))
+        for got, want, asked in zip(run(wanted), every, wanted):
+            assert torch.equal(got, want) if asked else got is None
+    pos, slot = torch.tensor([0, 2, 2, 4], dtype=torch.int32, device="cuda"), torch.tensor([0, 3, 1, 2], dtype=torch.int32, device="cuda")
+    y, go, gate = new(4, 33), new(3, 33), new(4)
+    both = nb.nacho_combine_grad(pos, slot, y, go, gate=gate)
+    only, none = nb.nacho_combine_grad(pos, slot, y, go, gate=gate, grad_gate=False)
+    assert torch.equal(only, both[0]) and none is None
+    none, only = nb.nacho_combine_grad(pos, slot, y, go, gate=gate, grad_y=False)
+    assert torch.equal(only, both[1]) and none is None

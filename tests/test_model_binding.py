@@ -113,3 +113,29 @@ def test_operands_arrays_lie_together():
     rows = ints(0, 1, 1, 2)
     with pytest.raises(ValueError):
         nb.coo(gaps(rows), crd, 3, 9, val)
+
+
+def test_gradients_that_are_not_wanted(monkeypatch, calls):
+    """False for a gradient: no array is made, NULL goes to the library, None comes back."""
+    given = {}
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                given[name] = args
+                if name.endswith("_workspace_bytes"):
+                    C.cast(args[-1], C.POINTER(C.c_size_t))[0] = 256
+                return 0
+            return call
+
+    monkeypatch.setattr(nb, "lib", lambda: Library())
+    x, w, y, bounds = torch.zeros((6, 16)), torch.zeros((2, 20, 16)), torch.zeros((6, 20)), ints(0, 3, 6)
+    for gx, gw in ((None, False), (False, None), (False, False)):
+        a, b = nb.nacho_experts_grad(y, x, w, bounds, grad_x=gx, grad_weight=gw, grad_bias=torch.zeros((2, 20)))
+        args = given["nacho_experts_grad"]
+        assert (a is None) == (gx is False) == (args[5] is None) and (b is None) == (gw is False) == (args[7] is None) and args[10] is not None
+    pos, slot, go = ints(0, 2, 4, 6), ints(0, 1, 2, 3, 4, 5), torch.zeros((3, 20))
+    for gy, gg in ((None, False), (False, None), (False, False)):
+        a, b = nb.nacho_combine_grad(pos, slot, y, go, grad_y=gy, grad_gate=gg)
+        args = given["nacho_combine_grad"]
+        assert (a is None) == (gy is False) == (args[7] is None) and (b is None) == (gg is False) == (args[9] is None)
