@@ -116,6 +116,9 @@ template <typename Args> __device__ inline int bound_of(const Args &a, int e)
     return at < (int)a.slots ? at : (int)a.slots;
 }
 
+// Tiles of kM rows that `rows` < 2^31 make (unsigned: the sum passes 31 bits where an expert has nearly all there can be).
+template <int kM> __device__ inline int tiles_of(int rows) { return rows > 0 ? (int)(((unsigned)rows + (kM - 1)) / kM) : 0; }
+
 // The expert and the first row of tile `tile` of kM rows, the experts' tiles one after the other; false behind the last.
 template <int kM, typename Args> __device__ inline bool find_tile(const Args &a, int tile, int &expert, int &row, int &end)
 {
@@ -128,7 +131,7 @@ template <int kM, typename Args> __device__ inline bool find_tile(const Args &a,
             first = bound_of(a, e);
             last = bound_of(a, e + 1);
         }
-        const int tiles = (last - first + kM - 1) / kM, upto = before + wave_inclusive_scan(tiles);
+        const int tiles = tiles_of<kM>(last - first), upto = before + wave_inclusive_scan(tiles);
         const unsigned long long past = __ballot(upto > tile);
         if (past != 0) {
             const int at = __ffsll((long long)past) - 1;
@@ -321,8 +324,8 @@ template <typename T, int kRows, int kStep, int kThreads, Access kAccess, int kS
         rows[set.value] = k - k0 - row_of_load(0);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int kk = k0 + row_of_load(i);
-            const T *from = address(i, kk < k ? kk : k - 1);
+            const int past = k - 1 - k0;
+            const T *from = address(i, k0 + (row_of_load(i) < past ? row_of_load(i) : past));
             if constexpr (kAccess == WORDS) word[set.value][i] = *reinterpret_cast<const v4u *>(from + (first < length ? first : length - n));
             else word[set.value][i] = last.load(from + first);
         }
@@ -431,6 +434,8 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
         k_begin = bound_of(a, expert);
         k = bound_of(a, expert + 1) - k_begin;
     } else if (!find_tile<kM>(a, tile, expert, m0, m_end) || n0 >= a.n) return;
+    // (sums of rows, or of steps of k, and what a tile has may pass 31 bits behind the last one: what is left is compared)
+    const int m_rows = m_end - m0;
     const T *const q = static_cast<const T *>(a.q);
     const T *const p = static_cast<const T *>(a.p) + (int64_t)expert * a.p_stride;
     SideQ side_q;
@@ -438,7 +443,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
     // rows behind the last: the last one again, whose results are not stored
     if constexpr (!kAcrossQ)
         side_q.start(q, a.ldq, [&](int r) {
-            const int row = m0 + r < m_end ? m0 + r : m_end - 1;
+            const int row = m0 + (r < m_rows ? r : m_rows - 1);
             return kForm == FORWARD && a.token ? a.token[row] : row;
         });
     if constexpr (!kAcrossP) side_p.start(p, a.ldp, [&](int r) { return n0 + r < a.n ? n0 + r : a.n - 1; });
@@ -449,8 +454,8 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
         if constexpr (kForm == WEIGHTS) {
 #pragma unroll
             for (int l = 0; l < SideP::kLoads; ++l) {
-                const int kk = k0 + SideP::row_of_load(l);
-                slot[l] = k_begin + (kk < k ? kk : k - 1);
+                const int past = k - 1 - k0;
+                slot[l] = k_begin + k0 + (SideP::row_of_load(l) < past ? SideP::row_of_load(l) : past);
             }
             if constexpr (kAccess != WORDS) {
                 // (without a branch, see Ragged)
@@ -470,12 +475,12 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
         if constexpr (kForm == ROWS) side_p.load(set, [&](int, int kk) { return p + (int64_t)kk * a.ldp; }, k0, k, a.n, n0);
         else if constexpr (kForm == WEIGHTS) {
             side_p.load(set, [&](int l, int) { return p + (int64_t)(kAccess != WORDS && a.token ? found[l] : slot[l]) * a.ldp; }, k0, k, a.n, n0);
-            look_up(k0 + kDepth<T, kStep> < k ? k0 + kDepth<T, kStep> : k0);
+            look_up(kDepth<T, kStep> < k - k0 ? k0 + kDepth<T, kStep> : k0);
         } else side_p.load(set, k0, k);
     };
     const int wave = (int)threadIdx.x / NACHO_WAVE, lane = lane_id();
     const int wm = wave / kWavesN * kTileM, wn = wave % kWavesN * kTileN;
-    const bool busy = __builtin_amdgcn_readfirstlane(m0 + wm < m_end && n0 + wn < a.n ? 1 : 0) != 0;
+    const bool busy = __builtin_amdgcn_readfirstlane(wm < m_rows && n0 + wn < a.n ? 1 : 0) != 0;
     v4f acc[kFragM][kFragN];
 #pragma unroll
     for (int i = 0; i < kFragM; ++i)
@@ -609,13 +614,13 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
             store(zero, stage0);
             __syncthreads();
             // (a loop of one turn: with the product in line the tiles of 256 x 256 need two registers more than there are)
-            for (; done < k; done += kDeep)
+            for (int left = k - done; left > 0; left -= kDeep)
                 if (busy) multiply_all(stage0);
         }
     } else if (k > 0) {
         // The next steps (two of them if there are registers) are on their way while one is multiplied.  (Behind the last step
         // it is loaded again: a load that is not there on every path would have the compiler wait for all of them.)
-        const int steps = (k + kDeep - 1) / kDeep;
+        const int steps = (k - 1) / kDeep + 1;
         auto at = [&](int t) { return (t < steps ? t : steps - 1) * kDeep; };
         load(zero, 0);
         if constexpr (kSets == 2) load(one, at(1));
@@ -683,8 +688,8 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
         wave_sync();
 #pragma unroll 1
         for (int r = lane / kLanes; r < kPhase * 16; r += NACHO_WAVE / kLanes) {
-            const int m = m0 + wm + i0 * 16 + r;
-            if (m >= m_end || width <= 0) break;
+            const int own = wm + i0 * 16 + r, m = m0 + own;
+            if (own >= m_rows || width <= 0) break;
             float v[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -718,6 +723,7 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
     const int tx = (int)threadIdx.x % 16, ty = (int)threadIdx.x / 16, c0 = (number - tile * tiles_n) * 16 * n, c = c0 + tx * n, width = a.cols - c;
     int expert, row, end;
     if (!find_tile<kSlopeRows>(a, tile, expert, row, end)) return;
+    const int rows = end - row;
     const T *gy = static_cast<const T *>(a.grad_y) + c, *pre = static_cast<const T *>(a.pre) + c;
     T *gz = static_cast<T *>(a.grad_z) + c;
     auto get = [&](const T *from) {
@@ -736,7 +742,7 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
     for (int i = 0; i < kRows; ++i) {
         const int m = row + ty + i * 16;
         g[i] = z[i] = v4u{0, 0, 0, 0};
-        if (m < end) {
+        if (ty + i * 16 < rows) {
             g[i] = get(gy + (int64_t)m * a.ldgy);
             if (a.act != NACHO_ACT_NONE) z[i] = get(pre + (int64_t)m * a.ldpre);
         }
@@ -758,7 +764,7 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
 #pragma unroll
             for (int e = 0; e < n; ++e) sum[e] += wide((T)v[e]);
         }
-        if (m < end && a.grad_z) {
+        if (ty + i * 16 < rows && a.grad_z) {
             T *to = gz + (int64_t)m * a.ldgz;
             if (width >= n) {
                 if constexpr (kAccess == WORDS) *reinterpret_cast<word *>(to) = v;
@@ -787,11 +793,11 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
 template <typename T> __global__ void __launch_bounds__(kThreads) experts_bias_kernel(SlopeArgs a, int tiles_n)
 {
     const int expert = (int)blockIdx.x / tiles_n, c = ((int)blockIdx.x - expert * tiles_n) * kThreads + (int)threadIdx.x;
-    auto tiles_of = [&](int e) { return (bound_of(a, e + 1) - bound_of(a, e) + kSlopeRows - 1) / kSlopeRows; };
+    auto tiles_at = [&](int e) { return tiles_of<kSlopeRows>(bound_of(a, e + 1) - bound_of(a, e)); };
     int first = 0;
-    for (int e0 = 0; e0 < expert; e0 += NACHO_WAVE) first += e0 + lane_id() < expert ? tiles_of(e0 + lane_id()) : 0;
+    for (int e0 = 0; e0 < expert; e0 += NACHO_WAVE) first += e0 + lane_id() < expert ? tiles_at(e0 + lane_id()) : 0;
     first = wave_sum(first);
-    const int tiles = tiles_of(expert);
+    const int tiles = tiles_at(expert);
     if (c >= a.cols) return;
     float total = 0.0f;
     constexpr int kBatch = 8;

@@ -309,3 +309,19 @@ def test_slopes_of_rows_past_the_types_range(act, outer, dtype):
     pre[2, 1] = float("nan")
     gx, gw = nb.nacho_experts_grad(torch.ones((4, outer), dtype=dtype, device="cuda"), x, w, bounds, act=act, pre=pre.cuda(), grad_bias=gb)
     assert torch.isnan(gx[:, 0]).tolist() == [False, False, True, False] and bool(torch.isnan(gb[0, 1])) and bool((gb[0, 2:] == 2).all())
+
+
+def test_slots_up_to_the_last_of_two_to_the_31():
+    """An expert whose slots start at any place and end at the last that there can be: sums of places pass 31 bits."""
+    slots = 2 ** 31 - 1                                      # rows of one element: 4.3 GB each
+    bounds = torch.tensor([0, 5, slots], dtype=torch.int32, device="cuda")
+    x = torch.full((slots, 1), 2.0, dtype=torch.bfloat16, device="cuda")
+    x[4], x[-1] = 3.0, 5.0
+    w = torch.tensor([3.0, 7.0], dtype=torch.bfloat16, device="cuda").reshape(2, 1, 1)
+    y = torch.zeros_like(x)
+    nb.nacho_experts(x, w, bounds, y=y)
+    assert y[:5, 0].tolist() == [6, 6, 6, 6, 9] and y[-1].item() == 35 and bool((y[5:-1] == 14).all())
+    x[-2] = -1.0                                             # (as rows before the activation)
+    y.fill_(1.0)
+    gx, _ = nb.nacho_experts_grad(y, x, w, bounds, act="relu", pre=x, grad_weight=False)
+    assert bool((gx[:5] == 3).all()) and gx[-2].item() == 0 and gx[-1].item() == 7 and bool((gx[5:-2] == 7).all())
