@@ -25,7 +25,17 @@ bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return a_bytes > 0 && b_bytes > 0 && x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
 }
-int64_t span(int64_t rows, int64_t cols, int64_t ld, int64_t elem) { return rows > 0 ? ((rows - 1) * ld + cols) * elem : 0; }
+// Bytes from a matrix's first element to its last one.  (Up to 2^31 rows, 2^40 elements apart: longer stretches than any
+// memory count as 2^62 bytes.)
+int64_t stretch(__int128 elements, int64_t elem)
+{
+    const __int128 bytes = elements * elem, most = (__int128)1 << 62;
+    return (int64_t)(bytes < most ? bytes : most);
+}
+int64_t span(int64_t rows, int64_t cols, int64_t ld, int64_t elem)
+{
+    return rows > 0 ? stretch((__int128)(rows - 1) * ld + cols, elem) : 0;
+}
 
 // Slices of a workspace, 256-byte aligned.
 struct Slices {
@@ -62,7 +72,7 @@ int32_t check_route(int64_t tokens, int64_t experts, int32_t top_k)
 {
     if (tokens < 0 || experts < 1 || top_k < 1 || top_k > experts) return NACHO_ERR_INVALID_ARG;
     if (experts > kMostExperts || top_k > kMostChoices) return NACHO_ERR_UNSUPPORTED;
-    return tokens * top_k > kMostRows || tokens > kMostRows ? NACHO_ERR_INVALID_ARG : NACHO_OK;
+    return tokens > kMostRows || tokens * top_k > kMostRows ? NACHO_ERR_INVALID_ARG : NACHO_OK;
 }
 bool check_routing(const nacho_routing *r)
 {
@@ -121,11 +131,11 @@ int32_t check_combine(const nacho_tensor *m, int64_t n, int32_t dtype, CombineAr
 bool matrices(const void *p, int64_t count, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int64_t elem)
 {
     if (!matrix(p, count > 0 ? rows : 0, cols, ld, elem) || stride > kMostStride) return false;
-    return count <= 1 || rows == 0 || stride >= (rows - 1) * ld + cols;
+    return count <= 1 || rows == 0 || stride >= (__int128)(rows - 1) * ld + cols;
 }
 int64_t span(int64_t count, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int64_t elem)
 {
-    return count > 0 ? (count - 1) * stride * elem + span(rows, cols, ld, elem) : 0;
+    return count > 0 && rows > 0 ? stretch((__int128)(count - 1) * stride + (__int128)(rows - 1) * ld + cols, elem) : 0;
 }
 
 int32_t check_layer(const nacho_experts_layer *l)

@@ -122,3 +122,18 @@ def test_sparse_algebra_still_takes_floats_and_doubles_alone(call):
     for dtype in (nb.BF16, nb.F16):
         for op in (nb.OP_SPMV, nb.OP_SPMM, nb.OP_SPADD):
             assert nb.lib().nacho_workspace_bytes(op, C.byref(t), 1, dtype, 8, 0, C.byref(n)) == BAD
+
+
+def test_sizes_whose_products_pass_64_bits():
+    """Stretches longer than any memory still overlap what lies in them."""
+    lib = nb.lib()
+    most, far = (1 << 31) - 1, 1 << 40
+    t = teacher(rows=most, cols=1, stored=10)
+    assert lib.nacho_distill(C.byref(t), B, far, nb.F32, None, 1.0, E, E + (1 << 36), B + 4096, 1, None, 0, None) == BAD
+    assert lib.nacho_distill_grad(C.byref(t), B, far, nb.F32, None, 1.0, E, B + 4096, far, None) == BAD
+    m = teacher(rows=5, cols=most, stored=12)
+    assert lib.nacho_combine(C.byref(m), B, far, 32, nb.F32, None, 0, B + (1 << 39), 32, None) == BAD
+    # experts that lie on each other
+    wide = layer(n_experts=3, outer=(1 << 24) - 1, inner=64, ldw=far, w_stride=1 << 30)
+    assert lib.nacho_experts(C.byref(wide), E, 1 << 24, None, 0, None) == BAD
+    assert size(lib.nacho_route_workspace_bytes, (1 << 62) + 1, 64, 4)[0] == BAD
