@@ -23,7 +23,7 @@ bool matrix(const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t elem)
 bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
 {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return a_bytes > 0 && b_bytes > 0 && x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+    return a && b && a_bytes > 0 && b_bytes > 0 && x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
 }
 // Bytes from a matrix's first element to its last one.  (Up to 2^31 rows, 2^40 elements apart: longer stretches than any
 // memory count as 2^62 bytes.)
@@ -35,6 +35,23 @@ int64_t stretch(__int128 elements, int64_t elem)
 int64_t span(int64_t rows, int64_t cols, int64_t ld, int64_t elem)
 {
     return rows > 0 ? stretch((__int128)(rows - 1) * ld + cols, elem) : 0;
+}
+
+// An array of a call.
+struct Array {
+    const void *at;
+    int64_t bytes;
+};
+// Whether the outputs share no byte with each other or with an input.
+bool apart(std::initializer_list<Array> outputs, std::initializer_list<Array> inputs)
+{
+    for (const Array *o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Array *p = outputs.begin(); p != o; ++p)
+            if (overlap(o->at, o->bytes, p->at, p->bytes)) return false;
+        for (const Array &p : inputs)
+            if (overlap(o->at, o->bytes, p.at, p.bytes)) return false;
+    }
+    return true;
 }
 
 // Slices of a workspace, 256-byte aligned.
@@ -99,12 +116,20 @@ int32_t check_distill(const nacho_tensor *teacher, const void *logits, int64_t l
     if (!aligned(teacher->lvl[1].crd, 16) || !aligned(teacher->val, 16)) return NACHO_ERR_INVALID_ARG;
     const int64_t elem = value_bytes(dtype);
     if (!matrix(logits, rows, cols, ldl, elem) || !(temperature >= 1e-30f && temperature <= 1e18f)) return NACHO_ERR_INVALID_ARG;
-    if (grad && (!matrix(grad, rows, cols, ldg, elem) ||
-                 overlap(logits, span(rows, cols, ldl, elem), grad, span(rows, cols, ldg, elem))))
-        return NACHO_ERR_INVALID_ARG;
+    if (grad && !matrix(grad, rows, cols, ldg, elem)) return NACHO_ERR_INVALID_ARG;
     *a = DistillArgs{teacher->lvl[1].pos, teacher->lvl[1].crd, static_cast<const float *>(teacher->val), logits, ldl, weight,
                      temperature, nullptr, nullptr, nullptr, grad, ldg, rows, (int32_t)cols, nullptr, false};
     return NACHO_OK;
+}
+
+// The arrays that a distillation call reads, and with them the outputs (`lse` is one or the other).
+bool check_distill_arrays(const nacho_tensor *teacher, const DistillArgs &a, int64_t elem, const float *lse_in, float *loss, float *lse,
+                          const void *ws, int64_t ws_bytes)
+{
+    const int64_t by_row = a.rows * 4, stored = teacher->lvl[1].count * 4;
+    return apart({{loss, by_row}, {lse, by_row}, {a.grad, a.grad ? span(a.rows, a.cols, a.ldg, elem) : 0}, {ws, ws_bytes}},
+                 {{a.pos, by_row + 4}, {a.crd, stored}, {a.val, stored}, {a.logits, span(a.rows, a.cols, a.ldl, elem)}, {a.weight, by_row},
+                  {lse_in, by_row}});
 }
 
 // The routing matrix of a combine call: CSR, tokens x slots.
@@ -154,11 +179,14 @@ bool check_w(const nacho_experts_layer *l, int64_t elem)
 {
     return matrices(l->w, l->n_experts, l->outer, l->inner, l->ldw, l->w_stride, elem);
 }
-bool overlaps_inputs(const nacho_experts_layer *l, const void *p, int64_t bytes, int64_t elem)
+// The arrays of a layer that a call reads.
+Array x_of(const nacho_experts_layer *l, int64_t elem) { return {l->x, l->x ? span(l->n_tokens, l->inner, l->ldx, elem) : 0}; }
+Array w_of(const nacho_experts_layer *l, int64_t elem)
 {
-    return overlap(p, bytes, l->x, l->x ? span(l->n_tokens, l->inner, l->ldx, elem) : 0) ||
-           overlap(p, bytes, l->w, l->w ? span(l->n_experts, l->outer, l->inner, l->ldw, l->w_stride, elem) : 0);
+    return {l->w, l->w ? span(l->n_experts, l->outer, l->inner, l->ldw, l->w_stride, elem) : 0};
 }
+Array bounds_of(const nacho_experts_layer *l) { return {l->expert_pos, l->n_experts * 4 + 4}; }
+Array token_of(const nacho_experts_layer *l) { return {l->token, l->n_slots * 4}; }
 
 // What a gradient call keeps: the gradient before the activation, and sums of its rows.
 struct GradWs {
@@ -190,6 +218,7 @@ int32_t nacho_distill(const nacho_tensor *teacher, const void *logits, int64_t l
     if (a.rows > 0 && (!loss || !lse)) return NACHO_ERR_INVALID_ARG;
     const size_t need = align_up((size_t)distill_partials(dtype, a.rows, a.cols, grad != nullptr) * sizeof(float), 256);
     if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return NACHO_ERR_WORKSPACE;
+    if (!check_distill_arrays(teacher, a, value_bytes(dtype), nullptr, loss, lse, ws, (int64_t)need)) return NACHO_ERR_INVALID_ARG;
     a.partial = static_cast<float *>(ws);
     a.loss = loss;
     a.lse = lse;
@@ -216,6 +245,7 @@ int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int6
     const int32_t rc = check_distill(teacher, logits, ldl, dtype, weight, temperature, grad, ldg, &a);
     if (rc != NACHO_OK) return rc;
     if (a.rows > 0 && a.cols > 0 && (!lse || !grad)) return NACHO_ERR_INVALID_ARG;
+    if (!check_distill_arrays(teacher, a, value_bytes(dtype), lse, nullptr, nullptr, nullptr, 0)) return NACHO_ERR_INVALID_ARG;
     a.lse_in = lse;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     profile_begin(s);
@@ -243,6 +273,11 @@ int32_t nacho_route(const void *logits, int64_t ldl, int64_t n_tokens, int64_t n
     size_t need = 0;
     const RouteScratch w = carve_route(ws, n_tokens, (int32_t)n_experts, top_k, &need);
     if (!ws || ws_bytes < need || !aligned(ws, 16)) return NACHO_ERR_WORKSPACE;
+    const int64_t room = n_tokens * top_k * 4;
+    if (!apart({{out->pos, n_tokens * 4 + 4}, {out->expert, room}, {out->gate, room}, {out->slot, room}, {out->expert_pos, n_experts * 4 + 4},
+                {out->token, room}, {out->counts, n_experts * 4}, {out->lse, n_tokens * 4}, {out->balance, 4}, {out->routed, 4}, {ws, (int64_t)need}},
+               {{logits, span(n_tokens, n_experts, ldl, value_bytes(dtype))}, {keep, n_tokens}}))
+        return NACHO_ERR_INVALID_ARG;
     const RouteArgs a{logits, ldl, keep, n_tokens, (int32_t)n_experts, top_k, normalise != 0, *out};
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     profile_begin(s);
@@ -257,8 +292,12 @@ int32_t nacho_route_grad(const void *logits, int64_t ldl, int64_t n_tokens, int6
     if (rc != NACHO_OK) return rc;
     if (!value_type(dtype) || !check_routing(routing) || !aligned(grad_gate, 4)) return NACHO_ERR_INVALID_ARG;
     const int64_t elem = value_bytes(dtype);
-    if (!matrix(logits, n_tokens, n_experts, ldl, elem) || !matrix(grad, n_tokens, n_experts, ldg, elem) ||
-        overlap(logits, span(n_tokens, n_experts, ldl, elem), grad, span(n_tokens, n_experts, ldg, elem)))
+    if (!matrix(logits, n_tokens, n_experts, ldl, elem) || !matrix(grad, n_tokens, n_experts, ldg, elem)) return NACHO_ERR_INVALID_ARG;
+    const int64_t room = n_tokens * top_k * 4;
+    if (!apart({{grad, span(n_tokens, n_experts, ldg, elem)}},
+               {{logits, span(n_tokens, n_experts, ldl, elem)}, {grad_gate, room}, {routing->pos, n_tokens * 4 + 4}, {routing->expert, room},
+                {routing->gate, room}, {routing->slot, room}, {routing->expert_pos, n_experts * 4 + 4}, {routing->token, room},
+                {routing->counts, n_experts * 4}, {routing->lse, n_tokens * 4}, {routing->balance, 4}, {routing->routed, 4}}))
         return NACHO_ERR_INVALID_ARG;
     const RouteGradArgs a{logits, ldl, n_tokens, (int32_t)n_experts, normalise != 0, *routing, grad_gate, balance, grad, ldg};
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -275,11 +314,12 @@ int32_t nacho_combine(const nacho_tensor *routing, const void *y, int64_t ldy, i
     const int32_t rc = check_combine(routing, n, dtype, &a);
     if (rc != NACHO_OK) return rc;
     const int64_t elem = value_bytes(dtype), slots = routing->lvl[1].extent, bytes = span(a.tokens, n, ldo, elem);
-    if (!matrix(y, slots, n, ldy, elem) || !matrix(out, a.tokens, n, ldo, elem) ||
-        overlap(y, span(slots, n, ldy, elem), out, bytes))
+    if (!matrix(y, slots, n, ldy, elem) || !matrix(out, a.tokens, n, ldo, elem) || (residual && !matrix(residual, a.tokens, n, ldr, elem)))
         return NACHO_ERR_INVALID_ARG;
-    if (residual && (!matrix(residual, a.tokens, n, ldr, elem) ||
-                     (!(residual == out && ldr == ldo) && overlap(residual, span(a.tokens, n, ldr, elem), out, bytes))))
+    const bool in_place = residual == out && ldr == ldo;
+    const int64_t stored = routing->lvl[1].count * 4;
+    if (!apart({{out, bytes}}, {{y, span(slots, n, ldy, elem)}, {in_place ? nullptr : residual, residual ? span(a.tokens, n, ldr, elem) : 0},
+                                {a.pos, a.tokens * 4 + 4}, {a.slot, stored}, {a.gate, stored}}))
         return NACHO_ERR_INVALID_ARG;
     a.y = y;
     a.ldy = ldy;
@@ -303,8 +343,12 @@ int32_t nacho_combine_grad(const nacho_tensor *routing, const void *y, int64_t l
     const int64_t elem = value_bytes(dtype), slots = routing->lvl[1].extent, bytes = span(slots, n, ldgy, elem);
     if (!aligned(grad_val, 4) || !matrix(grad_out, a.tokens, n, ldg, elem) || (grad_val && !matrix(y, slots, n, ldy, elem)))
         return NACHO_ERR_INVALID_ARG;
-    if (grad_y && (!matrix(grad_y, slots, n, ldgy, elem) || overlap(grad_out, span(a.tokens, n, ldg, elem), grad_y, bytes) ||
-                   (grad_val && overlap(y, span(slots, n, ldy, elem), grad_y, bytes))))
+    if (grad_y && !matrix(grad_y, slots, n, ldgy, elem)) return NACHO_ERR_INVALID_ARG;
+    const int64_t stored = routing->lvl[1].count * 4;
+    // (y is read for grad_val alone)
+    if (!apart({{grad_y, grad_y ? bytes : 0}, {grad_val, stored}},
+               {{grad_out, span(a.tokens, n, ldg, elem)}, {grad_val ? y : nullptr, grad_val ? span(slots, n, ldy, elem) : 0},
+                {a.pos, a.tokens * 4 + 4}, {a.slot, stored}, {a.gate, stored}}))
         return NACHO_ERR_INVALID_ARG;
     a.y = y;
     a.ldy = ldy;
@@ -336,13 +380,11 @@ int32_t nacho_experts(const nacho_experts_layer *layer, void *y, int64_t ldy, vo
     const int64_t elem = value_bytes(l.dtype), bytes = span(l.n_slots, l.outer, ldy, elem);
     if (!check_x(layer, elem) || !check_w(layer, elem) || !matrix(y, l.n_slots, l.outer, ldy, elem)) return NACHO_ERR_INVALID_ARG;
     if (l.bias && !matrices(l.bias, l.n_experts, 1, l.outer, l.outer, l.bias_stride, elem)) return NACHO_ERR_INVALID_ARG;
-    if (overlaps_inputs(layer, y, bytes, elem)) return NACHO_ERR_INVALID_ARG;
-    if (pre) {
-        const int64_t pre_bytes = span(l.n_slots, l.outer, ldpre, elem);
-        if (!matrix(pre, l.n_slots, l.outer, ldpre, elem) || overlaps_inputs(layer, pre, pre_bytes, elem) ||
-            overlap(y, bytes, pre, pre_bytes))
-            return NACHO_ERR_INVALID_ARG;
-    }
+    if (pre && !matrix(pre, l.n_slots, l.outer, ldpre, elem)) return NACHO_ERR_INVALID_ARG;
+    if (!apart({{y, bytes}, {pre, pre ? span(l.n_slots, l.outer, ldpre, elem) : 0}},
+               {x_of(layer, elem), w_of(layer, elem), bounds_of(layer), token_of(layer),
+                {l.bias, l.bias ? span(l.n_experts, 1, l.outer, l.outer, l.bias_stride, elem) : 0}}))
+        return NACHO_ERR_INVALID_ARG;
     const ProductArgs a{l.expert_pos, l.token, (int32_t)l.n_experts, 0, (int32_t)l.outer, (int32_t)l.inner, l.n_slots, l.x, l.w,
                         l.ldx, l.ldw, l.w_stride, y, ldy, 0, l.bias, l.bias_stride, pre, ldpre, l.act};
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -372,18 +414,12 @@ int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y,
         (grad_w && !matrices(grad_w, l.n_experts, l.outer, l.inner, ldgw, gw_stride, elem)) ||
         (grad_bias && !matrices(grad_bias, l.n_experts, 1, l.outer, l.outer, gb_stride, elem)))
         return NACHO_ERR_INVALID_ARG;
-    const void *outs[] = {grad_x, grad_w, grad_bias};
-    const int64_t sizes[] = {gx_bytes, gw_bytes, gb_bytes};
-    for (int i = 0; i < 3; ++i) {
-        if (overlaps_inputs(layer, outs[i], sizes[i], elem) || overlap(outs[i], sizes[i], grad_y, gy_bytes) ||
-            overlap(outs[i], sizes[i], pre, pre_bytes))
-            return NACHO_ERR_INVALID_ARG;
-        for (int j = 0; j < i; ++j)
-            if (overlap(outs[i], sizes[i], outs[j], sizes[j])) return NACHO_ERR_INVALID_ARG;
-    }
     const bool products = grad_x || grad_w;
     const GradWs w = carve_grad(ws, layer, slope && products, grad_bias != nullptr);
     if (w.bytes > 0 && (!ws || ws_bytes < w.bytes || !aligned(ws, 16))) return NACHO_ERR_WORKSPACE;
+    if (!apart({{grad_x, gx_bytes}, {grad_w, gw_bytes}, {grad_bias, gb_bytes}, {ws, (int64_t)w.bytes}},
+               {x_of(layer, elem), w_of(layer, elem), bounds_of(layer), token_of(layer), {grad_y, gy_bytes}, {pre, pre_bytes}}))
+        return NACHO_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     profile_begin(s);
     const void *gz = grad_y;

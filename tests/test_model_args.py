@@ -2,10 +2,11 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2604_17198_amd import binding as nb
 
-BAD, UNSUPPORTED, WORKSPACE = -1, -2, -3
+BAD, UNSUPPORTED, WORKSPACE, HIP = -1, -2, -3, -5
 A, B, D, E = 1 << 40, 2 << 40, 3 << 40, 4 << 40              # addresses far apart
 
 
@@ -137,3 +138,120 @@ def test_sizes_whose_products_pass_64_bits():
     wide = layer(n_experts=3, outer=(1 << 24) - 1, inner=64, ldw=far, w_stride=1 << 30)
     assert lib.nacho_experts(C.byref(wide), E, 1 << 24, None, 0, None) == BAD
     assert size(lib.nacho_route_workspace_bytes, (1 << 62) + 1, 64, 4)[0] == BAD
+
+
+# Arrays of a call as (address, bytes); every output of which is put over every other array in turn.
+def overlaps(arrays, outputs, call, allowed=()):
+    if not torch.cuda.is_available():                        # (where nothing can be launched: the arrays as they are pass)
+        assert call() == HIP
+    for out in outputs:
+        for other, (at, length) in arrays.items():
+            if other == out or (out, other) in allowed:
+                continue
+            for shift in (0, length - 4):                    # its first element there, or its first over the other's last
+                assert call(**{out: at + shift}) == BAD, (out, other, shift)
+
+
+def test_distill_outputs_over_other_arrays():
+    lib = nb.lib()
+    rows, cols, n = 4, 1 << 20, 10                           # (cut into parts: there is a workspace)
+    room = size(lib.nacho_distill_workspace_bytes, rows, cols, nb.F32)[1]
+    length = dict(pos=20, crd=40, val=40, logits=rows * cols * 4, weight=16, loss=16, lse=16, grad=rows * cols * 4, ws=room)
+    base = {name: (i + 1) << 40 for i, name in enumerate(length)}
+    arrays = {name: (base[name], length[name]) for name in length}
+
+    def call(**moved):
+        p = {**base, **moved}
+        return lib.nacho_distill(C.byref(teacher(rows, cols, n, p["pos"], p["crd"], p["val"])), p["logits"], cols, nb.F32, p["weight"], 1.0, p["loss"],
+                                 p["lse"], p["grad"], cols, p["ws"], room, None)
+
+    overlaps(arrays, ("loss", "lse", "grad"), call)
+    for name in ("crd", "val", "logits", "weight"):          # (a workspace starts at a multiple of 16 bytes)
+        assert call(ws=base[name]) == BAD, name
+
+    def back(**moved):
+        p = {**base, **moved}
+        return lib.nacho_distill_grad(C.byref(teacher(rows, cols, n, p["pos"], p["crd"], p["val"])), p["logits"], cols, nb.F32, p["weight"], 1.0,
+                                      p["lse"], p["grad"], cols, None)
+
+    overlaps({k: v for k, v in arrays.items() if k not in ("loss", "ws")}, ("grad",), back)
+
+
+def test_route_outputs_over_other_arrays():
+    lib = nb.lib()
+    tokens, experts, k = 100, 16, 2
+    room = size(lib.nacho_route_workspace_bytes, tokens, experts, k)[1]
+    names = [n for n, _ in nb._Routing._fields_]
+    length = dict(pos=404, expert=800, gate=800, slot=800, expert_pos=68, token=800, counts=64, lse=400, balance=4, routed=4,
+                  logits=tokens * experts * 4, keep=tokens, ws=room)
+    base = {name: (i + 1) << 40 for i, name in enumerate(length)}
+    arrays = {name: (base[name], length[name]) for name in length}
+
+    def call(**moved):
+        p = {**base, **moved}
+        return lib.nacho_route(p["logits"], experts, tokens, experts, nb.F32, k, 0, p["keep"], C.byref(nb._Routing(*[p[n] for n in names])), p["ws"], room, None)
+
+    overlaps(arrays, names, call)
+    for name in names + ["logits", "keep"]:
+        assert call(ws=base[name]) == BAD, name
+    length.update(grad=tokens * experts * 4, grad_gate=800)
+    del length["ws"], length["keep"]
+    base = {name: (i + 1) << 40 for i, name in enumerate(length)}
+
+    def back(**moved):
+        p = {**base, **moved}
+        return lib.nacho_route_grad(p["logits"], experts, tokens, experts, nb.F32, k, 0, C.byref(nb._Routing(*[p[n] for n in names])), p["grad_gate"], 0.1,
+                                    p["grad"], experts, None)
+
+    overlaps({name: (base[name], length[name]) for name in length}, ("grad",), back)
+
+
+def test_experts_outputs_over_other_arrays():
+    lib = nb.lib()
+    size_of = dict(expert_pos=16, token=200, x=20 * 64 * 4, w=3 * 96 * 64 * 4, bias=3 * 96 * 4, y=50 * 96 * 4, pre=50 * 96 * 4)
+    base = {name: (i + 1) << 40 for i, name in enumerate(size_of)}
+
+    def of(p, **more):
+        return layer(expert_pos=p["expert_pos"], token=p["token"], x=p["x"], w=p["w"], bias=p.get("bias"), bias_stride=96, **more)
+
+    def call(**moved):
+        p = {**base, **moved}
+        return lib.nacho_experts(C.byref(of(p)), p["y"], 96, p["pre"], 96, None)
+
+    overlaps({n: (base[n], size_of[n]) for n in size_of}, ("y", "pre"), call)
+    room = size(lib.nacho_experts_workspace_bytes, C.byref(layer(act=2)))[1]
+    del size_of["bias"], size_of["y"]
+    size_of.update(grad_y=50 * 96 * 4, grad_x=50 * 64 * 4, grad_w=3 * 96 * 64 * 4, grad_bias=3 * 96 * 4, ws=room)
+    base = {name: (i + 1) << 40 for i, name in enumerate(size_of)}
+
+    def back(**moved):
+        p = {**base, **moved}
+        return lib.nacho_experts_grad(C.byref(of(p, act=2)), p["grad_y"], 96, p["pre"], 96, p["grad_x"], 64, p["grad_w"], 64, 96 * 64, p["grad_bias"], 96,
+                                      p["ws"], room, None)
+
+    overlaps({n: (base[n], size_of[n]) for n in size_of}, ("grad_x", "grad_w", "grad_bias"), back)
+    for name in size_of:
+        if name != "ws":
+            assert back(ws=base[name]) == BAD, name
+
+
+def test_combine_outputs_over_other_arrays():
+    lib = nb.lib()
+    length = dict(pos=24, slot=48, gate=48, y=12 * 32 * 4, residual=5 * 32 * 4, out=5 * 32 * 4)
+    base = {name: (i + 1) << 40 for i, name in enumerate(length)}
+
+    def call(**moved):
+        p = {**base, **moved}
+        return lib.nacho_combine(C.byref(teacher(5, 12, 12, p["pos"], p["slot"], p["gate"])), p["y"], 32, 32, nb.F32, p["residual"], 32, p["out"], 32, None)
+
+    overlaps({n: (base[n], length[n]) for n in length}, ("out",), call, allowed=(("out", "residual"),))
+    assert call(out=base["residual"] + 128) == BAD           # (in place is the residual itself alone)
+    length = dict(pos=24, slot=48, gate=48, y=12 * 32 * 4, grad_out=5 * 32 * 4, grad_y=12 * 32 * 4, grad_val=48)
+    base = {name: (i + 1) << 40 for i, name in enumerate(length)}
+
+    def back(**moved):
+        p = {**base, **moved}
+        return lib.nacho_combine_grad(C.byref(teacher(5, 12, 12, p["pos"], p["slot"], p["gate"])), p["y"], 32, 32, nb.F32, p["grad_out"], 32, p["grad_y"], 32,
+                                      p["grad_val"], None)
+
+    overlaps({n: (base[n], length[n]) for n in length}, ("grad_y", "grad_val"), back)
