@@ -113,7 +113,8 @@ int32_t check_distill(const nacho_tensor *teacher, const void *logits, int64_t l
     if (rows < 0 || rows > kMostRows || cols < 0 || cols > kMostRows || stored < 0 || stored > kMostRows)
         return NACHO_ERR_INVALID_ARG;
     if (!teacher->lvl[1].pos || (stored > 0 && (!teacher->lvl[1].crd || !teacher->val))) return NACHO_ERR_INVALID_ARG;
-    if (!aligned(teacher->lvl[1].crd, 16) || !aligned(teacher->val, 16)) return NACHO_ERR_INVALID_ARG;
+    if (!aligned(teacher->lvl[1].pos, 4) || !aligned(teacher->lvl[1].crd, 16) || !aligned(teacher->val, 16) || !aligned(weight, 4))
+        return NACHO_ERR_INVALID_ARG;
     const int64_t elem = value_bytes(dtype);
     if (!matrix(logits, rows, cols, ldl, elem) || !(temperature >= 1e-30f && temperature <= 1e18f)) return NACHO_ERR_INVALID_ARG;
     if (grad && !matrix(grad, rows, cols, ldg, elem)) return NACHO_ERR_INVALID_ARG;
@@ -215,7 +216,7 @@ int32_t nacho_distill(const nacho_tensor *teacher, const void *logits, int64_t l
     DistillArgs a;
     const int32_t rc = check_distill(teacher, logits, ldl, dtype, weight, temperature, grad, ldg, &a);
     if (rc != NACHO_OK) return rc;
-    if (a.rows > 0 && (!loss || !lse)) return NACHO_ERR_INVALID_ARG;
+    if ((a.rows > 0 && (!loss || !lse)) || !aligned(loss, 4) || !aligned(lse, 4)) return NACHO_ERR_INVALID_ARG;
     const size_t need = align_up((size_t)distill_partials(dtype, a.rows, a.cols, grad != nullptr) * sizeof(float), 256);
     if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16))) return NACHO_ERR_WORKSPACE;
     if (!check_distill_arrays(teacher, a, value_bytes(dtype), nullptr, loss, lse, ws, (int64_t)need)) return NACHO_ERR_INVALID_ARG;
@@ -244,7 +245,7 @@ int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int6
     DistillArgs a;
     const int32_t rc = check_distill(teacher, logits, ldl, dtype, weight, temperature, grad, ldg, &a);
     if (rc != NACHO_OK) return rc;
-    if (a.rows > 0 && a.cols > 0 && (!lse || !grad)) return NACHO_ERR_INVALID_ARG;
+    if ((a.rows > 0 && a.cols > 0 && (!lse || !grad)) || !aligned(lse, 4)) return NACHO_ERR_INVALID_ARG;
     if (!check_distill_arrays(teacher, a, value_bytes(dtype), lse, nullptr, nullptr, nullptr, 0)) return NACHO_ERR_INVALID_ARG;
     a.lse_in = lse;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);

@@ -255,3 +255,18 @@ def test_combine_outputs_over_other_arrays():
                                       p["grad_val"], None)
 
     overlaps({n: (base[n], length[n]) for n in length}, ("grad_y", "grad_val"), back)
+
+
+def test_distill_arrays_between_elements():
+    """Positions, weights, losses and lse that start between two elements."""
+    lib = nb.lib()
+
+    def call(pos=A, weight=D, loss=E, lse=E + 4096):
+        return lib.nacho_distill(C.byref(teacher(pos=pos)), B, 100, nb.F32, weight, 1.0, loss, lse, None, 0, None, 0, None)
+
+    def back(pos=A, weight=D, lse=E):
+        return lib.nacho_distill_grad(C.byref(teacher(pos=pos)), B, 100, nb.F32, weight, 1.0, lse, E + (1 << 30), 100, None)
+
+    for f in (call, back):
+        assert f(pos=A + 2) == BAD and f(weight=D + 1) == BAD and f(lse=E + 4098) == BAD
+    assert call(loss=E + 2) == BAD
