@@ -144,3 +144,26 @@ def test_refusals():
         nb.nacho_combine(pos, slot, y, residual=y[2:4], out=y[3:5])
     with pytest.raises(nb.NachoError):
         nb.nacho_combine_grad(pos, slot, y, torch.ones((2, 16), device="cuda"), grad_y=y)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("words", [8, 9, 16, 17, 32, 33, 128, 129])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_rows_on_both_sides_of_every_number_of_lanes(words, odd, dtype):
+    """Rows of these numbers of words of 16 bytes, whole or with a last one that is not."""
+    rng = np.random.default_rng(words)
+    cols, tokens, most = words * (16 // torch.empty(0, dtype=dtype).element_size()) - odd, 37, 5
+    pos, slot, gate = routing(rng, tokens, most)
+    y, residual, go = (rows_of(rng, n, cols, cols, dtype) for n in (len(slot), tokens, tokens))
+    token = np.repeat(np.arange(tokens), np.diff(pos))
+    y64, r64, go64 = (t.float().cpu().numpy().astype(np.float64) for t in (y, residual, go))
+    want, size = r64.copy(), np.abs(r64)
+    np.add.at(want, token, y64[slot] * gate[:, None])
+    np.add.at(size, token, np.abs(y64[slot] * gate[:, None]))
+    assert near(nb.nacho_combine(dev(pos), dev(slot), y, gate=dev(gate), residual=residual), want, size, dtype, most + 1)
+    grad_y, grad_gate = nb.nacho_combine_grad(dev(pos), dev(slot), y, go, gate=dev(gate))
+    want_y = np.empty((len(slot), cols))
+    want_y[slot] = go64[token] * gate[:, None]
+    assert near(grad_y, want_y, np.abs(want_y), dtype, 1)
+    dots = go64[token] * y64[slot]
+    assert near(grad_gate, dots.sum(1), np.abs(dots).sum(1), torch.float32, cols)

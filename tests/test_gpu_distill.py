@@ -309,3 +309,33 @@ def test_temperatures_whose_square_is_no_number_are_refused():
             nb.nacho_distill(T, z, temperature=tau)
         with pytest.raises(nb.NachoError):
             nb.nacho_distill_grad(T, z, lse, temperature=tau)
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(130, 128_256, torch.bfloat16), (130, 128_256, torch.float16), (130, 60_001, torch.float32),
+                                             (130, 100_001, torch.bfloat16), (5, 131_072, torch.bfloat16), (4, 200_003, torch.float16),
+                                             (3, 131_080, torch.float32), (6, 65_536, torch.bfloat16), (5, 16_391, torch.float32),
+                                             (40, 2049, torch.float16), (70, 509, torch.bfloat16)], ids=str)
+@pytest.mark.parametrize("ld", [0, 3])
+def test_every_column_of_a_gradient(rows, cols, dtype, ld):
+    """A column's gradient w tau (q - p) next to its own q and p, however small.  Arguments of exponentials are up to 2^6 and have
+    a rounding of 2^-24 of that; Z is a sum of positive numbers, at most 2^9 additions deep: both are within 4e-5 of themselves, and
+    results are rounded once (weights are such that 16-bit types hold the smallest ones: half of an f16's smallest step is 2^-25)."""
+    rng = np.random.default_rng(rows + cols + ld)
+    tau = 1.25
+    pos, crd, val, z, weight = case(rng, rows, cols, 0, 60, dtype, 0.1, ld=cols + ld)
+    weight = (weight * 8192).astype(np.float32)
+    T, w = operand(pos, crd, val, rows, cols), torch.from_numpy(weight).cuda()
+    grad = torch.full_like(z, float("nan"))
+    _, lse = nb.nacho_distill(T, z, temperature=tau, weight=w, grad=grad)
+    both = (grad, nb.nacho_distill_grad(T, z, lse, temperature=tau, weight=w))
+    for i in range(rows):
+        j, u = crd[pos[i]:pos[i + 1]], val[pos[i]:pos[i + 1]].astype(np.float64) / tau
+        t, p = z[i].float().cpu().numpy().astype(np.float64) / tau, np.zeros(cols)
+        q = np.exp(t - t.max())
+        q /= q.sum()
+        if len(j):
+            p[j] = np.exp(u - u.max()) / np.exp(u - u.max()).sum()
+        scale = float(weight[i]) * tau * (len(j) > 0)
+        want, room = scale * (q - p), scale * 4e-5 * (q + p) + 1e-37 + 2.0 ** -25 * (dtype is torch.float16)
+        for g in both:
+            assert np.all(np.abs(g[i].float().cpu().numpy().astype(np.float64) - want) <= STEP[dtype] * np.abs(want) + room), i

@@ -325,3 +325,18 @@ def test_slots_up_to_the_last_of_two_to_the_31():
     y.fill_(1.0)
     gx, _ = nb.nacho_experts_grad(y, x, w, bounds, act="relu", pre=x, grad_weight=False)
     assert bool((gx[:5] == 3).all()) and gx[-2].item() == 0 and gx[-1].item() == 7 and bool((gx[5:-2] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("counts,inner,outer", [([520, 700], 16392, 264), ([577, 1100, 0], 16640, 264), ([520, 700], 16391, 263)])
+def test_the_largest_tiles_on_the_way_back(counts, inner, outer, dtype):
+    """512 slots an expert and more, and enough columns, for the largest tiles of each type in both gradients: whole steps of the
+    sum, even and odd numbers of them, and what is left of one; rows and columns that end inside a tile; an expert without a slot."""
+    check(problem(22, counts, 300, inner, outer, dtype, True), "gelu", dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_many_experts_of_some_hundred_slots(dtype):
+    """Fewer slots an expert than the largest tiles are for, and enough of all for tiles of 128 x 128 in all three products."""
+    counts = np.random.default_rng(23).integers(150, 450, 16).tolist()
+    check(problem(23, counts, 700, 2064, 2056, dtype, True), "relu", dtype)

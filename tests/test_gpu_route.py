@@ -242,3 +242,35 @@ def test_refusals():
         nb.nacho_route_grad(z, r, grad=z)
     with pytest.raises(ValueError):
         nb.nacho_route_grad(z, r, torch.ones(7, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("tokens,experts,top_k", [(140_000, 6, 2), (40_000, 120, 5)])
+def test_gradients_of_many_tokens(tokens, experts, top_k, dtype):
+    """More tokens than the gradient's workgroups take in one go each.  (Gates are normalised: the sum enters at the entries.)"""
+    rng = np.random.default_rng(tokens)
+    z = logits_of(rng, tokens, experts, dtype, 0.2)
+    keep = rng.random(tokens) < 0.9
+    grad_gate = rng.normal(0, 1, tokens * top_k).astype(np.float32)
+    want = definition(z.float().cpu().numpy(), top_k, True, keep, grad_gate, 0.5)
+    r = nb.nacho_route(z, top_k, normalise=True, keep=torch.from_numpy(keep).cuda())
+    compare(r, want, tokens, top_k)
+    # the sum over a token's entries, gate times gradient, is off by a share of its terms, not of what they leave
+    row, entries = np.repeat(np.arange(tokens), np.diff(want["pos"])), len(want["expert"])
+    terms = np.bincount(row, weights=want["gate"] * np.abs(grad_gate[:entries]), minlength=tokens)
+    want["size"][row, want["expert"]] += want["gate"] * terms[row]
+    compare_grad(nb.nacho_route_grad(z, r, torch.from_numpy(grad_gate).cuda(), balance=0.5), want, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("tokens,experts,top_k", [(50, 100, 6), (300, 300, 7), (130, 500, 32), (200, 1000, 9), (64, 129, 3)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_wide_rows_in_one_workgroup_and_in_several(tokens, experts, top_k, masked, dtype):
+    """Every number of lanes a token, for tokens of one workgroup and of more."""
+    rng = np.random.default_rng(tokens + experts)
+    z = logits_of(rng, tokens, experts, dtype, 0.3 if masked else 0.0)
+    keep = rng.random(tokens) < (0.8 if masked else 2.0)
+    r = nb.nacho_route(z, top_k, keep=torch.from_numpy(keep).cuda())
+    want = definition(z.float().cpu().numpy(), top_k, False, keep, None, 0.5)
+    compare(r, want, tokens, top_k)
+    compare_grad(nb.nacho_route_grad(z, r, balance=0.5), want, dtype)
