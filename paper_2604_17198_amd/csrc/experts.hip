@@ -846,14 +846,21 @@ hipError_t run(const ProductArgs &a, hipStream_t s)
 constexpr int64_t kUnits = 256;        // compute units
 
 // Tiles of 256 x 256 need half the LDS reads of tiles of 128 x 128 for the same results, but leave more of a tile empty
-// and fill the chip only if there are many of them.  16384 slots bf16, us: 16 experts (1024 slots each), 2048 x 8192, forward
-// 566 and 900, rows 616 and 749, weights 662 and 793; 32 experts (512 each), 1024 x 4096, 205 and 209, 219 and 241, 227 and 309.
+// and fill the chip only if there are many of them.  16384 slots bf16, us with 256 and with 128, in equal groups and in groups
+// whose sizes are as 0.6 of a normal logarithm (in brackets): 64 experts (256 slots each), 1024 x 4096, forward 185 and 215 (227
+// and 256), rows 151 and 192 (233 and 233), 2048 x 8192 670 and 779 (813 and 896), 543 and 689 (715 and 867); 128 experts (128
+// each), 1024 x 4096, 305 and 269 (340 and 312), 236 and 228 (343 and 266).  The weights' product, whatever the slots: 16 to 128
+// experts 165 and 200 to 393 and 502 (179 and 202, 476 and 540); with fewer tiles than compute units (2 experts, 8192 slots) 117
+// and 82.
 // Tiles of 32 x 128 for few slots an expert, where the weights are what is read, and where larger ones would leave compute
-// units without one: 16 slots of 32 experts, 2048 x 4096, forward 26 (128 x 128: 37), rows 37 (47); 1200 of 24, 1024 x 4096, 36
-// (43), 41 (50).  Their steps are of 256 bytes: 8 tokens, 2 of 32 experts, 49 us a call, with 128 bytes 53.
+// units without one.  1024 x 4096 bf16, us with 32 and with 128: 32 experts of 32 slots forward 46 and 49 (59 and 50), of 48 58
+// and 51 (71 and 68); rows, for the number of larger tiles, 8 experts of 192 slots (96 tiles) 38 and 52 (39 and 52), 32 of 64 (128)
+// 59 and 64 (92 and 69), 32 of 96 (192) 87 and 72 (96 and 75).  Rows that start anywhere gain more: 1023 x 4097, 32 experts of 48
+// forward 0.91 of the time (0.92), of 64 0.94 (1.07), of 96 1.17 (1.24).  Their steps are of 256 bytes: 8 tokens, 2 of 32 experts,
+// 49 us a call, with 128 bytes 53.
 // Floats need four times as many matrix instructions for what is loaded: tiles of 64 x 64, which are as many again.  3000 slots
 // of 7 experts, 777 x 499, us: weights 73 (64 x 128: 95), forward 42 (32 x 128: 45), rows 44 (50); with two steps on their way
-// in registers 54, 43 and 42.
+// in registers 54, 43 and 42.  512 x 2048, 32 experts of 64 and 128 slots, us with 32, 64 and 128: rows 51, 52 and 141, 87, 81 and 149.
 template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, Access access, hipStream_t s)
 {
     const int64_t each = a.slots / a.experts, n128 = (a.n + 127) / 128;
@@ -869,10 +876,11 @@ template <typename T, Form kForm> hipError_t by_size(const ProductArgs &a, Acces
         return words ? run<T, kForm, 128, 128, 2, 2, WORDS>(a, s) : run<T, kForm, 128, 128, 2, 2, ANYWHERE>(a, s);
     } else {
         if constexpr (sizeof(T) == 2) {
-            if (words && each >= 512 && a.n >= 256 && a.slots / 256 * ((a.n + 255) / 256) >= kUnits)
+            if (words && each >= 256 && a.n >= 256 && a.slots / 256 * ((a.n + 255) / 256) >= kUnits)
                 return run<T, kForm, 256, 256, 2, 4, WORDS>(a, s);
         }
-        const bool small = each <= 64 || a.slots / 128 * n128 < 2 * kUnits;
+        const int64_t few = words && sizeof(T) == 2 ? 32 : 64, most = sizeof(T) == 2 ? kUnits / 2 : 2 * kUnits - 1;
+        const bool small = each <= few || a.slots / 128 * n128 <= most;
         if constexpr (sizeof(T) == 4) {
             if (small && each > 64) return words ? run<T, kForm, 64, 64, 2, 2, WORDS>(a, s) : run<T, kForm, 64, 64, 2, 2, ANYWHERE>(a, s);
         }
