@@ -324,8 +324,8 @@ template <typename T, int kRows, int kStep, int kThreads, Access kAccess, int kS
         rows[set.value] = k - k0 - row_of_load(0);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int past = k - 1 - k0;
-            const T *from = address(i, k0 + (row_of_load(i) < past ? row_of_load(i) : past));
+            const unsigned kk = (unsigned)k0 + row_of_load(i);
+            const T *from = address(i, kk < (unsigned)k ? (int)kk : k - 1);
             if constexpr (kAccess == WORDS) word[set.value][i] = *reinterpret_cast<const v4u *>(from + (first < length ? first : length - n));
             else word[set.value][i] = last.load(from + first);
         }
@@ -434,8 +434,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
         k_begin = bound_of(a, expert);
         k = bound_of(a, expert + 1) - k_begin;
     } else if (!find_tile<kM>(a, tile, expert, m0, m_end) || n0 >= a.n) return;
-    // (sums of rows, or of steps of k, and what a tile has may pass 31 bits behind the last one: what is left is compared)
-    const int m_rows = m_end - m0;
+    // (sums of a row, or a step of k, and what a tile has may pass 31 bits behind the last one: compared in 32)
     const T *const q = static_cast<const T *>(a.q);
     const T *const p = static_cast<const T *>(a.p) + (int64_t)expert * a.p_stride;
     SideQ side_q;
@@ -443,7 +442,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
     // rows behind the last: the last one again, whose results are not stored
     if constexpr (!kAcrossQ)
         side_q.start(q, a.ldq, [&](int r) {
-            const int row = m0 + (r < m_rows ? r : m_rows - 1);
+            const int row = (unsigned)m0 + r < (unsigned)m_end ? m0 + r : m_end - 1;
             return kForm == FORWARD && a.token ? a.token[row] : row;
         });
     if constexpr (!kAcrossP) side_p.start(p, a.ldp, [&](int r) { return n0 + r < a.n ? n0 + r : a.n - 1; });
@@ -454,8 +453,8 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
         if constexpr (kForm == WEIGHTS) {
 #pragma unroll
             for (int l = 0; l < SideP::kLoads; ++l) {
-                const int past = k - 1 - k0;
-                slot[l] = k_begin + k0 + (SideP::row_of_load(l) < past ? SideP::row_of_load(l) : past);
+                const unsigned kk = (unsigned)k0 + SideP::row_of_load(l);
+                slot[l] = k_begin + (kk < (unsigned)k ? (int)kk : k - 1);
             }
             if constexpr (kAccess != WORDS) {
                 // (without a branch, see Ragged)
@@ -480,7 +479,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
     };
     const int wave = (int)threadIdx.x / NACHO_WAVE, lane = lane_id();
     const int wm = wave / kWavesN * kTileM, wn = wave % kWavesN * kTileN;
-    const bool busy = __builtin_amdgcn_readfirstlane(wm < m_rows && n0 + wn < a.n ? 1 : 0) != 0;
+    const bool busy = __builtin_amdgcn_readfirstlane((unsigned)m0 + wm < (unsigned)m_end && n0 + wn < a.n ? 1 : 0) != 0;
     v4f acc[kFragM][kFragN];
 #pragma unroll
     for (int i = 0; i < kFragM; ++i)
@@ -688,8 +687,8 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
         wave_sync();
 #pragma unroll 1
         for (int r = lane / kLanes; r < kPhase * 16; r += NACHO_WAVE / kLanes) {
-            const int own = wm + i0 * 16 + r, m = m0 + own;
-            if (own >= m_rows || width <= 0) break;
+            const unsigned m = (unsigned)m0 + wm + i0 * 16 + r;
+            if (m >= (unsigned)m_end || width <= 0) break;
             float v[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -723,7 +722,6 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
     const int tx = (int)threadIdx.x % 16, ty = (int)threadIdx.x / 16, c0 = (number - tile * tiles_n) * 16 * n, c = c0 + tx * n, width = a.cols - c;
     int expert, row, end;
     if (!find_tile<kSlopeRows>(a, tile, expert, row, end)) return;
-    const int rows = end - row;
     const T *gy = static_cast<const T *>(a.grad_y) + c, *pre = static_cast<const T *>(a.pre) + c;
     T *gz = static_cast<T *>(a.grad_z) + c;
     auto get = [&](const T *from) {
@@ -740,16 +738,16 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
     v4u g[kRows], z[kRows];
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-        const int m = row + ty + i * 16;
+        const unsigned m = (unsigned)row + ty + i * 16;
         g[i] = z[i] = v4u{0, 0, 0, 0};
-        if (ty + i * 16 < rows) {
+        if (m < (unsigned)end) {
             g[i] = get(gy + (int64_t)m * a.ldgy);
             if (a.act != NACHO_ACT_NONE) z[i] = get(pre + (int64_t)m * a.ldpre);
         }
     }
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-        const int m = row + ty + i * 16;
+        const unsigned m = (unsigned)row + ty + i * 16;
         word v = __builtin_bit_cast(word, g[i]);
         // (what the sums take is not rounded to the type yet; behind the last row it is zero)
         if (a.act != NACHO_ACT_NONE) {
@@ -764,7 +762,7 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
 #pragma unroll
             for (int e = 0; e < n; ++e) sum[e] += wide((T)v[e]);
         }
-        if (ty + i * 16 < rows && a.grad_z) {
+        if (m < (unsigned)end && a.grad_z) {
             T *to = gz + (int64_t)m * a.ldgz;
             if (width >= n) {
                 if constexpr (kAccess == WORDS) *reinterpret_cast<word *>(to) = v;
