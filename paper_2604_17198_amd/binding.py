@@ -519,10 +519,7 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _on_gpu(t, what):
-    """The call's first array: on the GPU whose stream the kernels go to (all others have to be where it is)."""
-    if not t.is_cuda or t.get_device() != _current_device():
-        raise ValueError(f"{what}: on {t.device}, and not on the current GPU")
+_HOST = -1                                                   # the number of the device of tensors that are on no GPU
 
 
 def _matrix(t, what, rows=None, cols=None, dtype=None, device=None):
@@ -537,7 +534,9 @@ def _matrix(t, what, rows=None, cols=None, dtype=None, device=None):
     if (rows is not None and r != rows) or (cols is not None and c != cols):
         raise ValueError(f"{what}: {r} x {c}, expected {rows} x {cols}")
     if device is None:
-        _on_gpu(t, what)
+        number = t.get_device()
+        if number == _HOST or number != _current_device():
+            raise ValueError(f"{what}: on {t.device}, and not on the current GPU")
     elif t.dtype is not dtype or t.device != device:
         raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype} on {device}")
     return ld if r > 1 else (ld if ld > c else c)
@@ -551,9 +550,7 @@ def _vector_of(t, what, n, dtype, device):
 
 
 def _room(ws, device):
-    """The bytes of a workspace."""
-    if ws is None:
-        return 0
+    """The bytes of a workspace that the caller brings."""
     if ws.device != device or not ws.is_contiguous():
         raise ValueError(f"ws: contiguous memory on {device} is needed")
     return ws.numel()
@@ -567,8 +564,9 @@ def _floats(n, device):
 def _check_teacher(teacher, logits, weight):
     if teacher.nlevels != 2 or teacher.c.lvl[0].kind != DENSE or teacher.c.lvl[1].kind != COMPRESSED:
         raise NachoError(-2, "teacher: a CSR operand is needed")
-    _need(teacher.val is not None, "teacher: values are needed")
-    _vector_of(teacher.val, "teacher's values", teacher.nnz, torch.float32, logits.device)
+    val = teacher.val                                        # (an operand's arrays are contiguous and on one device)
+    if val is None or val.numel() != teacher.nnz or val.dtype is not torch.float32 or val.device != logits.device:
+        raise ValueError(f"teacher: {teacher.nnz} values of torch.float32 on {logits.device} are needed")
     rows, cols = teacher.c.lvl[0].extent, teacher.c.lvl[1].extent
     _need(teacher.keep[0].numel() == rows + 1, "teacher: rows + 1 positions are needed")
     ld = _matrix(logits, "logits", rows, cols)
@@ -588,9 +586,12 @@ def nacho_distill(teacher: Operand, logits, temperature=1.0, weight=None, grad=N
     if ws is None:
         n = C.c_size_t(0)
         _check(lib().nacho_distill_workspace_bytes(rows, cols, dt, C.byref(n)), "nacho_distill_workspace_bytes")
-        ws = _workspace(n.value, dev) if n.value else None
+        room = n.value
+        ws = _workspace(room, dev) if room else None
+    else:
+        room = _room(ws, dev)
     _check(lib().nacho_distill(_pack([teacher]), _ptr(logits), ld, dt, _ptr(weight), temperature, _ptr(loss), _ptr(lse),
-                               _ptr(grad), ldg, _ptr(ws), _room(ws, dev), _stream()), "nacho_distill")
+                               _ptr(grad), ldg, _ptr(ws), room, _stream()), "nacho_distill")
     return loss, lse
 
 
@@ -652,9 +653,12 @@ def nacho_route(logits, top_k, normalise=False, keep=None, out=None, ws=None):
     if ws is None:
         n = C.c_size_t(0)
         _check(lib().nacho_route_workspace_bytes(tokens, experts, top_k, C.byref(n)), "nacho_route_workspace_bytes")
-        ws = _workspace(n.value, dev)
+        room = n.value
+        ws = _workspace(room, dev)
+    else:
+        room = _room(ws, dev)
     _check(lib().nacho_route(_ptr(logits), ld, tokens, experts, dt, top_k, out.normalise, _ptr(keep), C.byref(out.c),
-                             _ptr(ws), _room(ws, dev), _stream()), "nacho_route")
+                             _ptr(ws), room, _stream()), "nacho_route")
     return out
 
 
@@ -755,9 +759,12 @@ def nacho_experts_grad(grad_y, x, weight, expert_pos, token=None, act="none", pr
     if ws is None:
         n = C.c_size_t(0)
         _check(lib().nacho_experts_workspace_bytes(C.byref(c), C.byref(n)), "nacho_experts_workspace_bytes")
-        ws = _workspace(n.value, dev) if n.value else None
+        room = n.value
+        ws = _workspace(room, dev) if room else None
+    else:
+        room = _room(ws, dev)
     _check(lib().nacho_experts_grad(C.byref(c), _ptr(grad_y), ldgy, _ptr(pre), ldpre, _ptr(grad_x), ldgx, _ptr(grad_weight),
-                                    ldgw, gap, _ptr(grad_bias), gb, _ptr(ws), _room(ws, dev), _stream()),
+                                    ldgw, gap, _ptr(grad_bias), gb, _ptr(ws), room, _stream()),
            "nacho_experts_grad")
     return grad_x, grad_weight
 

@@ -24,7 +24,8 @@ def calls(monkeypatch):
 
     monkeypatch.setattr(nb, "lib", lambda: Library())
     monkeypatch.setattr(nb, "_stream", lambda: 0)
-    monkeypatch.setattr(nb, "_on_gpu", lambda t, what: None)
+    monkeypatch.setattr(nb, "_HOST", None)
+    monkeypatch.setattr(nb, "_current_device", lambda: -1)
     return made
 
 
