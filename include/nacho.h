@@ -551,7 +551,8 @@ int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y,
  *   grad_y[crd_i] = val_i grad_out[t]        (NULL: not wanted; slots of no entry
  *                                             are not written; no slot may be in two)
  *   grad_val[i]   = sum_c grad_out[t, c] y[crd_i, c]   (float, NULL: not wanted,
- *                                             then y may be NULL)
+ *                                             then y may be NULL; places behind the
+ *                                             last entry are not written)
  */
 int32_t nacho_combine(const nacho_tensor *routing, const void *y, int64_t ldy, int64_t n, int32_t dtype,
                       const void *residual, int64_t ldr, void *out, int64_t ldo, void *hip_stream);

@@ -5,8 +5,8 @@
 // rows are short, else a workgroup), a lane words of 16 bytes; it keeps its columns of the token's row in registers while it
 // goes over the entries, four at a time: their slots first, then the rows, so that four rows are on their way at once.  Rows
 // that start anywhere are read and written in words too (global memory takes any alignment).  16384 x 4 x 4096 bf16: sums
-// 155 us, gradients 244, 5.1 TB/s (a row asked for before the next one's slot is known: 160 and 250); 16384 x 4 x 4095 168 and
-// 266 (with a branch around each load 184 and 291).
+// 156 to 163 us, gradients 215, 5.2 TB/s (a row asked for before the next one's slot is known: 160 and 250 where it measured 155
+// and 244); 16384 x 4 x 4095 168 and 266 (with a branch around each load 184 and 291).
 #include "kernels.hpp"
 #include "model.hpp"
 

@@ -78,10 +78,9 @@ template <int kThreads, int N, typename... Ops> __device__ inline void group_all
     (joined(ops), ...);
 }
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kInfinity = __builtin_inff();
+constexpr float kLog2e = 1.4426950408889634f, kInfinity = __builtin_inff();
 
-// 2^x (results below the smallest normal number are zero) and log2 of a normal number, one instruction each.
+// 2^x in one instruction (results below the smallest normal number are zero).
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 }  // namespace nacho

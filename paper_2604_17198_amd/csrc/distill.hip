@@ -13,7 +13,7 @@
 // are cut into parts: one launch leaves every part's maximum and sum (STATS), the next one joins them and writes its part of
 // the gradient (APPLY).  The backward call knows the row's sum (GIVEN) and is cut likewise.
 // 4096 x 65536 bf16 with gradients 229 us, 4.7 TB/s (logits read twice: 344); 4 x 131072 floats 4 + 5 us in two launches (a
-// workgroup a row: 65 a call); 1021 x 100003 f16 statistics 34 to 39 us, join 9, gradients from the sums 65 to 76.
+// workgroup a row: 65 a call); 1021 x 100003 f16 statistics 39 us, join 9, gradients from the sums 73 to 75.
 #include "kernels.hpp"
 #include "model.hpp"
 
@@ -244,6 +244,7 @@ template <typename T> hipError_t forward(const DistillArgs &a, hipStream_t s)
     if (words <= 256 * 8) return run<T, 256, 8, 0, WHOLE>(a, part, 1, s);
     if (words <= 512 * 8) return run<T, 512, 8, 0, WHOLE>(a, part, 1, s);
     if (words <= 512 * 16) return run<T, 512, 16, 0, WHOLE>(a, part, 1, s);
+    // (9 words a thread in LDS, 74 KB, are the most that leave a compute unit two workgroups)
     if (words <= 512 * 25) return run<T, 512, 16, 9, WHOLE>(a, part, 1, s);
     return run<T, 512, 16, 16, WHOLE>(a, part, 1, s);
 }

@@ -12,9 +12,9 @@
 // Which expert a tile belongs to is found by its workgroup from expert_pos alone (a prefix sum of the experts' tiles
 // over the lanes), so nothing about the routing is read on the host.
 //
-// Bound by the matrix units for many slots an expert (16384 bf16 slots of 16 experts, 2048 x 8192: 622 us a call, 885 TFLOP/s
-// of the 1211 of a library's product of 8192^3), by the weights for few (16 of 32 experts, 2048 x 4096: 47 to 58 us a call for
-// 213 MB; 31 us a kernel where the last cache still has most of them).
+// Bound by the matrix units for many slots an expert (16384 bf16 slots of 16 experts, 2048 x 8192: 612 to 657 us a call by the
+// card, 837 to 898 TFLOP/s of the 1211 of a library's product of 8192^3), by the weights for few (16 of 32 experts, 2048 x 4096:
+// 44 to 55 us a call for 213 MB; 32 us a kernel where the last cache still has most of them).
 #include "kernels.hpp"
 #include "model.hpp"
 
@@ -48,10 +48,10 @@ template <typename T> __device__ inline v4f matrix_step(v4u p, v4u q, v4f acc)
 }
 
 // Activations and their slopes.  Rows of floats take the library's functions, and slopes in 64 bits: next to its root a
-// slope is a difference of nearly equal numbers.  For rows of 16 bits the normal distribution comes from a polynomial
-// (fitted here): erfc(x) exp(x^2) = t P(t) with t = 1 / (1 + 0.38 x), relative error below 4e-7 for all x >= 0 in 32 bits,
-// a hundredth of what the rounding to the type takes; and it shares its exponential with the density.  (16384 x 4096
-// bf16, slopes of gelu: 143 us with erfcf, bound by its instructions.)
+// slope is a difference of nearly equal numbers.  For rows of 16 bits the normal distribution comes from a polynomial (in the
+// form of Abramowitz and Stegun 7.1.26, fitted here): erfc(x) exp(x^2) = t P(t) with t = 1 / (1 + 0.38 x), relative error below
+// 4e-7 for all x >= 0 in 32 bits, a hundredth of what the rounding to the type takes; and it shares its exponential with the
+// density.  (16384 x 4096 bf16, slopes of gelu: 143 us with erfcf, bound by its instructions.)
 struct Normal {
     float below, density;
     __device__ explicit Normal(float z)
@@ -565,7 +565,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
                         read_q(stage(other), zero, zero);
                     }
                     multiply(step, part);
-                    // (behind the part: its matrix instructions run while the loads are asked for; 16384 slots, 2048 x 8192, us:
+                    // (behind the part: its matrix instructions run while the loads are asked for; 16384 slots, 2048 x 8192, us, before and after:
                     // forward 579 and 566, rows 661 and 616.  The weights' product has no registers left for that.)
                     if constexpr (kForm != WEIGHTS && h + 1 == kParts && s + 1 == kSteps)
                         if (t + 2 < steps) ask(t + 2, which);
@@ -709,8 +709,10 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
     });
 }
 
-// grad_z = grad_y act'(pre), and the sums of its rows over tiles of kSlopeRows rows of an expert: a workgroup has a tile and
-// 16 words of 16 bytes of its columns, 16 threads along them and 16 along the rows.
+// grad_z = grad_y act'(pre), rounded to the type that the matrix units take (pre is kept in it as well, which halves what is
+// written and read of it), and the sums of its rows before that rounding, over tiles of kSlopeRows rows of an expert: a workgroup
+// has a tile and 16 words of 16 bytes of its columns, 16 threads along them and 16 along the rows.  Bound by memory: 16384 x 4096
+// bf16, gelu, 88 us, 4.6 TB/s.
 constexpr int kSlopeRows = 64;
 template <typename T, Access kAccess>
 __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, int tiles_n)

@@ -7,8 +7,8 @@
 // every workgroup then knows where its entries lie in both orders.  Few tokens are one workgroup's, in one launch (16 x 64
 // bf16: 15.6 us a call, in three launches 22).  All sums are in a fixed order.
 //
-// Bound by instructions: 65536 x 128 floats, 8 each, 24 us to choose (the logits are 6 us of memory), 6 to 9 for
-// the scan, 6 to 9 to place, and 21 for the gradient, which waits for a token's entries before it can weigh them (11 us of memory).
+// Bound by instructions: 65536 x 128 floats, 8 each, 23 to 25 us to choose (the logits are 6 us of memory), 9 for
+// the scan, 9 to place, and 21 to 22 for the gradient, which waits for a token's entries before it can weigh them (11 us of memory).
 #include "kernels.hpp"
 #include "model.hpp"
 
