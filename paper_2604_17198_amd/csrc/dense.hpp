@@ -83,4 +83,38 @@ constexpr float kLog2e = 1.4426950408889634f, kInfinity = __builtin_inff();
 // 2^x in one instruction (results below the smallest normal number are zero).
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A float as an unsigned number of the same order; 0 for what is never chosen (-inf, not a number).
+__device__ inline unsigned order_of(float v)
+{
+    const unsigned u = __float_as_uint(v + 0.0f);              // (-0 counts as 0)
+    return v > -kInfinity ? ((int)u < 0 ? ~u : u | 0x80000000u) : 0u;
+}
+
+// One value over the L lanes of a group, the same bits in every lane.  (Moves inside 16 lanes are part of an instruction;
+// a shuffle is a round trip through the LDS unit.)
+template <int kCtrl> __device__ inline unsigned moved(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, 0xf, 0xf, true);
+}
+template <int L, typename Op> __device__ inline unsigned group_all_bits(unsigned v, Op op)
+{
+    if constexpr (L > 1) v = op(v, moved<0xb1>(v));            // lanes 1, 0, 3, 2
+    if constexpr (L > 2) v = op(v, moved<0x4e>(v));            // lanes 2, 3, 0, 1
+    if constexpr (L > 4) v = op(v, moved<0x141>(v));           // 8 lanes backwards
+    if constexpr (L > 8) v = op(v, moved<0x140>(v));           // 16 lanes backwards
+    if constexpr (L > 16) v = op(v, (unsigned)__shfl_xor((int)v, 16, NACHO_WAVE));
+    if constexpr (L > 32) v = op(v, (unsigned)__shfl_xor((int)v, 32, NACHO_WAVE));
+    return v;
+}
+template <int L, typename Op> __device__ inline float group_reduce(float v, Op op)
+{
+    return __uint_as_float(group_all_bits<L>(__float_as_uint(v), [&](unsigned x, unsigned y) {
+        return __float_as_uint(op(__uint_as_float(x), __uint_as_float(y)));
+    }));
+}
+template <int L> __device__ inline unsigned group_max(unsigned v)
+{
+    return group_all_bits<L>(v, [](unsigned x, unsigned y) { return x > y ? x : y; });
+}
+
 }  // namespace nacho
