@@ -538,6 +538,52 @@ int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y,
                            void *grad_bias, int64_t gb_stride, void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
+ * nacho_experts_step: a whole layer of a mixture of experts for a few tokens, as a
+ * program that answers needs it (nacho_route, nacho_experts twice and nacho_combine
+ * in one call, for up to 64 tokens):
+ *   out[t] = residual[t] + sum_i g_i (down[e_i] h_i + down.bias[e_i])   over the top_k
+ *            experts e_i of token t, chosen and weighted as by nacho_route (keep,
+ *            normalise, ties, -inf and NaN as there; a token that chooses nothing
+ *            gets its residual, or 0)
+ *   h_i    = act(up[e_i] x[t] + up.bias[e_i]), or, where gate.w is given,
+ *            act(gate[e_i] x[t] + gate.bias[e_i]) (up[e_i] x[t] + up.bias[e_i]);
+ *            rounded to the type
+ *   logits   [n_tokens x n_experts], the router's
+ *   x        [n_tokens x inner]
+ *   up, gate [n_experts][hidden x inner], down [n_experts][outer x hidden]: w of a
+ *            leading dimension ld, experts `stride` elements apart; bias, or NULL, of
+ *            experts bias_stride apart
+ *   residual [n_tokens x outer], or NULL; out may be residual itself (same leading
+ *            dimension)
+ * All of one type; sums, gates and the weighted sum are held in 32 bits, out is rounded
+ * once.  Weights of experts that no token chose are not read.
+ * Limits: n_tokens <= 64, n_experts <= 1024, top_k <= min(32, n_experts); inner, hidden,
+ * outer < 2^24.  Workspace: nacho_experts_step_workspace_bytes.
+ */
+typedef struct {
+    const void *w;
+    int64_t ld, stride;
+    const void *bias;
+    int64_t bias_stride;
+} nacho_dense;
+typedef struct {
+    int64_t n_tokens, n_experts, inner, hidden, outer;
+    const void *logits;
+    int64_t ldl;
+    const uint8_t *keep;
+    const void *x;
+    int64_t ldx;
+    nacho_dense up, gate, down;
+    const void *residual;
+    int64_t ldr;
+    void *out;
+    int64_t ldo;
+    int32_t top_k, normalise, act, dtype;
+} nacho_experts_step_layer;
+int32_t nacho_experts_step_workspace_bytes(const nacho_experts_step_layer *layer, size_t *bytes);
+int32_t nacho_experts_step(const nacho_experts_step_layer *layer, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
  * nacho_combine: for every token the weighted sum of its experts' rows,
  *   out[t] = residual[t] + sum_i val_i y[crd_i]   over the entries i of row t of
  *   routing   CSR [n_tokens x n_slots]: crd the slots, values F32 the gates (val

@@ -32,6 +32,7 @@ EXPORTS = [
     "nacho_distill_workspace_bytes", "nacho_distill", "nacho_distill_grad",
     "nacho_route_workspace_bytes", "nacho_route", "nacho_route_grad", "nacho_combine",
     "nacho_combine_grad", "nacho_experts_workspace_bytes", "nacho_experts", "nacho_experts_grad",
+    "nacho_experts_step_workspace_bytes", "nacho_experts_step",
 ]
 
 
@@ -72,6 +73,17 @@ class _ExpertsLayer(C.Structure):
                 ("n_tokens", C.c_int64), ("inner", C.c_int64), ("outer", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
                 ("w", C.c_void_p), ("ldw", C.c_int64), ("w_stride", C.c_int64), ("bias", C.c_void_p),
                 ("bias_stride", C.c_int64), ("act", C.c_int32), ("dtype", C.c_int32)]
+
+
+class _Dense(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("ld", C.c_int64), ("stride", C.c_int64), ("bias", C.c_void_p), ("bias_stride", C.c_int64)]
+
+
+class _StepLayer(C.Structure):
+    _fields_ = [("n_tokens", C.c_int64), ("n_experts", C.c_int64), ("inner", C.c_int64), ("hidden", C.c_int64), ("outer", C.c_int64),
+                ("logits", C.c_void_p), ("ldl", C.c_int64), ("keep", C.c_void_p), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("up", _Dense), ("gate", _Dense), ("down", _Dense), ("residual", C.c_void_p), ("ldr", C.c_int64), ("out", C.c_void_p),
+                ("ldo", C.c_int64), ("top_k", C.c_int32), ("normalise", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32)]
 
 
 _lib = None
@@ -150,6 +162,8 @@ def lib():
         L.nacho_experts_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                          C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t,
                                          C.c_void_p]
+        L.nacho_experts_step_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+        L.nacho_experts_step.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         _libs[_instrumented] = L
         _lib = L
     return _lib
@@ -767,6 +781,55 @@ def nacho_experts_grad(grad_y, x, weight, expert_pos, token=None, act="none", pr
                                     ldgw, gap, _ptr(grad_bias), gb, _ptr(ws), room, _stream()),
            "nacho_experts_grad")
     return grad_x, grad_weight
+
+
+def _dense(weight, bias, what, experts, rows, cols, dtype, device):
+    """The descriptor of an experts' product: weights [experts, rows, cols], biases [experts, rows] or None."""
+    ld, stride = _stack(weight, what, (experts, rows, cols), dtype, device)
+    if bias is None:
+        return _Dense(weight.data_ptr(), ld, stride, None, 0)
+    return _Dense(weight.data_ptr(), ld, stride, bias.data_ptr(), _stack(bias, what + "_bias", (experts, rows), dtype, device)[1])
+
+
+def nacho_experts_step(x, logits, top_k, up, down, gate=None, up_bias=None, gate_bias=None, down_bias=None, act="silu", normalise=False,
+                       keep=None, residual=None, out=None, ws=None):
+    """A whole layer of experts for up to 64 tokens: out[t] = residual[t] + the weighted sum over the top_k experts of token t (by
+    `logits`, as nacho_route chooses and weighs them) of down h + down_bias, with h = act(up x + up_bias) or, with `gate`,
+    act(gate x + gate_bias) * (up x + up_bias).  up, gate [experts, hidden, inner], down [experts, outer, hidden].  `out` may be
+    `residual` itself."""
+    dtype, dev = x.dtype, x.device
+    dt = model_dtype_code(dtype)
+    ldx = _matrix(x, "x")
+    tokens, inner = x.shape
+    if up.dim() != 3 or down.dim() != 3:
+        raise ValueError("up, down: [experts, rows, columns] is needed")
+    experts, hidden, outer = up.shape[0], up.shape[1], down.shape[1]
+    ldl = _matrix(logits, "logits", tokens, experts, dtype, dev)
+    if keep is not None:
+        _vector_of(keep, "keep", tokens, torch.bool if keep.dtype is torch.bool else torch.uint8, dev)
+    if act not in _ACTS:
+        raise ValueError(f"act: one of {', '.join(_ACTS)}")
+    _need(gate is not None or gate_bias is None, "gate_bias: without a gate")
+    ldr = _matrix(residual, "residual", tokens, outer, dtype, dev) if residual is not None else 0
+    if out is None:
+        out = torch.empty((tokens, outer), dtype=dtype, device=dev)
+        ldo = outer
+    else:
+        ldo = _matrix(out, "out", tokens, outer, dtype, dev)
+    c = _StepLayer(tokens, experts, inner, hidden, outer, logits.data_ptr(), ldl, _ptr(keep), x.data_ptr(), ldx,
+                   _dense(up, up_bias, "up", experts, hidden, inner, dtype, dev),
+                   _Dense() if gate is None else _dense(gate, gate_bias, "gate", experts, hidden, inner, dtype, dev),
+                   _dense(down, down_bias, "down", experts, outer, hidden, dtype, dev), _ptr(residual), ldr, out.data_ptr(), ldo, top_k,
+                   bool(normalise), _ACTS[act], dt)
+    if ws is None:
+        n = C.c_size_t(0)
+        _check(lib().nacho_experts_step_workspace_bytes(C.byref(c), C.byref(n)), "nacho_experts_step_workspace_bytes")
+        room = n.value
+        ws = _workspace(room, dev)
+    else:
+        room = _room(ws, dev)
+    _check(lib().nacho_experts_step(C.byref(c), _ptr(ws), room, _stream()), "nacho_experts_step")
+    return out
 
 
 def _slots_of(pos, slot, gate, n_slots, device):

@@ -205,6 +205,45 @@ GradWs carve_grad(void *ws, const nacho_experts_layer *l, bool grad_z, bool sums
     return w;
 }
 
+// The sizes of a layer of single steps.
+int32_t check_step(const nacho_experts_step_layer *l)
+{
+    if (!l || !value_type(l->dtype) || l->act < NACHO_ACT_NONE || l->act > NACHO_ACT_SILU) return NACHO_ERR_INVALID_ARG;
+    if (l->n_tokens < 0 || l->n_experts < 1 || l->inner < 1 || l->hidden < 1 || l->outer < 1 || l->top_k < 1 || l->top_k > l->n_experts)
+        return NACHO_ERR_INVALID_ARG;
+    return l->n_tokens > kMostStepTokens || l->n_experts > kMostExperts || l->top_k > kMostChoices || l->inner >= 1 << 24 ||
+                   l->hidden >= 1 << 24 || l->outer >= 1 << 24
+               ? NACHO_ERR_UNSUPPORTED
+               : NACHO_OK;
+}
+// The weights [n_experts][rows x cols] and biases of one of its products.
+bool check_dense(const nacho_dense &d, int64_t experts, int64_t rows, int64_t cols, int64_t elem)
+{
+    return d.w && matrices(d.w, experts, rows, cols, d.ld, d.stride, elem) && (!d.bias || matrices(d.bias, experts, 1, rows, rows, d.bias_stride, elem));
+}
+Array weights_of(const nacho_dense &d, int64_t experts, int64_t rows, int64_t cols, int64_t elem)
+{
+    return {d.w, d.w ? span(experts, rows, cols, d.ld, d.stride, elem) : 0};
+}
+Array biases_of(const nacho_dense &d, int64_t experts, int64_t rows, int64_t elem)
+{
+    return {d.bias, d.bias ? span(experts, 1, rows, rows, d.bias_stride, elem) : 0};
+}
+size_t carve_step(void *ws, const nacho_experts_step_layer *l, StepArgs *a)
+{
+    Slices c(ws);
+    const int64_t slots = l->n_tokens * l->top_k;
+    step_plan(l->dtype, l->n_tokens, l->n_experts, l->top_k, l->hidden, l->outer, &a->tiles, &a->parts);
+    a->ldh = (l->hidden + 7) / 8 * 8;
+    a->h = c.take<char>(slots * a->ldh * value_bytes(l->dtype));
+    a->choice = c.take<uint16_t>(slots);
+    a->share = c.take<float>(slots);
+    a->active = c.take<int32_t>(1 + (slots < l->n_experts ? slots : l->n_experts));
+    a->partial = c.take<float>(a->parts > 1 ? (int64_t)a->tiles * a->parts * l->n_tokens * 16 : 0);
+    a->arrived = c.take<int32_t>(a->tiles);
+    return align_up(c.off, 256);
+}
+
 }  // namespace
 
 extern "C" {
@@ -447,6 +486,63 @@ int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y,
         if (const hipError_t e = launch_experts_weights(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
         profile_mark("experts_weights");
     }
+    return NACHO_OK;
+}
+
+int32_t nacho_experts_step_workspace_bytes(const nacho_experts_step_layer *layer, size_t *bytes)
+{
+    if (!bytes) return NACHO_ERR_INVALID_ARG;
+    const int32_t rc = check_step(layer);
+    StepArgs a{};
+    if (rc == NACHO_OK) *bytes = carve_step(nullptr, layer, &a);
+    return rc;
+}
+
+int32_t nacho_experts_step(const nacho_experts_step_layer *layer, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    const int32_t rc = check_step(layer);
+    if (rc != NACHO_OK) return rc;
+    const nacho_experts_step_layer &l = *layer;
+    const int64_t elem = value_bytes(l.dtype), tokens = l.n_tokens, n = l.n_experts;
+    if (!matrix(l.logits, tokens, n, l.ldl, elem) || !matrix(l.x, tokens, l.inner, l.ldx, elem) || !matrix(l.out, tokens, l.outer, l.ldo, elem) ||
+        (l.residual && !matrix(l.residual, tokens, l.outer, l.ldr, elem)) || !check_dense(l.up, n, l.hidden, l.inner, elem) ||
+        (l.gate.w && !check_dense(l.gate, n, l.hidden, l.inner, elem)) || (!l.gate.w && l.gate.bias) || !check_dense(l.down, n, l.outer, l.hidden, elem))
+        return NACHO_ERR_INVALID_ARG;
+    StepArgs a{};
+    const size_t need = carve_step(ws, layer, &a);
+    if (!ws || ws_bytes < need || !aligned(ws, 16)) return NACHO_ERR_WORKSPACE;
+    const bool in_place = l.residual == l.out && l.ldr == l.ldo;
+    if (!apart({{l.out, span(tokens, l.outer, l.ldo, elem)}, {ws, (int64_t)need}},
+               {{l.logits, span(tokens, n, l.ldl, elem)}, {l.keep, tokens}, {l.x, span(tokens, l.inner, l.ldx, elem)},
+                weights_of(l.up, n, l.hidden, l.inner, elem), biases_of(l.up, n, l.hidden, elem), weights_of(l.gate, n, l.hidden, l.inner, elem),
+                biases_of(l.gate, n, l.hidden, elem), weights_of(l.down, n, l.outer, l.hidden, elem), biases_of(l.down, n, l.outer, elem),
+                {in_place ? nullptr : l.residual, l.residual ? span(tokens, l.outer, l.ldr, elem) : 0}}))
+        return NACHO_ERR_INVALID_ARG;
+    if (tokens == 0) return NACHO_OK;
+    a.logits = l.logits;
+    a.ldl = l.ldl;
+    a.keep = l.keep;
+    a.tokens = (int32_t)tokens;
+    a.experts = (int32_t)n;
+    a.top_k = l.top_k;
+    a.normalise = l.normalise != 0;
+    a.inner = (int32_t)l.inner;
+    a.hidden = (int32_t)l.hidden;
+    a.outer = (int32_t)l.outer;
+    a.act = l.act;
+    a.x = l.x;
+    a.ldx = l.ldx;
+    a.up = l.up;
+    a.gate = l.gate;
+    a.down = l.down;
+    a.residual = l.residual;
+    a.ldr = l.ldr;
+    a.out = l.out;
+    a.ldo = l.ldo;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (launch_step(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
+    profile_mark("experts_step");
     return NACHO_OK;
 }
 

@@ -120,4 +120,32 @@ struct SlopeArgs {
 int64_t experts_slope_tiles(int64_t slots, int64_t experts);
 hipError_t launch_experts_slope(int dtype, const SlopeArgs &a, hipStream_t s);
 
+// ---- a whole layer of experts for a few tokens -----------------------------------
+constexpr int kMostStepTokens = 64;
+struct StepArgs {
+    const void *logits;            // [tokens] rows of `ldl` elements
+    int64_t ldl;
+    const uint8_t *keep;           // may be NULL: every token
+    int32_t tokens, experts, top_k, normalise, inner, hidden, outer, act;
+    const void *x;
+    int64_t ldx;
+    nacho_dense up, gate, down;    // gate.w: may be NULL
+    const void *residual;          // may be NULL
+    int64_t ldr;
+    void *out;
+    int64_t ldo;
+    // workspace: the rows between the products by slot (token x top_k + choice), the choice, its gates, the experts that a token
+    // chose behind their number
+    void *h;
+    int64_t ldh;
+    uint16_t *choice;
+    float *share;
+    int32_t *active;
+    int32_t tiles, parts;          // of the second product: tiles of rows, workgroups that share one
+    float *partial;                // [tiles][parts][tokens][16], several parts
+    int32_t *arrived;              // [tiles]
+};
+void step_plan(int dtype, int64_t tokens, int64_t experts, int64_t top_k, int64_t hidden, int64_t outer, int32_t *tiles, int32_t *parts);
+hipError_t launch_step(int dtype, const StepArgs &a, hipStream_t s);
+
 }  // namespace nacho
