@@ -447,6 +447,46 @@ int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int6
                            void *hip_stream);
 
 /*
+ * nacho_xent: the softmax cross entropy of rows against a large vocabulary, from the
+ * rows and the vocabulary's weights; the logits are never stored.
+ *   x       [n_rows x inner], head [vocabulary x inner], of one type
+ *   label   device integers [n_rows] of label_bytes (4 or 8) each
+ *   weight  device float[n_rows], a factor of every row, or NULL for ones
+ * With z_iv the product of x[i] and head[v], summed in 32 bits,
+ *   lse[i]  = log sum_v exp(z_iv)
+ *   loss[i] = weight[i] (lse[i] - z_i,label[i])
+ * Rows whose label lies outside the vocabulary (a negative one: a position that is not
+ * to be learned) and rows of weight 0 have loss, lse and gradients 0, whatever they
+ * hold; they are not computed.  A row with a NaN or an infinity among its logits has
+ * no distribution: NaN.
+ * nacho_xent_grad: from the lse of an earlier nacho_xent on the same operands
+ *   g_iv      = weight[i] (exp(z_iv - lse[i]) - [v = label[i]]), rounded to the type for
+ *               the products (of f16 after multiplication by a power of two, which the
+ *               results are divided by: small probabilities do not vanish)
+ *   grad_x    = g head, grad_head = g^T x, each NULL where it is not wanted
+ * weight then is the factor of the loss times the gradient that arrives at it.  A NaN
+ * in a row that counts is one in all of grad_head.  g is made a piece of the vocabulary
+ * at a time, and takes 256 MiB at most (more of over 524288 rows of 16 bits).
+ * Limits: vocabulary, inner < 2^24.  Workspaces: nacho_xent_workspace_bytes,
+ * nacho_xent_grad_workspace_bytes.
+ */
+typedef struct {
+    int64_t n_rows, vocabulary, inner;
+    const void *x;
+    int64_t ldx;
+    const void *head;
+    int64_t ldh;
+    const void *label;
+    const float *weight;
+    int32_t label_bytes, dtype;
+} nacho_xent_layer;
+int32_t nacho_xent_workspace_bytes(const nacho_xent_layer *layer, size_t *bytes);
+int32_t nacho_xent(const nacho_xent_layer *layer, float *loss, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+int32_t nacho_xent_grad_workspace_bytes(const nacho_xent_layer *layer, size_t *bytes);
+int32_t nacho_xent_grad(const nacho_xent_layer *layer, const float *lse, void *grad_x, int64_t ldgx, void *grad_head, int64_t ldgh,
+                        void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
  * nacho_route: the routing matrix of a mixture of experts.  Every token goes to the
  * top_k experts with the largest logits (ties: the lowest index; a logit of -inf or
  * NaN is never chosen, so a token may store fewer), and the matrix comes in the two

@@ -33,6 +33,7 @@ EXPORTS = [
     "nacho_route_workspace_bytes", "nacho_route", "nacho_route_grad", "nacho_combine",
     "nacho_combine_grad", "nacho_experts_workspace_bytes", "nacho_experts", "nacho_experts_grad",
     "nacho_experts_step_workspace_bytes", "nacho_experts_step",
+    "nacho_xent_workspace_bytes", "nacho_xent", "nacho_xent_grad_workspace_bytes", "nacho_xent_grad",
 ]
 
 
@@ -84,6 +85,12 @@ class _StepLayer(C.Structure):
                 ("logits", C.c_void_p), ("ldl", C.c_int64), ("keep", C.c_void_p), ("x", C.c_void_p), ("ldx", C.c_int64),
                 ("up", _Dense), ("gate", _Dense), ("down", _Dense), ("residual", C.c_void_p), ("ldr", C.c_int64), ("out", C.c_void_p),
                 ("ldo", C.c_int64), ("top_k", C.c_int32), ("normalise", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32)]
+
+
+class _XentLayer(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("vocabulary", C.c_int64), ("inner", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("head", C.c_void_p), ("ldh", C.c_int64), ("label", C.c_void_p), ("weight", C.c_void_p), ("label_bytes", C.c_int32),
+                ("dtype", C.c_int32)]
 
 
 _lib = None
@@ -164,6 +171,11 @@ def lib():
                                          C.c_void_p]
         L.nacho_experts_step_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
         L.nacho_experts_step.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.nacho_xent_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+        L.nacho_xent_grad_workspace_bytes.argtypes = L.nacho_xent_workspace_bytes.argtypes
+        L.nacho_xent.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.nacho_xent_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t,
+                                      C.c_void_p]
         _libs[_instrumented] = L
         _lib = L
     return _lib
@@ -623,6 +635,62 @@ def nacho_distill_grad(teacher: Operand, logits, lse, temperature=1.0, weight=No
     return grad
 
 
+def _xent_layer(x, head, label, weight):
+    """The descriptor of a cross entropy against a vocabulary."""
+    dtype, dev = x.dtype, x.device
+    dt = model_dtype_code(dtype)
+    ldx = _matrix(x, "x")
+    rows, inner = x.shape
+    ldh = _matrix(head, "head", None, inner, dtype, dev)
+    wide = label.dtype is torch.int64
+    _vector_of(label, "label", rows, torch.int64 if wide else torch.int32, dev)
+    _vector_of(weight, "weight", rows, torch.float32, dev)
+    return _XentLayer(rows, head.shape[0], inner, x.data_ptr(), ldx, head.data_ptr(), ldh, label.data_ptr(), _ptr(weight), 8 if wide else 4, dt)
+
+
+def _room_for(call, c, ws, device):
+    """A workspace of the size that `call` names, or the caller's; and its bytes."""
+    if ws is not None:
+        return ws, _room(ws, device)
+    n = C.c_size_t(0)
+    _check(getattr(lib(), call)(C.byref(c), C.byref(n)), call)
+    return _workspace(n.value, device), n.value
+
+
+def nacho_xent(x, head, label, weight=None, loss=None, lse=None, ws=None):
+    """Cross entropy of the rows x against the vocabulary whose weights are the rows of `head`, without its logits; rows whose
+    label (int32 or int64) lies outside the vocabulary do not count.  Returns (loss[rows], lse[rows])."""
+    c = _xent_layer(x, head, label, weight)
+    rows, dev = x.shape[0], x.device
+    loss = _vector_of(loss, "loss", rows, torch.float32, dev) if loss is not None else _floats(rows, dev)
+    lse = _vector_of(lse, "lse", rows, torch.float32, dev) if lse is not None else _floats(rows, dev)
+    ws, room = _room_for("nacho_xent_workspace_bytes", c, ws, dev)
+    _check(lib().nacho_xent(C.byref(c), _ptr(loss), _ptr(lse), _ptr(ws), room, _stream()), "nacho_xent")
+    return loss, lse
+
+
+def nacho_xent_grad(x, head, label, lse, weight=None, grad_x=None, grad_head=None, ws=None):
+    """(gradient of x, gradient of head) from the lse of an earlier nacho_xent; `weight` is the factor of each row's loss times the
+    gradient that arrives at it.  One that is False is not wanted: it is not computed, and None is returned."""
+    c = _xent_layer(x, head, label, weight)
+    dev = x.device
+    _vector_of(lse, "lse", x.shape[0], torch.float32, dev)
+    if grad_x is False:
+        grad_x = None
+    elif grad_x is None:
+        grad_x = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    if grad_head is False:
+        grad_head = None
+    elif grad_head is None:
+        grad_head = torch.empty(head.shape, dtype=x.dtype, device=dev)
+    ldgx = _matrix(grad_x, "grad_x", *x.shape, x.dtype, dev) if grad_x is not None else 0
+    ldgh = _matrix(grad_head, "grad_head", *head.shape, x.dtype, dev) if grad_head is not None else 0
+    ws, room = _room_for("nacho_xent_grad_workspace_bytes", c, ws, dev)
+    _check(lib().nacho_xent_grad(C.byref(c), _ptr(lse), _ptr(grad_x), ldgx, _ptr(grad_head), ldgh, _ptr(ws), room, _stream()),
+           "nacho_xent_grad")
+    return grad_x, grad_head
+
+
 class Routing:
     """The arrays nacho_route fills: the routing matrix by tokens (pos, expert, gate), by experts (expert_pos, token; slot:
     the place there of every entry), counts, lse, the balance loss and the number of tokens that store an entry."""
@@ -821,13 +889,7 @@ def nacho_experts_step(x, logits, top_k, up, down, gate=None, up_bias=None, gate
                    _Dense() if gate is None else _dense(gate, gate_bias, "gate", experts, hidden, inner, dtype, dev),
                    _dense(down, down_bias, "down", experts, outer, hidden, dtype, dev), _ptr(residual), ldr, out.data_ptr(), ldo, top_k,
                    bool(normalise), _ACTS[act], dt)
-    if ws is None:
-        n = C.c_size_t(0)
-        _check(lib().nacho_experts_step_workspace_bytes(C.byref(c), C.byref(n)), "nacho_experts_step_workspace_bytes")
-        room = n.value
-        ws = _workspace(room, dev)
-    else:
-        room = _room(ws, dev)
+    ws, room = _room_for("nacho_experts_step_workspace_bytes", c, ws, dev)
     _check(lib().nacho_experts_step(C.byref(c), _ptr(ws), room, _stream()), "nacho_experts_step")
     return out
 

@@ -205,6 +205,59 @@ GradWs carve_grad(void *ws, const nacho_experts_layer *l, bool grad_z, bool sums
     return w;
 }
 
+int32_t check_xent(const nacho_xent_layer *l)
+{
+    if (!l || !value_type(l->dtype) || (l->label_bytes != 4 && l->label_bytes != 8)) return NACHO_ERR_INVALID_ARG;
+    if (l->n_rows < 0 || l->n_rows > kMostRows || l->vocabulary < 1 || l->inner < 1) return NACHO_ERR_INVALID_ARG;
+    return l->vocabulary >= 1 << 24 || l->inner >= 1 << 24 ? NACHO_ERR_UNSUPPORTED : NACHO_OK;
+}
+// The arrays that both calls read, into the kernels' arguments.
+bool take_xent(const nacho_xent_layer *l, XentArgs *a)
+{
+    const int64_t elem = value_bytes(l->dtype);
+    if (!matrix(l->x, l->n_rows, l->inner, l->ldx, elem) || !matrix(l->head, l->vocabulary, l->inner, l->ldh, elem)) return false;
+    if ((l->n_rows > 0 && !l->label) || !aligned(l->label, (uintptr_t)l->label_bytes) || !aligned(l->weight, 4)) return false;
+    *a = XentArgs{};
+    a->x = l->x;
+    a->ldx = l->ldx;
+    a->head = l->head;
+    a->ldh = l->ldh;
+    a->rows = l->n_rows;
+    a->vocabulary = l->vocabulary;
+    a->inner = (int32_t)l->inner;
+    a->elem = (int32_t)elem;
+    a->label_bytes = l->label_bytes;
+    a->half = l->dtype == NACHO_F16;
+    a->label = l->label;
+    a->weight = l->weight;
+    return true;
+}
+size_t carve_xent(void *ws, const nacho_xent_layer *l, XentArgs *a)
+{
+    Slices c(ws);
+    a->bounds = c.take<int32_t>(2);
+    a->token = c.take<int32_t>(l->n_rows);
+    a->slot_label = c.take<int32_t>(l->n_rows);
+    a->at_label = c.take<float>(l->n_rows);
+    a->partial = c.take<float2>(xent_partials((int)value_bytes(l->dtype), l->n_rows, l->vocabulary));
+    return align_up(c.off, 256);
+}
+size_t carve_xent_grad(void *ws, const nacho_xent_layer *l, const XentPlan &plan, bool sums, XentArgs *a)
+{
+    Slices c(ws);
+    a->bounds = c.take<int32_t>(2);
+    a->scale = c.take<float>(2);
+    a->token = c.take<int32_t>(l->n_rows);
+    a->slot_label = c.take<int32_t>(l->n_rows);
+    a->slot_lse = c.take<float>(l->n_rows);
+    a->factor = c.take<float>(l->n_rows);
+    a->slot_of = c.take<int32_t>(l->n_rows);
+    a->g = c.take<char>(l->n_rows * plan.ldg * value_bytes(l->dtype));
+    if (sums && plan.sums) a->sums = c.take<float>(plan.stretches * l->n_rows * plan.lds);
+    return align_up(c.off, 256);
+}
+XentPlan plan_of(const nacho_xent_layer *l) { return xent_plan((int)value_bytes(l->dtype), l->n_rows, l->vocabulary, l->inner); }
+
 // The sizes of a layer of single steps.
 int32_t check_step(const nacho_experts_step_layer *l)
 {
@@ -543,6 +596,79 @@ int32_t nacho_experts_step(const nacho_experts_step_layer *layer, void *ws, size
     profile_begin(s);
     if (launch_step(l.dtype, a, s) != hipSuccess) return NACHO_ERR_HIP;
     profile_mark("experts_step");
+    return NACHO_OK;
+}
+
+int32_t nacho_xent_workspace_bytes(const nacho_xent_layer *layer, size_t *bytes)
+{
+    if (!bytes) return NACHO_ERR_INVALID_ARG;
+    const int32_t rc = check_xent(layer);
+    XentArgs a{};
+    if (rc == NACHO_OK) *bytes = carve_xent(nullptr, layer, &a);
+    return rc;
+}
+
+int32_t nacho_xent_grad_workspace_bytes(const nacho_xent_layer *layer, size_t *bytes)
+{
+    if (!bytes) return NACHO_ERR_INVALID_ARG;
+    const int32_t rc = check_xent(layer);
+    XentArgs a{};
+    if (rc == NACHO_OK) *bytes = carve_xent_grad(nullptr, layer, plan_of(layer), true, &a);
+    return rc;
+}
+
+int32_t nacho_xent(const nacho_xent_layer *layer, float *loss, float *lse, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    const int32_t rc = check_xent(layer);
+    if (rc != NACHO_OK) return rc;
+    const nacho_xent_layer &l = *layer;
+    XentArgs a;
+    if (!take_xent(layer, &a) || (l.n_rows > 0 && (!loss || !lse)) || !aligned(loss, 4) || !aligned(lse, 4)) return NACHO_ERR_INVALID_ARG;
+    const size_t need = carve_xent(ws, layer, &a);
+    if (!ws || ws_bytes < need || !aligned(ws, 16)) return NACHO_ERR_WORKSPACE;
+    const int64_t elem = a.elem, by_row = l.n_rows * 4;
+    if (!apart({{loss, by_row}, {lse, by_row}, {ws, (int64_t)need}},
+               {{l.x, span(l.n_rows, l.inner, l.ldx, elem)}, {l.head, span(l.vocabulary, l.inner, l.ldh, elem)}, {l.label, l.n_rows * l.label_bytes},
+                {l.weight, by_row}}))
+        return NACHO_ERR_INVALID_ARG;
+    a.loss = loss;
+    a.lse = lse;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (const hipError_t e = launch_xent(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+    profile_mark("xent");
+    return NACHO_OK;
+}
+
+int32_t nacho_xent_grad(const nacho_xent_layer *layer, const float *lse, void *grad_x, int64_t ldgx, void *grad_head, int64_t ldgh,
+                        void *ws, size_t ws_bytes, void *hip_stream)
+{
+    const int32_t rc = check_xent(layer);
+    if (rc != NACHO_OK) return rc;
+    const nacho_xent_layer &l = *layer;
+    XentArgs a;
+    if (!take_xent(layer, &a) || (l.n_rows > 0 && !lse) || !aligned(lse, 4)) return NACHO_ERR_INVALID_ARG;
+    const int64_t elem = a.elem, by_row = l.n_rows * 4;
+    if ((grad_x && !matrix(grad_x, l.n_rows, l.inner, ldgx, elem)) || (grad_head && !matrix(grad_head, l.vocabulary, l.inner, ldgh, elem)))
+        return NACHO_ERR_INVALID_ARG;
+    const XentPlan plan = plan_of(layer);
+    const size_t need = carve_xent_grad(ws, layer, plan, grad_x != nullptr, &a);
+    if (!ws || ws_bytes < need || !aligned(ws, 16)) return NACHO_ERR_WORKSPACE;
+    if (!apart({{grad_x, grad_x ? span(l.n_rows, l.inner, ldgx, elem) : 0}, {grad_head, grad_head ? span(l.vocabulary, l.inner, ldgh, elem) : 0},
+                {ws, (int64_t)need}},
+               {{l.x, span(l.n_rows, l.inner, l.ldx, elem)}, {l.head, span(l.vocabulary, l.inner, l.ldh, elem)}, {l.label, l.n_rows * l.label_bytes},
+                {l.weight, by_row}, {lse, by_row}}))
+        return NACHO_ERR_INVALID_ARG;
+    if (!grad_x && !grad_head) return NACHO_OK;
+    a.lse = const_cast<float *>(lse);
+    a.grad_x = grad_x;
+    a.ldgx = ldgx;
+    a.grad_head = grad_head;
+    a.ldgh = ldgh;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (const hipError_t e = launch_xent_grad(l.dtype, a, plan, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+    profile_mark("xent_grad");
     return NACHO_OK;
 }
 

@@ -21,7 +21,7 @@ struct Rows {
     static constexpr bool kParts = false;
     static constexpr unsigned parts() { return 1; }
     template <typename Tile>
-    __device__ void end(const ProductArgs &a, const Place &at, const v4f (&acc)[Tile::kFragM][Tile::kFragN], char *stage0, char *stage1) const
+    __device__ void end(const ProductArgs &a, const Place &at, v4f (&acc)[Tile::kFragM][Tile::kFragN], char *stage0, char *stage1) const
     {
         typedef typename Tile::type T;
         T *const out = static_cast<T *>(a.out) + (Tile::form == WEIGHTS ? (int64_t)at.expert * a.out_stride : 0);

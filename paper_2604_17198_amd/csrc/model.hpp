@@ -148,4 +148,39 @@ struct StepArgs {
 void step_plan(int dtype, int64_t tokens, int64_t experts, int64_t top_k, int64_t hidden, int64_t outer, int32_t *tiles, int32_t *parts);
 hipError_t launch_step(int dtype, const StepArgs &a, hipStream_t s);
 
+// ---- cross entropy against a vocabulary ---------------------------------------------
+struct XentArgs {
+    const void *x;                 // [rows], `ldx` apart
+    int64_t ldx;
+    const void *head;              // [vocabulary], `ldh` apart
+    int64_t ldh;
+    int64_t rows, vocabulary;
+    int32_t inner, elem, label_bytes, half;      // elem: bytes of a value; half: f16
+    const void *label;
+    const float *weight;           // may be NULL: ones
+    float *loss, *lse;             // loss: NULL in a gradient call, which reads lse
+    void *grad_x, *grad_head;      // may be NULL
+    int64_t ldgx, ldgh;
+    // workspace: the rows that count (slots) and their number
+    int32_t *bounds, *token, *slot_label;
+    // of the loss: [tiles of the vocabulary][rows], and the label's logit by slot
+    float2 *partial;
+    float *at_label;
+    // of the gradient: by slot, the slot of a row (or -1), {a power of two that g is multiplied by, its inverse}, g of a piece, sums
+    float *slot_lse, *factor;
+    int32_t *slot_of;
+    float *scale;
+    void *g;
+    float *sums;
+};
+// How a gradient call goes through the vocabulary: `pieces` of `words`, each in `stretches` of `k_part` for the rows' sums.
+struct XentPlan {
+    int64_t pieces, words, ldg, stretches, k_part, lds;
+    bool sums;                     // (of the rows' gradients, in 32 bits: `lds` apart, one set a stretch)
+};
+int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary);
+XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner);
+hipError_t launch_xent(int dtype, const XentArgs &a, hipStream_t s);
+hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s);
+
 }  // namespace nacho

@@ -731,33 +731,48 @@ constexpr int64_t kUnits = 256;        // compute units
 // Floats need four times as many matrix instructions for what is loaded: tiles of 64 x 64, which are as many again.  3000 slots
 // of 7 experts, 777 x 499, us: weights 73 (64 x 128: 95), forward 42 (32 x 128: 45), rows 44 (50); with two steps on their way
 // in registers 54, 43 and 42.  512 x 2048, 32 experts of 64 and 128 slots, us with 32, 64 and 128: rows 51, 52 and 141, 87, 81 and 149.
-template <typename T, Form kForm, typename Finish> hipError_t by_size(const ProductArgs &a, const Finish &f, Access access, hipStream_t s)
+enum Shape { TILES_256, TILES_128, TILES_64, TILES_32 };
+// Rows and columns of these tiles (of rows shorter than a word: 128 x 128 for the weights, 32 x 128).
+constexpr int tall_of(Shape s) { return s == TILES_256 ? 256 : s == TILES_128 ? 128 : s == TILES_64 ? 64 : 32; }
+constexpr int wide_of(Shape s) { return s == TILES_256 ? 256 : s == TILES_64 ? 64 : 128; }
+// `parts`: stretches of k that workgroups share a tile's sum by.
+template <typename T, Form kForm> Shape shape_of(const ProductArgs &a, Access access, int64_t parts = 1)
 {
     const int64_t each = a.slots / a.experts, n128 = (a.n + 127) / 128;
     const bool words = access == WORDS;
-    if (access == TINY) return run<T, kForm, kForm == WEIGHTS ? 128 : 32, 128, kForm == WEIGHTS ? 2 : 1, kForm == WEIGHTS ? 2 : 4, TINY>(a, f, s);
+    if (access == TINY) return kForm == WEIGHTS ? TILES_128 : TILES_32;
     if constexpr (kForm == WEIGHTS) {
         const int64_t tiles = (int64_t)a.experts * ((a.m + 255) / 256) * ((a.n + 255) / 256);
-        if constexpr (sizeof(T) == 2) {
-            if (words && a.m >= 256 && a.n >= 256 && tiles >= kUnits) return run<T, kForm, 256, 256, 2, 4, WORDS>(a, f, s);
-        } else if (tiles < kUnits) {
-            return words ? run<T, kForm, 64, 64, 2, 2, WORDS>(a, f, s) : run<T, kForm, 64, 64, 2, 2, ANYWHERE>(a, f, s);
-        }
-        return words ? run<T, kForm, 128, 128, 2, 2, WORDS>(a, f, s) : run<T, kForm, 128, 128, 2, 2, ANYWHERE>(a, f, s);
+        if (sizeof(T) == 2) return words && a.m >= 256 && a.n >= 256 && tiles >= kUnits ? TILES_256 : TILES_128;
+        return tiles < kUnits ? TILES_64 : TILES_128;
     } else {
-        if constexpr (sizeof(T) == 2) {
-            if (words && each >= 256 && a.n >= 256 && a.slots / 256 * ((a.n + 255) / 256) >= kUnits)
-                return run<T, kForm, 256, 256, 2, 4, WORDS>(a, f, s);
-        }
+        if (sizeof(T) == 2 && words && each >= 256 && a.n >= 256 && a.slots / 256 * ((a.n + 255) / 256) * parts >= kUnits) return TILES_256;
         const int64_t few = words && sizeof(T) == 2 ? 32 : 64, most = sizeof(T) == 2 ? kUnits / 2 : 2 * kUnits - 1;
-        const bool small = each <= few || a.slots / 128 * n128 <= most;
-        if constexpr (sizeof(T) == 4) {
-            if (small && each > 64) return words ? run<T, kForm, 64, 64, 2, 2, WORDS>(a, f, s) : run<T, kForm, 64, 64, 2, 2, ANYWHERE>(a, f, s);
-        }
-        if (small)
-            return words ? run<T, kForm, 32, 128, 1, 4, WORDS, 256>(a, f, s) : run<T, kForm, 32, 128, 1, 4, ANYWHERE>(a, f, s);
-        return words ? run<T, kForm, 128, 128, 2, 2, WORDS>(a, f, s) : run<T, kForm, 128, 128, 2, 2, ANYWHERE>(a, f, s);
+        const bool small = each <= few || a.slots / 128 * n128 * parts <= most;
+        return !small ? TILES_128 : sizeof(T) == 4 && each > 64 ? TILES_64 : TILES_32;
     }
+}
+
+template <typename T, Form kForm, typename Finish> hipError_t by_size(const ProductArgs &a, const Finish &f, Access access, hipStream_t s)
+{
+    const Shape shape = shape_of<T, kForm>(a, access, f.parts());
+    const bool words = access == WORDS;
+    if (access == TINY) return run<T, kForm, kForm == WEIGHTS ? 128 : 32, 128, kForm == WEIGHTS ? 2 : 1, kForm == WEIGHTS ? 2 : 4, TINY>(a, f, s);
+    if constexpr (sizeof(T) == 2) {
+        if (shape == TILES_256) return run<T, kForm, 256, 256, 2, 4, WORDS>(a, f, s);
+    } else if (shape == TILES_64) return words ? run<T, kForm, 64, 64, 2, 2, WORDS>(a, f, s) : run<T, kForm, 64, 64, 2, 2, ANYWHERE>(a, f, s);
+    if constexpr (kForm != WEIGHTS) {
+        if (shape == TILES_32)
+            return words ? run<T, kForm, 32, 128, 1, 4, WORDS, 256>(a, f, s) : run<T, kForm, 32, 128, 1, 4, ANYWHERE>(a, f, s);
+    }
+    return words ? run<T, kForm, 128, 128, 2, 2, WORDS>(a, f, s) : run<T, kForm, 128, 128, 2, 2, ANYWHERE>(a, f, s);
+}
+
+// How rows that no 16-byte boundary fits are read, by the shorter ones.
+template <Form kForm> Access access_of(const ProductArgs &a, int elem)
+{
+    const int64_t along = kForm == WEIGHTS ? a.m : a.k, other = kForm == FORWARD ? a.k : a.n, least = along < other ? along : other;
+    return least * elem < 16 ? TINY : ANYWHERE;
 }
 
 template <Form kForm, typename Finish> hipError_t launch(int dtype, const ProductArgs &a, const Finish &f, hipStream_t s)
@@ -767,9 +782,7 @@ template <Form kForm, typename Finish> hipError_t launch(int dtype, const Produc
     const bool words = a.ldq < 0x7fffffff && a.ldp < 0x7fffffff &&
                        in_words({{a.q, a.ldq}, {a.p, a.ldp}, {a.p, a.p_stride}, {a.out, a.ldo}, {a.out, a.out_stride}, {a.pre, a.ldpre},
                                  {a.q, kForm == WEIGHTS ? 0 : a.k}, {a.q, kForm == WEIGHTS ? a.m : 0}, {a.q, a.n}}, elem);
-    // the shorter rows that are read
-    const int64_t along = kForm == WEIGHTS ? a.m : a.k, other = kForm == FORWARD ? a.k : a.n, least = along < other ? along : other;
-    const Access access = words ? WORDS : least * elem < 16 ? TINY : ANYWHERE;
+    const Access access = words ? WORDS : access_of<kForm>(a, elem);
     hipError_t rc = hipSuccess;
     by_type(dtype, [&](auto zero) { rc = by_size<decltype(zero), kForm>(a, f, access, s); });
     return rc;

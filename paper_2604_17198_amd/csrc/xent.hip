@@ -1,0 +1,476 @@
+// Softmax cross entropy of rows against a large vocabulary, from the rows x and the vocabulary's weights W, without keeping the
+// logits z_iv = <x_i, W_v>:
+//
+//   lse_i = log sum_v exp z_iv        loss_i = w_i (lse_i - z_i,label)
+//   g_iv  = w_i (exp(z_iv - lse_i) - [v = label_i])        grad_x = g W        grad_W = g^T x
+//
+// Three products on the tiles of products.hpp.  The loss: a tile of logits leaves the matrix units as the largest one of each row
+// and the sum of exponentials under it; a small kernel joins the tiles of a row.  The gradient makes the logits again, in pieces of
+// the vocabulary whose g (rounded to the type, which the matrix units take) fits a fixed room, from where both products read it.
+// grad_x then is a sum over pieces, and over stretches of the vocabulary where there are too few tiles for the chip, held in 32 bits.
+//
+// Rows that do not count (no label in the vocabulary, weight 0) are left out before the first product: it reads the others by a list.
+#include "products.hpp"
+
+namespace nacho {
+
+namespace {
+
+constexpr int kRowThreads = 1024;
+
+// The list of the rows that count, ascending, and by it their labels (and weights and lse, for the gradient).  Every workgroup has
+// kRowThreads rows and counts those before them itself.  The loss's call clears the results of the other rows.
+template <typename Label> __global__ void __launch_bounds__(kRowThreads) xent_rows_kernel(XentArgs a)
+{
+    constexpr int kWaves = kRowThreads / NACHO_WAVE;
+    __shared__ int counts[kWaves];
+    __shared__ float share[kWaves];
+    const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / NACHO_WAVE;
+    const int64_t begin = (int64_t)blockIdx.x * kRowThreads;
+    const Label *labels = static_cast<const Label *>(a.label);
+    auto counts_at = [&](int64_t i) { return labels[i] >= 0 && labels[i] < (Label)a.vocabulary && (!a.weight || a.weight[i] != 0.0f); };
+    int before = 0;
+#pragma unroll 4
+    for (int64_t i = tid; i < begin; i += kRowThreads) before += counts_at(i);
+    before = wave_sum(before);
+    if (lane == 0) counts[wave] = before;
+    __syncthreads();
+    before = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) before += counts[w];
+    __syncthreads();
+    const int64_t i = begin + tid;
+    const bool held = i < a.rows && counts_at(i);
+    const unsigned long long who = __ballot(held);
+    if (lane == 0) counts[wave] = __popcll((long long)who);
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w == wave) before += total;
+        total += counts[w];
+    }
+    const int slot = before + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0));
+    if (held) {
+        a.token[slot] = (int32_t)i;
+        a.slot_label[slot] = (int32_t)labels[i];
+        if (a.slot_lse) {
+            a.slot_lse[slot] = a.lse[i];
+            a.factor[slot] = a.weight ? a.weight[i] : 1.0f;
+        }
+    } else if (i < a.rows && a.loss) a.loss[i] = a.lse[i] = 0.0f;
+    if (a.slot_of && i < a.rows) a.slot_of[i] = held ? slot : -1;
+    if (blockIdx.x == gridDim.x - 1 && tid == kRowThreads - 1) {
+        a.bounds[0] = 0;
+        a.bounds[1] = before + (int)__popcll((long long)who);
+    }
+    if (!a.scale || blockIdx.x != 0) return;
+    // In f16 the products read g times a power of two that brings the largest weight next to 2^15: the small probabilities of most
+    // of a vocabulary, under weights of one by the number of rows, would vanish.
+    float most = 0.0f;
+    if (a.weight)
+        for (int64_t j = tid; j < a.rows; j += kRowThreads) most = counts_at(j) ? fmaxf(most, fabsf(a.weight[j])) : most;
+    most = wave_all(most, MaxOf());
+    if (lane == 0) share[wave] = most;
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, share[w]);
+        if (!a.weight) most = 1.0f;
+        const int e = most > 0.0f && most < kInfinity ? 14 - ilogbf(most) : 0, by = a.half ? (e < 100 ? e : 100) : 0;
+        a.scale[0] = ldexpf(1.0f, by);
+        a.scale[1] = ldexpf(1.0f, -by);
+    }
+}
+
+// The loss: of every row of a tile the largest logit and the sum of exponentials under it; and the label's logit, from the tile
+// that has it.
+struct Statistics {
+    static constexpr bool kParts = false;
+    static constexpr unsigned parts() { return 1; }
+    const int32_t *label;
+    float2 *partial;               // [tiles of columns][rows]
+    int64_t rows;
+    float *at_label;
+    template <typename Tile>
+    __device__ void end(const ProductArgs &a, const Place &at, v4f (&acc)[Tile::kFragM][Tile::kFragN], char *stage0, char *) const
+    {
+        const int lane = lane_id(), c0 = at.n0 + at.wn + lane / 16 * 4;
+        float2 *const share = reinterpret_cast<float2 *>(stage0);                  // [wavefronts along n][rows]
+        const bool whole = at.n0 + at.wn + Tile::kTileN <= a.n;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < Tile::kFragM; ++i) {
+            if (!whole) {
+#pragma unroll
+                for (int j = 0; j < Tile::kFragN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = c0 + j * 16 + e < a.n ? acc[i][j][e] : -kInfinity;
+            }
+            float top = -kInfinity;
+#pragma unroll
+            for (int j = 0; j < Tile::kFragN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][j][e]);
+            top = fmaxf(top, __shfl_xor(top, 16, NACHO_WAVE));
+            top = fmaxf(top, __shfl_xor(top, 32, NACHO_WAVE));
+            const float base = top == -kInfinity ? 0.0f : top;
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < Tile::kFragN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += exp2_of((acc[i][j][e] - base) * kLog2e);
+            sum += __shfl_xor(sum, 16, NACHO_WAVE);
+            sum += __shfl_xor(sum, 32, NACHO_WAVE);
+            const int r = at.wm + i * 16 + lane % 16;
+            const unsigned m = (unsigned)at.m0 + r;
+            const bool there = m < (unsigned)at.m_end;
+            const int c = there ? label[m] - c0 : -1;
+            if (__any(c >= 0 && c < Tile::kTileN)) {
+#pragma unroll
+                for (int j = 0; j < Tile::kFragN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c == j * 16 + e) at_label[m] = acc[i][j][e];
+            }
+            if (lane < 16) share[at.wn / Tile::kTileN * Tile::kTall + r] = make_float2(top, sum);
+        }
+        __syncthreads();
+        for (int r = (int)threadIdx.x; r < Tile::kTall; r += Tile::kThreads) {
+            const unsigned m = (unsigned)at.m0 + r;
+            if (m >= (unsigned)at.m_end) break;
+            float top = -kInfinity, sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < Tile::kColumns; ++w) top = fmaxf(top, share[w * Tile::kTall + r].x);
+#pragma unroll
+            for (int w = 0; w < Tile::kColumns; ++w) {
+                const float2 part = share[w * Tile::kTall + r];
+                sum += part.x == top ? part.y : part.y * exp2_of((part.x - top) * kLog2e);
+            }
+            partial[at.n0 / Tile::kWide * rows + m] = make_float2(top, sum);
+        }
+    }
+};
+
+// The tiles of a row: 16 rows a workgroup, 64 threads each.
+constexpr int kJoinRows = 16, kJoinParts = 64;
+__global__ void __launch_bounds__(kJoinRows *kJoinParts) xent_join_kernel(XentArgs a, int tiles)
+{
+    __shared__ float2 share[kJoinParts][kJoinRows];
+    const int r = (int)threadIdx.x % kJoinRows, part = (int)threadIdx.x / kJoinRows;
+    const int64_t m = (int64_t)blockIdx.x * kJoinRows + r, held = a.bounds[1];
+    if ((int64_t)blockIdx.x * kJoinRows >= held) return;
+    auto join = [](float2 x, float2 y) {
+        const float top = fmaxf(x.x, y.x);
+        const float sx = x.x == top ? x.y : x.y * exp2_of((x.x - top) * kLog2e), sy = y.x == top ? y.y : y.y * exp2_of((y.x - top) * kLog2e);
+        return make_float2(top, sx + sy);
+    };
+    float2 v = make_float2(-kInfinity, 0.0f);
+    if (m < held) {
+        constexpr int kBatch = 4;
+        for (int t = part; t < tiles; t += kBatch * kJoinParts) {
+            float2 next[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) next[i] = a.partial[(int64_t)(t + i * kJoinParts < tiles ? t + i * kJoinParts : t) * a.rows + m];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (t + i * kJoinParts < tiles) v = join(v, next[i]);
+        }
+    }
+    share[part][r] = v;
+    __syncthreads();
+    for (int half = kJoinParts / 2; half > 0; half /= 2) {
+        if (part < half) share[part][r] = join(share[part][r], share[part + half][r]);
+        __syncthreads();
+    }
+    if (part != 0 || m >= held) return;
+    v = share[0][r];
+    // (a row of nothing but -inf has no distribution)
+    const float lse = v.x == -kInfinity ? __builtin_nanf("") : v.x + logf(v.y);
+    const int64_t t = a.token[m];
+    a.lse[t] = lse;
+    a.loss[t] = (a.weight ? a.weight[t] : 1.0f) * (lse - a.at_label[m]);
+}
+
+// The gradient of a piece's logits, as rows of the type.
+struct Gradient {
+    static constexpr bool kParts = false;
+    static constexpr unsigned parts() { return 1; }
+    const int32_t *label;
+    const float *lse, *factor, *scale;
+    int32_t first;                 // the piece's first word of the vocabulary
+    template <typename Tile>
+    __device__ void end(const ProductArgs &a, const Place &at, v4f (&acc)[Tile::kFragM][Tile::kFragN], char *stage0, char *stage1) const
+    {
+        typedef typename Tile::type T;
+        const int lane = lane_id(), c0 = at.n0 + at.wn + lane / 16 * 4;
+        const float by = scale[0];
+        float l[Tile::kFragM], w[Tile::kFragM];
+        int c[Tile::kFragM];
+#pragma unroll
+        for (int i = 0; i < Tile::kFragM; ++i) {
+            const unsigned m = (unsigned)at.m0 + at.wm + i * 16 + lane % 16;
+            const unsigned row = m < (unsigned)at.m_end ? m : (unsigned)at.m_end - 1;
+            l[i] = lse[row];
+            w[i] = factor[row] * by;
+            c[i] = label[row] - first - c0;
+        }
+#pragma unroll
+        for (int i = 0; i < Tile::kFragM; ++i) {
+#pragma unroll
+            for (int j = 0; j < Tile::kFragN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = exp2_of((acc[i][j][e] - l[i]) * kLog2e);
+            if (__any(c[i] >= 0 && c[i] < Tile::kTileN)) {
+#pragma unroll
+                for (int j = 0; j < Tile::kFragN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] -= c[i] == j * 16 + e ? 1.0f : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < Tile::kFragN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] *= w[i];
+        }
+        // (rows of g are whole words of 8 elements: zeros behind the piece's last one)
+        T *const out = static_cast<T *>(a.out);
+        Tile::each_row(a, at, acc, stage0, stage1, [&](unsigned m, int n, int width, float (&v)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < width ? v[e] : 0.0f;
+            Tile::put(out + (int64_t)m * a.ldo + n, v, 8);
+        });
+    }
+};
+
+// Gradients of the rows: sums in 32 bits by stretches of the vocabulary, or, where there is one, the result itself.
+struct RowGradients {
+    static constexpr bool kParts = true;
+    unsigned parts() const { return stretches; }
+    unsigned stretches;
+    int k_part;
+    float *sums;                   // [stretches][rows][ld], or NULL
+    int64_t part_stride, ld;
+    bool first;                    // (the sums hold nothing yet)
+    const int32_t *token;
+    const float *scale;
+    template <typename Tile>
+    __device__ void end(const ProductArgs &a, const Place &at, v4f (&acc)[Tile::kFragM][Tile::kFragN], char *stage0, char *stage1) const
+    {
+        typedef typename Tile::type T;
+        if (sums) {
+            float *const to = sums + (int64_t)blockIdx.z * part_stride;
+            Tile::each_row(a, at, acc, stage0, stage1, [&](unsigned m, int n, int, float (&v)[8]) {
+                v4f *const p = reinterpret_cast<v4f *>(to + (int64_t)m * ld + n);
+                v4f lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
+                if (!first) {
+                    lo += p[0];
+                    hi += p[1];
+                }
+                p[0] = lo;
+                p[1] = hi;
+            });
+        } else {
+            const float by = scale[1];
+            T *const out = static_cast<T *>(a.out);
+            Tile::each_row(a, at, acc, stage0, stage1, [&](unsigned m, int n, int width, float (&v)[8]) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= by;
+                Tile::put(out + (int64_t)token[m] * a.ldo + n, v, width);
+            });
+        }
+    }
+};
+
+// Gradients of the vocabulary's weights, without the scale.
+struct HeadGradients {
+    static constexpr bool kParts = false;
+    static constexpr unsigned parts() { return 1; }
+    const float *scale;
+    int32_t last;                  // words of the piece (the rows of g may have more)
+    template <typename Tile>
+    __device__ void end(const ProductArgs &a, const Place &at, v4f (&acc)[Tile::kFragM][Tile::kFragN], char *stage0, char *stage1) const
+    {
+        typedef typename Tile::type T;
+        const float by = scale[1];
+        T *const out = static_cast<T *>(a.out);
+        Place mine = at;
+        mine.m_end = last;
+        Tile::each_row(a, mine, acc, stage0, stage1, [&](unsigned m, int n, int width, float (&v)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= by;
+            Tile::put(out + (int64_t)m * a.ldo + n, v, width);
+        });
+    }
+};
+
+// A row's gradient from its sums, zeros for a row that does not count (without sums: these alone).
+template <typename T> __global__ void __launch_bounds__(256) xent_row_gradients_kernel(XentArgs a, int stretches, int64_t part_stride, int64_t ld)
+{
+    const int64_t t = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (t >= a.rows) return;
+    const int slot = a.slot_of[t];
+    if (slot >= 0 && !a.sums) return;
+    const float by = a.scale[1];
+    T *const out = static_cast<T *>(a.grad_x) + t * a.ldgx;
+    for (int c = (int)threadIdx.x * 4; c < a.inner; c += 256 * 4) {
+        v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (slot >= 0)
+            for (int p = 0; p < stretches; ++p) v += *reinterpret_cast<const v4f *>(a.sums + (int64_t)p * part_stride + slot * ld + c);
+        if (c + 4 <= a.inner) {
+            typedef T four __attribute__((ext_vector_type(4)));
+            const four w = {(T)(v[0] * by), (T)(v[1] * by), (T)(v[2] * by), (T)(v[3] * by)};
+            __builtin_memcpy(out + c, &w, sizeof w);
+        } else {
+            for (int e = 0; c + e < a.inner; ++e) out[c + e] = (T)(v[e] * by);
+        }
+    }
+}
+
+int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
+
+ProductArgs logits_of(const XentArgs &a, int64_t first, int64_t words)
+{
+    const int elem = a.elem;
+    ProductArgs p{};
+    p.bounds = a.bounds;
+    p.token = a.token;
+    p.experts = 1;
+    p.n = (int32_t)words;
+    p.k = a.inner;
+    p.slots = a.rows;
+    p.q = a.x;
+    p.ldq = a.ldx;
+    p.p = static_cast<const char *>(a.head) + first * a.ldh * elem;
+    p.ldp = a.ldh;
+    return p;
+}
+Access access_logits(const XentArgs &a)
+{
+    const bool words = a.ldx < 0x7fffffff && a.ldh < 0x7fffffff && in_words({{a.x, a.ldx}, {a.head, a.ldh}, {a.x, a.inner}}, a.elem);
+    return words ? WORDS : a.inner * a.elem < 16 ? TINY : ANYWHERE;
+}
+
+template <typename T> Shape shape_of_logits(const XentArgs &a, int64_t words) { return shape_of<T, FORWARD>(logits_of(a, 0, words), access_logits(a)); }
+
+// (the rows' access is not known where workspaces are sized: the narrowest tiles there can be)
+int64_t tiles_of_loss(int elem, int64_t vocabulary) { return (vocabulary + (elem == 4 ? 63 : 127)) / (elem == 4 ? 64 : 128); }
+
+hipError_t list_rows(const XentArgs &a, hipStream_t s)
+{
+    const int64_t groups = a.rows > 0 ? (a.rows + kRowThreads - 1) / kRowThreads : 1;
+    if (a.label_bytes == 8) xent_rows_kernel<int64_t><<<(unsigned)groups, kRowThreads, 0, s>>>(a);
+    else xent_rows_kernel<int32_t><<<(unsigned)groups, kRowThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary) { return tiles_of_loss(elem, vocabulary) * rows; }
+
+// The pieces of the vocabulary: g of one takes at most 256 MiB (which the last cache holds), or 256 words of it.
+XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner)
+{
+    constexpr int64_t kRoom = 256 << 20;
+    XentPlan p;
+    const int64_t most = rows > 0 ? kRoom / (rows * elem) / 256 * 256 : vocabulary, least = most > 256 ? most : 256;
+    p.pieces = (vocabulary + least - 1) / least;
+    p.words = p.pieces > 1 ? ((vocabulary + p.pieces - 1) / p.pieces + 255) / 256 * 256 : vocabulary;
+    p.pieces = (vocabulary + p.words - 1) / p.words;
+    p.ldg = padded(p.words);
+    // stretches of a piece, where its rows alone are too few tiles for the chip
+    const int64_t tall = rows >= 256 && elem == 2 ? 256 : rows > 32 ? 64 : 32, wide = rows >= 256 && elem == 2 ? 256 : rows > 32 ? 64 : 128;
+    const int64_t tiles = ((rows + tall - 1) / tall) * ((inner + wide - 1) / wide), wanted = tiles > 0 ? 2 * kUnits / tiles : 1;
+    const int64_t longest = (p.words + 1023) / 1024;
+    p.stretches = wanted < longest ? wanted : longest;
+    if (p.stretches < 1) p.stretches = 1;
+    p.k_part = ((p.words + p.stretches - 1) / p.stretches + 127) / 128 * 128;
+    p.stretches = (p.words + p.k_part - 1) / p.k_part;
+    p.lds = padded(inner);
+    p.sums = p.pieces > 1 || p.stretches > 1;
+    return p;
+}
+
+hipError_t launch_xent(int dtype, const XentArgs &a, hipStream_t s)
+{
+    if (a.rows == 0) return hipSuccess;
+    if (const hipError_t e = list_rows(a, s)) return e;
+    hipError_t rc = hipSuccess;
+    by_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        const ProductArgs p = logits_of(a, 0, a.vocabulary);
+        const int wide = wide_of(shape_of_logits<T>(a, a.vocabulary));
+        rc = by_size<T, FORWARD>(p, Statistics{a.slot_label, a.partial, a.rows, a.at_label}, access_logits(a), s);
+        if (rc != hipSuccess) return;
+        xent_join_kernel<<<(unsigned)((a.rows + kJoinRows - 1) / kJoinRows), kJoinRows * kJoinParts, 0, s>>>(a, (int)((a.vocabulary + wide - 1) / wide));
+        rc = hipGetLastError();
+    });
+    return rc;
+}
+
+hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s)
+{
+    hipError_t rc = list_rows(a, s);
+    if (rc != hipSuccess) return rc;
+    const int elem = a.elem;
+    const bool head_words = a.ldh < 0x7fffffff && in_words({{a.head, a.ldh}, {a.head, a.inner}}, elem);
+    const bool x_words = a.ldx < 0x7fffffff && in_words({{a.x, a.ldx}, {a.x, a.inner}}, elem);
+    by_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        for (int64_t first = 0; first < a.vocabulary; first += plan.words) {
+            const int64_t words = a.vocabulary - first < plan.words ? a.vocabulary - first : plan.words;
+            ProductArgs p = logits_of(a, first, words);
+            p.out = a.g;
+            p.ldo = plan.ldg;
+            rc = by_size<T, FORWARD>(p, Gradient{a.slot_label, a.slot_lse, a.factor, a.scale, (int32_t)first}, access_logits(a), s);
+            if (rc != hipSuccess) return;
+            if (a.grad_x) {
+                p = ProductArgs{};
+                p.bounds = a.bounds;
+                p.experts = 1;
+                p.n = a.inner;
+                p.k = (int32_t)words;
+                p.slots = a.rows;
+                p.q = a.g;
+                p.ldq = plan.ldg;
+                p.p = static_cast<const T *>(a.head) + first * a.ldh;
+                p.ldp = a.ldh;
+                p.out = a.grad_x;
+                p.ldo = a.ldgx;
+                const unsigned stretches = (unsigned)((words + plan.k_part - 1) / plan.k_part);
+                const bool in = head_words && plan.ldg < 0x7fffffff && (plan.sums || in_words({{a.grad_x, a.ldgx}}, elem));
+                rc = by_size<T, ROWS>(p, RowGradients{stretches, (int)plan.k_part, plan.sums ? a.sums : nullptr, a.rows * plan.lds, plan.lds, first == 0, a.token, a.scale},
+                                      in ? WORDS : access_of<ROWS>(p, elem), s);
+                if (rc != hipSuccess) return;
+            }
+            if (a.grad_head) {
+                p = ProductArgs{};
+                p.bounds = a.bounds;
+                p.token = a.token;
+                p.experts = 1;
+                p.n = a.inner;
+                p.slots = a.rows;
+                p.q = a.g;
+                p.ldq = plan.ldg;
+                p.p = a.x;
+                p.ldp = a.ldx;
+                p.out = static_cast<T *>(a.grad_head) + first * a.ldgh;
+                p.ldo = a.ldgh;
+                const bool in = x_words && plan.ldg < 0x7fffffff && in_words({{a.grad_head, a.ldgh}}, elem);
+                p.m = (int32_t)(in ? padded(words) : words);
+                rc = by_size<T, WEIGHTS>(p, HeadGradients{a.scale, (int32_t)words}, in ? WORDS : access_of<WEIGHTS>(p, elem), s);
+                if (rc != hipSuccess) return;
+            }
+        }
+        if (a.grad_x && a.rows > 0) {
+            XentArgs b = a;
+            if (!plan.sums) b.sums = nullptr;
+            const int64_t row = a.rows < (1 << 22) ? a.rows : 1 << 22;
+            xent_row_gradients_kernel<T><<<dim3((unsigned)row, (unsigned)((a.rows + row - 1) / row)), 256, 0, s>>>(
+                b, (int)plan.stretches, a.rows * plan.lds, plan.lds);
+            rc = hipGetLastError();
+        }
+    });
+    return rc;
+}
+
+}  // namespace nacho

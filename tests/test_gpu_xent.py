@@ -1,0 +1,248 @@
+"""nacho_xent, nacho_xent_grad against the definition in 64 bits.
+
+Tolerances: a logit, a sum of n products held in 32 bits, is within dz = (n + 8) 2^-24 of the sum of their magnitudes.  An lse is off
+by the largest dz of its row, 2^-21 for the exponentials (an argument and an instruction of 2^-22 each where a share is not
+negligible), 2^-24 for every step of a sum (64 in a tile, then the tiles of a row), and two roundings of itself.  Of the gradient's
+g = w (q - [label]) the share q is off by dz, the lse's error, 2^-21 + |z - lse| 2^-22 of itself; g is then rounded to the type (f16:
+at a scale that leaves 2^-38 of the largest weight).  A share below 2^-126, the smallest normal number of 32 bits, is 0: the
+exponential's instruction makes nothing smaller, so q is off by as much.  Products of g are sums as above; results are rounded to the type once."""
+import pytest
+import torch
+
+from paper_2604_17198_amd import binding as nb
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+F32 = 2.0 ** -24
+
+
+def apart(t, pad):
+    """The same values in rows `pad` elements further apart, the gaps filled with NaN."""
+    wide = torch.full((t.shape[0], t.shape[1] + pad), float("nan"), dtype=t.dtype, device=t.device)
+    wide[:, :t.shape[1]] = t
+    return wide[:, :t.shape[1]]
+
+
+def problem(seed, rows, vocabulary, inner, dtype, weighted=True, masked=0.0, size=2.0, pad=0, label=torch.int64):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    new = lambda *shape: torch.randn(shape, generator=g, device="cuda", dtype=torch.float32)
+    labels = torch.randint(0, vocabulary, (rows,), generator=g, device="cuda", dtype=label)
+    labels[torch.rand(rows, generator=g, device="cuda") < masked] = -100
+    d = dict(x=new(rows, inner).to(dtype), head=(new(vocabulary, inner) * size * inner ** -0.5).to(dtype), label=labels,
+             weight=0.25 + torch.rand(rows, generator=g, device="cuda") if weighted else None)
+    if pad:
+        d["x"], d["head"] = apart(d["x"], pad), apart(d["head"], pad)
+    return d
+
+
+def definition(d, dtype):
+    """Results in 64 bits and by how much they may be off: {name: (value, room)}."""
+    x, w = d["x"].double(), d["head"].double()
+    rows, vocabulary, inner = x.shape[0], w.shape[0], x.shape[1]
+    weight = d["weight"].double() if d["weight"] is not None else torch.ones(rows, dtype=torch.float64, device="cuda")
+    held = (d["label"] >= 0) & (d["label"] < vocabulary) & (weight != 0)
+    x, weight = torch.where(held[:, None], x, torch.zeros_like(x)), torch.where(held, weight, torch.zeros_like(weight))
+    at = torch.where(held, d["label"], torch.zeros_like(d["label"])).long()[:, None]
+    z, dz = x @ w.t().contiguous(), (inner + 8) * F32 * (x.abs() @ w.abs().t().contiguous())
+    lse = torch.logsumexp(z, dim=1)
+    d_lse = dz.max(dim=1)[0] + 2.0 ** -21 + (64 + vocabulary / 2048) * F32 + 2 * F32 * lse.abs()
+    zl, dzl = torch.gather(z, 1, at)[:, 0], torch.gather(dz, 1, at)[:, 0]
+    out = dict(lse=(torch.where(held, lse, 0.0), d_lse),
+               loss=(weight * (lse - zl), weight.abs() * (d_lse + dzl + 4 * F32 * (lse - zl).abs() + 2 * F32 * (lse.abs() + zl.abs()))))
+    q = torch.exp(z - lse[:, None])
+    g = q.scatter_add(1, at, -torch.ones_like(zl)[:, None]) * weight[:, None]
+    half = 0.0 if dtype is torch.float32 else HALF[dtype]
+    dg = weight.abs()[:, None] * (q * (dz + d_lse[:, None] + 2.0 ** -21 + 2.0 ** -22 * (z - lse[:, None]).abs()) + 2 * F32 * g.abs() + 2 * F32 * q + 2.0 ** -126)
+    dg = dg + half * (g.abs() + dg) + (2.0 ** -38 * weight.abs().max() * held[:, None] if dtype is torch.float16 and rows else 0.0)
+    tiny = 2.0 ** -25 * (dtype is torch.float16)
+    for name, a, da, b in (("grad_x", g, dg, w), ("grad_head", g.t().contiguous(), dg.t().contiguous(), x)):
+        value, size = a @ b, a.abs() @ b.abs()
+        room = da @ b.abs() + (b.shape[0] + 16) * F32 * size
+        out[name] = (value, room + HALF[dtype] * (value.abs() + room) + tiny)
+    return out
+
+
+def close(got, want, name):
+    value, room = want
+    over = ((got.double() - value).abs() - room).max() if got.numel() else torch.zeros(())
+    assert bool(((got.double() - value).abs() <= room).all()), (name, float(over))
+
+
+def check(d, dtype, pad=0):
+    rows, inner = d["x"].shape
+    vocabulary = d["head"].shape[0]
+    loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+    gx = torch.full((rows + 1, inner + pad), 7.0, dtype=dtype, device="cuda")
+    gh = torch.full((vocabulary + 1, inner + pad), 7.0, dtype=dtype, device="cuda")
+    nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, weight=d["weight"], grad_x=gx[:rows, :inner], grad_head=gh[:vocabulary, :inner])
+    want = definition(d, dtype)
+    close(lse, want["lse"], "lse")
+    close(loss, want["loss"], "loss")
+    close(gx[:rows, :inner], want["grad_x"], "grad_x")
+    close(gh[:vocabulary, :inner], want["grad_head"], "grad_head")
+    for t, n in ((gx, rows), (gh, vocabulary)):
+        assert bool((t[n:] == 7.0).all()) and bool((t[:, inner:] == 7.0).all())
+    again = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+    assert torch.equal(again[0], loss) and torch.equal(again[1], lse)
+    more = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, weight=d["weight"])
+    assert torch.equal(more[0], gx[:rows, :inner]) and torch.equal(more[1], gh[:vocabulary, :inner])
+
+
+SIZES = [(1, 1, 1), (1, 2, 8), (2, 3, 3), (3, 7, 5), (5, 300, 64), (31, 129, 40), (33, 1000, 96), (64, 513, 24), (130, 1003, 97), (257, 515, 72),
+         (300, 4100, 256), (2, 50_000, 128), (700, 33, 513), (1025, 130, 8), (2049, 264, 16)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sizes", SIZES)
+def test_against_the_definition(sizes, dtype):
+    seed = sum(sizes)
+    check(problem(seed, *sizes, dtype, weighted=seed % 3 != 0, masked=0.3 if seed % 2 else 0.0), dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sizes", [(2048, 8192, 64), (2100, 8200, 72), (4096, 2056, 320), (520, 16_384, 520)])
+def test_large_tiles(sizes, dtype):
+    check(problem(1, *sizes, dtype, masked=0.1), dtype)
+
+
+@pytest.mark.parametrize("dtype,rows", [(torch.float32, 8200), (torch.bfloat16, 8200), (torch.float16, 9001)])
+def test_pieces_of_the_vocabulary(dtype, rows):
+    """More rows than g of a whole vocabulary has room for."""
+    check(problem(2, rows, 20_003, 40, dtype, masked=0.2), dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pad", [1, 4, 8])
+def test_rows_apart(dtype, pad):
+    check(problem(3, 70, 333, 56, dtype, masked=0.2, pad=pad), dtype, pad)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("label", [torch.int32, torch.int64])
+def test_rows_that_do_not_count(dtype, label):
+    """Labels outside the vocabulary and weights of 0: zeros, whatever the rows hold, and the others as without them."""
+    d = problem(4, 1100, 200, 48, dtype, label=label)
+    out = torch.zeros(1100, dtype=torch.bool, device="cuda")
+    for i, l in ((0, -1), (7, 200), (64, -100), (500, 2 ** 31 - 1), (1023, -2 ** 31), (1024, 201), (1099, -5)):
+        d["label"][i] = l
+        out[i] = True
+    if label is torch.int64:
+        d["label"][8], out[8] = 2 ** 40 + 3, True
+    d["weight"][[1, 65, 1050]], out[[1, 65, 1050]] = 0.0, True
+    d["x"][out] = float("nan")
+    check(d, dtype)
+    loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+    gx, gh = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, weight=d["weight"])
+    assert bool((loss[out] == 0).all()) and bool((lse[out] == 0).all()) and bool((gx[out] == 0).all())
+    keep = ~out
+    few = nb.nacho_xent(d["x"][keep], d["head"], d["label"][keep], weight=d["weight"][keep])
+    assert torch.equal(few[0], loss[keep]) and torch.equal(few[1], lse[keep])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_no_row_counts(dtype):
+    d = problem(5, 40, 300, 64, dtype)
+    d["label"].fill_(-100)
+    d["x"].fill_(float("nan"))
+    loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"])
+    gx, gh = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse)
+    for t in (loss, lse, gx, gh):
+        assert bool((t == 0).all())
+    none = [t[:0] for t in (d["x"], d["label"])]
+    loss, lse = nb.nacho_xent(none[0], d["head"], none[1])
+    gx, gh = nb.nacho_xent_grad(none[0], d["head"], none[1], lse)
+    assert loss.shape == (0,) and gx.shape == (0, 64) and bool((gh == 0).all())
+
+
+def test_weights_of_many_sizes():
+    """f16 gradients under weights of one by a large number of rows, and under large ones: the probabilities do not vanish."""
+    for size in (2.0 ** -14, 1.0, 2.0 ** 9):
+        d = problem(6, 96, 2000, 64, torch.float16)
+        d["weight"] *= size
+        # (grad_head's values are f16 themselves: as many large ones as make them normal numbers)
+        d["head"] = d["head"] / max(1.0, size ** 0.5)
+        check(d, torch.float16)
+
+
+def test_not_a_number_and_infinities():
+    d = problem(7, 50, 300, 32, torch.float32)
+    clean = nb.nacho_xent(d["x"], d["head"], d["label"])
+    d["x"][3, 5], d["x"][9, 0] = float("nan"), float("inf")
+    loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"])
+    bad = torch.zeros(50, dtype=torch.bool, device="cuda")
+    bad[[3, 9]] = True
+    assert bool(loss[bad].isnan().all()) and bool(lse[bad].isnan().all())
+    assert torch.equal(loss[~bad], clean[0][~bad]) and torch.equal(lse[~bad], clean[1][~bad])
+    gx, gh = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse)
+    assert bool(gx[bad].isnan().all()) and not bool(gx[~bad].isnan().any()) and bool(gh.isnan().all())
+
+
+def test_logits_far_apart():
+    """Logits of thousands: the softmax is one column."""
+    d = problem(8, 20, 130, 16, torch.float32, size=2000.0)
+    check(d, torch.float32)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_that_are_not_wanted(dtype):
+    d = problem(9, 300, 700, 40, dtype, masked=0.2)
+    loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"])
+    both = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse)
+    one, none = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, grad_head=False)
+    assert none is None and torch.equal(one, both[0])
+    none, one = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, grad_x=False)
+    assert none is None and torch.equal(one, both[1])
+
+
+def test_gradients_against_differences():
+    """Central differences of the loss along random directions, in 32 bits.  With M the largest change of a row's logits along the
+    direction, the third derivative of its lse is at most 8 M^3; the losses themselves are off by `room`."""
+    d = problem(10, 40, 200, 48, torch.float32)
+    loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+    gx, gh = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, weight=d["weight"])
+    room = float(definition(d, torch.float32)["loss"][1].sum())
+    step = 2.0 ** -5
+    for name, grad in (("x", gx), ("head", gh)):
+        torch.manual_seed(1)
+        u = torch.randn_like(d[name]) / 8
+        change = u @ d["head"].T if name == "x" else d["x"] @ u.T
+        ends = []
+        for sign in (1, -1):
+            moved = {**d, name: d[name] + sign * step * u}
+            ends.append(nb.nacho_xent(moved["x"], moved["head"], d["label"], weight=d["weight"])[0].double().sum())
+        slope = float(ends[0] - ends[1]) / (2 * step)
+        third = 8 * float((d["weight"].double() * change.double().abs().max(dim=1)[0] ** 3).sum())
+        assert abs(slope - float((grad.double() * u.double()).sum())) <= third * step ** 2 / 6 + 2 * room / step
+
+
+def test_on_another_stream_and_under_captured_graphs():
+    d = problem(11, 400, 3000, 64, torch.bfloat16, masked=0.2)
+
+    def work():
+        loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+        return [loss, lse, *nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, weight=d["weight"])]
+
+    want = work()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = work()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graphs, results = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for graph in graphs:
+        with torch.cuda.graph(graph):
+            results.append(work())
+    for seed in range(4):
+        torch.manual_seed(seed)
+        d["x"].normal_()
+        d["label"].random_(-500, 3000)
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        eager = work()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for result in results:
+            assert all(torch.equal(a, b) for a, b in zip(result, eager))
