@@ -624,6 +624,42 @@ int32_t nacho_experts_step_workspace_bytes(const nacho_experts_step_layer *layer
 int32_t nacho_experts_step(const nacho_experts_step_layer *layer, void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
+ * nacho_keep8: rows kept for the way back in 8 bits, to be restored or read where the
+ * other rows are.  Every 32 columns of a row (the last ones may be fewer) share a step,
+ * 2^(e - 127), with e = floor(log2 of their largest magnitude) + 121, at least 0:
+ *   code      [n_rows x n] int8, leading dimension ldc: the nearest whole number of
+ *             steps, ties to even, -127 .. 127
+ *   exponent  [n_rows x ceil(n / 32)] bytes, leading dimension lde: e
+ * A value is off by half a step, a 128th of the largest of its 32 at most (by one step
+ * next to that one, where it has more than 127.5).  32 columns with a NaN or an
+ * infinity among them have e = 255, and are restored as NaN.
+ * nacho_restore8: the values that rows in 8 bits stand for, in a type; exact in BF16,
+ * and in F16 and F32 where these have the value.
+ *
+ * nacho_experts_keep8: nacho_experts with the rows before the activation left in 8 bits
+ * (from their sums in 32 bits).
+ * nacho_experts_keep8_grad: nacho_experts_grad with x, pre or both of them from rows in
+ * 8 bits (kept_x, kept_pre; NULL: those of layer and pre are read, as there): the
+ * gradients are those at what the codes stand for.  (relu's slope is 0 at a row that was
+ * kept as 0, up to half a step above it.)
+ * Workspace: nacho_experts_keep8_workspace_bytes (may be 0: then ws may be NULL).
+ */
+typedef struct {
+    int8_t *code;
+    int64_t ldc;
+    uint8_t *exponent;
+    int64_t lde;
+} nacho_kept;
+int32_t nacho_keep8(const void *x, int64_t ldx, int64_t n_rows, int64_t n, int32_t dtype, const nacho_kept *kept, void *hip_stream);
+int32_t nacho_restore8(const nacho_kept *kept, int64_t n_rows, int64_t n, int32_t dtype, void *out, int64_t ldo, void *hip_stream);
+int32_t nacho_experts_keep8(const nacho_experts_layer *layer, void *y, int64_t ldy, const nacho_kept *pre, void *hip_stream);
+int32_t nacho_experts_keep8_workspace_bytes(const nacho_experts_layer *layer, size_t *bytes);
+int32_t nacho_experts_keep8_grad(const nacho_experts_layer *layer, const nacho_kept *kept_x, const void *grad_y, int64_t ldgy,
+                                 const void *pre, int64_t ldpre, const nacho_kept *kept_pre, void *grad_x, int64_t ldgx, void *grad_w,
+                                 int64_t ldgw, int64_t gw_stride, void *grad_bias, int64_t gb_stride, void *ws, size_t ws_bytes,
+                                 void *hip_stream);
+
+/*
  * nacho_combine: for every token the weighted sum of its experts' rows,
  *   out[t] = residual[t] + sum_i val_i y[crd_i]   over the entries i of row t of
  *   routing   CSR [n_tokens x n_slots]: crd the slots, values F32 the gates (val

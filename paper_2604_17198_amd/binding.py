@@ -34,6 +34,7 @@ EXPORTS = [
     "nacho_combine_grad", "nacho_experts_workspace_bytes", "nacho_experts", "nacho_experts_grad",
     "nacho_experts_step_workspace_bytes", "nacho_experts_step",
     "nacho_xent_workspace_bytes", "nacho_xent", "nacho_xent_grad_workspace_bytes", "nacho_xent_grad",
+    "nacho_keep8", "nacho_restore8", "nacho_experts_keep8", "nacho_experts_keep8_workspace_bytes", "nacho_experts_keep8_grad",
 ]
 
 
@@ -85,6 +86,10 @@ class _StepLayer(C.Structure):
                 ("logits", C.c_void_p), ("ldl", C.c_int64), ("keep", C.c_void_p), ("x", C.c_void_p), ("ldx", C.c_int64),
                 ("up", _Dense), ("gate", _Dense), ("down", _Dense), ("residual", C.c_void_p), ("ldr", C.c_int64), ("out", C.c_void_p),
                 ("ldo", C.c_int64), ("top_k", C.c_int32), ("normalise", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32)]
+
+
+class _Kept(C.Structure):
+    _fields_ = [("code", C.c_void_p), ("ldc", C.c_int64), ("exponent", C.c_void_p), ("lde", C.c_int64)]
 
 
 class _XentLayer(C.Structure):
@@ -176,6 +181,13 @@ def lib():
         L.nacho_xent.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.nacho_xent_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t,
                                       C.c_void_p]
+        L.nacho_keep8.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]
+        L.nacho_restore8.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+        L.nacho_experts_keep8.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.nacho_experts_keep8_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+        L.nacho_experts_keep8_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                               C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t,
+                                               C.c_void_p]
         _libs[_instrumented] = L
         _lib = L
     return _lib
@@ -760,6 +772,53 @@ def nacho_route_grad(logits, routing: Routing, grad_gate=None, balance=0.0, keep
     return grad
 
 
+class Kept8:
+    """Rows kept in 8 bits: codes (int8 [rows, cols]) and the exponents of their steps (uint8 [rows, ceil(cols / 32)])."""
+
+    BLOCK = 32                                               # columns that share a step
+
+    def __init__(self, codes, exponent):
+        if codes.dim() != 2 or codes.dtype is not torch.int8 or exponent.dtype is not torch.uint8 or exponent.device != codes.device:
+            raise ValueError("Kept8: int8 codes [rows, cols] and uint8 exponents on one device are needed")
+        rows, cols = codes.shape
+        _matrix(exponent, "exponent", rows, -(-cols // self.BLOCK), torch.uint8, codes.device)
+        self.codes, self.exponent, self.shape, self.device = codes, exponent, codes.shape, codes.device
+
+    @classmethod
+    def empty(cls, rows, cols, device):
+        """Room for rows of cols columns (16 bytes from one row's codes to the next, or a multiple of them)."""
+        return cls(torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=device)[:, :cols],
+                   torch.empty((rows, -(-cols // cls.BLOCK)), dtype=torch.uint8, device=device))
+
+    def descriptor(self, what, rows=None, cols=None, device=None):
+        ldc = _matrix(self.codes, what, rows, cols, torch.int8, device)
+        return _Kept(self.codes.data_ptr(), ldc, self.exponent.data_ptr(), _matrix(self.exponent, what, None, None, torch.uint8, self.device))
+
+
+def nacho_keep8(x, out=None):
+    """The rows of x in 8 bits, as a Kept8."""
+    dt = model_dtype_code(x.dtype)
+    ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    if out is None:
+        out = Kept8.empty(rows, cols, x.device)
+    c = out.descriptor("out", rows, cols, x.device)
+    _check(lib().nacho_keep8(_ptr(x), ldx, rows, cols, dt, C.byref(c), _stream()), "nacho_keep8")
+    return out
+
+
+def nacho_restore8(kept: Kept8, dtype=torch.float32, out=None):
+    """The values that rows in 8 bits stand for."""
+    c = kept.descriptor("kept")
+    rows, cols = kept.shape
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype, device=kept.device)
+    dt = model_dtype_code(out.dtype)
+    ldo = _matrix(out, "out", rows, cols, out.dtype, kept.device)
+    _check(lib().nacho_restore8(C.byref(c), rows, cols, dt, _ptr(out), ldo, _stream()), "nacho_restore8")
+    return out
+
+
 _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
@@ -779,14 +838,15 @@ def _stack(t, what, shape, dtype, device):
 
 
 def _layer(x, weight, expert_pos, token, bias, act):
-    """The descriptor of a layer of experts, and its number of slots."""
-    dtype, dev = x.dtype, x.device
+    """The descriptor of a layer of experts, and its number of slots (x in 8 bits is not in it)."""
+    kept = type(x) is Kept8
+    dtype, dev = weight.dtype if kept else x.dtype, x.device
     dt = model_dtype_code(dtype)
     if weight.dim() != 3:
         raise ValueError("weight: [experts, outer, inner] is needed")
     shape = tuple(weight.shape)
     experts, outer, inner = shape
-    ldx = _matrix(x, "x", None, inner)
+    ldx = _matrix(x.codes if kept else x, "x", None, inner)
     ldw, stride = _stack(weight, "weight", shape, dtype, dev)
     _vector_of(expert_pos, "expert_pos", experts + 1, torch.int32, dev)
     bounds, tokens = expert_pos.data_ptr(), x.shape[0]
@@ -799,13 +859,14 @@ def _layer(x, weight, expert_pos, token, bias, act):
     if act not in _ACTS:
         raise ValueError(f"act: one of {', '.join(_ACTS)}")
     gap = _stack(bias, "bias", (experts, outer), dtype, dev)[1] if bias is not None else 0
-    return _ExpertsLayer(bounds, where, experts, slots, tokens, inner, outer, x.data_ptr(), ldx, weight.data_ptr(), ldw, stride,
+    return _ExpertsLayer(bounds, where, experts, slots, tokens, inner, outer, None if kept else x.data_ptr(), ldx, weight.data_ptr(), ldw, stride,
                          _ptr(bias), gap, _ACTS[act], dt), slots
 
 
 def nacho_experts(x, weight, expert_pos, token=None, bias=None, act="none", y=None, pre=None):
     """y[s] = act(x[token[s]] weight[e]^T + bias[e]) for the slots s = expert_pos[e] .. expert_pos[e+1] of every expert e
-    (expert_pos, token: a Routing's).  `pre`, when given, receives the rows before the activation."""
+    (expert_pos, token: a Routing's).  `pre`, when given, receives the rows before the activation (a Kept8: in 8 bits)."""
+    _need(type(x) is not Kept8, "x: rows in 8 bits are for the way back")
     c, slots = _layer(x, weight, expert_pos, token, bias, act)
     outer = c.outer
     if y is None:
@@ -813,6 +874,10 @@ def nacho_experts(x, weight, expert_pos, token=None, bias=None, act="none", y=No
         ldy = outer
     else:
         ldy = _matrix(y, "y", slots, outer, x.dtype, x.device)
+    if type(pre) is Kept8:
+        kept = pre.descriptor("pre", slots, outer, x.device)
+        _check(lib().nacho_experts_keep8(C.byref(c), _ptr(y), ldy, C.byref(kept), _stream()), "nacho_experts_keep8")
+        return y
     ldpre = _matrix(pre, "pre", slots, outer, x.dtype, x.device) if pre is not None else 0
     _check(lib().nacho_experts(C.byref(c), _ptr(y), ldy, _ptr(pre), ldpre, _stream()), "nacho_experts")
     return y
@@ -821,30 +886,34 @@ def nacho_experts(x, weight, expert_pos, token=None, bias=None, act="none", y=No
 def nacho_experts_grad(grad_y, x, weight, expert_pos, token=None, act="none", pre=None, grad_x=None, grad_weight=None,
                        grad_bias=None, ws=None):
     """(gradient of every slot's row of x, gradient of the weights); `grad_bias`, when given, receives the biases'.  A
-    `grad_x` or `grad_weight` that is False is not wanted: it is not computed, and None is returned."""
+    `grad_x` or `grad_weight` that is False is not wanted: it is not computed, and None is returned.  x, pre or both may be rows
+    kept in 8 bits (Kept8)."""
     c, slots = _layer(x, weight, expert_pos, token, None, act)
     experts, outer, inner = weight.shape
     dev = x.device
-    ldgy = _matrix(grad_y, "grad_y", slots, outer, x.dtype, dev)
-    ldpre = _matrix(pre, "pre", slots, outer, x.dtype, dev) if pre is not None else 0
+    kept_x, kept_pre, dtype = type(x) is Kept8, type(pre) is Kept8, weight.dtype
+    ldgy = _matrix(grad_y, "grad_y", slots, outer, dtype, dev)
+    ldpre = _matrix(pre, "pre", slots, outer, dtype, dev) if pre is not None and not kept_pre else 0
     if grad_x is False:
         grad_x = None
     elif grad_x is None:
-        grad_x = torch.empty((slots, inner), dtype=x.dtype, device=dev)
+        grad_x = torch.empty((slots, inner), dtype=dtype, device=dev)
     if grad_weight is False:
         grad_weight = None
     elif grad_weight is None:
-        grad_weight = torch.empty((experts, outer, inner), dtype=x.dtype, device=dev)
-    ldgx = _matrix(grad_x, "grad_x", slots, inner, x.dtype, dev) if grad_x is not None else 0
-    ldgw, gap = _stack(grad_weight, "grad_weight", (experts, outer, inner), x.dtype, dev) if grad_weight is not None else (0, 0)
-    gb = _stack(grad_bias, "grad_bias", (experts, outer), x.dtype, dev)[1] if grad_bias is not None else 0
-    if ws is None:
-        n = C.c_size_t(0)
-        _check(lib().nacho_experts_workspace_bytes(C.byref(c), C.byref(n)), "nacho_experts_workspace_bytes")
-        room = n.value
-        ws = _workspace(room, dev) if room else None
-    else:
-        room = _room(ws, dev)
+        grad_weight = torch.empty((experts, outer, inner), dtype=dtype, device=dev)
+    ldgx = _matrix(grad_x, "grad_x", slots, inner, dtype, dev) if grad_x is not None else 0
+    ldgw, gap = _stack(grad_weight, "grad_weight", (experts, outer, inner), dtype, dev) if grad_weight is not None else (0, 0)
+    gb = _stack(grad_bias, "grad_bias", (experts, outer), dtype, dev)[1] if grad_bias is not None else 0
+    if kept_x or kept_pre:
+        cx = x.descriptor("x", None, inner, dev) if kept_x else None
+        cp = pre.descriptor("pre", slots, outer, dev) if kept_pre else None
+        ws, room = _room_for("nacho_experts_keep8_workspace_bytes", c, ws, dev)
+        _check(lib().nacho_experts_keep8_grad(C.byref(c), C.byref(cx) if kept_x else None, _ptr(grad_y), ldgy, None if kept_pre else _ptr(pre), ldpre,
+                                              C.byref(cp) if kept_pre else None, _ptr(grad_x), ldgx, _ptr(grad_weight), ldgw, gap,
+                                              _ptr(grad_bias), gb, _ptr(ws), room, _stream()), "nacho_experts_keep8_grad")
+        return grad_x, grad_weight
+    ws, room = _room_for("nacho_experts_workspace_bytes", c, ws, dev)
     _check(lib().nacho_experts_grad(C.byref(c), _ptr(grad_y), ldgy, _ptr(pre), ldpre, _ptr(grad_x), ldgx, _ptr(grad_weight),
                                     ldgw, gap, _ptr(grad_bias), gb, _ptr(ws), room, _stream()),
            "nacho_experts_grad")

@@ -189,18 +189,30 @@ Array w_of(const nacho_experts_layer *l, int64_t elem)
 Array bounds_of(const nacho_experts_layer *l) { return {l->expert_pos, l->n_experts * 4 + 4}; }
 Array token_of(const nacho_experts_layer *l) { return {l->token, l->n_slots * 4}; }
 
-// What a gradient call keeps: the gradient before the activation, and sums of its rows.
+// Rows in 8 bits of a call, or NULL.
+bool check_kept(const nacho_kept *k, int64_t rows, int64_t cols)
+{
+    return !k || (matrix(k->code, rows, cols, k->ldc, 1) && matrix(k->exponent, rows, (cols + 31) / 32, k->lde, 1));
+}
+Array codes_of(const nacho_kept *k, int64_t rows, int64_t cols) { return {k ? k->code : nullptr, k ? span(rows, cols, k->ldc, 1) : 0}; }
+Array exponents_of(const nacho_kept *k, int64_t rows, int64_t cols)
+{
+    return {k ? k->exponent : nullptr, k ? span(rows, (cols + 31) / 32, k->lde, 1) : 0};
+}
+
+// What a gradient call keeps: the gradient before the activation, sums of its rows, and x restored from 8 bits.
 struct GradWs {
-    void *grad_z;
+    void *grad_z, *x;
     float *sums;
     size_t bytes;
 };
-GradWs carve_grad(void *ws, const nacho_experts_layer *l, bool grad_z, bool sums)
+GradWs carve_grad(void *ws, const nacho_experts_layer *l, bool grad_z, bool sums, bool x)
 {
     Slices c(ws);
     GradWs w{};
     if (grad_z) w.grad_z = c.take<char>(l->n_slots * ((l->outer + 7) / 8 * 8) * value_bytes(l->dtype));
     if (sums) w.sums = c.take<float>(experts_slope_tiles(l->n_slots, l->n_experts) * l->outer);
+    if (x) w.x = c.take<char>(l->n_tokens * ((l->inner + 7) / 8 * 8) * value_bytes(l->dtype));
     w.bytes = align_up(c.off, 256);
     return w;
 }
@@ -295,6 +307,97 @@ size_t carve_step(void *ws, const nacho_experts_step_layer *l, StepArgs *a)
     a->partial = c.take<float>(a->parts > 1 ? (int64_t)a->tiles * a->parts * l->n_tokens * 16 : 0);
     a->arrived = c.take<int32_t>(a->tiles);
     return align_up(c.off, 256);
+}
+
+int32_t experts_forward(const nacho_experts_layer *layer, void *y, int64_t ldy, void *pre, int64_t ldpre, const nacho_kept *kept, void *hip_stream)
+{
+    const int32_t rc = check_layer(layer);
+    if (rc != NACHO_OK) return rc;
+    const nacho_experts_layer &l = *layer;
+    const int64_t elem = value_bytes(l.dtype), bytes = span(l.n_slots, l.outer, ldy, elem);
+    if (!check_x(layer, elem) || !check_w(layer, elem) || !matrix(y, l.n_slots, l.outer, ldy, elem)) return NACHO_ERR_INVALID_ARG;
+    if (l.bias && !matrices(l.bias, l.n_experts, 1, l.outer, l.outer, l.bias_stride, elem)) return NACHO_ERR_INVALID_ARG;
+    if ((pre && !matrix(pre, l.n_slots, l.outer, ldpre, elem)) || !check_kept(kept, l.n_slots, l.outer)) return NACHO_ERR_INVALID_ARG;
+    if (!apart({{y, bytes}, {pre, pre ? span(l.n_slots, l.outer, ldpre, elem) : 0}, codes_of(kept, l.n_slots, l.outer), exponents_of(kept, l.n_slots, l.outer)},
+               {x_of(layer, elem), w_of(layer, elem), bounds_of(layer), token_of(layer),
+                {l.bias, l.bias ? span(l.n_experts, 1, l.outer, l.outer, l.bias_stride, elem) : 0}}))
+        return NACHO_ERR_INVALID_ARG;
+    const ProductArgs a{l.expert_pos, l.token, (int32_t)l.n_experts, 0, (int32_t)l.outer, (int32_t)l.inner, l.n_slots, l.x, l.w,
+                        l.ldx, l.ldw, l.w_stride, y, ldy, 0, l.bias, l.bias_stride, pre, ldpre, l.act};
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (const hipError_t e = kept ? launch_experts_forward_kept(l.dtype, a, *kept, s) : launch_experts_forward(l.dtype, a, s))
+        return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+    profile_mark("experts");
+    return NACHO_OK;
+}
+
+int32_t experts_backward(const nacho_experts_layer *layer, const nacho_kept *kept_x, const void *grad_y, int64_t ldgy, const void *pre,
+                         int64_t ldpre, const nacho_kept *kept_pre, void *grad_x, int64_t ldgx, void *grad_w, int64_t ldgw, int64_t gw_stride,
+                         void *grad_bias, int64_t gb_stride, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    const int32_t rc = check_layer(layer);
+    if (rc != NACHO_OK) return rc;
+    const nacho_experts_layer &l = *layer;
+    const int64_t elem = value_bytes(l.dtype), gy_bytes = span(l.n_slots, l.outer, ldgy, elem);
+    const bool slope = l.act != NACHO_ACT_NONE;
+    if (!matrix(grad_y, l.n_slots, l.outer, ldgy, elem) || (slope && !kept_pre && !matrix(pre, l.n_slots, l.outer, ldpre, elem)) ||
+        !check_kept(kept_pre, l.n_slots, l.outer) || !check_kept(kept_x, l.n_tokens, l.inner) || (grad_x && !check_w(layer, elem)) ||
+        (grad_w && !kept_x && !check_x(layer, elem)))
+        return NACHO_ERR_INVALID_ARG;
+    const int64_t pre_bytes = slope && !kept_pre ? span(l.n_slots, l.outer, ldpre, elem) : 0;
+    const int64_t gx_bytes = grad_x ? span(l.n_slots, l.inner, ldgx, elem) : 0;
+    const int64_t gw_bytes = grad_w ? span(l.n_experts, l.outer, l.inner, ldgw, gw_stride, elem) : 0;
+    const int64_t gb_bytes = grad_bias ? span(l.n_experts, 1, l.outer, l.outer, gb_stride, elem) : 0;
+    if ((grad_x && !matrix(grad_x, l.n_slots, l.inner, ldgx, elem)) ||
+        (grad_w && !matrices(grad_w, l.n_experts, l.outer, l.inner, ldgw, gw_stride, elem)) ||
+        (grad_bias && !matrices(grad_bias, l.n_experts, 1, l.outer, l.outer, gb_stride, elem)))
+        return NACHO_ERR_INVALID_ARG;
+    const bool products = grad_x || grad_w;
+    const GradWs w = carve_grad(ws, layer, slope && products, grad_bias != nullptr, kept_x && grad_w);
+    if (w.bytes > 0 && (!ws || ws_bytes < w.bytes || !aligned(ws, 16))) return NACHO_ERR_WORKSPACE;
+    if (!apart({{grad_x, gx_bytes}, {grad_w, gw_bytes}, {grad_bias, gb_bytes}, {ws, (int64_t)w.bytes}},
+               {kept_x ? Array{nullptr, 0} : x_of(layer, elem), w_of(layer, elem), bounds_of(layer), token_of(layer), {grad_y, gy_bytes}, {pre, pre_bytes},
+                codes_of(kept_x, l.n_tokens, l.inner), exponents_of(kept_x, l.n_tokens, l.inner), codes_of(kept_pre, l.n_slots, l.outer),
+                exponents_of(kept_pre, l.n_slots, l.outer)}))
+        return NACHO_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    const void *gz = grad_y;
+    int64_t ldgz = ldgy;
+    if ((slope && products) || grad_bias) {
+        SlopeArgs a{l.expert_pos, (int32_t)l.n_experts, (int32_t)l.outer, l.act, l.n_slots, grad_y, pre, ldgy, ldpre, nullptr, 0,
+                    grad_bias, gb_stride, w.sums, slope && kept_pre ? *kept_pre : nacho_kept{}};
+        if (slope && products) {
+            gz = a.grad_z = w.grad_z;
+            ldgz = a.ldgz = (l.outer + 7) / 8 * 8;
+        }
+        if (const hipError_t e = launch_experts_slope(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+        profile_mark("experts_slope");
+    }
+    if (grad_x) {
+        const ProductArgs a{l.expert_pos, nullptr, (int32_t)l.n_experts, 0, (int32_t)l.inner, (int32_t)l.outer, l.n_slots, gz, l.w,
+                            ldgz, l.ldw, l.w_stride, grad_x, ldgx, 0, nullptr, 0, nullptr, 0, NACHO_ACT_NONE};
+        if (const hipError_t e = launch_experts_rows(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+        profile_mark("experts_rows");
+    }
+    if (grad_w) {
+        const void *x = l.x;
+        int64_t ldx = l.ldx;
+        if (kept_x) {
+            // (the matrix units take the type, so x is restored first, exactly)
+            ldx = (l.inner + 7) / 8 * 8;
+            x = w.x;
+            if (const hipError_t e = launch_restore(l.dtype, KeepArgs{nullptr, w.x, ldx, l.n_tokens, (int32_t)l.inner, *kept_x}, s))
+                return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+            profile_mark("restore8");
+        }
+        const ProductArgs a{l.expert_pos, l.token, (int32_t)l.n_experts, (int32_t)l.outer, (int32_t)l.inner, 0, l.n_slots, gz, x,
+                            ldgz, ldx, 0, grad_w, ldgw, gw_stride, nullptr, 0, nullptr, 0, NACHO_ACT_NONE};
+        if (const hipError_t e = launch_experts_weights(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+        profile_mark("experts_weights");
+    }
+    return NACHO_OK;
 }
 
 }  // namespace
@@ -461,85 +564,71 @@ int32_t nacho_experts_workspace_bytes(const nacho_experts_layer *layer, size_t *
 {
     if (!bytes) return NACHO_ERR_INVALID_ARG;
     const int32_t rc = check_layer(layer);
-    if (rc == NACHO_OK) *bytes = carve_grad(nullptr, layer, layer->act != NACHO_ACT_NONE, true).bytes;
+    if (rc == NACHO_OK) *bytes = carve_grad(nullptr, layer, layer->act != NACHO_ACT_NONE, true, false).bytes;
     return rc;
 }
 
 int32_t nacho_experts(const nacho_experts_layer *layer, void *y, int64_t ldy, void *pre, int64_t ldpre, void *hip_stream)
 {
-    const int32_t rc = check_layer(layer);
-    if (rc != NACHO_OK) return rc;
-    const nacho_experts_layer &l = *layer;
-    const int64_t elem = value_bytes(l.dtype), bytes = span(l.n_slots, l.outer, ldy, elem);
-    if (!check_x(layer, elem) || !check_w(layer, elem) || !matrix(y, l.n_slots, l.outer, ldy, elem)) return NACHO_ERR_INVALID_ARG;
-    if (l.bias && !matrices(l.bias, l.n_experts, 1, l.outer, l.outer, l.bias_stride, elem)) return NACHO_ERR_INVALID_ARG;
-    if (pre && !matrix(pre, l.n_slots, l.outer, ldpre, elem)) return NACHO_ERR_INVALID_ARG;
-    if (!apart({{y, bytes}, {pre, pre ? span(l.n_slots, l.outer, ldpre, elem) : 0}},
-               {x_of(layer, elem), w_of(layer, elem), bounds_of(layer), token_of(layer),
-                {l.bias, l.bias ? span(l.n_experts, 1, l.outer, l.outer, l.bias_stride, elem) : 0}}))
-        return NACHO_ERR_INVALID_ARG;
-    const ProductArgs a{l.expert_pos, l.token, (int32_t)l.n_experts, 0, (int32_t)l.outer, (int32_t)l.inner, l.n_slots, l.x, l.w,
-                        l.ldx, l.ldw, l.w_stride, y, ldy, 0, l.bias, l.bias_stride, pre, ldpre, l.act};
-    hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    profile_begin(s);
-    if (const hipError_t e = launch_experts_forward(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
-    profile_mark("experts");
-    return NACHO_OK;
+    return experts_forward(layer, y, ldy, pre, ldpre, nullptr, hip_stream);
 }
 
 int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y, int64_t ldgy, const void *pre, int64_t ldpre,
                            void *grad_x, int64_t ldgx, void *grad_w, int64_t ldgw, int64_t gw_stride, void *grad_bias,
                            int64_t gb_stride, void *ws, size_t ws_bytes, void *hip_stream)
 {
-    const int32_t rc = check_layer(layer);
-    if (rc != NACHO_OK) return rc;
-    const nacho_experts_layer &l = *layer;
-    const int64_t elem = value_bytes(l.dtype), gy_bytes = span(l.n_slots, l.outer, ldgy, elem);
-    const bool slope = l.act != NACHO_ACT_NONE;
-    if (!matrix(grad_y, l.n_slots, l.outer, ldgy, elem) || (slope && !matrix(pre, l.n_slots, l.outer, ldpre, elem)) ||
-        (grad_x && !check_w(layer, elem)) || (grad_w && !check_x(layer, elem)))
-        return NACHO_ERR_INVALID_ARG;
-    const int64_t pre_bytes = slope ? span(l.n_slots, l.outer, ldpre, elem) : 0;
-    const int64_t gx_bytes = grad_x ? span(l.n_slots, l.inner, ldgx, elem) : 0;
-    const int64_t gw_bytes = grad_w ? span(l.n_experts, l.outer, l.inner, ldgw, gw_stride, elem) : 0;
-    const int64_t gb_bytes = grad_bias ? span(l.n_experts, 1, l.outer, l.outer, gb_stride, elem) : 0;
-    if ((grad_x && !matrix(grad_x, l.n_slots, l.inner, ldgx, elem)) ||
-        (grad_w && !matrices(grad_w, l.n_experts, l.outer, l.inner, ldgw, gw_stride, elem)) ||
-        (grad_bias && !matrices(grad_bias, l.n_experts, 1, l.outer, l.outer, gb_stride, elem)))
-        return NACHO_ERR_INVALID_ARG;
-    const bool products = grad_x || grad_w;
-    const GradWs w = carve_grad(ws, layer, slope && products, grad_bias != nullptr);
-    if (w.bytes > 0 && (!ws || ws_bytes < w.bytes || !aligned(ws, 16))) return NACHO_ERR_WORKSPACE;
-    if (!apart({{grad_x, gx_bytes}, {grad_w, gw_bytes}, {grad_bias, gb_bytes}, {ws, (int64_t)w.bytes}},
-               {x_of(layer, elem), w_of(layer, elem), bounds_of(layer), token_of(layer), {grad_y, gy_bytes}, {pre, pre_bytes}}))
-        return NACHO_ERR_INVALID_ARG;
+    return experts_backward(layer, nullptr, grad_y, ldgy, pre, ldpre, nullptr, grad_x, ldgx, grad_w, ldgw, gw_stride, grad_bias, gb_stride, ws,
+                            ws_bytes, hip_stream);
+}
+
+int32_t nacho_keep8(const void *x, int64_t ldx, int64_t n_rows, int64_t n, int32_t dtype, const nacho_kept *kept, void *hip_stream)
+{
+    if (!value_type(dtype) || !kept || n_rows < 0 || n_rows > kMostRows || n < 0 || n > kMostRows) return NACHO_ERR_INVALID_ARG;
+    const int64_t elem = value_bytes(dtype);
+    if (!matrix(x, n_rows, n, ldx, elem) || !check_kept(kept, n_rows, n)) return NACHO_ERR_INVALID_ARG;
+    if (!apart({codes_of(kept, n_rows, n), exponents_of(kept, n_rows, n)}, {{x, span(n_rows, n, ldx, elem)}})) return NACHO_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     profile_begin(s);
-    const void *gz = grad_y;
-    int64_t ldgz = ldgy;
-    if ((slope && products) || grad_bias) {
-        SlopeArgs a{l.expert_pos, (int32_t)l.n_experts, (int32_t)l.outer, l.act, l.n_slots, grad_y, pre, ldgy, ldpre, nullptr, 0,
-                    grad_bias, gb_stride, w.sums};
-        if (slope && products) {
-            gz = a.grad_z = w.grad_z;
-            ldgz = a.ldgz = (l.outer + 7) / 8 * 8;
-        }
-        if (const hipError_t e = launch_experts_slope(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
-        profile_mark("experts_slope");
-    }
-    if (grad_x) {
-        const ProductArgs a{l.expert_pos, nullptr, (int32_t)l.n_experts, 0, (int32_t)l.inner, (int32_t)l.outer, l.n_slots, gz, l.w,
-                            ldgz, l.ldw, l.w_stride, grad_x, ldgx, 0, nullptr, 0, nullptr, 0, NACHO_ACT_NONE};
-        if (const hipError_t e = launch_experts_rows(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
-        profile_mark("experts_rows");
-    }
-    if (grad_w) {
-        const ProductArgs a{l.expert_pos, l.token, (int32_t)l.n_experts, (int32_t)l.outer, (int32_t)l.inner, 0, l.n_slots, gz, l.x,
-                            ldgz, l.ldx, 0, grad_w, ldgw, gw_stride, nullptr, 0, nullptr, 0, NACHO_ACT_NONE};
-        if (const hipError_t e = launch_experts_weights(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
-        profile_mark("experts_weights");
-    }
+    if (const hipError_t e = launch_keep(dtype, KeepArgs{x, nullptr, ldx, n_rows, (int32_t)n, *kept}, s))
+        return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+    profile_mark("keep8");
     return NACHO_OK;
+}
+
+int32_t nacho_restore8(const nacho_kept *kept, int64_t n_rows, int64_t n, int32_t dtype, void *out, int64_t ldo, void *hip_stream)
+{
+    if (!value_type(dtype) || !kept || n_rows < 0 || n_rows > kMostRows || n < 0 || n > kMostRows) return NACHO_ERR_INVALID_ARG;
+    const int64_t elem = value_bytes(dtype);
+    if (!matrix(out, n_rows, n, ldo, elem) || !check_kept(kept, n_rows, n)) return NACHO_ERR_INVALID_ARG;
+    if (!apart({{out, span(n_rows, n, ldo, elem)}}, {codes_of(kept, n_rows, n), exponents_of(kept, n_rows, n)})) return NACHO_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    profile_begin(s);
+    if (const hipError_t e = launch_restore(dtype, KeepArgs{nullptr, out, ldo, n_rows, (int32_t)n, *kept}, s))
+        return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+    profile_mark("restore8");
+    return NACHO_OK;
+}
+
+int32_t nacho_experts_keep8(const nacho_experts_layer *layer, void *y, int64_t ldy, const nacho_kept *pre, void *hip_stream)
+{
+    return pre ? experts_forward(layer, y, ldy, nullptr, 0, pre, hip_stream) : NACHO_ERR_INVALID_ARG;
+}
+
+int32_t nacho_experts_keep8_workspace_bytes(const nacho_experts_layer *layer, size_t *bytes)
+{
+    if (!bytes) return NACHO_ERR_INVALID_ARG;
+    const int32_t rc = check_layer(layer);
+    if (rc == NACHO_OK) *bytes = carve_grad(nullptr, layer, layer->act != NACHO_ACT_NONE, true, true).bytes;
+    return rc;
+}
+
+int32_t nacho_experts_keep8_grad(const nacho_experts_layer *layer, const nacho_kept *kept_x, const void *grad_y, int64_t ldgy,
+                                 const void *pre, int64_t ldpre, const nacho_kept *kept_pre, void *grad_x, int64_t ldgx, void *grad_w,
+                                 int64_t ldgw, int64_t gw_stride, void *grad_bias, int64_t gb_stride, void *ws, size_t ws_bytes,
+                                 void *hip_stream)
+{
+    return experts_backward(layer, kept_x, grad_y, ldgy, pre, ldpre, kept_pre, grad_x, ldgx, grad_w, ldgw, gw_stride, grad_bias, gb_stride, ws,
+                            ws_bytes, hip_stream);
 }
 
 int32_t nacho_experts_step_workspace_bytes(const nacho_experts_step_layer *layer, size_t *bytes)

@@ -8,6 +8,7 @@
 // card, 837 to 898 TFLOP/s of the 1211 of a library's product of 8192^3), by the weights for few (16 of 32 experts, 2048 x 4096:
 // 44 to 55 us a call for 213 MB; 32 us a kernel where the last cache still has most of them).
 #include "activation.hpp"
+#include "kept.hpp"
 #include "products.hpp"
 
 namespace nacho {
@@ -47,7 +48,7 @@ struct Rows {
 // has a tile and 16 words of 16 bytes of its columns, 16 threads along them and 16 along the rows.  Bound by memory: 16384 x 4096
 // bf16, gelu, 88 us, 4.6 TB/s.
 constexpr int kSlopeRows = 64;
-template <typename T, Access kAccess>
+template <typename T, Access kAccess, bool kKept>
 __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, int tiles_n)
 {
     constexpr int n = Word<T>::n;
@@ -70,14 +71,28 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
 #pragma unroll
     for (int e = 0; e < n; ++e) sum[e] = 0.0f;
     constexpr int kRows = kSlopeRows / 16;
-    v4u g[kRows], z[kRows];
+    v4u g[kRows], z[kKept ? 1 : kRows];
+    unsigned codes[kKept ? kRows : 1][n / 4], exponent[kKept ? kRows : 1];
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
         const unsigned m = (unsigned)row + ty + i * 16;
-        g[i] = z[i] = v4u{0, 0, 0, 0};
+        g[i] = v4u{0, 0, 0, 0};
+        if constexpr (kKept) {
+#pragma unroll
+            for (int e = 0; e < n / 4; ++e) codes[i][e] = 0;
+            exponent[i] = 0;
+        } else z[i] = v4u{0, 0, 0, 0};
         if (m < (unsigned)end) {
             g[i] = get(gy + (int64_t)m * a.ldgy);
-            if (a.act != NACHO_ACT_NONE) z[i] = get(pre + (int64_t)m * a.ldpre);
+            if constexpr (kKept) {
+                const int8_t *from = a.kept.code + (int64_t)m * a.kept.ldc + c;
+                if (width >= n) __builtin_memcpy(codes[i], from, n);
+                else {
+#pragma unroll
+                    for (int e = 0; e < n; ++e) codes[i][e / 4] |= e < width ? (unsigned)(uint8_t)from[e] << (8 * (e % 4)) : 0u;
+                }
+                if (width > 0) exponent[i] = a.kept.exponent[(int64_t)m * a.kept.lde + c / kBlock];
+            } else if (a.act != NACHO_ACT_NONE) z[i] = get(pre + (int64_t)m * a.ldpre);
         }
     }
 #pragma unroll
@@ -86,10 +101,19 @@ __global__ void __launch_bounds__(kThreads) experts_slope_kernel(SlopeArgs a, in
         word v = __builtin_bit_cast(word, g[i]);
         // (what the sums take is not rounded to the type yet; behind the last row it is zero)
         if (a.act != NACHO_ACT_NONE) {
-            const word at = __builtin_bit_cast(word, z[i]);
+            float at[n];
+            if constexpr (kKept) {
+                const float step = step_of(exponent[i]);
+#pragma unroll
+                for (int e = 0; e < n; ++e) at[e] = value_of(codes[i][e / 4], e % 4, step);
+            } else {
+                const word rows = __builtin_bit_cast(word, z[i]);
+#pragma unroll
+                for (int e = 0; e < n; ++e) at[e] = wide((T)rows[e]);
+            }
 #pragma unroll
             for (int e = 0; e < n; ++e) {
-                const float x = wide((T)v[e]) * slope_at<T>(wide((T)at[e]), a.act);
+                const float x = wide((T)v[e]) * slope_at<T>(at[e], a.act);
                 v[e] = (T)x;
                 sum[e] += x;
             }
@@ -156,7 +180,7 @@ int64_t experts_slope_tiles(int64_t slots, int64_t experts) { return slots / kSl
 hipError_t launch_experts_slope(int dtype, const SlopeArgs &a, hipStream_t s)
 {
     const int elem = dtype == NACHO_F32 ? 4 : 2;
-    const bool words = in_words({{a.grad_y, a.ldgy}, {a.act ? a.pre : nullptr, a.ldpre}, {a.grad_z, a.ldgz}, {a.grad_y, a.cols}}, elem);
+    const bool words = in_words({{a.grad_y, a.ldgy}, {a.act && !a.kept.code ? a.pre : nullptr, a.ldpre}, {a.grad_z, a.ldgz}, {a.grad_y, a.cols}}, elem);
     hipError_t rc = hipSuccess;
     by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
@@ -169,9 +193,14 @@ hipError_t launch_experts_slope(int dtype, const SlopeArgs &a, hipStream_t s)
         }
         if (tiles > 0) {
             const dim3 grid((unsigned)row, (unsigned)((tiles + row - 1) / row));
-            if (words) experts_slope_kernel<T, WORDS><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
-            else if (a.cols >= Word<T>::n) experts_slope_kernel<T, ANYWHERE><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
-            else experts_slope_kernel<T, TINY><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
+            auto run = [&](auto kept) {
+                constexpr bool kKept = decltype(kept)::value;
+                if (words) experts_slope_kernel<T, WORDS, kKept><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
+                else if (a.cols >= Word<T>::n) experts_slope_kernel<T, ANYWHERE, kKept><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
+                else experts_slope_kernel<T, TINY, kKept><<<grid, kThreads, 0, s>>>(a, (int)tiles_n);
+            };
+            if (a.kept.code) run(std::true_type());
+            else run(std::false_type());
             rc = hipGetLastError();
         }
         if (rc == hipSuccess && a.grad_bias) {

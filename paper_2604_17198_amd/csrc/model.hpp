@@ -102,6 +102,7 @@ struct ProductArgs {
     int32_t act;
 };
 hipError_t launch_experts_forward(int dtype, const ProductArgs &a, hipStream_t s);
+hipError_t launch_experts_forward_kept(int dtype, const ProductArgs &a, const nacho_kept &pre, hipStream_t s);
 hipError_t launch_experts_rows(int dtype, const ProductArgs &a, hipStream_t s);
 hipError_t launch_experts_weights(int dtype, const ProductArgs &a, hipStream_t s);
 // grad_z = grad_y act'(pre), and the sums of its rows by expert (grad_bias, may be NULL).  grad_z may be NULL: not wanted.
@@ -116,9 +117,22 @@ struct SlopeArgs {
     void *grad_bias;
     int64_t bias_stride;
     float *sums;                   // [experts_slope_tiles][cols], with grad_bias
+    nacho_kept kept;               // code: pre in 8 bits, or NULL
 };
 int64_t experts_slope_tiles(int64_t slots, int64_t experts);
 hipError_t launch_experts_slope(int dtype, const SlopeArgs &a, hipStream_t s);
+
+// ---- rows kept in 8 bits ----------------------------------------------------------
+struct KeepArgs {
+    const void *x;                 // rows to keep
+    void *out;                     // restored rows
+    int64_t ldx;                   // of either
+    int64_t rows;
+    int32_t cols;
+    nacho_kept kept;
+};
+hipError_t launch_keep(int dtype, const KeepArgs &a, hipStream_t s);
+hipError_t launch_restore(int dtype, const KeepArgs &a, hipStream_t s);
 
 // ---- a whole layer of experts for a few tokens -----------------------------------
 constexpr int kMostStepTokens = 64;
