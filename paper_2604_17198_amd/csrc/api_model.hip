@@ -303,7 +303,10 @@ size_t carve_step(void *ws, const nacho_experts_step_layer *l, StepArgs *a)
     a->h = c.take<char>(slots * a->ldh * value_bytes(l->dtype));
     a->choice = c.take<uint16_t>(slots);
     a->share = c.take<float>(slots);
-    a->active = c.take<int32_t>(1 + (slots < l->n_experts ? slots : l->n_experts));
+    const int64_t most = slots < l->n_experts ? slots : l->n_experts;
+    a->active = c.take<int32_t>(1 + most);
+    a->order = c.take<uint16_t>(slots);
+    a->first = c.take<int32_t>(1 + most);
     a->partial = c.take<float>(a->parts > 1 ? (int64_t)a->tiles * a->parts * l->n_tokens * 16 : 0);
     a->arrived = c.take<int32_t>(a->tiles);
     return align_up(c.off, 256);

@@ -155,6 +155,8 @@ struct StepArgs {
     uint16_t *choice;
     float *share;
     int32_t *active;
+    uint16_t *order;               // the slots by these experts, from `first` of each on
+    int32_t *first;
     int32_t tiles, parts;          // of the second product: tiles of rows, workgroups that share one
     float *partial;                // [tiles][parts][tokens][16], several parts
     int32_t *arrived;              // [tiles]

@@ -8,9 +8,9 @@
 // registers that the matrix units read (16 rows x 64 bytes of k an instruction), and the tokens' rows the same way from the
 // caches; wavefronts share out k, and their sums meet in LDS.
 //
-// The choice of experts is made by every workgroup of the first launch for itself: a wavefront a token, a round for each of the
-// k largest.  That is less than a launch of its own would take.
+// The choice of experts is made by every workgroup of the first launch for itself, which takes less than a launch of its own.
 #include "activation.hpp"
+#include "choose.hpp"
 #include "products.hpp"
 
 namespace nacho {
@@ -18,83 +18,77 @@ namespace nacho {
 namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * NACHO_WAVE;
-constexpr int kTall = 16;              // rows of weights a workgroup
+constexpr int kTall = 16;              // rows of weights that a wavefront multiplies at a time
 constexpr int kMostTokens = kMostStepTokens, kMostSlots = kMostTokens * kMostChoices;
 constexpr uint16_t kNone = 0xffff;     // a choice that is not there
 
-// 16 bytes of a row of k elements from element `from` on, zeros behind its end.
-template <typename T, Access kAccess> __device__ inline v4u piece(const T *row, int from, int k)
+// Rows of k elements that the matrix units read in stretches of kBatch x 64 bytes (as many as leave registers for two
+// workgroups a compute unit): a lane has 16 of every 64.  Loads have no branch
+// around them (behind one the compiler waits for all loads): past the row's end its last word is loaded, and made zeros when it is
+// used, if the stretch is not whole.
+template <typename T, Access kAccess, bool kShort> struct Stretch {
+    static constexpr int kBatch = kAccess == TINY ? 1 : kAccess == ANYWHERE || kShort ? 2 : 4, n = Word<T>::n, kStep = 64 / (int)sizeof(T), kLong = kBatch * kStep;
+    static __device__ int from(int stretch, int i) { return stretch * kLong + i * kStep + lane_id() / 16 * n; }
+    static __device__ v4u load(const T *row, int at, int k)
+    {
+        if constexpr (kAccess == WORDS) return *reinterpret_cast<const v4u *>(row + (at < k ? at : k - n));
+        else return Ragged<T, kAccess == TINY>(k, at).load(row + at);
+    }
+    static __device__ v4u settled(v4u w, int at, int k)
+    {
+        if constexpr (kAccess == WORDS) return at < k ? w : v4u{0, 0, 0, 0};
+        else return Ragged<T, kAccess == TINY>(k, at).placed(w);
+    }
+};
+
+// The experts of every token, ascending, into `choice`; how many tokens chose each; and the gates, of one workgroup.
+template <typename T, int L, int I> __device__ inline void choose_experts(const StepArgs &a, uint16_t *choice, int *takers, bool shares)
 {
-    if constexpr (kAccess == WORDS) return from < k ? *reinterpret_cast<const v4u *>(row + from) : v4u{0, 0, 0, 0};
-    else {
-        const Ragged<T, kAccess == TINY> r(k, from);
-        return r.placed(r.load(row + from));
+    constexpr int kGroups = kThreads / L;
+    const int tid = (int)threadIdx.x, group = tid / L, lane = tid % L, first = lane * I, n = a.experts, k = a.top_k;
+    const T *logits = static_cast<const T *>(a.logits);
+    const bool words = nacho::in_words<T, I>(logits, a.ldl);
+    // (every lane of a wavefront stays in the loop: the lanes of a group ask each other)
+    for (int t0 = 0; t0 < a.tokens; t0 += kGroups) {
+        const int t = t0 + group;
+        const bool there = t < a.tokens, live = there && (!a.keep || a.keep[t] != 0);
+        float v[I];
+        if (live) row_part<T, I>(logits + t * a.ldl, first, n, words, v);
+        else {
+#pragma unroll
+            for (int i = 0; i < I; ++i) v[i] = -kInfinity;
+        }
+        const unsigned taken = choose<L, I>(v, k);
+        // places of the lane's entries among the token's: those of the lanes before it come first
+        const int own = __popc(taken), upto = group_scan<L>(own), held = __shfl(upto, L - 1, L);
+        int place = t * k + upto - own;
+        for (unsigned rest = taken; rest != 0; rest &= rest - 1, ++place) {
+            const int e = first + __ffs((int)rest) - 1;
+            choice[place] = (uint16_t)e;
+            atomicAdd(&takers[e], 1);
+        }
+        for (int j = held + lane; there && j < k; j += L) choice[t * k + j] = kNone;
+        if (!shares) continue;
+        float e[I], top, sum, whole = 0.0f;
+        exponentials<L, I>(v, e, top, sum);
+#pragma unroll
+        for (int i = 0; i < I; ++i) whole += taken >> i & 1 ? e[i] : 0.0f;
+        whole = group_reduce<L>(whole, SumOf());
+        whole = !a.normalise || sum != sum ? sum : whole;                          // (a NaN among the logits)
+        place = t * k + upto - own;
+        for (unsigned rest = taken; rest != 0; rest &= rest - 1, ++place) {
+            const int at = __ffs((int)rest) - 1;
+            float mine = e[0];
+#pragma unroll
+            for (int i = 1; i < I; ++i) mine = at == i ? e[i] : mine;
+            a.share[place] = mine / whole;
+        }
+        for (int j = held + lane; there && j < k; j += L) a.share[t * k + j] = 0.0f;
     }
 }
 
-// The experts of a wavefront's tokens, into `choice`, and as bits.  `logits`: the wavefront's room for a token's.
-template <typename T>
-__device__ inline void choose_experts(const StepArgs &a, float *logits, uint16_t *choice, unsigned *bits, bool shares)
-{
-    const int lane = lane_id(), wave = (int)threadIdx.x / NACHO_WAVE, k = a.top_k, n = a.experts;
-    const int each = (n + NACHO_WAVE - 1) / NACHO_WAVE, first = lane * each;       // a lane's experts, one after the other
-    for (int t = wave; t < a.tokens; t += kWaves) {
-        const bool kept = !a.keep || a.keep[t] != 0;
-        const T *row = static_cast<const T *>(a.logits) + t * a.ldl;
-        float top = -kInfinity;
-        for (int i = 0; i < each; ++i) {
-            const int e = first + i;
-            const float v = kept && e < n ? wide(row[e]) : -kInfinity;
-            logits[e] = v;
-            top = fmaxf(top, v);
-        }
-        // the lane's largest logit that is left, of equal ones the first
-        unsigned best = 0, gone = 0;
-        int at = first;
-        auto look = [&] {
-            best = 0;
-            for (int i = 0; i < each; ++i) {
-                const unsigned key = gone >> i & 1 ? 0u : order_of(logits[first + i]);
-                if (key > best) {
-                    best = key;
-                    at = first + i;
-                }
-            }
-        };
-        look();
-        int held = 0;
-        for (; held < k; ++held) {
-            const unsigned most = group_max<NACHO_WAVE>(best);
-            if (most == 0) break;
-            const int who = __ffsll((long long)__ballot(best == most)) - 1, e = __builtin_amdgcn_readlane(at, who);
-            if (lane == 0) {
-                choice[t * k + held] = (uint16_t)e;
-                atomicOr(&bits[e >> 5], 1u << (e & 31));
-            }
-            if (lane == who) {
-                gone |= 1u << (e - first);
-                look();
-            }
-        }
-        if (lane >= held && lane < k) choice[t * k + lane] = kNone;
-        wave_sync();
-        if (shares) {
-            top = group_reduce<NACHO_WAVE>(top, MaxOf());
-            auto part = [&](float v) { return v == -kInfinity ? 0.0f : exp2_of((v - top) * kLog2e); };
-            float sum = 0.0f;
-            for (int i = 0; i < each; ++i) sum += part(logits[first + i]);
-            sum = group_reduce<NACHO_WAVE>(sum, SumOf());
-            const float mine = lane < held ? part(logits[choice[t * k + lane]]) : 0.0f;
-            float whole = group_reduce<NACHO_WAVE>(mine, SumOf());
-            whole = !a.normalise || sum != sum ? sum : whole;                      // (a NaN among the logits)
-            if (lane < k) a.share[t * k + lane] = lane < held ? mine / whole : 0.0f;
-        }
-        wave_sync();
-    }
-}
-
-// The slots (token x k + choice) that chose expert e, by tokens; how many they are.  All lanes of a wavefront.
-__device__ inline int slots_of(const StepArgs &a, const uint16_t *choice, int e, int16_t *list)
+// The slots (token x k + choice) that chose expert e, by tokens.  All lanes of a wavefront.
+__device__ inline int slots_of(const StepArgs &a, const uint16_t *choice, int e, uint16_t *list)
 {
     const int lane = lane_id(), k = a.top_k;
     int slot = -1;
@@ -103,144 +97,235 @@ __device__ inline int slots_of(const StepArgs &a, const uint16_t *choice, int e,
             if (choice[lane * k + j] == e) slot = lane * k + j;
     const unsigned long long who = __ballot(slot >= 0);
     const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0));
-    if (slot >= 0) list[before] = (int16_t)slot;
+    if (slot >= 0) list[before] = (uint16_t)slot;
     return __popcll((long long)who);
 }
 
-template <typename T, bool kGated, Access kAccess> __global__ void __launch_bounds__(kThreads) step_up_kernel(StepArgs a)
+// The first product.  An item is 16 rows of an expert's weights, and belongs to a wavefront, or, where there are few items, to a
+// workgroup whose wavefronts have a part of k each (kShared).
+template <typename T, bool kGated, Access kAccess, bool kShared>
+__global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_kernel(StepArgs a)
 {
-    __shared__ __attribute__((aligned(16))) char room[kWaves * kMostExperts * 4];
-    __shared__ uint16_t choice[kMostSlots], active[kMostExperts];
-    __shared__ unsigned bits[kMostExperts / 32];
-    __shared__ int16_t list[kMostTokens];
-    __shared__ int members;
-    const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / NACHO_WAVE, k = a.top_k;
-    if (tid < kMostExperts / 32) bits[tid] = 0;
+    constexpr int kMatrices = 1 + kGated;
+    typedef Stretch<T, kAccess, kGated || kShared> Part;
+    constexpr int kBatch = Part::kBatch;
+    __shared__ __attribute__((aligned(16))) v4f sums[kShared ? kMatrices * kWaves * NACHO_WAVE : 1];
+    __shared__ uint16_t choice[kMostSlots], active[kMostExperts], lists[kWaves][kMostTokens];
+    __shared__ int takers[kMostExperts], counts[kThreads / NACHO_WAVE];
+    const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / NACHO_WAVE), k = a.top_k;
+    for (int e = tid; e < a.experts; e += kThreads) takers[e] = 0;
     __syncthreads();
-    choose_experts<T>(a, reinterpret_cast<float *>(room) + wave * kMostExperts, choice, bits, blockIdx.x == 0);
+    if (a.experts <= 64) choose_experts<T, 16, 4>(a, choice, takers, blockIdx.x == 0);
+    else if (a.experts <= 256) choose_experts<T, 16, 16>(a, choice, takers, blockIdx.x == 0);
+    else choose_experts<T, 64, 16>(a, choice, takers, blockIdx.x == 0);
     __syncthreads();
+    // the experts that a token chose, ascending
     int count = 0;
-    for (int w = 0; w < kMostExperts / 32; ++w) count += __popc(bits[w]);
-    for (int e = tid; e < a.experts; e += kThreads)
-        if (bits[e >> 5] >> (e & 31) & 1) {
-            int place = __popc(bits[e >> 5] & ((1u << (e & 31)) - 1u));
-            for (int w = 0; w < e >> 5; ++w) place += __popc(bits[w]);
-            active[place] = (uint16_t)e;
+    for (int e0 = 0; e0 < a.experts; e0 += kThreads) {
+        const int e = e0 + tid;
+        const unsigned long long chosen = __ballot(e < a.experts && takers[e] > 0);
+        if (lane == 0) counts[wave] = __popcll((long long)chosen);
+        __syncthreads();
+        int place = count + __builtin_amdgcn_mbcnt_hi((unsigned)(chosen >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)chosen, 0));
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) place += counts[w];
+            count += counts[w];
         }
-    __syncthreads();
+        if (e < a.experts && takers[e] > 0) active[place] = (uint16_t)e;
+        __syncthreads();
+    }
     if (blockIdx.x == 0) {
         // what the second launch needs of the choice
         if (tid == 0) a.active[0] = count;
         for (int i = tid; i < count; i += kThreads) a.active[1 + i] = active[i];
         for (int i = tid; i < a.tokens * k; i += kThreads) a.choice[i] = choice[i];
         for (int i = tid; i < a.tiles; i += kThreads) a.arrived[i] = 0;
-    }
-    constexpr int n = Word<T>::n, kStep = 64 / (int)sizeof(T), kBatch = 4;
-    const int tiles = (a.hidden + kTall - 1) / kTall, steps = (a.inner + kStep - 1) / kStep, pairs = (steps + 1) / 2;
-    const int begin = pairs * wave / kWaves * 2, until = pairs * (wave + 1) / kWaves * 2, end = until < steps ? until : steps;
-    v4f *const sums = reinterpret_cast<v4f *>(room);                               // [2][kWaves][64]
-    for (int item = (int)blockIdx.x; item < count * tiles; item += (int)gridDim.x) {
-        const int number = item / tiles, row0 = (item - number * tiles) * kTall, e = active[number];
-        if (wave == 0) {
-            const int m = slots_of(a, choice, e, list);
-            if (lane == 0) members = m;
+        int before = 0;
+        for (int i = 0; i < count; i += NACHO_WAVE) {
+            const int mine = i + lane < count ? takers[active[i + lane]] : 0, upto = before + wave_inclusive_scan(mine);
+            if (wave == 0 && i + lane < count) a.first[i + lane] = upto - mine;
+            for (int j = wave; j < NACHO_WAVE && i + j < count; j += kWaves)
+                slots_of(a, choice, active[i + j], a.order + __builtin_amdgcn_readlane(upto - mine, j));
+            before = __builtin_amdgcn_readlane(upto, NACHO_WAVE - 1);
         }
-        __syncthreads();
-        const int m = members, row = row0 + lane % 16 < a.hidden ? row0 + lane % 16 : a.hidden - 1, off = lane / 16 * n;
-        const T *up = static_cast<const T *>(a.up.w) + e * a.up.stride + row * a.up.ld;
-        const T *gate = kGated ? static_cast<const T *>(a.gate.w) + e * a.gate.stride + row * a.gate.ld : up;
+        if (tid == 0) a.first[count] = before;
+    }
+    const int tiles = (a.hidden + kTall - 1) / kTall, stretches = (a.inner + Part::kLong - 1) / Part::kLong, items = count * tiles;
+    const int begin = kShared ? stretches * wave / kWaves : 0, end = kShared ? stretches * (wave + 1) / kWaves : stretches;
+    uint16_t *const list = lists[wave];
+    const int step = (int)gridDim.x * (kShared ? 1 : kWaves);
+    for (int item = kShared ? (int)blockIdx.x : (int)blockIdx.x + (int)gridDim.x * wave; item < items; item += step) {
+        const int number = item / tiles, row0 = (item - number * tiles) * kTall, e = __builtin_amdgcn_readfirstlane(active[number]);
+        const int row = row0 + lane % 16 < a.hidden ? row0 + lane % 16 : a.hidden - 1;
+        const T *rows[kMatrices];
+        rows[0] = static_cast<const T *>(a.up.w) + e * a.up.stride + row * a.up.ld;
+        if constexpr (kGated) rows[1] = static_cast<const T *>(a.gate.w) + e * a.gate.stride + row * a.gate.ld;
         auto groups_of = [&](auto most) {
             constexpr int kGroups = decltype(most)::value;
-            v4f acc[kGroups][2];
-            const T *x[kGroups];
+            struct Loaded {
+                v4u p[kMatrices][kBatch], q[kBatch];
+            } one, two;
+            v4f acc[kGroups][kMatrices];
+            int token[kGroups];
+            int m = 0;
+            auto fetch_rows = [&](Loaded &to, int s) {
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                acc[g][0] = acc[g][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-                const int i = g * 16 + lane % 16;
-                x[g] = static_cast<const T *>(a.x) + list[i < m ? i : m - 1] / k * a.ldx;
-            }
-            for (int s = begin; s < end; s += kBatch) {
-                v4u p[kBatch], q[kBatch], r[kBatch];
+                for (int h = 0; h < kMatrices; ++h)
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    const int from = s + i < end ? (s + i) * kStep + off : a.inner;
-                    p[i] = piece<T, kAccess>(up, from, a.inner);
-                    if (kGated) r[i] = piece<T, kAccess>(gate, from, a.inner);
+                    for (int i = 0; i < kBatch; ++i) to.p[h][i] = Part::load(rows[h], Part::from(s, i), a.inner);
+            };
+            auto fetch_x = [&](Loaded &to, int s, int g) {
+                const T *x = static_cast<const T *>(a.x) + token[g] * a.ldx;
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) to.q[i] = Part::load(x, Part::from(s, i), a.inner);
+            };
+            auto multiply = [&](Loaded &of, int s) {
+                const bool whole = (s + 1) * Part::kLong <= a.inner;
+                if (!whole) {
+#pragma unroll
+                    for (int h = 0; h < kMatrices; ++h)
+#pragma unroll
+                        for (int i = 0; i < kBatch; ++i) of.p[h][i] = Part::settled(of.p[h][i], Part::from(s, i), a.inner);
                 }
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
-                    if (kGroups > 1 && g * 16 >= m) break;
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) q[i] = piece<T, kAccess>(x[g], s + i < end ? (s + i) * kStep + off : a.inner, a.inner);
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
-                        acc[g][0] = matrix_step<T>(p[i], q[i], acc[g][0]);
-                        if (kGated) acc[g][1] = matrix_step<T>(r[i], q[i], acc[g][1]);
+                    if (g > 0) {
+                        if (g * 16 >= m) break;
+                        fetch_x(of, s, g);
                     }
+                    if (!whole) {
+#pragma unroll
+                        for (int i = 0; i < kBatch; ++i) of.q[i] = Part::settled(of.q[i], Part::from(s, i), a.inner);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+                        for (int h = 0; h < kMatrices; ++h) acc[g][h] = matrix_step<T>(of.p[h][i], of.q[i], acc[g][h]);
                 }
+            };
+            // (weights first: they have the longest way)
+            if (begin < end) fetch_rows(one, begin);
+            m = slots_of(a, choice, e, list);
+            wave_sync();
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int i = g * 16 + lane % 16;
+                token[g] = list[i < m ? i : m - 1] / k;
+#pragma unroll
+                for (int h = 0; h < kMatrices; ++h) acc[g][h] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
             }
-            // 16 tokens at a time: a thread adds up the wavefronts' sums of one token and one row
+            if (begin < end) fetch_x(one, begin, 0);
+            for (int s = begin; s < end; s += 2) {
+                const int next = s + 1 < end ? s + 1 : s, after = s + 2 < end ? s + 2 : s;
+                fetch_rows(two, next);
+                fetch_x(two, next, 0);
+                multiply(one, s);
+                fetch_rows(one, after);
+                fetch_x(one, after, 0);
+                if (s + 1 < end) multiply(two, next);
+            }
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 if (g * 16 >= m) break;
-                sums[wave * NACHO_WAVE + lane] = acc[g][0];
-                if (kGated) sums[(kWaves + wave) * NACHO_WAVE + lane] = acc[g][1];
-                __syncthreads();
-                const int r = tid % kTall, token = tid / kTall, i = g * 16 + token, out = row0 + r;
-                if (tid < 16 * kTall && i < m && out < a.hidden) {
-                    const float *from = reinterpret_cast<const float *>(sums) + (token + r / 4 * 16) * 4 + r % 4;
-                    float v[2] = {0.0f, 0.0f};
+                if constexpr (kShared) {
+                    __syncthreads();
 #pragma unroll
-                    for (int h = 0; h < 1 + kGated; ++h)
+                    for (int h = 0; h < kMatrices; ++h) sums[(h * kWaves + wave) * NACHO_WAVE + lane] = acc[g][h];
+                    __syncthreads();
+                    if (wave != 0) continue;
 #pragma unroll
-                        for (int w = 0; w < kWaves; ++w) v[h] += from[(h * kWaves + w) * NACHO_WAVE * 4];
-                    if (a.up.bias) v[0] += wide(static_cast<const T *>(a.up.bias)[e * a.up.bias_stride + out]);
-                    if (kGated) {
-                        if (a.gate.bias) v[1] += wide(static_cast<const T *>(a.gate.bias)[e * a.gate.bias_stride + out]);
-                        v[0] *= activated<T>(v[1], a.act);
-                    } else v[0] = activated<T>(v[0], a.act);
-                    static_cast<T *>(a.h)[list[i] * a.ldh + out] = (T)v[0];
+                    for (int h = 0; h < kMatrices; ++h) {
+                        acc[g][h] = sums[h * kWaves * NACHO_WAVE + lane];
+#pragma unroll
+                        for (int w = 1; w < kWaves; ++w) acc[g][h] += sums[(h * kWaves + w) * NACHO_WAVE + lane];
+                    }
                 }
-                __syncthreads();
+                // a lane has four rows of one token
+                const int i = g * 16 + lane % 16, out = row0 + lane / 16 * 4;
+                if (i >= m || out >= a.hidden) continue;
+                typedef T four __attribute__((ext_vector_type(4)));
+                four v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float z[kMatrices];
+#pragma unroll
+                    for (int h = 0; h < kMatrices; ++h) {
+                        const nacho_dense &d = h == 0 ? a.up : a.gate;
+                        z[h] = acc[g][h][j];
+                        if (d.bias && out + j < a.hidden) z[h] += wide(static_cast<const T *>(d.bias)[e * d.bias_stride + out + j]);
+                    }
+                    v[j] = (T)(kGated ? activated<T>(z[kMatrices - 1], a.act) * z[0] : activated<T>(z[0], a.act));
+                }
+                // (rows are padded to words of 8 elements)
+                *reinterpret_cast<four *>(static_cast<T *>(a.h) + list[i] * a.ldh + out) = v;
             }
+            wave_sync();
         };
-        if (m <= 16) groups_of(std::integral_constant<int, 1>());
+        if (takers[e] <= 16) groups_of(std::integral_constant<int, 1>());
         else groups_of(std::integral_constant<int, kMostTokens / 16>());
     }
 }
 
-template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads) step_down_kernel(StepArgs a)
+// The second product and the weighted sum.  A workgroup has 16 rows of every chosen expert's weights, or a part of their k (with
+// others, `parts` of them); its wavefronts share out what it has, a stretch of k of an expert at a time, and keep sums of their own
+// for every token in LDS.
+template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_down_kernel(StepArgs a)
 {
-    constexpr int kSlab = kMostTokens * kTall, kGroups = kMostTokens / 16;
+    typedef Stretch<T, kAccess, false> Part;
+    constexpr int kSlab = kMostTokens * kTall, kGroups = kMostTokens / 16, kBatch = Part::kBatch;
     __shared__ __attribute__((aligned(16))) float slab[kWaves][kSlab];             // [token][row] of every wavefront
     __shared__ float share[kMostSlots];
-    __shared__ uint16_t choice[kMostSlots], active[kMostExperts];
-    __shared__ int16_t lists[kWaves][kMostTokens];
-    __shared__ int last;
-    const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / NACHO_WAVE, k = a.top_k;
+    __shared__ uint16_t order[kMostSlots], active[kMostExperts];
+    __shared__ int firsts[kMostExperts + 1], last;
+    const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / NACHO_WAVE), k = a.top_k;
     const int tile = (int)blockIdx.x, part = (int)blockIdx.y, parts = (int)gridDim.y, row0 = tile * kTall, count = a.active[0];
-    for (int i = tid; i < a.tokens * k; i += kThreads) {
-        choice[i] = a.choice[i];
+    const int slots = a.tokens * k, most = slots < a.experts ? slots : a.experts;
+    for (int i = tid; i < slots; i += kThreads) {
+        order[i] = a.order[i];
         share[i] = a.share[i];
     }
-    for (int i = tid; i < count; i += kThreads) active[i] = (uint16_t)a.active[1 + i];
+    // (as many as there can be: nothing waits for how many there are)
+    for (int i = tid; i <= most; i += kThreads) {
+        firsts[i] = a.first[i];
+        if (i < most) active[i] = (uint16_t)a.active[1 + i];
+    }
     for (int i = lane; i < a.tokens * kTall; i += NACHO_WAVE) slab[wave][i] = 0.0f;
     __syncthreads();
-    // a unit of work: eight steps of k of one expert; a wavefront has consecutive ones
-    constexpr int n = Word<T>::n, kStep = 64 / (int)sizeof(T), kBatch = 8;
-    const int units = (a.hidden + kStep * kBatch - 1) / (kStep * kBatch), all = count * units;
+    const int units = (a.hidden + Part::kLong - 1) / Part::kLong, all = count * units;
     const int workers = parts * kWaves, worker = part * kWaves + wave;
     const int begin = (int)((int64_t)all * worker / workers), end = (int)((int64_t)all * (worker + 1) / workers);
-    const int row = row0 + lane % 16 < a.outer ? row0 + lane % 16 : a.outer - 1, off = lane / 16 * n;
-    int16_t *const list = lists[wave];
-    int number = -1, m = 0;
+    const int row = row0 + lane % 16 < a.outer ? row0 + lane % 16 : a.outer - 1;
+    struct Unit {
+        int expert, stretch;       // (the expert by its number among the chosen ones)
+    };
+    struct Loaded {
+        Unit at;
+        v4u p[kBatch], q[kBatch];
+    } one, two;
     v4f acc[kGroups];
-    auto add_up = [&] {
+    auto slot_of = [&](int expert, int g) {
+        const int first = firsts[expert], m = firsts[expert + 1] - first, i = g * 16 + lane % 16;
+        return order[first + (i < m ? i : m - 1)];
+    };
+    auto row_of = [&](int expert, int g) { return static_cast<const T *>(a.h) + slot_of(expert, g) * a.ldh; };
+    auto fetch = [&](Loaded &to, Unit at) {
+        to.at = at;
+        const int e = __builtin_amdgcn_readfirstlane(active[at.expert]);
+        const T *down = static_cast<const T *>(a.down.w) + e * a.down.stride + row * a.down.ld;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) to.p[i] = Part::load(down, Part::from(at.stretch, i), a.hidden);
+        const T *h = row_of(at.expert, 0);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) to.q[i] = Part::load(h, Part::from(at.stretch, i), a.hidden);
+    };
+    auto add_up = [&](int expert) {
+        const int m = __builtin_amdgcn_readfirstlane(firsts[expert + 1] - firsts[expert]);
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            const int i = g * 16 + lane % 16;
-            if (i < m) {
-                const int slot = list[i];
+            if (g * 16 >= m) break;
+            if (g * 16 + lane % 16 < m) {
+                const int slot = slot_of(expert, g);
                 v4f *to = reinterpret_cast<v4f *>(&slab[wave][slot / k * kTall + lane / 16 * 4]);
                 const float by = share[slot];
                 v4f v = *to;
@@ -250,40 +335,60 @@ template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads
             }
         }
     };
-    for (int u = begin; u < end; ++u) {
-        const int expert = u / units, from = (u - expert * units) * kBatch * kStep + off, e = active[expert];
-        const T *down = static_cast<const T *>(a.down.w) + e * a.down.stride + row * a.down.ld;
-        v4u p[kBatch], q[kBatch];
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) p[i] = piece<T, kAccess>(down, from + i * kStep, a.hidden);
-        if (expert != number) {
-            if (number >= 0) add_up();
-            wave_sync();
-            number = expert;
-            m = slots_of(a, choice, e, list);
-            wave_sync();
+    int number = -1;
+    auto multiply = [&](Loaded &of) {
+        const Unit at = of.at;
+        if (at.expert != number) {
+            if (number >= 0) add_up(number);
+            number = at.expert;
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) acc[g] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         }
+        const bool whole = (at.stretch + 1) * Part::kLong <= a.hidden;
+        const int m = __builtin_amdgcn_readfirstlane(firsts[number + 1] - firsts[number]);
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) of.p[i] = Part::settled(of.p[i], Part::from(at.stretch, i), a.hidden);
+        }
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            if (g * 16 >= m) break;
-            const int i = g * 16 + lane % 16;
-            const T *h = static_cast<const T *>(a.h) + list[i < m ? i : m - 1] * a.ldh;
+            if (g > 0) {
+                if (g * 16 >= m) break;
+                const T *h = row_of(number, g);
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) q[j] = piece<T, kAccess>(h, from + j * kStep, a.hidden);
+                for (int i = 0; i < kBatch; ++i) of.q[i] = Part::load(h, Part::from(at.stretch, i), a.hidden);
+            }
+            if (!whole) {
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) acc[g] = matrix_step<T>(p[j], q[j], acc[g]);
+                for (int i = 0; i < kBatch; ++i) of.q[i] = Part::settled(of.q[i], Part::from(at.stretch, i), a.hidden);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) acc[g] = matrix_step<T>(of.p[i], of.q[i], acc[g]);
         }
+    };
+    if (begin < end) {
+        auto behind = [&](Unit at) { return at.stretch + 1 < units ? Unit{at.expert, at.stretch + 1} : Unit{at.expert + 1, 0}; };
+        Unit at{begin / units, 0};
+        at.stretch = begin - at.expert * units;
+        fetch(one, at);
+        for (int u = begin; u < end; u += 2) {
+            // (behind the last unit it is loaded again: no branch around a load)
+            if (u + 1 < end) at = behind(at);
+            fetch(two, at);
+            multiply(one);
+            if (u + 2 < end) at = behind(at);
+            fetch(one, at);
+            if (u + 1 < end) multiply(two);
+        }
+        add_up(number);
     }
-    if (number >= 0) add_up();
     __syncthreads();
     // the sum of the wavefronts' parts; of several workgroups the last one to be there adds up all of theirs
     auto finish = [&](int t, int r, float v) {
         const int out = row0 + r;
         if (a.down.bias)
             for (int j = 0; j < k; ++j)
-                if (const int e = choice[t * k + j]; e != kNone)
+                if (const int e = a.choice[t * k + j]; e != kNone)
                     v += share[t * k + j] * wide(static_cast<const T *>(a.down.bias)[e * a.down.bias_stride + out]);
         if (a.residual) v += wide(static_cast<const T *>(a.residual)[t * a.ldr + out]);
         static_cast<T *>(a.out)[t * a.ldo + out] = (T)v;
@@ -313,15 +418,23 @@ template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads
     }
 }
 
+// Below this number of items (of 16 rows) a workgroup has one at a time.
+constexpr int64_t kSharedBelow = 2048;
+
 // The most experts that tokens can reach.
 int64_t most_active(int64_t tokens, int64_t experts, int64_t top_k) { return tokens * top_k < experts ? tokens * top_k : experts; }
 
 template <typename T, Access kAccess> hipError_t run_step(const StepArgs &a, hipStream_t s)
 {
     const int64_t items = most_active(a.tokens, a.experts, a.top_k) * ((a.hidden + kTall - 1) / kTall);
-    const unsigned groups = (unsigned)(items < 2 * kUnits ? items : 2 * kUnits);
-    if (a.gate.w) step_up_kernel<T, true, kAccess><<<groups, kThreads, 0, s>>>(a);
-    else step_up_kernel<T, false, kAccess><<<groups, kThreads, 0, s>>>(a);
+    const bool shared = items < kSharedBelow;
+    const int64_t groups = shared ? items : (items + kWaves - 1) / kWaves;
+    auto up = [&](auto gated, auto together) {
+        step_up_kernel<T, decltype(gated)::value, kAccess, decltype(together)::value>
+            <<<(unsigned)(groups < 2 * kUnits ? groups : 2 * kUnits), kThreads, 0, s>>>(a);
+    };
+    auto up_of = [&](auto gated) { shared ? up(gated, std::true_type()) : up(gated, std::false_type()); };
+    a.gate.w ? up_of(std::true_type()) : up_of(std::false_type());
     if (const hipError_t e = hipGetLastError()) return e;
     step_down_kernel<T, kAccess><<<dim3((unsigned)a.tiles, (unsigned)a.parts), kThreads, 0, s>>>(a);
     return hipGetLastError();
@@ -334,8 +447,8 @@ void step_plan(int dtype, int64_t tokens, int64_t experts, int64_t top_k, int64_
     const int elem = dtype == NACHO_F32 ? 4 : 2;
     *tiles = (int32_t)((outer + kTall - 1) / kTall);
     // workgroups for every compute unit, as long as each of their wavefronts has something to read
-    const int64_t units = most_active(tokens, experts, top_k) * ((hidden * elem + 511) / 512), wanted = (2 * kUnits + *tiles - 1) / *tiles;
-    const int64_t most = units / kWaves < 16 ? units / kWaves : 16;
+    const int64_t units = most_active(tokens, experts, top_k) * ((hidden * elem + 255) / 256), wanted = (kUnits + *tiles - 1) / *tiles;
+    const int64_t each = units / (2 * kWaves), most = each < 16 ? each : 16;
     *parts = (int32_t)(wanted < most ? wanted : (most > 1 ? most : 1));
 }
 
