@@ -172,6 +172,25 @@ template <typename T, bool kTiny> struct Ragged {
     }
 };
 
+// Rows of k elements that go from memory right into the registers that the matrix units read, in stretches of kBatch x 64 bytes: a lane
+// has 16 of every 64.  Loads have no branch
+// around them (behind one the compiler waits for all loads): past the row's end its last word is loaded, and made zeros when it is
+// used, if the stretch is not whole.
+template <typename T, Access kAccess, int kSteps> struct Stretch {
+    static constexpr int kBatch = kAccess == TINY ? 1 : kSteps, n = Word<T>::n, kStep = 64 / (int)sizeof(T), kLong = kBatch * kStep;
+    static __device__ int from(int stretch, int i) { return stretch * kLong + i * kStep + lane_id() / 16 * n; }
+    static __device__ v4u load(const T *row, int at, int k)
+    {
+        if constexpr (kAccess == WORDS) return *reinterpret_cast<const v4u *>(row + (at < k ? at : k - n));
+        else return Ragged<T, kAccess == TINY>(k, at).load(row + at);
+    }
+    static __device__ v4u settled(v4u w, int at, int k)
+    {
+        if constexpr (kAccess == WORDS) return at < k ? w : v4u{0, 0, 0, 0};
+        else return Ragged<T, kAccess == TINY>(k, at).placed(w);
+    }
+};
+
 // Rows that run along k.  A thread loads words of 16 bytes, the same one of several rows.
 template <typename T, int kRows, int kStep, int kThreads, Access kAccess, int kSets> struct AlongK {
     static constexpr int kUnits = kStep / 16, kApart = kThreads / kUnits;

@@ -22,25 +22,6 @@ constexpr int kTall = 16;              // rows of weights that a wavefront multi
 constexpr int kMostTokens = kMostStepTokens, kMostSlots = kMostTokens * kMostChoices;
 constexpr uint16_t kNone = 0xffff;     // a choice that is not there
 
-// Rows of k elements that the matrix units read in stretches of kBatch x 64 bytes (as many as leave registers for two
-// workgroups a compute unit): a lane has 16 of every 64.  Loads have no branch
-// around them (behind one the compiler waits for all loads): past the row's end its last word is loaded, and made zeros when it is
-// used, if the stretch is not whole.
-template <typename T, Access kAccess, bool kShort> struct Stretch {
-    static constexpr int kBatch = kAccess == TINY ? 1 : kAccess == ANYWHERE || kShort ? 2 : 4, n = Word<T>::n, kStep = 64 / (int)sizeof(T), kLong = kBatch * kStep;
-    static __device__ int from(int stretch, int i) { return stretch * kLong + i * kStep + lane_id() / 16 * n; }
-    static __device__ v4u load(const T *row, int at, int k)
-    {
-        if constexpr (kAccess == WORDS) return *reinterpret_cast<const v4u *>(row + (at < k ? at : k - n));
-        else return Ragged<T, kAccess == TINY>(k, at).load(row + at);
-    }
-    static __device__ v4u settled(v4u w, int at, int k)
-    {
-        if constexpr (kAccess == WORDS) return at < k ? w : v4u{0, 0, 0, 0};
-        else return Ragged<T, kAccess == TINY>(k, at).placed(w);
-    }
-};
-
 // The experts of every token, ascending, into `choice`; how many tokens chose each; and the gates, of one workgroup.
 template <typename T, int L, int I> __device__ inline void choose_experts(const StepArgs &a, uint16_t *choice, int *takers, bool shares)
 {
@@ -107,7 +88,7 @@ template <typename T, bool kGated, Access kAccess, bool kShared>
 __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_kernel(StepArgs a)
 {
     constexpr int kMatrices = 1 + kGated;
-    typedef Stretch<T, kAccess, kGated || kShared> Part;
+    typedef Stretch<T, kAccess, kAccess == WORDS && !kGated && !kShared ? 4 : 2> Part;
     constexpr int kBatch = Part::kBatch;
     __shared__ __attribute__((aligned(16))) v4f sums[kShared ? kMatrices * kWaves * NACHO_WAVE : 1];
     __shared__ uint16_t choice[kMostSlots], active[kMostExperts], lists[kWaves][kMostTokens];
@@ -205,7 +186,13 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
                 }
             };
             // (weights first: they have the longest way)
-            if (begin < end) fetch_rows(one, begin);
+            // (every wavefront starts somewhere else along k: rows are often a power of two apart, and so would be what is read at a time)
+            const int turn = kShared ? 0 : item % stretches;
+            auto at = [&](int s) {
+                const int t = (s < end ? s : end - 1) + turn;      // (behind the last stretch it is loaded again: no branch around a load)
+                return kShared || t < stretches ? t : t - stretches;
+            };
+            if (begin < end) fetch_rows(one, at(begin));
             m = slots_of(a, choice, e, list);
             wave_sync();
 #pragma unroll
@@ -215,15 +202,14 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
 #pragma unroll
                 for (int h = 0; h < kMatrices; ++h) acc[g][h] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
             }
-            if (begin < end) fetch_x(one, begin, 0);
+            if (begin < end) fetch_x(one, at(begin), 0);
             for (int s = begin; s < end; s += 2) {
-                const int next = s + 1 < end ? s + 1 : s, after = s + 2 < end ? s + 2 : s;
-                fetch_rows(two, next);
-                fetch_x(two, next, 0);
-                multiply(one, s);
-                fetch_rows(one, after);
-                fetch_x(one, after, 0);
-                if (s + 1 < end) multiply(two, next);
+                fetch_rows(two, at(s + 1));
+                fetch_x(two, at(s + 1), 0);
+                multiply(one, at(s));
+                fetch_rows(one, at(s + 2));
+                fetch_x(one, at(s + 2), 0);
+                if (s + 1 < end) multiply(two, at(s + 1));
             }
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
@@ -272,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
 // for every token in LDS.
 template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_down_kernel(StepArgs a)
 {
-    typedef Stretch<T, kAccess, false> Part;
+    typedef Stretch<T, kAccess, kAccess == WORDS ? 4 : 2> Part;
     constexpr int kSlab = kMostTokens * kTall, kGroups = kMostTokens / 16, kBatch = Part::kBatch;
     __shared__ __attribute__((aligned(16))) float slab[kWaves][kSlab];             // [token][row] of every wavefront
     __shared__ float share[kMostSlots];

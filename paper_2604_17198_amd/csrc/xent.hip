@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kJoinRows *kJoinParts) xent_join_kernel(XentAr
     };
     float2 v = make_float2(-kInfinity, 0.0f);
     if (m < held) {
-        constexpr int kBatch = 4;
+        constexpr int kBatch = 16;
         for (int t = part; t < tiles; t += kBatch * kJoinParts) {
             float2 next[kBatch];
 #pragma unroll
@@ -303,30 +303,53 @@ struct HeadGradients {
     }
 };
 
-// A row's gradient from its sums, zeros for a row that does not count (without sums: these alone).
-template <typename T> __global__ void __launch_bounds__(256) xent_row_gradients_kernel(XentArgs a, int stretches, int64_t part_stride, int64_t ld)
+// A row's gradient from its sums, zeros for a row that does not count (without sums: these alone).  A workgroup has 256 columns of a
+// row, a wavefront every fourth stretch.
+constexpr int kSumColumns = 256;
+template <typename T> __global__ void __launch_bounds__(256) xent_row_gradients_kernel(XentArgs a, int stretches, int64_t part_stride, int64_t ld, int chunks)
 {
-    const int64_t t = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    constexpr int kWaves = 4, kBatch = 8;
+    __shared__ v4f share[kWaves][NACHO_WAVE];
+    const int64_t number = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, t = number / chunks;
     if (t >= a.rows) return;
-    const int slot = a.slot_of[t];
+    const int slot = a.slot_of[t], lane = lane_id(), wave = (int)threadIdx.x / NACHO_WAVE;
     if (slot >= 0 && !a.sums) return;
-    const float by = a.scale[1];
-    T *const out = static_cast<T *>(a.grad_x) + t * a.ldgx;
-    for (int c = (int)threadIdx.x * 4; c < a.inner; c += 256 * 4) {
-        v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (slot >= 0)
-            for (int p = 0; p < stretches; ++p) v += *reinterpret_cast<const v4f *>(a.sums + (int64_t)p * part_stride + slot * ld + c);
-        if (c + 4 <= a.inner) {
-            typedef T four __attribute__((ext_vector_type(4)));
-            const four w = {(T)(v[0] * by), (T)(v[1] * by), (T)(v[2] * by), (T)(v[3] * by)};
-            __builtin_memcpy(out + c, &w, sizeof w);
-        } else {
-            for (int e = 0; c + e < a.inner; ++e) out[c + e] = (T)(v[e] * by);
+    const int c = (int)(number - t * chunks) * kSumColumns + lane * 4;
+    v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (slot >= 0) {
+        const float *from = a.sums + slot * ld + (c < ld ? c : 0);
+        for (int p = wave; p < stretches; p += kBatch * kWaves) {
+            v4f next[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                next[i] = *reinterpret_cast<const v4f *>(from + (int64_t)(p + i * kWaves < stretches ? p + i * kWaves : p) * part_stride);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (p + i * kWaves < stretches) v += next[i];
         }
+        share[wave][lane] = v;
+        __syncthreads();
+        v = share[0][lane];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) v += share[w][lane];
+    }
+    if (wave != 0 || c >= a.inner) return;
+    const float by = a.scale[1];
+    T *const out = static_cast<T *>(a.grad_x) + t * a.ldgx + c;
+    if (c + 4 <= a.inner) {
+        typedef T four __attribute__((ext_vector_type(4)));
+        const four w = {(T)(v[0] * by), (T)(v[1] * by), (T)(v[2] * by), (T)(v[3] * by)};
+        __builtin_memcpy(out, &w, sizeof w);
+    } else {
+        for (int e = 0; c + e < a.inner; ++e) out[e] = (T)(v[e] * by);
     }
 }
 
 int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
+
+// Rows for the choice of tiles: one group, whose last tile counts as a whole one from 33 rows on (tiles of 32 rows would read the
+// vocabulary's weights several times).
+int64_t counted(int64_t rows) { return rows > 32 ? (rows + 127) / 128 * 128 : rows; }
 
 ProductArgs logits_of(const XentArgs &a, int64_t first, int64_t words)
 {
@@ -337,7 +360,7 @@ ProductArgs logits_of(const XentArgs &a, int64_t first, int64_t words)
     p.experts = 1;
     p.n = (int32_t)words;
     p.k = a.inner;
-    p.slots = a.rows;
+    p.slots = counted(a.rows);
     p.q = a.x;
     p.ldq = a.ldx;
     p.p = static_cast<const char *>(a.head) + first * a.ldh * elem;
@@ -349,6 +372,10 @@ Access access_logits(const XentArgs &a)
     const bool words = a.ldx < 0x7fffffff && a.ldh < 0x7fffffff && in_words({{a.x, a.ldx}, {a.head, a.ldh}, {a.x, a.inner}}, a.elem);
     return words ? WORDS : a.inner * a.elem < 16 ? TINY : ANYWHERE;
 }
+
+// Few rows of words of 16 bytes.  (Rows that start anywhere go through LDS all the same: 16 rows against 100003 x 999 bf16, 66 us by
+// tiles, 86 without.)
+bool few_rows(const XentArgs &a) { return a.rows <= kFewRows && access_logits(a) == WORDS; }
 
 template <typename T> Shape shape_of_logits(const XentArgs &a, int64_t words) { return shape_of<T, FORWARD>(logits_of(a, 0, words), access_logits(a)); }
 
@@ -365,7 +392,11 @@ hipError_t list_rows(const XentArgs &a, hipStream_t s)
 
 }  // namespace
 
-int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary) { return tiles_of_loss(elem, vocabulary) * rows; }
+int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary)
+{
+    const int64_t few = rows <= kFewRows ? xent_few_groups(rows, vocabulary) : 0, tiles = tiles_of_loss(elem, vocabulary);
+    return (few > tiles ? few : tiles) * rows;
+}
 
 // The pieces of the vocabulary: g of one takes at most 256 MiB (which the last cache holds), or 256 words of it.
 XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner)
@@ -378,7 +409,8 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner)
     p.pieces = (vocabulary + p.words - 1) / p.words;
     p.ldg = padded(p.words);
     // stretches of a piece, where its rows alone are too few tiles for the chip
-    const int64_t tall = rows >= 256 && elem == 2 ? 256 : rows > 32 ? 64 : 32, wide = rows >= 256 && elem == 2 ? 256 : rows > 32 ? 64 : 128;
+    const bool large = rows >= 256 && inner >= 256;
+    const int64_t tall = rows <= 32 ? 32 : elem == 4 ? 64 : large ? 256 : 128, wide = rows <= 32 ? 128 : elem == 4 ? 64 : large ? 256 : 128;
     const int64_t tiles = ((rows + tall - 1) / tall) * ((inner + wide - 1) / wide), wanted = tiles > 0 ? 2 * kUnits / tiles : 1;
     const int64_t longest = (p.words + 1023) / 1024;
     p.stretches = wanted < longest ? wanted : longest;
@@ -397,11 +429,18 @@ hipError_t launch_xent(int dtype, const XentArgs &a, hipStream_t s)
     hipError_t rc = hipSuccess;
     by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        const ProductArgs p = logits_of(a, 0, a.vocabulary);
-        const int wide = wide_of(shape_of_logits<T>(a, a.vocabulary));
-        rc = by_size<T, FORWARD>(p, Statistics{a.slot_label, a.partial, a.rows, a.at_label}, access_logits(a), s);
+        int64_t parts;
+        if (few_rows(a)) {
+            parts = xent_few_groups(a.rows, a.vocabulary);
+            rc = launch_xent_few(dtype, a, 0, a.vocabulary, 0, s);
+        } else {
+            const ProductArgs p = logits_of(a, 0, a.vocabulary);
+            const int wide = wide_of(shape_of_logits<T>(a, a.vocabulary));
+            parts = (a.vocabulary + wide - 1) / wide;
+            rc = by_size<T, FORWARD>(p, Statistics{a.slot_label, a.partial, a.rows, a.at_label}, access_logits(a), s);
+        }
         if (rc != hipSuccess) return;
-        xent_join_kernel<<<(unsigned)((a.rows + kJoinRows - 1) / kJoinRows), kJoinRows * kJoinParts, 0, s>>>(a, (int)((a.vocabulary + wide - 1) / wide));
+        xent_join_kernel<<<(unsigned)((a.rows + kJoinRows - 1) / kJoinRows), kJoinRows * kJoinParts, 0, s>>>(a, (int)parts);
         rc = hipGetLastError();
     });
     return rc;
@@ -421,7 +460,8 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
             ProductArgs p = logits_of(a, first, words);
             p.out = a.g;
             p.ldo = plan.ldg;
-            rc = by_size<T, FORWARD>(p, Gradient{a.slot_label, a.slot_lse, a.factor, a.scale, (int32_t)first}, access_logits(a), s);
+            rc = few_rows(a) ? launch_xent_few(dtype, a, first, words, plan.ldg, s)
+                             : by_size<T, FORWARD>(p, Gradient{a.slot_label, a.slot_lse, a.factor, a.scale, (int32_t)first}, access_logits(a), s);
             if (rc != hipSuccess) return;
             if (a.grad_x) {
                 p = ProductArgs{};
@@ -429,7 +469,7 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
                 p.experts = 1;
                 p.n = a.inner;
                 p.k = (int32_t)words;
-                p.slots = a.rows;
+                p.slots = counted(a.rows);
                 p.q = a.g;
                 p.ldq = plan.ldg;
                 p.p = static_cast<const T *>(a.head) + first * a.ldh;
@@ -448,7 +488,7 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
                 p.token = a.token;
                 p.experts = 1;
                 p.n = a.inner;
-                p.slots = a.rows;
+                p.slots = counted(a.rows);
                 p.q = a.g;
                 p.ldq = plan.ldg;
                 p.p = a.x;
@@ -464,9 +504,13 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
         if (a.grad_x && a.rows > 0) {
             XentArgs b = a;
             if (!plan.sums) b.sums = nullptr;
-            const int64_t row = a.rows < (1 << 22) ? a.rows : 1 << 22;
-            xent_row_gradients_kernel<T><<<dim3((unsigned)row, (unsigned)((a.rows + row - 1) / row)), 256, 0, s>>>(
-                b, (int)plan.stretches, a.rows * plan.lds, plan.lds);
+            const int64_t chunks = (a.inner + kSumColumns - 1) / kSumColumns, all = a.rows * chunks, row = all < (1 << 22) ? all : 1 << 22;
+            if ((all + row - 1) / row > 65535) {
+                rc = hipErrorNotSupported;
+                return;
+            }
+            xent_row_gradients_kernel<T><<<dim3((unsigned)row, (unsigned)((all + row - 1) / row)), 256, 0, s>>>(
+                b, (int)plan.stretches, a.rows * plan.lds, plan.lds, (int)chunks);
             rc = hipGetLastError();
         }
     });
