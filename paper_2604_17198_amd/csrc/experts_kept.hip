@@ -34,10 +34,8 @@ struct KeptRows {
             if (width <= 0) return;
             const unsigned exponent = exponent_of(most);
             const float by = steps_per(exponent);
-            float w[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = exponent == 255 ? 0.0f : v[e];
-            const unsigned codes[2] = {four_codes(w[0], w[1], w[2], w[3], by), four_codes(w[4], w[5], w[6], w[7], by)};
+            unsigned codes[2] = {four_codes(v[0], v[1], v[2], v[3], by), four_codes(v[4], v[5], v[6], v[7], by)};
+            if (exponent == 255) codes[0] = codes[1] = 0;
             int8_t *to = kept.code + (int64_t)m * kept.ldc + n;
             if (width >= 8) __builtin_memcpy(to, codes, 8);
             else {

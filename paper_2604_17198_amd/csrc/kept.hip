@@ -49,12 +49,9 @@ template <typename T, bool kWords> __global__ void __launch_bounds__(kThreads) k
     for (int i = 0; i < kColumns; ++i) most = magnitude(v[i]) > most ? magnitude(v[i]) : most;
     const unsigned other = moved<0xb1>(most), exponent = exponent_of(other > most ? other : most);
     const float by = steps_per(exponent);
-    // (of a block with a NaN the codes are 0)
-#pragma unroll
-    for (int i = 0; i < kColumns; ++i) v[i] = exponent == 255 ? 0.0f : v[i];
     unsigned codes[kColumns / 4];
 #pragma unroll
-    for (int i = 0; i < kColumns / 4; ++i) codes[i] = four_codes(v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3], by);
+    for (int i = 0; i < kColumns / 4; ++i) codes[i] = exponent == 255 ? 0 : four_codes(v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3], by);
     if (width <= 0) return;
     int8_t *to = a.kept.code + part.row * a.kept.ldc + part.column;
     if (width >= kColumns) {

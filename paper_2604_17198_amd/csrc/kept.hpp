@@ -27,10 +27,10 @@ __device__ inline float step_of(unsigned exponent)
 }
 __device__ inline unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-// Four codes.  (The sum with 3 x 2^22 rounds to whole numbers, and ends in their lowest byte.)
+// Four codes of finite values.  (The sum with 3 x 2^22 rounds to whole numbers, and ends in their lowest byte.)
 __device__ inline unsigned four_codes(float a, float b, float c, float d, float by)
 {
-    auto code = [&](float v) { return __float_as_uint(fminf(fmaxf(v * by, -127.0f), 127.0f) + 12582912.0f); };
+    auto code = [&](float v) { return __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fmaf(v, by, 12582912.0f), 12582785.0f, 12583039.0f)); };
     const unsigned low = __builtin_amdgcn_perm(code(b), code(a), 0x0c0c0400u), high = __builtin_amdgcn_perm(code(d), code(c), 0x04000c0cu);
     return low | high;
 }

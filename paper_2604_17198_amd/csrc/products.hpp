@@ -721,6 +721,7 @@ hipError_t run(const ProductArgs &a, const Finish &finish, hipStream_t s)
     const int tiles_n = (a.n + kN - 1) / kN;
     // tiles of rows: as many as the slots fill, and a part of one for every expert that may have any
     const int64_t tiles_m = kForm == WEIGHTS ? (int64_t)a.experts * ((a.m + kM - 1) / kM)
+                             : a.experts == 1 ? (a.slots + kM - 1) / kM
                                              : a.slots / kM + (a.slots < a.experts ? a.slots : a.experts);
     if (tiles_m == 0) return hipSuccess;
     // (a launch holds 2^32 threads along its first dimension)
