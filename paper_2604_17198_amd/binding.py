@@ -780,19 +780,35 @@ class Kept8:
     def __init__(self, codes, exponent):
         if codes.dim() != 2 or codes.dtype is not torch.int8 or exponent.dtype is not torch.uint8 or exponent.device != codes.device:
             raise ValueError("Kept8: int8 codes [rows, cols] and uint8 exponents on one device are needed")
-        rows, cols = codes.shape
-        _matrix(exponent, "exponent", rows, -(-cols // self.BLOCK), torch.uint8, codes.device)
-        self.codes, self.exponent, self.shape, self.device = codes, exponent, codes.shape, codes.device
+        device, (rows, cols) = codes.device, codes.shape
+        ldc = _matrix(codes, "codes", None, None, torch.int8, device)
+        lde = _matrix(exponent, "exponent", rows, -(-cols // self.BLOCK), torch.uint8, device)
+        self._take(codes, exponent, ldc, lde, device)
+
+    def _take(self, codes, exponent, ldc, lde, device):
+        self.codes, self.exponent, self.shape, self.device = codes, exponent, codes.shape, device
+        self.c = _Kept(codes.data_ptr(), ldc, exponent.data_ptr(), lde)
 
     @classmethod
     def empty(cls, rows, cols, device):
         """Room for rows of cols columns (16 bytes from one row's codes to the next, or a multiple of them)."""
-        return cls(torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=device)[:, :cols],
-                   torch.empty((rows, -(-cols // cls.BLOCK)), dtype=torch.uint8, device=device))
+        new, ldc, lde = cls.__new__(cls), -(-cols // 16) * 16, -(-cols // cls.BLOCK)
+        codes = torch.empty((rows, ldc), dtype=torch.int8, device=device)
+        new._take(codes if ldc == cols else codes[:, :cols], torch.empty((rows, lde), dtype=torch.uint8, device=device), ldc, lde, codes.device)
+        return new
 
     def descriptor(self, what, rows=None, cols=None, device=None):
-        ldc = _matrix(self.codes, what, rows, cols, torch.int8, device)
-        return _Kept(self.codes.data_ptr(), ldc, self.exponent.data_ptr(), _matrix(self.exponent, what, None, None, torch.uint8, self.device))
+        """For a call on `device`, or else on the current GPU."""
+        r, c = self.shape
+        if (rows is not None and r != rows) or (cols is not None and c != cols):
+            raise ValueError(f"{what}: {r} x {c}, expected {rows} x {cols}")
+        if device is not None:
+            _need(self.device == device, f"{what}: on {self.device}, expected {device}")
+        else:
+            number = self.codes.get_device()
+            if number == _HOST or number != _current_device():
+                raise ValueError(f"{what}: on {self.device}, and not on the current GPU")
+        return C.byref(self.c)
 
 
 def nacho_keep8(x, out=None):
@@ -802,8 +818,7 @@ def nacho_keep8(x, out=None):
     rows, cols = x.shape
     if out is None:
         out = Kept8.empty(rows, cols, x.device)
-    c = out.descriptor("out", rows, cols, x.device)
-    _check(lib().nacho_keep8(_ptr(x), ldx, rows, cols, dt, C.byref(c), _stream()), "nacho_keep8")
+    _check(lib().nacho_keep8(x.data_ptr(), ldx, rows, cols, dt, out.descriptor("out", rows, cols, x.device), _stream()), "nacho_keep8")
     return out
 
 
@@ -812,10 +827,12 @@ def nacho_restore8(kept: Kept8, dtype=torch.float32, out=None):
     c = kept.descriptor("kept")
     rows, cols = kept.shape
     if out is None:
-        out = torch.empty((rows, cols), dtype=dtype, device=kept.device)
-    dt = model_dtype_code(out.dtype)
-    ldo = _matrix(out, "out", rows, cols, out.dtype, kept.device)
-    _check(lib().nacho_restore8(C.byref(c), rows, cols, dt, _ptr(out), ldo, _stream()), "nacho_restore8")
+        out, ldo = torch.empty((rows, cols), dtype=dtype, device=kept.device), cols
+    else:
+        dtype = out.dtype
+        ldo = _matrix(out, "out", rows, cols, dtype, kept.device)
+    dt = model_dtype_code(dtype)
+    _check(lib().nacho_restore8(c, rows, cols, dt, _ptr(out), ldo, _stream()), "nacho_restore8")
     return out
 
 
@@ -824,7 +841,7 @@ _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 def _stack(t, what, shape, dtype, device):
     """Matrices (or rows) of one size, each with contiguous rows: leading dimension and distance."""
-    if tuple(t.shape) != shape or t.dtype is not dtype or t.device != device:
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {shape} of {dtype} on {device}")
     stride, cols = t.stride(), shape[-1]
     if stride[-1] != 1 and cols > 1:
@@ -846,7 +863,11 @@ def _layer(x, weight, expert_pos, token, bias, act):
         raise ValueError("weight: [experts, outer, inner] is needed")
     shape = tuple(weight.shape)
     experts, outer, inner = shape
-    ldx = _matrix(x.codes if kept else x, "x", None, inner)
+    if kept:
+        x.descriptor("x", None, inner)
+        ldx = inner
+    else:
+        ldx = _matrix(x, "x", None, inner)
     ldw, stride = _stack(weight, "weight", shape, dtype, dev)
     _vector_of(expert_pos, "expert_pos", experts + 1, torch.int32, dev)
     bounds, tokens = expert_pos.data_ptr(), x.shape[0]
@@ -876,7 +897,7 @@ def nacho_experts(x, weight, expert_pos, token=None, bias=None, act="none", y=No
         ldy = _matrix(y, "y", slots, outer, x.dtype, x.device)
     if type(pre) is Kept8:
         kept = pre.descriptor("pre", slots, outer, x.device)
-        _check(lib().nacho_experts_keep8(C.byref(c), _ptr(y), ldy, C.byref(kept), _stream()), "nacho_experts_keep8")
+        _check(lib().nacho_experts_keep8(C.byref(c), _ptr(y), ldy, kept, _stream()), "nacho_experts_keep8")
         return y
     ldpre = _matrix(pre, "pre", slots, outer, x.dtype, x.device) if pre is not None else 0
     _check(lib().nacho_experts(C.byref(c), _ptr(y), ldy, _ptr(pre), ldpre, _stream()), "nacho_experts")
@@ -909,8 +930,7 @@ def nacho_experts_grad(grad_y, x, weight, expert_pos, token=None, act="none", pr
         cx = x.descriptor("x", None, inner, dev) if kept_x else None
         cp = pre.descriptor("pre", slots, outer, dev) if kept_pre else None
         ws, room = _room_for("nacho_experts_keep8_workspace_bytes", c, ws, dev)
-        _check(lib().nacho_experts_keep8_grad(C.byref(c), C.byref(cx) if kept_x else None, _ptr(grad_y), ldgy, None if kept_pre else _ptr(pre), ldpre,
-                                              C.byref(cp) if kept_pre else None, _ptr(grad_x), ldgx, _ptr(grad_weight), ldgw, gap,
+        _check(lib().nacho_experts_keep8_grad(C.byref(c), cx, _ptr(grad_y), ldgy, None if kept_pre else _ptr(pre), ldpre, cp, _ptr(grad_x), ldgx, _ptr(grad_weight), ldgw, gap,
                                               _ptr(grad_bias), gb, _ptr(ws), room, _stream()), "nacho_experts_keep8_grad")
         return grad_x, grad_weight
     ws, room = _room_for("nacho_experts_workspace_bytes", c, ws, dev)
