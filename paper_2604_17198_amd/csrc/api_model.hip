@@ -223,12 +223,10 @@ int32_t check_xent(const nacho_xent_layer *l)
     if (l->n_rows < 0 || l->n_rows > kMostRows || l->vocabulary < 1 || l->inner < 1) return NACHO_ERR_INVALID_ARG;
     return l->vocabulary >= 1 << 24 || l->inner >= 1 << 24 ? NACHO_ERR_UNSUPPORTED : NACHO_OK;
 }
-// The arrays that both calls read, into the kernels' arguments.
-bool take_xent(const nacho_xent_layer *l, XentArgs *a)
+// What both calls read, as the kernels' arguments.
+void take_xent(const nacho_xent_layer *l, XentArgs *a)
 {
     const int64_t elem = value_bytes(l->dtype);
-    if (!matrix(l->x, l->n_rows, l->inner, l->ldx, elem) || !matrix(l->head, l->vocabulary, l->inner, l->ldh, elem)) return false;
-    if ((l->n_rows > 0 && !l->label) || !aligned(l->label, (uintptr_t)l->label_bytes) || !aligned(l->weight, 4)) return false;
     *a = XentArgs{};
     a->x = l->x;
     a->ldx = l->ldx;
@@ -242,9 +240,22 @@ bool take_xent(const nacho_xent_layer *l, XentArgs *a)
     a->half = l->dtype == NACHO_F16;
     a->label = l->label;
     a->weight = l->weight;
+}
+bool check_xent_arrays(const nacho_xent_layer *l)
+{
+    const int64_t elem = value_bytes(l->dtype);
+    if (!matrix(l->x, l->n_rows, l->inner, l->ldx, elem) || !matrix(l->head, l->vocabulary, l->inner, l->ldh, elem)) return false;
+    if ((l->n_rows > 0 && !l->label) || !aligned(l->label, (uintptr_t)l->label_bytes) || !aligned(l->weight, 4)) return false;
     return true;
 }
-size_t carve_xent(void *ws, const nacho_xent_layer *l, XentArgs *a)
+void carve_copies(Slices *c, const nacho_xent_layer *l, const XentPlan &plan, XentArgs *a)
+{
+    const int64_t row = (l->inner + 7) / 8 * 8 * value_bytes(l->dtype);
+    if (!xent_pads(*a)) return;
+    a->padded_x = c->take<char>(l->n_rows * row);
+    a->padded_head = c->take<char>(plan.words * row);
+}
+size_t carve_xent(void *ws, const nacho_xent_layer *l, const XentPlan &plan, XentArgs *a)
 {
     Slices c(ws);
     a->bounds = c.take<int32_t>(2);
@@ -252,6 +263,7 @@ size_t carve_xent(void *ws, const nacho_xent_layer *l, XentArgs *a)
     a->slot_label = c.take<int32_t>(l->n_rows);
     a->at_label = c.take<float>(l->n_rows);
     a->partial = c.take<float2>(xent_partials((int)value_bytes(l->dtype), l->n_rows, l->vocabulary));
+    carve_copies(&c, l, plan, a);
     return align_up(c.off, 256);
 }
 size_t carve_xent_grad(void *ws, const nacho_xent_layer *l, const XentPlan &plan, bool sums, XentArgs *a)
@@ -266,9 +278,13 @@ size_t carve_xent_grad(void *ws, const nacho_xent_layer *l, const XentPlan &plan
     a->slot_of = c.take<int32_t>(l->n_rows);
     a->g = c.take<char>(l->n_rows * plan.ldg * value_bytes(l->dtype));
     if (sums && plan.sums) a->sums = c.take<float>(plan.stretches * l->n_rows * plan.lds);
+    carve_copies(&c, l, plan, a);
     return align_up(c.off, 256);
 }
-XentPlan plan_of(const nacho_xent_layer *l) { return xent_plan((int)value_bytes(l->dtype), l->n_rows, l->vocabulary, l->inner); }
+XentPlan plan_of(const nacho_xent_layer *l, const XentArgs &a, bool gradient)
+{
+    return xent_plan(a.elem, l->n_rows, l->vocabulary, l->inner, xent_pads(a), gradient);
+}
 
 // The sizes of a layer of single steps.
 int32_t check_step(const nacho_experts_step_layer *l)
@@ -695,18 +711,22 @@ int32_t nacho_xent_workspace_bytes(const nacho_xent_layer *layer, size_t *bytes)
 {
     if (!bytes) return NACHO_ERR_INVALID_ARG;
     const int32_t rc = check_xent(layer);
-    XentArgs a{};
-    if (rc == NACHO_OK) *bytes = carve_xent(nullptr, layer, &a);
-    return rc;
+    if (rc != NACHO_OK) return rc;
+    XentArgs a;
+    take_xent(layer, &a);
+    *bytes = carve_xent(nullptr, layer, plan_of(layer, a, false), &a);
+    return NACHO_OK;
 }
 
 int32_t nacho_xent_grad_workspace_bytes(const nacho_xent_layer *layer, size_t *bytes)
 {
     if (!bytes) return NACHO_ERR_INVALID_ARG;
     const int32_t rc = check_xent(layer);
-    XentArgs a{};
-    if (rc == NACHO_OK) *bytes = carve_xent_grad(nullptr, layer, plan_of(layer), true, &a);
-    return rc;
+    if (rc != NACHO_OK) return rc;
+    XentArgs a;
+    take_xent(layer, &a);
+    *bytes = carve_xent_grad(nullptr, layer, plan_of(layer, a, true), true, &a);
+    return NACHO_OK;
 }
 
 int32_t nacho_xent(const nacho_xent_layer *layer, float *loss, float *lse, void *ws, size_t ws_bytes, void *hip_stream)
@@ -715,8 +735,10 @@ int32_t nacho_xent(const nacho_xent_layer *layer, float *loss, float *lse, void 
     if (rc != NACHO_OK) return rc;
     const nacho_xent_layer &l = *layer;
     XentArgs a;
-    if (!take_xent(layer, &a) || (l.n_rows > 0 && (!loss || !lse)) || !aligned(loss, 4) || !aligned(lse, 4)) return NACHO_ERR_INVALID_ARG;
-    const size_t need = carve_xent(ws, layer, &a);
+    if (!check_xent_arrays(layer) || (l.n_rows > 0 && (!loss || !lse)) || !aligned(loss, 4) || !aligned(lse, 4)) return NACHO_ERR_INVALID_ARG;
+    take_xent(layer, &a);
+    const XentPlan plan = plan_of(layer, a, false);
+    const size_t need = carve_xent(ws, layer, plan, &a);
     if (!ws || ws_bytes < need || !aligned(ws, 16)) return NACHO_ERR_WORKSPACE;
     const int64_t elem = a.elem, by_row = l.n_rows * 4;
     if (!apart({{loss, by_row}, {lse, by_row}, {ws, (int64_t)need}},
@@ -727,7 +749,7 @@ int32_t nacho_xent(const nacho_xent_layer *layer, float *loss, float *lse, void 
     a.lse = lse;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     profile_begin(s);
-    if (const hipError_t e = launch_xent(l.dtype, a, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
+    if (const hipError_t e = launch_xent(l.dtype, a, plan, s)) return e == hipErrorNotSupported ? NACHO_ERR_UNSUPPORTED : NACHO_ERR_HIP;
     profile_mark("xent");
     return NACHO_OK;
 }
@@ -739,11 +761,12 @@ int32_t nacho_xent_grad(const nacho_xent_layer *layer, const float *lse, void *g
     if (rc != NACHO_OK) return rc;
     const nacho_xent_layer &l = *layer;
     XentArgs a;
-    if (!take_xent(layer, &a) || (l.n_rows > 0 && !lse) || !aligned(lse, 4)) return NACHO_ERR_INVALID_ARG;
+    if (!check_xent_arrays(layer) || (l.n_rows > 0 && !lse) || !aligned(lse, 4)) return NACHO_ERR_INVALID_ARG;
+    take_xent(layer, &a);
     const int64_t elem = a.elem, by_row = l.n_rows * 4;
     if ((grad_x && !matrix(grad_x, l.n_rows, l.inner, ldgx, elem)) || (grad_head && !matrix(grad_head, l.vocabulary, l.inner, ldgh, elem)))
         return NACHO_ERR_INVALID_ARG;
-    const XentPlan plan = plan_of(layer);
+    const XentPlan plan = plan_of(layer, a, true);
     const size_t need = carve_xent_grad(ws, layer, plan, grad_x != nullptr, &a);
     if (!ws || ws_bytes < need || !aligned(ws, 16)) return NACHO_ERR_WORKSPACE;
     if (!apart({{grad_x, grad_x ? span(l.n_rows, l.inner, ldgx, elem) : 0}, {grad_head, grad_head ? span(l.vocabulary, l.inner, ldgh, elem) : 0},

@@ -188,15 +188,19 @@ struct XentArgs {
     float *scale;
     void *g;
     float *sums;
+    // of either, where rows start anywhere: the rows that count and a piece of head as rows of whole words (NULL: not wanted)
+    void *padded_x, *padded_head;
 };
-// How a gradient call goes through the vocabulary: `pieces` of `words`, each in `stretches` of `k_part` for the rows' sums.
+// How a call goes through the vocabulary: `pieces` of `words`, each in `stretches` of `k_part` for the rows' sums.
 struct XentPlan {
     int64_t pieces, words, ldg, stretches, k_part, lds;
     bool sums;                     // (of the rows' gradients, in 32 bits: `lds` apart, one set a stretch)
 };
 int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary);
-XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner);
-hipError_t launch_xent(int dtype, const XentArgs &a, hipStream_t s);
+XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bool pads, bool gradient);
+constexpr int64_t kPaddedFrom = 512;   // rows
+bool xent_pads(const XentArgs &a);
+hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s);
 // The logits of up to kFewRows rows of words of 16 bytes (words `first` .. of the vocabulary): statistics by workgroup in a.partial, or,
 // where there is a.g, g.
 constexpr int kFewRows = 64;

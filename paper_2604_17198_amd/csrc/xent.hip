@@ -89,9 +89,10 @@ struct Statistics {
     static constexpr bool kParts = false;
     static constexpr unsigned parts() { return 1; }
     const int32_t *label;
-    float2 *partial;               // [tiles of columns][rows]
+    float2 *partial;               // [tiles of columns][rows], of the piece
     int64_t rows;
     float *at_label;
+    int32_t first;                 // the piece's first word of the vocabulary
     template <typename Tile>
     __device__ void end(const ProductArgs &a, const Place &at, v4f (&acc)[Tile::kFragM][Tile::kFragN], char *stage0, char *) const
     {
@@ -125,7 +126,7 @@ struct Statistics {
             const int r = at.wm + i * 16 + lane % 16;
             const unsigned m = (unsigned)at.m0 + r;
             const bool there = m < (unsigned)at.m_end;
-            const int c = there ? label[m] - c0 : -1;
+            const int c = there ? label[m] - first - c0 : -1;
             if (__any(c >= 0 && c < Tile::kTileN)) {
 #pragma unroll
                 for (int j = 0; j < Tile::kFragN; ++j)
@@ -242,6 +243,20 @@ struct Gradient {
     }
 };
 
+// Eight results of a row that starts anywhere.
+template <typename T> __device__ inline void put_anywhere(T *to, const float (&v)[8], int width)
+{
+    typename Word<T>::type w[8 / Word<T>::n];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e / Word<T>::n][e % Word<T>::n] = (T)v[e];
+    if (width >= 8) __builtin_memcpy(to, w, sizeof w);
+    else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < width) to[e] = w[e / Word<T>::n][e % Word<T>::n];
+    }
+}
+
 // Gradients of the rows: sums in 32 bits by stretches of the vocabulary, or, where there is one, the result itself.
 struct RowGradients {
     static constexpr bool kParts = true;
@@ -253,6 +268,7 @@ struct RowGradients {
     bool first;                    // (the sums hold nothing yet)
     const int32_t *token;
     const float *scale;
+    int32_t inner;                 // columns of the result (the product may have a few more)
     template <typename Tile>
     __device__ void end(const ProductArgs &a, const Place &at, v4f (&acc)[Tile::kFragM][Tile::kFragN], char *stage0, char *stage1) const
     {
@@ -272,10 +288,10 @@ struct RowGradients {
         } else {
             const float by = scale[1];
             T *const out = static_cast<T *>(a.out);
-            Tile::each_row(a, at, acc, stage0, stage1, [&](unsigned m, int n, int width, float (&v)[8]) {
+            Tile::each_row(a, at, acc, stage0, stage1, [&](unsigned m, int n, int, float (&v)[8]) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= by;
-                Tile::put(out + (int64_t)token[m] * a.ldo + n, v, width);
+                put_anywhere(out + (int64_t)token[m] * a.ldo + n, v, inner - n);
             });
         }
     }
@@ -286,7 +302,7 @@ struct HeadGradients {
     static constexpr bool kParts = false;
     static constexpr unsigned parts() { return 1; }
     const float *scale;
-    int32_t last;                  // words of the piece (the rows of g may have more)
+    int32_t last, inner;           // words of the piece, columns (rows of g, and the product, may have a few more)
     template <typename Tile>
     __device__ void end(const ProductArgs &a, const Place &at, v4f (&acc)[Tile::kFragM][Tile::kFragN], char *stage0, char *stage1) const
     {
@@ -295,10 +311,10 @@ struct HeadGradients {
         T *const out = static_cast<T *>(a.out);
         Place mine = at;
         mine.m_end = last;
-        Tile::each_row(a, mine, acc, stage0, stage1, [&](unsigned m, int n, int width, float (&v)[8]) {
+        Tile::each_row(a, mine, acc, stage0, stage1, [&](unsigned m, int n, int, float (&v)[8]) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] *= by;
-            Tile::put(out + (int64_t)m * a.ldo + n, v, width);
+            put_anywhere(out + (int64_t)m * a.ldo + n, v, inner - n);
         });
     }
 };
@@ -345,39 +361,79 @@ template <typename T> __global__ void __launch_bounds__(256) xent_row_gradients_
     }
 }
 
+// Rows (by a list, or all of them) whose words of 16 bytes start anywhere, as rows of whole words with zeros behind their end.
+template <typename T>
+__global__ void __launch_bounds__(256) xent_pad_kernel(const void *from, int64_t ld, int cols, const int32_t *list, const int32_t *held, int64_t rows,
+                                                       void *to, int64_t ldp)
+{
+    const int words = (int)(ldp / Word<T>::n);
+    const int64_t most = held ? (int64_t)*held : rows, each = (int64_t)gridDim.x * (256 / NACHO_WAVE);
+    for (int64_t r = (int64_t)blockIdx.x * (256 / NACHO_WAVE) + (int)threadIdx.x / NACHO_WAVE; r < most; r += each) {
+        const T *row = static_cast<const T *>(from) + (list ? (int64_t)list[r] : r) * ld;
+        for (int w = lane_id(); w < words; w += NACHO_WAVE) {
+            const Ragged<T, false> word(cols, w * Word<T>::n);
+            *reinterpret_cast<v4u *>(static_cast<T *>(to) + r * ldp + w * Word<T>::n) = word.placed(word.load(row + w * Word<T>::n));
+        }
+    }
+}
+
 int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
 
 // Rows for the choice of tiles: one group, whose last tile counts as a whole one from 33 rows on (tiles of 32 rows would read the
 // vocabulary's weights several times).
 int64_t counted(int64_t rows) { return rows > 32 ? (rows + 127) / 128 * 128 : rows; }
 
-ProductArgs logits_of(const XentArgs &a, int64_t first, int64_t words)
-{
-    const int elem = a.elem;
-    ProductArgs p{};
-    p.bounds = a.bounds;
-    p.token = a.token;
-    p.experts = 1;
-    p.n = (int32_t)words;
-    p.k = a.inner;
-    p.slots = counted(a.rows);
-    p.q = a.x;
-    p.ldq = a.ldx;
-    p.p = static_cast<const char *>(a.head) + first * a.ldh * elem;
-    p.ldp = a.ldh;
-    return p;
-}
-Access access_logits(const XentArgs &a)
+// The rows that count and a piece of the vocabulary as the products read them: where they lie, or from the workspace as rows of whole
+// words.
+struct Sides {
+    const void *x, *head;
+    int64_t ldx, ldh;
+    const int32_t *token;          // rows of x, or NULL: they lie one after the other
+    int32_t inner;
+    Access access;
+};
+Access access_of_rows(const XentArgs &a)
 {
     const bool words = a.ldx < 0x7fffffff && a.ldh < 0x7fffffff && in_words({{a.x, a.ldx}, {a.head, a.ldh}, {a.x, a.inner}}, a.elem);
     return words ? WORDS : a.inner * a.elem < 16 ? TINY : ANYWHERE;
 }
+template <typename T> hipError_t pad(const void *from, int64_t ld, const XentArgs &a, const int32_t *list, const int32_t *held, int64_t rows, void *to, hipStream_t s)
+{
+    const int64_t groups = (rows + 3) / 4;
+    xent_pad_kernel<T><<<(unsigned)(groups < 8 * kUnits ? groups : 8 * kUnits), 256, 0, s>>>(from, ld, a.inner, list, held, rows, to, padded(a.inner));
+    return hipGetLastError();
+}
+// (the rows of x are copied with the first piece)
+template <typename T> hipError_t sides_of(const XentArgs &a, int64_t first, int64_t words, Sides *v, hipStream_t s)
+{
+    const void *head = static_cast<const T *>(a.head) + first * a.ldh;
+    *v = Sides{a.x, head, a.ldx, a.ldh, a.token, a.inner, access_of_rows(a)};
+    if (!a.padded_x) return hipSuccess;
+    *v = Sides{a.padded_x, a.padded_head, padded(a.inner), padded(a.inner), nullptr, (int32_t)padded(a.inner), WORDS};
+    if (first == 0)
+        if (const hipError_t e = pad<T>(a.x, a.ldx, a, a.token, a.bounds + 1, a.rows, a.padded_x, s)) return e;
+    return pad<T>(head, a.ldh, a, nullptr, nullptr, words, a.padded_head, s);
+}
+
+ProductArgs logits_of(const XentArgs &a, const Sides &v, int64_t words)
+{
+    ProductArgs p{};
+    p.bounds = a.bounds;
+    p.token = v.token;
+    p.experts = 1;
+    p.n = (int32_t)words;
+    p.k = v.inner;
+    p.slots = counted(a.rows);
+    p.q = v.x;
+    p.ldq = v.ldx;
+    p.p = v.head;
+    p.ldp = v.ldh;
+    return p;
+}
 
 // Few rows of words of 16 bytes.  (Rows that start anywhere go through LDS all the same: 16 rows against 100003 x 999 bf16, 66 us by
 // tiles, 86 without.)
-bool few_rows(const XentArgs &a) { return a.rows <= kFewRows && access_logits(a) == WORDS; }
-
-template <typename T> Shape shape_of_logits(const XentArgs &a, int64_t words) { return shape_of<T, FORWARD>(logits_of(a, 0, words), access_logits(a)); }
+bool few_rows(const XentArgs &a) { return a.rows <= kFewRows && access_of_rows(a) == WORDS; }
 
 // (the rows' access is not known where workspaces are sized: the narrowest tiles there can be)
 int64_t tiles_of_loss(int elem, int64_t vocabulary) { return (vocabulary + (elem == 4 ? 63 : 127)) / (elem == 4 ? 64 : 128); }
@@ -398,12 +454,18 @@ int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary)
     return (few > tiles ? few : tiles) * rows;
 }
 
-// The pieces of the vocabulary: g of one takes at most 256 MiB (which the last cache holds), or 256 words of it.
-XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner)
+// Whether the products read copies of the rows and of the vocabulary's weights.  Rows that start anywhere take twice the time in the
+// products; the copies are two passes over the weights a call.
+bool xent_pads(const XentArgs &a) { return a.elem == 2 && a.rows >= kPaddedFrom && access_of_rows(a) == ANYWHERE; }
+
+// The pieces of the vocabulary: g of one takes at most 256 MiB (which the last cache holds), or 256 words of it; and so do its weights
+// where they are copied.  The loss's call, which has no g, goes by these alone.
+XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bool pads, bool gradient)
 {
     constexpr int64_t kRoom = 256 << 20;
     XentPlan p;
-    const int64_t most = rows > 0 ? kRoom / (rows * elem) / 256 * 256 : vocabulary, least = most > 256 ? most : 256;
+    const int64_t by_g = rows > 0 && gradient ? kRoom / (rows * elem) / 256 * 256 : vocabulary, by_copy = pads ? kRoom / (padded(inner) * elem) / 256 * 256 : vocabulary;
+    const int64_t most = by_g < by_copy ? by_g : by_copy, least = most > 256 ? most : 256;
     p.pieces = (vocabulary + least - 1) / least;
     p.words = p.pieces > 1 ? ((vocabulary + p.pieces - 1) / p.pieces + 255) / 256 * 256 : vocabulary;
     p.pieces = (vocabulary + p.words - 1) / p.words;
@@ -422,22 +484,29 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner)
     return p;
 }
 
-hipError_t launch_xent(int dtype, const XentArgs &a, hipStream_t s)
+hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s)
 {
     if (a.rows == 0) return hipSuccess;
     if (const hipError_t e = list_rows(a, s)) return e;
     hipError_t rc = hipSuccess;
     by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        int64_t parts;
+        int64_t parts = 0;
         if (few_rows(a)) {
             parts = xent_few_groups(a.rows, a.vocabulary);
             rc = launch_xent_few(dtype, a, 0, a.vocabulary, 0, s);
         } else {
-            const ProductArgs p = logits_of(a, 0, a.vocabulary);
-            const int wide = wide_of(shape_of_logits<T>(a, a.vocabulary));
-            parts = (a.vocabulary + wide - 1) / wide;
-            rc = by_size<T, FORWARD>(p, Statistics{a.slot_label, a.partial, a.rows, a.at_label}, access_logits(a), s);
+            for (int64_t first = 0; first < a.vocabulary; first += plan.words) {
+                const int64_t words = a.vocabulary - first < plan.words ? a.vocabulary - first : plan.words;
+                Sides v;
+                rc = sides_of<T>(a, first, words, &v, s);
+                if (rc != hipSuccess) return;
+                const ProductArgs p = logits_of(a, v, words);
+                const int wide = wide_of(shape_of<T, FORWARD>(p, v.access));
+                rc = by_size<T, FORWARD>(p, Statistics{a.slot_label, a.partial + parts * a.rows, a.rows, a.at_label, (int32_t)first}, v.access, s);
+                if (rc != hipSuccess) return;
+                parts += (words + wide - 1) / wide;
+            }
         }
         if (rc != hipSuccess) return;
         xent_join_kernel<<<(unsigned)((a.rows + kJoinRows - 1) / kJoinRows), kJoinRows * kJoinParts, 0, s>>>(a, (int)parts);
@@ -451,53 +520,53 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
     hipError_t rc = list_rows(a, s);
     if (rc != hipSuccess) return rc;
     const int elem = a.elem;
-    const bool head_words = a.ldh < 0x7fffffff && in_words({{a.head, a.ldh}, {a.head, a.inner}}, elem);
-    const bool x_words = a.ldx < 0x7fffffff && in_words({{a.x, a.ldx}, {a.x, a.inner}}, elem);
     by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
         for (int64_t first = 0; first < a.vocabulary; first += plan.words) {
             const int64_t words = a.vocabulary - first < plan.words ? a.vocabulary - first : plan.words;
-            ProductArgs p = logits_of(a, first, words);
+            Sides v;
+            rc = sides_of<T>(a, first, words, &v, s);
+            if (rc != hipSuccess) return;
+            ProductArgs p = logits_of(a, v, words);
             p.out = a.g;
             p.ldo = plan.ldg;
             rc = few_rows(a) ? launch_xent_few(dtype, a, first, words, plan.ldg, s)
-                             : by_size<T, FORWARD>(p, Gradient{a.slot_label, a.slot_lse, a.factor, a.scale, (int32_t)first}, access_logits(a), s);
+                             : by_size<T, FORWARD>(p, Gradient{a.slot_label, a.slot_lse, a.factor, a.scale, (int32_t)first}, v.access, s);
             if (rc != hipSuccess) return;
             if (a.grad_x) {
                 p = ProductArgs{};
                 p.bounds = a.bounds;
                 p.experts = 1;
-                p.n = a.inner;
+                p.n = v.inner;
                 p.k = (int32_t)words;
                 p.slots = counted(a.rows);
                 p.q = a.g;
                 p.ldq = plan.ldg;
-                p.p = static_cast<const T *>(a.head) + first * a.ldh;
-                p.ldp = a.ldh;
+                p.p = v.head;
+                p.ldp = v.ldh;
                 p.out = a.grad_x;
                 p.ldo = a.ldgx;
                 const unsigned stretches = (unsigned)((words + plan.k_part - 1) / plan.k_part);
-                const bool in = head_words && plan.ldg < 0x7fffffff && (plan.sums || in_words({{a.grad_x, a.ldgx}}, elem));
-                rc = by_size<T, ROWS>(p, RowGradients{stretches, (int)plan.k_part, plan.sums ? a.sums : nullptr, a.rows * plan.lds, plan.lds, first == 0, a.token, a.scale},
-                                      in ? WORDS : access_of<ROWS>(p, elem), s);
+                const RowGradients f{stretches, (int)plan.k_part, plan.sums ? a.sums : nullptr, a.rows * plan.lds, plan.lds, first == 0, a.token, a.scale, a.inner};
+                rc = by_size<T, ROWS>(p, f, v.access == WORDS && plan.ldg < 0x7fffffff ? WORDS : access_of<ROWS>(p, elem), s);
                 if (rc != hipSuccess) return;
             }
             if (a.grad_head) {
                 p = ProductArgs{};
                 p.bounds = a.bounds;
-                p.token = a.token;
+                p.token = v.token;
                 p.experts = 1;
-                p.n = a.inner;
+                p.n = v.inner;
                 p.slots = counted(a.rows);
                 p.q = a.g;
                 p.ldq = plan.ldg;
-                p.p = a.x;
-                p.ldp = a.ldx;
+                p.p = v.x;
+                p.ldp = v.ldx;
                 p.out = static_cast<T *>(a.grad_head) + first * a.ldgh;
                 p.ldo = a.ldgh;
-                const bool in = x_words && plan.ldg < 0x7fffffff && in_words({{a.grad_head, a.ldgh}}, elem);
+                const bool in = v.access == WORDS && plan.ldg < 0x7fffffff;
                 p.m = (int32_t)(in ? padded(words) : words);
-                rc = by_size<T, WEIGHTS>(p, HeadGradients{a.scale, (int32_t)words}, in ? WORDS : access_of<WEIGHTS>(p, elem), s);
+                rc = by_size<T, WEIGHTS>(p, HeadGradients{a.scale, (int32_t)words, a.inner}, in ? WORDS : access_of<WEIGHTS>(p, elem), s);
                 if (rc != hipSuccess) return;
             }
         }

@@ -114,6 +114,19 @@ def test_pieces_of_the_vocabulary(dtype, rows):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sizes", [(511, 1000, 41), (512, 1000, 41), (600, 4097, 333), (2300, 9000, 131), (8300, 20_003, 41), (530, 40_000, 4097)])
+def test_many_rows_that_start_anywhere(sizes, dtype):
+    """Rows of odd lengths, copied or not, in one piece of the vocabulary or in several."""
+    check(problem(12, *sizes, dtype, masked=0.2), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_many_rows_apart(dtype):
+    check(problem(13, 700, 900, 56, dtype, masked=0.2, pad=3), dtype, 3)
+    check(problem(13, 700, 900, 56, dtype, masked=0.2), dtype, 5)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("pad", [1, 4, 8])
 def test_rows_apart(dtype, pad):
     check(problem(3, 70, 333, 56, dtype, masked=0.2, pad=pad), dtype, pad)
