@@ -221,7 +221,10 @@ int32_t check_xent(const nacho_xent_layer *l)
 {
     if (!l || !value_type(l->dtype) || (l->label_bytes != 4 && l->label_bytes != 8)) return NACHO_ERR_INVALID_ARG;
     if (l->n_rows < 0 || l->n_rows > kMostRows || l->vocabulary < 1 || l->inner < 1) return NACHO_ERR_INVALID_ARG;
-    return l->vocabulary >= 1 << 24 || l->inner >= 1 << 24 ? NACHO_ERR_UNSUPPORTED : NACHO_OK;
+    if (l->vocabulary >= 1 << 24 || l->inner >= 1 << 24) return NACHO_ERR_UNSUPPORTED;
+    // (the smallest tiles of each product; launches of the gradient's sums)
+    const int64_t rows = (l->n_rows + 63) / 64, words = (l->vocabulary + 63) / 64, columns = (l->inner + 63) / 64, most = 0x7fffffff - (1 << 22);
+    return rows * words > most || rows * columns > most || words * columns > most ? NACHO_ERR_UNSUPPORTED : NACHO_OK;
 }
 // What both calls read, as the kernels' arguments.
 void take_xent(const nacho_xent_layer *l, XentArgs *a)

@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
             }
             wave_sync();
         };
-        if (takers[e] <= 16) groups_of(std::integral_constant<int, 1>());
+        if (__builtin_amdgcn_readfirstlane(takers[e]) <= 16) groups_of(std::integral_constant<int, 1>());
         else groups_of(std::integral_constant<int, kMostTokens / 16>());
     }
 }

@@ -159,8 +159,8 @@ __global__ void __launch_bounds__(kJoinRows *kJoinParts) xent_join_kernel(XentAr
 {
     __shared__ float2 share[kJoinParts][kJoinRows];
     const int r = (int)threadIdx.x % kJoinRows, part = (int)threadIdx.x / kJoinRows;
-    const int64_t m = (int64_t)blockIdx.x * kJoinRows + r, held = a.bounds[1];
-    if ((int64_t)blockIdx.x * kJoinRows >= held) return;
+    const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kJoinRows, m = first + r, held = a.bounds[1];
+    if (first >= held) return;
     auto join = [](float2 x, float2 y) {
         const float top = fmaxf(x.x, y.x);
         const float sx = x.x == top ? x.y : x.y * exp2_of((x.x - top) * kLog2e), sy = y.x == top ? y.y : y.y * exp2_of((y.x - top) * kLog2e);
@@ -509,7 +509,9 @@ hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipSt
             }
         }
         if (rc != hipSuccess) return;
-        xent_join_kernel<<<(unsigned)((a.rows + kJoinRows - 1) / kJoinRows), kJoinRows * kJoinParts, 0, s>>>(a, (int)parts);
+        // (a launch holds 2^32 threads along its first dimension)
+        const int64_t groups = (a.rows + kJoinRows - 1) / kJoinRows, row = groups < (1 << 20) ? groups : 1 << 20;
+        xent_join_kernel<<<dim3((unsigned)row, (unsigned)((groups + row - 1) / row)), kJoinRows * kJoinParts, 0, s>>>(a, (int)parts);
         rc = hipGetLastError();
     });
     return rc;
@@ -574,10 +576,6 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
             XentArgs b = a;
             if (!plan.sums) b.sums = nullptr;
             const int64_t chunks = (a.inner + kSumColumns - 1) / kSumColumns, all = a.rows * chunks, row = all < (1 << 22) ? all : 1 << 22;
-            if ((all + row - 1) / row > 65535) {
-                rc = hipErrorNotSupported;
-                return;
-            }
             xent_row_gradients_kernel<T><<<dim3((unsigned)row, (unsigned)((all + row - 1) / row)), 256, 0, s>>>(
                 b, (int)plan.stretches, a.rows * plan.lds, plan.lds, (int)chunks);
             rc = hipGetLastError();

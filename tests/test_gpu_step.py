@@ -117,7 +117,8 @@ def check(d, top_k, act, normalise, dtype, pad=0):
 
 SIZES = [(1, 1, 1, 1, 1, 1), (1, 4, 2, 8, 16, 24), (1, 64, 8, 256, 64, 128), (3, 5, 3, 7, 9, 5), (2, 3, 2, 1, 40, 17), (4, 3, 2, 40, 3, 50), (16, 8, 2, 64, 96, 48),
          (17, 8, 2, 64, 96, 40), (64, 6, 6, 72, 130, 33), (64, 70, 4, 33, 65, 31), (64, 2, 1, 128, 64, 64), (33, 1, 1, 48, 32, 16), (5, 1024, 32, 16, 24, 20),
-         (2, 200, 8, 264, 520, 264), (9, 65, 5, 1025, 257, 129), (1, 8, 1, 2048, 2048, 512)]
+         (2, 200, 8, 264, 520, 264), (9, 65, 5, 1025, 257, 129), (1, 8, 1, 2048, 2048, 512),
+         (3, 40, 32, 24, 40, 24), (64, 33, 32, 24, 16, 24), (2, 300, 32, 24, 40, 24), (40, 1, 1, 512, 264, 48)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -199,6 +200,30 @@ def test_in_place_of_the_residual():
     got = nb.nacho_experts_step(d["x"].cuda(), d["logits"].cuda(), 2, d["up"].cuda(), d["down"].cuda(), act="silu", normalise=True,
                                 residual=d["residual"], out=d["residual"])
     assert got is d["residual"] and torch.equal(got, want)
+
+
+def test_no_token_takes_part():
+    d = problem(9, 4, 6, 64, 48, 72, torch.bfloat16, bias=True, residual=True)
+    d["keep"] = torch.zeros(4, dtype=torch.bool)
+    assert torch.equal(run(d, 2, "silu", True).cpu(), d["residual"])
+    d["residual"] = None
+    assert int(run(d, 2, "silu", False).count_nonzero()) == 0
+
+
+def test_more_than_2_31_weights():
+    """The last experts' weights lie more than 2^32 bytes behind the first ones'."""
+    experts, hidden, inner, outer = 300, 2048, 4096, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    up = torch.zeros((experts, hidden, inner), dtype=torch.bfloat16, device="cuda")
+    d = problem(1, 2, experts, inner, 8, outer, torch.bfloat16)
+    d["logits"][:, [3, 297, 299]] = 9.0
+    for e in (3, 297, 299):
+        up[e] = torch.randn((hidden, inner), generator=g, device="cuda") * inner ** -0.5
+    down = (torch.randn((experts, outer, hidden), generator=g, device="cuda") * hidden ** -0.5).to(torch.bfloat16)
+    got = nb.nacho_experts_step(d["x"].cuda(), d["logits"].cuda(), 3, up, down, act="silu", normalise=True)
+    small = {**d, "up": up[[3, 297, 299]].cpu(), "down": down[[3, 297, 299]].cpu(), "logits": d["logits"][:, [3, 297, 299]]}
+    want, room = reference(small, 3, True, "silu", torch.bfloat16)
+    assert bool(((got.cpu().double() - want).abs() <= room).all())
 
 
 def test_no_token():

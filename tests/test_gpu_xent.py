@@ -169,6 +169,29 @@ def test_no_row_counts(dtype):
     assert loss.shape == (0,) and gx.shape == (0, 64) and bool((gh == 0).all())
 
 
+@pytest.mark.parametrize("rows", [5, 70])
+def test_more_than_2_31_weights(rows):
+    """Weights of the vocabulary's last words lie more than 2^32 bytes behind the first ones'; those between are zero."""
+    vocabulary, inner = 140_000, 16_384
+    g = torch.Generator(device="cuda").manual_seed(1)
+    some = torch.tensor([0, 1, 77_777, 131_071, 131_072, 139_998, 139_999], device="cuda")
+    head = torch.zeros((vocabulary, inner), dtype=torch.bfloat16, device="cuda")
+    head[some] = (torch.randn((len(some), inner), generator=g, device="cuda") * 3 * inner ** -0.5).to(torch.bfloat16)
+    x = torch.randn((rows, inner), generator=g, device="cuda").to(torch.bfloat16)
+    label = some[torch.arange(rows, device="cuda") % len(some)]
+    loss, lse = nb.nacho_xent(x, head, label)
+    gx, gh = nb.nacho_xent_grad(x, head, label, lse)
+    z, dz = x.double() @ head[some].double().T.contiguous(), (inner + 8) * F32 * (x.double().abs() @ head[some].double().abs().T.contiguous())
+    all_z = torch.cat([z, torch.zeros((rows, 1), dtype=torch.float64, device="cuda").expand(-1, vocabulary - len(some))], dim=1)
+    want = torch.logsumexp(all_z, dim=1)
+    d_lse = dz.max(dim=1)[0] + 2.0 ** -21 + (64 + vocabulary / 2048) * F32 + 2 * F32 * want.abs()
+    assert bool(((lse.double() - want).abs() <= d_lse).all())
+    q = torch.exp(z - want[:, None]) - (label[:, None] == some).double()
+    d_q = dz + d_lse[:, None] + 2.0 ** -18 + 2.0 ** -8 * q.abs()
+    for got, value, room in ((gx, q @ head[some].double(), d_q @ head[some].double().abs()), (gh[some], q.T @ x.double(), d_q.T @ x.double().abs())):
+        assert bool(((got.double() - value).abs() <= room * 1.01 + 2.0 ** -8 * value.abs() + 1e-6).all())
+
+
 def test_weights_of_many_sizes():
     """f16 gradients under weights of one by a large number of rows, and under large ones: the probabilities do not vanish."""
     for size in (2.0 ** -14, 1.0, 2.0 ** 9):

@@ -178,8 +178,10 @@ def test_sizes_whose_products_pass_64_bits():
     most, far = (1 << 31) - 1, 1 << 40
     assert lib.nacho_keep8(A, far, most, 32, nb.BF16, C.byref(kept(A + (1 << 50), far, E, far)), None) == BAD
     assert lib.nacho_restore8(C.byref(kept(A, far, E, far)), most, 32, nb.BF16, A + 4096, far, None) == BAD
-    rc, n = size(lib.nacho_xent_grad_workspace_bytes, C.byref(xent(n_rows=most, vocabulary=(1 << 24) - 1, ldx=far, ldh=far)))
+    rc, n = size(lib.nacho_xent_grad_workspace_bytes, C.byref(xent(n_rows=most, vocabulary=2000, ldx=far, ldh=far)))
     assert rc == 0 and n > 256 * most * 4
+    assert size(lib.nacho_xent_grad_workspace_bytes, C.byref(xent(n_rows=most, vocabulary=(1 << 24) - 1, ldx=far, ldh=far)))[0] == UNSUPPORTED
+    assert size(lib.nacho_xent_workspace_bytes, C.byref(xent(vocabulary=(1 << 24) - 1, inner=(1 << 24) - 1, ldx=far, ldh=far)))[0] == UNSUPPORTED
     assert lib.nacho_xent_grad(C.byref(xent(n_rows=most, ldx=far)), E, B, 64, None, 0, E + (1 << 45), 1 << 62, None) == BAD
 
 
