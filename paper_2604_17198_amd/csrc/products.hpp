@@ -173,23 +173,61 @@ template <typename T, bool kTiny> struct Ragged {
 };
 
 // Rows of k elements that go from memory right into the registers that the matrix units read, in stretches of kBatch x 64 bytes: a lane
-// has 16 of every 64.  Loads have no branch
-// around them (behind one the compiler waits for all loads): past the row's end its last word is loaded, and made zeros when it is
-// used, if the stretch is not whole.
+// has 16 of every 64.  Loads have no branch around them (behind one the compiler waits for all loads): past the row's end its last word is
+// loaded, and made zeros when it is used, if the stretch is not whole.
+// Rows of 16 bits that start anywhere: 16 bytes from a multiple of 4, which take half the time of 16 bytes from between two, and the
+// word's last element; a word that starts between is put together from both.  (The first row of all starts at a multiple of 4.)
 template <typename T, Access kAccess, int kSteps> struct Stretch {
     static constexpr int kBatch = kAccess == TINY ? 1 : kSteps, n = Word<T>::n, kStep = 64 / (int)sizeof(T), kLong = kBatch * kStep;
+    static constexpr bool kHalves = kAccess == ANYWHERE && sizeof(T) == 2;
+    struct Joined {
+        v4u word;
+        unsigned last;
+    };
+    typedef std::conditional_t<kHalves, Joined, v4u> Loaded;
+    // f(whole): the two kinds of stretches apart.
+    template <typename F> static __device__ void by_end(int stretch, int k, F f)
+    {
+        if ((stretch + 1) * kLong <= k) f(std::true_type());
+        else f(std::false_type());
+    }
     static __device__ int from(int stretch, int i) { return stretch * kLong + i * kStep + lane_id() / 16 * n; }
-    static __device__ v4u load(const T *row, int at, int k)
+    static __device__ Loaded load(const T *row, int at, int k)
     {
         if constexpr (kAccess == WORDS) return *reinterpret_cast<const v4u *>(row + (at < k ? at : k - n));
-        else return Ragged<T, kAccess == TINY>(k, at).load(row + at);
+        else {
+            const Ragged<T, kAccess == TINY> r(k, at);
+            if constexpr (kHalves) {
+                typedef unsigned words __attribute__((ext_vector_type(4), aligned(4)));
+                const T *const first = row + at - r.back;
+                return {*reinterpret_cast<const words *>((uintptr_t)first & ~(uintptr_t)3), *reinterpret_cast<const unsigned short *>(first + n - 1)};
+            } else return r.load(row + at);
+        }
     }
-    static __device__ v4u settled(v4u w, int at, int k)
+    // What was loaded, with zeros behind the row's end (whole: it does not end in the stretch).
+    template <typename Whole> static __device__ v4u value(const Loaded &v, const T *row, int at, int k, Whole)
     {
-        if constexpr (kAccess == WORDS) return at < k ? w : v4u{0, 0, 0, 0};
-        else return Ragged<T, kAccess == TINY>(k, at).placed(w);
+        constexpr bool whole = Whole::value;
+        if constexpr (kAccess == WORDS) return whole || at < k ? v : v4u{0, 0, 0, 0};
+        else {
+            v4u w;
+            if constexpr (kHalves) {
+                const T *first = row;                                              // (words of a whole stretch all start as the row does)
+                if (!whole) first += at - Ragged<T, false>(k, at).back;
+                const unsigned by = (unsigned)((uintptr_t)first & 2) * 8;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_alignbit(e < 3 ? v.word[e + 1] : v.last, v.word[e], by);
+            } else w = v;
+            return whole ? w : Ragged<T, kAccess == TINY>(k, at).placed(w);
+        }
     }
 };
+// How matrices whose first rows are these are read so.
+template <typename... Rows> Access stretch_access(bool words, bool tiny, int elem, Rows... rows)
+{
+    const uintptr_t bits = ((uintptr_t)rows | ...);
+    return words ? WORDS : tiny || (elem == 2 && (bits & 2) != 0) ? TINY : ANYWHERE;
+}
 
 // Rows that run along k.  A thread loads words of 16 bytes, the same one of several rows.
 template <typename T, int kRows, int kStep, int kThreads, Access kAccess, int kSets> struct AlongK {

@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
         auto groups_of = [&](auto most) {
             constexpr int kGroups = decltype(most)::value;
             struct Loaded {
-                v4u p[kMatrices][kBatch], q[kBatch];
+                typename Part::Loaded p[kMatrices][kBatch], q[kBatch];
             } one, two;
             v4f acc[kGroups][kMatrices];
             int token[kGroups];
@@ -162,27 +162,29 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
                 for (int i = 0; i < kBatch; ++i) to.q[i] = Part::load(x, Part::from(s, i), a.inner);
             };
             auto multiply = [&](Loaded &of, int s) {
-                const bool whole = (s + 1) * Part::kLong <= a.inner;
-                if (!whole) {
+                v4u p[kMatrices][kBatch];
+                Part::by_end(s, a.inner, [&](auto whole) {
 #pragma unroll
                     for (int h = 0; h < kMatrices; ++h)
 #pragma unroll
-                        for (int i = 0; i < kBatch; ++i) of.p[h][i] = Part::settled(of.p[h][i], Part::from(s, i), a.inner);
-                }
+                        for (int i = 0; i < kBatch; ++i) p[h][i] = Part::value(of.p[h][i], rows[h], Part::from(s, i), a.inner, whole);
+                });
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
                     if (g > 0) {
                         if (g * 16 >= m) break;
                         fetch_x(of, s, g);
                     }
-                    if (!whole) {
+                    const T *x = static_cast<const T *>(a.x) + token[g] * a.ldx;
+                    v4u q[kBatch];
+                    Part::by_end(s, a.inner, [&](auto whole) {
 #pragma unroll
-                        for (int i = 0; i < kBatch; ++i) of.q[i] = Part::settled(of.q[i], Part::from(s, i), a.inner);
-                    }
+                        for (int i = 0; i < kBatch; ++i) q[i] = Part::value(of.q[i], x, Part::from(s, i), a.inner, whole);
+                    });
 #pragma unroll
                     for (int i = 0; i < kBatch; ++i)
 #pragma unroll
-                        for (int h = 0; h < kMatrices; ++h) acc[g][h] = matrix_step<T>(of.p[h][i], of.q[i], acc[g][h]);
+                        for (int h = 0; h < kMatrices; ++h) acc[g][h] = matrix_step<T>(p[h][i], q[i], acc[g][h]);
                 }
             };
             // (weights first: they have the longest way)
@@ -229,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
                 }
                 // a lane has four rows of one token
                 const int i = g * 16 + lane % 16, out = row0 + lane / 16 * 4;
-                if (i >= m || out >= a.hidden) continue;
+                if (i >= m || out >= a.ldh) continue;
                 typedef T four __attribute__((ext_vector_type(4)));
                 four v;
 #pragma unroll
@@ -241,9 +243,10 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
                         z[h] = acc[g][h][j];
                         if (d.bias && out + j < a.hidden) z[h] += wide(static_cast<const T *>(d.bias)[e * d.bias_stride + out + j]);
                     }
-                    v[j] = (T)(kGated ? activated<T>(z[kMatrices - 1], a.act) * z[0] : activated<T>(z[0], a.act));
+                    const float h = kGated ? activated<T>(z[kMatrices - 1], a.act) * z[0] : activated<T>(z[0], a.act);
+                    v[j] = (T)(out + j < a.hidden ? h : 0.0f);
                 }
-                // (rows are padded to words of 8 elements)
+                // (rows are whole words of 8 elements, with zeros behind the last)
                 *reinterpret_cast<four *>(static_cast<T *>(a.h) + list[i] * a.ldh + out) = v;
             }
             wave_sync();
@@ -259,6 +262,7 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
 template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_down_kernel(StepArgs a)
 {
     typedef Stretch<T, kAccess, kAccess == WORDS ? 4 : 2> Part;
+    typedef Stretch<T, WORDS, Part::kBatch> Whole;                                 // (the rows between the products)
     constexpr int kSlab = kMostTokens * kTall, kGroups = kMostTokens / 16, kBatch = Part::kBatch;
     __shared__ __attribute__((aligned(16))) float slab[kWaves][kSlab];             // [token][row] of every wavefront
     __shared__ float share[kMostSlots];
@@ -287,7 +291,9 @@ template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads
     };
     struct Loaded {
         Unit at;
-        v4u p[kBatch], q[kBatch];
+        const T *row;
+        typename Part::Loaded p[kBatch];
+        v4u q[kBatch];
     } one, two;
     v4f acc[kGroups];
     auto slot_of = [&](int expert, int g) {
@@ -298,12 +304,12 @@ template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads
     auto fetch = [&](Loaded &to, Unit at) {
         to.at = at;
         const int e = __builtin_amdgcn_readfirstlane(active[at.expert]);
-        const T *down = static_cast<const T *>(a.down.w) + e * a.down.stride + row * a.down.ld;
+        to.row = static_cast<const T *>(a.down.w) + e * a.down.stride + row * a.down.ld;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) to.p[i] = Part::load(down, Part::from(at.stretch, i), a.hidden);
+        for (int i = 0; i < kBatch; ++i) to.p[i] = Part::load(to.row, Part::from(at.stretch, i), a.hidden);
         const T *h = row_of(at.expert, 0);
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) to.q[i] = Part::load(h, Part::from(at.stretch, i), a.hidden);
+        for (int i = 0; i < kBatch; ++i) to.q[i] = Whole::load(h, Part::from(at.stretch, i), (int)a.ldh);
     };
     auto add_up = [&](int expert) {
         const int m = __builtin_amdgcn_readfirstlane(firsts[expert + 1] - firsts[expert]);
@@ -330,26 +336,26 @@ template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) acc[g] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        const bool whole = (at.stretch + 1) * Part::kLong <= a.hidden;
         const int m = __builtin_amdgcn_readfirstlane(firsts[number + 1] - firsts[number]);
-        if (!whole) {
+        v4u p[kBatch];
+        Part::by_end(at.stretch, a.hidden, [&](auto whole) {
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) of.p[i] = Part::settled(of.p[i], Part::from(at.stretch, i), a.hidden);
-        }
+            for (int i = 0; i < kBatch; ++i) p[i] = Part::value(of.p[i], of.row, Part::from(at.stretch, i), a.hidden, whole);
+        });
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
             if (g > 0) {
                 if (g * 16 >= m) break;
                 const T *h = row_of(number, g);
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) of.q[i] = Part::load(h, Part::from(at.stretch, i), a.hidden);
+                for (int i = 0; i < kBatch; ++i) of.q[i] = Whole::load(h, Part::from(at.stretch, i), (int)a.ldh);
             }
-            if (!whole) {
+            Part::by_end(at.stretch, a.hidden, [&](auto whole) {
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) of.q[i] = Part::settled(of.q[i], Part::from(at.stretch, i), a.hidden);
-            }
+                for (int i = 0; i < kBatch; ++i) of.q[i] = Whole::value(of.q[i], nullptr, Part::from(at.stretch, i), (int)a.ldh, whole);
+            });
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) acc[g] = matrix_step<T>(of.p[i], of.q[i], acc[g]);
+            for (int i = 0; i < kBatch; ++i) acc[g] = matrix_step<T>(p[i], of.q[i], acc[g]);
         }
     };
     if (begin < end) {
@@ -447,7 +453,8 @@ hipError_t launch_step(int dtype, const StepArgs &a, hipStream_t s)
     hipError_t rc = hipSuccess;
     by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        rc = words ? run_step<T, WORDS>(a, s) : tiny ? run_step<T, TINY>(a, s) : run_step<T, ANYWHERE>(a, s);
+        const Access access = stretch_access(words, tiny, elem, a.x, a.up.w, a.gate.w, a.down.w);
+        rc = access == WORDS ? run_step<T, WORDS>(a, s) : access == TINY ? run_step<T, TINY>(a, s) : run_step<T, ANYWHERE>(a, s);
     });
     return rc;
 }

@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kThreads) xent_few_kernel(XentArgs a, int firs
     const int tiles = (words + kWords - 1) / kWords, stretches = (a.inner + Part::kLong - 1) / Part::kLong, k = a.inner;
     const T *const head = static_cast<const T *>(a.head) + (int64_t)first * a.ldh;
     struct Loaded {
-        v4u p[kTiles][kBatch], q[kBatch];
+        typename Part::Loaded p[kTiles][kBatch], q[kBatch];
     } one, two;
     for (int tile = (int)blockIdx.x * kWaves + wave; tile < tiles; tile += (int)gridDim.x * kWaves) {
         const T *rows[kTiles];
@@ -62,23 +62,22 @@ __global__ void __launch_bounds__(kThreads) xent_few_kernel(XentArgs a, int firs
             fetch_x(to, s, 0);
         };
         auto multiply = [&](Loaded &of, int s) {
-            const bool whole = (s + 1) * Part::kLong <= k;
-            if (!whole) {
+            Part::by_end(s, k, [&](auto whole) {
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-                    for (int b = 0; b < kBatch; ++b) of.p[i][b] = Part::settled(of.p[i][b], Part::from(s, b), k);
-            }
+                    for (int b = 0; b < kBatch; ++b) of.p[i][b] = Part::value(of.p[i][b], rows[i], Part::from(s, b), k, whole);
+            });
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 if (g > 0) {
                     if (g * 16 >= held) break;
                     fetch_x(of, s, g);
                 }
-                if (!whole) {
+                Part::by_end(s, k, [&](auto whole) {
 #pragma unroll
-                    for (int b = 0; b < kBatch; ++b) of.q[b] = Part::settled(of.q[b], Part::from(s, b), k);
-                }
+                    for (int b = 0; b < kBatch; ++b) of.q[b] = Part::value(of.q[b], x[g], Part::from(s, b), k, whole);
+                });
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b)
 #pragma unroll
