@@ -10,7 +10,7 @@
 // grad_x then is a sum over pieces, and over stretches of the vocabulary where there are too few tiles for the chip, held in 32 bits.
 //
 // Rows that do not count (no label in the vocabulary, weight 0) are left out before the first product: it reads the others by a list.
-#include "products.hpp"
+#include "xent.hpp"
 
 namespace nacho {
 
@@ -65,8 +65,6 @@ template <typename Label> __global__ void __launch_bounds__(kRowThreads) xent_ro
         a.bounds[1] = before + (int)__popcll((long long)who);
     }
     if (!a.scale || blockIdx.x != 0) return;
-    // In f16 the products read g times a power of two that brings the largest weight next to 2^15: the small probabilities of most
-    // of a vocabulary, under weights of one by the number of rows, would vanish.
     float most = 0.0f;
     if (a.weight)
         for (int64_t j = tid; j < a.rows; j += kRowThreads) most = counts_at(j) ? fmaxf(most, fabsf(a.weight[j])) : most;
@@ -77,7 +75,7 @@ template <typename Label> __global__ void __launch_bounds__(kRowThreads) xent_ro
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) most = fmaxf(most, share[w]);
         if (!a.weight) most = 1.0f;
-        const int e = most > 0.0f && most < kInfinity ? 14 - ilogbf(most) : 0, by = a.half ? (e < 100 ? e : 100) : 0;
+        const int by = a.half ? scale_exponent(most) : 0;
         a.scale[0] = ldexpf(1.0f, by);
         a.scale[1] = ldexpf(1.0f, -by);
     }
@@ -474,7 +472,7 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bo
     const bool large = rows >= 256 && inner >= 256;
     const int64_t tall = rows <= 32 ? 32 : elem == 4 ? 64 : large ? 256 : 128, wide = rows <= 32 ? 128 : elem == 4 ? 64 : large ? 256 : 128;
     const int64_t tiles = ((rows + tall - 1) / tall) * ((inner + wide - 1) / wide), wanted = tiles > 0 ? 2 * kUnits / tiles : 1;
-    const int64_t longest = (p.words + 1023) / 1024;
+    const int64_t shortest = large ? 1024 : 256, longest = (p.words + shortest - 1) / shortest;
     p.stretches = wanted < longest ? wanted : longest;
     if (p.stretches < 1) p.stretches = 1;
     p.k_part = ((p.words + p.stretches - 1) / p.stretches + 127) / 128 * 128;
@@ -487,8 +485,8 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bo
 hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s)
 {
     if (a.rows == 0) return hipSuccess;
-    if (const hipError_t e = list_rows(a, s)) return e;
-    hipError_t rc = hipSuccess;
+    hipError_t rc = few_rows(a) ? hipSuccess : list_rows(a, s);
+    if (rc != hipSuccess) return rc;
     by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
         int64_t parts = 0;
@@ -519,7 +517,7 @@ hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipSt
 
 hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s)
 {
-    hipError_t rc = list_rows(a, s);
+    hipError_t rc = few_rows(a) ? hipSuccess : list_rows(a, s);
     if (rc != hipSuccess) return rc;
     const int elem = a.elem;
     by_type(dtype, [&](auto zero) {

@@ -2,7 +2,7 @@
 // that of reading them.  A wavefront takes 16 or 64 words of the vocabulary at a time from memory right into the registers that the
 // matrix units read, and the rows of x the same way from the caches; for the loss it keeps the largest logit of each row and the sum of
 // exponentials under it over all words that it has.
-#include "products.hpp"
+#include "xent.hpp"
 
 namespace nacho {
 
@@ -10,25 +10,73 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * NACHO_WAVE;
 
+// The rows that count, which are so few that every workgroup lists them for itself: what xent_rows_kernel does for many.  One workgroup
+// leaves what the kernels behind need.  Returns how many there are.
+struct RowList {
+    int row[kFewRows], label[kFewRows];
+};
+template <typename Label> __device__ inline int list_rows(const XentArgs &a, RowList &list, float &scale)
+{
+    const int lane = lane_id();
+    int64_t label = -1;
+    float weight = 0.0f;
+    if (lane < a.rows) {
+        label = (int64_t)static_cast<const Label *>(a.label)[lane];
+        weight = a.weight ? a.weight[lane] : 1.0f;
+    }
+    const bool held = lane < a.rows && label >= 0 && label < a.vocabulary && weight != 0.0f;
+    const unsigned long long who = __ballot(held);
+    const int slot = __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0)), count = __popcll((long long)who);
+    if (held) {
+        list.row[slot] = lane;
+        list.label[slot] = (int)label;
+    }
+    wave_sync();
+    int by = 0;
+    if (a.scale) by = a.half ? scale_exponent(wave_all(held ? fabsf(weight) : 0.0f, MaxOf())) : 0;
+    scale = ldexpf(1.0f, by);
+    if (blockIdx.x == 0 && threadIdx.x < NACHO_WAVE) {
+        if (lane == 0) {
+            a.bounds[0] = 0;
+            a.bounds[1] = count;
+            if (a.scale) {
+                a.scale[0] = scale;
+                a.scale[1] = ldexpf(1.0f, -by);
+            }
+        }
+        if (held) {
+            a.token[slot] = lane;
+            a.slot_label[slot] = (int)label;
+        } else if (lane < a.rows && a.loss) a.loss[lane] = a.lse[lane] = 0.0f;
+        if (a.slot_of && lane < a.rows) a.slot_of[lane] = held ? slot : -1;
+    }
+    return count;
+}
+
 template <typename T, int kGroups, int kTiles, int kSteps, bool kGradient>
 __global__ void __launch_bounds__(kThreads) xent_few_kernel(XentArgs a, int first, int words, int64_t ldg)
 {
     typedef Stretch<T, WORDS, kSteps> Part;
     constexpr int kBatch = Part::kBatch, kWords = 16 * kTiles;
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / NACHO_WAVE), held = a.bounds[1];
+    const int lane = lane_id(), lane_row = lane % 16, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / NACHO_WAVE);
+    __shared__ RowList lists[kWaves];
+    RowList &list = lists[wave];
+    float scale;
+    const int held = __builtin_amdgcn_readfirstlane(a.label_bytes == 8 ? list_rows<int64_t>(a, list, scale) : list_rows<int32_t>(a, list, scale));
     if (held == 0) return;
     int slot[kGroups], label[kGroups];
     const T *x[kGroups];
     float lse[kGroups], factor[kGroups], top[kGroups], sum[kGroups];
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-        slot[g] = g * 16 + lane % 16;
+        slot[g] = g * 16 + lane_row;
         const int there = slot[g] < held ? slot[g] : held - 1;
-        x[g] = static_cast<const T *>(a.x) + a.token[there] * a.ldx;
-        label[g] = a.slot_label[there] - first;
+        const int row = list.row[there];
+        x[g] = static_cast<const T *>(a.x) + row * a.ldx;
+        label[g] = list.label[there] - first;
         if constexpr (kGradient) {
-            lse[g] = a.slot_lse[there];
-            factor[g] = a.factor[there] * a.scale[0];
+            lse[g] = a.lse[row];
+            factor[g] = (a.weight ? a.weight[row] : 1.0f) * scale;
         }
         top[g] = -kInfinity;
         sum[g] = 0.0f;
