@@ -318,36 +318,41 @@ struct HeadGradients {
 };
 
 // A row's gradient from its sums, zeros for a row that does not count (without sums: these alone).  A workgroup has 256 columns of a
-// row, a wavefront every fourth stretch.
-constexpr int kSumColumns = 256;
+// row, a wavefront every fourth stretch of them, or, where there are few stretches, 1024 columns.
+constexpr int kSumColumns = 256, kSumWaves = 4;
+constexpr bool sums_apart(int64_t stretches) { return stretches > 2 * kSumWaves; }
 template <typename T> __global__ void __launch_bounds__(256) xent_row_gradients_kernel(XentArgs a, int stretches, int64_t part_stride, int64_t ld, int chunks)
 {
-    constexpr int kWaves = 4, kBatch = 8;
+    constexpr int kWaves = kSumWaves, kBatch = 8;
     __shared__ v4f share[kWaves][NACHO_WAVE];
+    const bool apart = sums_apart(stretches);
     const int64_t number = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, t = number / chunks;
     if (t >= a.rows) return;
     const int slot = a.slot_of[t], lane = lane_id(), wave = (int)threadIdx.x / NACHO_WAVE;
     if (slot >= 0 && !a.sums) return;
-    const int c = (int)(number - t * chunks) * kSumColumns + lane * 4;
+    const int c = (int)(number - t * chunks) * (apart ? kSumColumns : kSumColumns * kWaves) + (apart ? lane : (int)threadIdx.x) * 4;
+    const int first = apart ? wave : 0, step = apart ? kWaves : 1;
     v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
     if (slot >= 0) {
         const float *from = a.sums + slot * ld + (c < ld ? c : 0);
-        for (int p = wave; p < stretches; p += kBatch * kWaves) {
+        for (int p = first; p < stretches; p += kBatch * step) {
             v4f next[kBatch];
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
-                next[i] = *reinterpret_cast<const v4f *>(from + (int64_t)(p + i * kWaves < stretches ? p + i * kWaves : p) * part_stride);
+                next[i] = *reinterpret_cast<const v4f *>(from + (int64_t)(p + i * step < stretches ? p + i * step : p) * part_stride);
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
-                if (p + i * kWaves < stretches) v += next[i];
+                if (p + i * step < stretches) v += next[i];
         }
-        share[wave][lane] = v;
-        __syncthreads();
-        v = share[0][lane];
+        if (apart) {
+            share[wave][lane] = v;
+            __syncthreads();
+            v = share[0][lane];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) v += share[w][lane];
+            for (int w = 1; w < kWaves; ++w) v += share[w][lane];
+        }
     }
-    if (wave != 0 || c >= a.inner) return;
+    if ((apart && wave != 0) || c >= a.inner) return;
     const float by = a.scale[1];
     T *const out = static_cast<T *>(a.grad_x) + t * a.ldgx + c;
     if (c + 4 <= a.inner) {
@@ -471,7 +476,18 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bo
     // stretches of a piece, where its rows alone are too few tiles for the chip
     const bool large = rows >= 256 && inner >= 256;
     const int64_t tall = rows <= 32 ? 32 : elem == 4 ? 64 : large ? 256 : 128, wide = rows <= 32 ? 128 : elem == 4 ? 64 : large ? 256 : 128;
-    const int64_t tiles = ((rows + tall - 1) / tall) * ((inner + wide - 1) / wide), wanted = tiles > 0 ? 2 * kUnits / tiles : 1;
+    const int64_t tiles = ((rows + tall - 1) / tall) * ((inner + wide - 1) / wide);
+    int64_t wanted = tiles > 0 ? 2 * kUnits / tiles : 1;
+    if (elem == 2 && large && tiles > 0 && (tiles < kUnits || p.pieces > 1)) {
+        // (A compute unit has one such tile at a time.)  As few stretches as fill whole rounds of workgroups; or else about two rounds, or,
+        // where these leave a tenth of the chip without work, up to four.
+        auto empty = [&](int64_t n) { return 1000 - 1000 * n * tiles / ((n * tiles + kUnits - 1) / kUnits * kUnits); };      // of a thousand
+        const int64_t two = wanted > 1 ? wanted : 1;
+        wanted = two;
+        if (empty(two) > 100)
+            for (int64_t n = 1; n * tiles <= 4 * kUnits; ++n) wanted = empty(n) < empty(wanted) ? n : wanted;
+        for (int64_t n = two; n >= 1; --n) wanted = empty(n) <= 20 ? n : wanted;
+    }
     const int64_t shortest = large ? 1024 : 256, longest = (p.words + shortest - 1) / shortest;
     p.stretches = wanted < longest ? wanted : longest;
     if (p.stretches < 1) p.stretches = 1;
@@ -573,7 +589,7 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
         if (a.grad_x && a.rows > 0) {
             XentArgs b = a;
             if (!plan.sums) b.sums = nullptr;
-            const int64_t chunks = (a.inner + kSumColumns - 1) / kSumColumns, all = a.rows * chunks, row = all < (1 << 22) ? all : 1 << 22;
+            const int64_t each = kSumColumns * (sums_apart(plan.stretches) ? 1 : kSumWaves), chunks = (a.inner + each - 1) / each, all = a.rows * chunks, row = all < (1 << 22) ? all : 1 << 22;
             xent_row_gradients_kernel<T><<<dim3((unsigned)row, (unsigned)((all + row - 1) / row)), 256, 0, s>>>(
                 b, (int)plan.stretches, a.rows * plan.lds, plan.lds, (int)chunks);
             rc = hipGetLastError();
