@@ -469,7 +469,7 @@ int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int6
  * at a time, and takes 256 MiB at most (more of over 524288 rows of 16 bits).
  * Limits: vocabulary, inner < 2^24, and the products of every two of n_rows,
  * vocabulary and inner < 2^42.  Workspaces: nacho_xent_workspace_bytes,
- * nacho_xent_grad_workspace_bytes, of the layer with the arrays that it will have (512
+ * nacho_xent_grad_workspace_bytes, of the layer with the arrays that it will have (384
  * rows and more of 16 bits that do not start at multiples of 16 bytes are copied so that
  * they do: the rows, and 256 MiB of the vocabulary's at a time).
  */

@@ -198,13 +198,13 @@ struct XentPlan {
 };
 int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary);
 XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bool pads, bool gradient);
-constexpr int64_t kPaddedFrom = 512;   // rows
+constexpr int64_t kPaddedFrom = 384;   // rows
 bool xent_pads(const XentArgs &a);
 hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s);
 // The logits of up to kFewRows rows of words of 16 bytes (words `first` .. of the vocabulary): statistics by workgroup in a.partial, or,
 // where there is a.g, g.
-constexpr int kFewRows = 64;
-int64_t xent_few_groups(int64_t rows, int64_t vocabulary);
+constexpr int kFewRows = 16;
+int64_t xent_few_groups(int64_t vocabulary);
 hipError_t launch_xent_few(int dtype, const XentArgs &a, int64_t first, int64_t words, int64_t ldg, hipStream_t s);
 hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s);
 

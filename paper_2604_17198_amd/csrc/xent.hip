@@ -434,8 +434,9 @@ ProductArgs logits_of(const XentArgs &a, const Sides &v, int64_t words)
     return p;
 }
 
-// Few rows of words of 16 bytes.  (Rows that start anywhere go through LDS all the same: 16 rows against 100003 x 999 bf16, 66 us by
-// tiles, 86 without.)
+// Few rows of words of 16 bytes go without LDS.  (65536 x 2048 bf16, us a call without LDS and by tiles, a graph's start included: 1 row 58
+// and 79, 16 rows 62 and 79, 48 rows 85 and 85, 64 rows 92 and 84; x 1024: 16 rows 41 and 41, 24 rows 44 and 41.  Rows that start anywhere go
+// by tiles all the same: 16 rows against 100003 x 999, 66 us by tiles, 86 without LDS.)
 bool few_rows(const XentArgs &a) { return a.rows <= kFewRows && access_of_rows(a) == WORDS; }
 
 // (the rows' access is not known where workspaces are sized: the narrowest tiles there can be)
@@ -453,12 +454,14 @@ hipError_t list_rows(const XentArgs &a, hipStream_t s)
 
 int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary)
 {
-    const int64_t few = rows <= kFewRows ? xent_few_groups(rows, vocabulary) : 0, tiles = tiles_of_loss(elem, vocabulary);
+    const int64_t few = rows <= kFewRows ? xent_few_groups(vocabulary) : 0, tiles = tiles_of_loss(elem, vocabulary);
     return (few > tiles ? few : tiles) * rows;
 }
 
-// Whether the products read copies of the rows and of the vocabulary's weights.  Rows that start anywhere take twice the time in the
-// products; the copies are two passes over the weights a call.
+// Whether the products read copies of the rows and of the vocabulary's weights.  Rows that start anywhere take up to twice the time in the
+// products; the copies are two passes over the weights a call.  (Loss and gradients, us a pass with copies and without, bf16, 32003 x 1001
+// and 100003 x 499: 200 rows 217 and 197, 347 and 330; 300 rows 291 and 295, 464 and 427; 400 rows 284 and 315, 493 and 511; 1500 rows 557
+// and 773.  4000 rows, 50001 x 1999: 3575 and 5374.)
 bool xent_pads(const XentArgs &a) { return a.elem == 2 && a.rows >= kPaddedFrom && access_of_rows(a) == ANYWHERE; }
 
 // The pieces of the vocabulary: g of one takes at most 256 MiB (which the last cache holds), or 256 words of it; and so do its weights
@@ -507,7 +510,7 @@ hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipSt
         typedef decltype(zero) T;
         int64_t parts = 0;
         if (few_rows(a)) {
-            parts = xent_few_groups(a.rows, a.vocabulary);
+            parts = xent_few_groups(a.vocabulary);
             rc = launch_xent_few(dtype, a, 0, a.vocabulary, 0, s);
         } else {
             for (int64_t first = 0; first < a.vocabulary; first += plan.words) {
