@@ -9,6 +9,10 @@
 // caches; wavefronts share out k, and their sums meet in LDS.
 //
 // The choice of experts is made by every workgroup of the first launch for itself, which takes less than a launch of its own.
+//
+// Bound by the weights' bytes.  us a kernel: 64 tokens, 8 of 128 experts, gated, 2048 x 1024 x 2048 f16 (all 1.6 GB of weights) 175 and 82,
+// 6.3 TB/s; 16 tokens, 2 of 32 experts, 2048 x 4096 x 2048 bf16 69 and 55; one token, 8 of 64 experts, gated, 2048 x 1024 x 2048, 101 MB that the
+// last cache holds, 19 and 11.
 #include "activation.hpp"
 #include "choose.hpp"
 #include "products.hpp"
@@ -85,10 +89,10 @@ __device__ inline int slots_of(const StepArgs &a, const uint16_t *choice, int e,
 // The first product.  An item is 16 rows of an expert's weights, and belongs to a wavefront, or, where there are few items, to a
 // workgroup whose wavefronts have a part of k each (kShared).
 template <typename T, bool kGated, Access kAccess, bool kShared>
-__global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_kernel(StepArgs a)
+__global__ void __launch_bounds__(kThreads, 2) step_up_kernel(StepArgs a)
 {
     constexpr int kMatrices = 1 + kGated;
-    typedef Stretch<T, kAccess, kAccess == WORDS && !kGated && !kShared ? 4 : 2> Part;
+    typedef Stretch<T, kAccess, 2> Part;
     constexpr int kBatch = Part::kBatch;
     __shared__ __attribute__((aligned(16))) v4f sums[kShared ? kMatrices * kWaves * NACHO_WAVE : 1];
     __shared__ uint16_t choice[kMostSlots], active[kMostExperts], lists[kWaves][kMostTokens];
@@ -259,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_up_ke
 // The second product and the weighted sum.  A workgroup has 16 rows of every chosen expert's weights, or a part of their k (with
 // others, `parts` of them); its wavefronts share out what it has, a stretch of k of an expert at a time, and keep sums of their own
 // for every token in LDS.
-template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads, kAccess == WORDS ? 4 : 2) step_down_kernel(StepArgs a)
+template <typename T, Access kAccess> __global__ void __launch_bounds__(kThreads, 2) step_down_kernel(StepArgs a)
 {
     typedef Stretch<T, kAccess, kAccess == WORDS ? 4 : 2> Part;
     typedef Stretch<T, WORDS, Part::kBatch> Whole;                                 // (the rows between the products)
@@ -440,7 +444,8 @@ void step_plan(int dtype, int64_t tokens, int64_t experts, int64_t top_k, int64_
 {
     const int elem = dtype == NACHO_F32 ? 4 : 2;
     *tiles = (int32_t)((outer + kTall - 1) / kTall);
-    // workgroups for every compute unit, as long as each of their wavefronts has something to read
+    // workgroups for every compute unit, as long as each of their wavefronts has something to read (2048 x 4096 x 2048 bf16, us a call so and
+    // with one workgroup for 16 rows: 1 token, 2 experts 35 and 37; 64 tokens, 32 experts 189 and 244; with twice as many parts 1 token 35.5)
     const int64_t units = most_active(tokens, experts, top_k) * ((hidden * elem + 255) / 256), wanted = (kUnits + *tiles - 1) / *tiles;
     const int64_t each = units / (2 * kWaves), most = each < 16 ? each : 16;
     *parts = (int32_t)(wanted < most ? wanted : (most > 1 ? most : 1));

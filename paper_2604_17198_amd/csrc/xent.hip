@@ -10,6 +10,9 @@
 // grad_x then is a sum over pieces, and over stretches of the vocabulary where there are too few tiles for the chip, held in 32 bits.
 //
 // Rows that do not count (no label in the vocabulary, weight 0) are left out before the first product: it reads the others by a list.
+//
+// Bound by the matrix units: 4096 x 65536 x 2048 bf16, loss and gradients, 3.9 ms for 4 products of 1.1 TFLOP (1120 TFLOP/s; the loss 915 us
+// a kernel, 1200; the pieces' g 2 x 491, grad_x 2 x 479, grad_W 2 x 561, what joins them 60).  Few rows by the weights: xent_few.hip.
 #include "xent.hpp"
 
 namespace nacho {
@@ -318,41 +321,37 @@ struct HeadGradients {
 };
 
 // A row's gradient from its sums, zeros for a row that does not count (without sums: these alone).  A workgroup has 256 columns of a
-// row, a wavefront every fourth stretch of them, or, where there are few stretches, 1024 columns.
-constexpr int kSumColumns = 256, kSumWaves = 4;
-constexpr bool sums_apart(int64_t stretches) { return stretches > 2 * kSumWaves; }
+// row, a wavefront every fourth stretch of them.  (16 rows, 32 stretches of 512 columns: a thread with all stretches of 4 columns took 6 us
+// more a call; with 2 stretches both take the same.)
+constexpr int kSumColumns = 256;
 template <typename T> __global__ void __launch_bounds__(256) xent_row_gradients_kernel(XentArgs a, int stretches, int64_t part_stride, int64_t ld, int chunks)
 {
-    constexpr int kWaves = kSumWaves, kBatch = 8;
+    constexpr int kWaves = 256 / NACHO_WAVE, kBatch = 8;
     __shared__ v4f share[kWaves][NACHO_WAVE];
-    const bool apart = sums_apart(stretches);
     const int64_t number = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, t = number / chunks;
     if (t >= a.rows) return;
     const int slot = a.slot_of[t], lane = lane_id(), wave = (int)threadIdx.x / NACHO_WAVE;
     if (slot >= 0 && !a.sums) return;
-    const int c = (int)(number - t * chunks) * (apart ? kSumColumns : kSumColumns * kWaves) + (apart ? lane : (int)threadIdx.x) * 4;
-    const int first = apart ? wave : 0, step = apart ? kWaves : 1;
+    const int c = (int)(number - t * chunks) * kSumColumns + lane * 4;
     v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
     if (slot >= 0) {
         const float *from = a.sums + slot * ld + (c < ld ? c : 0);
-        for (int p = first; p < stretches; p += kBatch * step) {
+        for (int p = wave; p < stretches; p += kBatch * kWaves) {
             v4f next[kBatch];
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
-                next[i] = *reinterpret_cast<const v4f *>(from + (int64_t)(p + i * step < stretches ? p + i * step : p) * part_stride);
+                next[i] = *reinterpret_cast<const v4f *>(from + (int64_t)(p + i * kWaves < stretches ? p + i * kWaves : p) * part_stride);
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
-                if (p + i * step < stretches) v += next[i];
+                if (p + i * kWaves < stretches) v += next[i];
         }
-        if (apart) {
-            share[wave][lane] = v;
-            __syncthreads();
-            v = share[0][lane];
+        share[wave][lane] = v;
+        __syncthreads();
+        v = share[0][lane];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) v += share[w][lane];
-        }
+        for (int w = 1; w < kWaves; ++w) v += share[w][lane];
     }
-    if ((apart && wave != 0) || c >= a.inner) return;
+    if (wave != 0 || c >= a.inner) return;
     const float by = a.scale[1];
     T *const out = static_cast<T *>(a.grad_x) + t * a.ldgx + c;
     if (c + 4 <= a.inner) {
@@ -382,9 +381,11 @@ __global__ void __launch_bounds__(256) xent_pad_kernel(const void *from, int64_t
 
 int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
 
-// Rows for the choice of tiles: one group, whose last tile counts as a whole one from 33 rows on (tiles of 32 rows would read the
-// vocabulary's weights several times).
-int64_t counted(int64_t rows) { return rows > 32 ? (rows + 127) / 128 * 128 : rows; }
+// Rows for the choice of tiles: one group, whose last tile counts as a whole one of 128 from 33 rows of 16 bits on (tiles of 32 rows would
+// read the vocabulary's weights several times).  (Loss and gradients, us a pass with whole tiles and without, a graph's start included, bf16:
+// 40 x 65536 x 2048 292 and 322, 500 x 65536 x 1024 362 and 381, 2000 x 32000 x 1024 549 and 583.  f32, whose time is the matrix units':
+// 64 x 32000 x 1024 328 and 240, 300 x 30001 x 777 827 and 725.)
+int64_t counted(int elem, int64_t rows) { return elem == 2 && rows > 32 ? (rows + 127) / 128 * 128 : rows; }
 
 // The rows that count and a piece of the vocabulary as the products read them: where they lie, or from the workspace as rows of whole
 // words.
@@ -426,7 +427,7 @@ ProductArgs logits_of(const XentArgs &a, const Sides &v, int64_t words)
     p.experts = 1;
     p.n = (int32_t)words;
     p.k = v.inner;
-    p.slots = counted(a.rows);
+    p.slots = counted(a.elem, a.rows);
     p.q = v.x;
     p.ldq = v.ldx;
     p.p = v.head;
@@ -465,7 +466,8 @@ int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary)
 bool xent_pads(const XentArgs &a) { return a.elem == 2 && a.rows >= kPaddedFrom && access_of_rows(a) == ANYWHERE; }
 
 // The pieces of the vocabulary: g of one takes at most 256 MiB (which the last cache holds), or 256 words of it; and so do its weights
-// where they are copied.  The loss's call, which has no g, goes by these alone.
+// where they are copied.  The loss's call, which has no g, goes by these alone.  (Loss and gradients, bf16, us with 128, 256 and 512 MiB:
+// 4096 x 65536 x 2048 3740, 3850 and 3876; 16384 x 32000 x 1024 4743, 4258 and 4300.)
 XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bool pads, bool gradient)
 {
     constexpr int64_t kRoom = 256 << 20;
@@ -476,14 +478,16 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bo
     p.words = p.pieces > 1 ? ((vocabulary + p.pieces - 1) / p.pieces + 255) / 256 * 256 : vocabulary;
     p.pieces = (vocabulary + p.words - 1) / p.words;
     p.ldg = padded(p.words);
-    // stretches of a piece, where its rows alone are too few tiles for the chip
+    // stretches of a piece, where its rows alone are too few tiles for the chip (loss and gradients, us a pass with stretches and without,
+    // bf16: 64 x 32000 x 1024 112 and 281, 500 x 65536 x 1024 362 and 653; 4096 x 65536 x 2048, with twice the pieces' 128 tiles, 3850 and 4087)
     const bool large = rows >= 256 && inner >= 256;
     const int64_t tall = rows <= 32 ? 32 : elem == 4 ? 64 : large ? 256 : 128, wide = rows <= 32 ? 128 : elem == 4 ? 64 : large ? 256 : 128;
     const int64_t tiles = ((rows + tall - 1) / tall) * ((inner + wide - 1) / wide);
     int64_t wanted = tiles > 0 ? 2 * kUnits / tiles : 1;
     if (elem == 2 && large && tiles > 0 && (tiles < kUnits || p.pieces > 1)) {
         // (A compute unit has one such tile at a time.)  As few stretches as fill whole rounds of workgroups; or else about two rounds, or,
-        // where these leave a tenth of the chip without work, up to four.
+        // where these leave a tenth of the chip without work, up to four.  (us so and with two rounds whatever they fill: 500 x 65536 x 1024
+        // 362 and 405, 2000 x 32000 x 1024 549 and 589, 16384 x 32000 x 1024 4258 and 4363.)
         auto empty = [&](int64_t n) { return 1000 - 1000 * n * tiles / ((n * tiles + kUnits - 1) / kUnits * kUnits); };      // of a thousand
         const int64_t two = wanted > 1 ? wanted : 1;
         wanted = two;
@@ -558,7 +562,7 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
                 p.experts = 1;
                 p.n = v.inner;
                 p.k = (int32_t)words;
-                p.slots = counted(a.rows);
+                p.slots = counted(a.elem, a.rows);
                 p.q = a.g;
                 p.ldq = plan.ldg;
                 p.p = v.head;
@@ -576,7 +580,7 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
                 p.token = v.token;
                 p.experts = 1;
                 p.n = v.inner;
-                p.slots = counted(a.rows);
+                p.slots = counted(a.elem, a.rows);
                 p.q = a.g;
                 p.ldq = plan.ldg;
                 p.p = v.x;
@@ -592,7 +596,7 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
         if (a.grad_x && a.rows > 0) {
             XentArgs b = a;
             if (!plan.sums) b.sums = nullptr;
-            const int64_t each = kSumColumns * (sums_apart(plan.stretches) ? 1 : kSumWaves), chunks = (a.inner + each - 1) / each, all = a.rows * chunks, row = all < (1 << 22) ? all : 1 << 22;
+            const int64_t chunks = (a.inner + kSumColumns - 1) / kSumColumns, all = a.rows * chunks, row = all < (1 << 22) ? all : 1 << 22;
             xent_row_gradients_kernel<T><<<dim3((unsigned)row, (unsigned)((all + row - 1) / row)), 256, 0, s>>>(
                 b, (int)plan.stretches, a.rows * plan.lds, plan.lds, (int)chunks);
             rc = hipGetLastError();
