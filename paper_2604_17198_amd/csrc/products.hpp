@@ -452,6 +452,9 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
         else return stage1;
     };
     int tile, n0;
+    // (of one group only the rows that are there are dealt out: tiles without any, among the others, cost 400 us instead of 275 where 1213 of
+    // 2021 rows are, 100003 x 1024 f16)
+    if (kForm != WEIGHTS && a.experts == 1) tiles_m = tiles_of<kM>(bound_of(a, 1) - bound_of(a, 0));
     place_tile<kN>(tiles_m, tiles_n, tile, n0);
     int expert, m0, m_end, k_begin = 0, k = a.k;
     if (kForm == WEIGHTS) {
