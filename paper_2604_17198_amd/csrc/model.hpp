@@ -193,7 +193,7 @@ struct XentArgs {
 };
 // How a call goes through the vocabulary: `pieces` of `words`, each in `stretches` of `k_part` for the rows' sums.
 struct XentPlan {
-    int64_t pieces, words, ldg, stretches, k_part, lds;
+    int64_t pieces, words, ldg, stretches, shortest, k_part, lds;      // (no stretch shorter than `shortest`)
     bool sums;                     // (of the rows' gradients, in 32 bits: `lds` apart, one set a stretch)
 };
 int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary);

@@ -82,10 +82,9 @@ template <int kM, typename Args> __device__ inline bool find_tile(const Args &a,
 // the chip's eight parts one by one, each of which has a cache; 32 of a part's that run at a time get 4 x 8 neighbouring
 // tiles, which need 12 stretches of Q and P between them.  (16384 slots of 16 experts, 2048 x 8192, bf16, us: weights 662, in
 // the order of rows 687; of 32 experts, 1024 x 4096, forward 205 and 217.)
-template <int kN> __device__ inline void place_tile(int tiles_m, int tiles_n, int &tile, int &n0)
+template <int kN> __device__ inline void place_tile(int number, int tiles_m, int tiles_n, int &tile, int &n0)
 {
     constexpr int kRound = 256, kParts = 8, kTall = 4;
-    int number = (int)(blockIdx.y * gridDim.x + blockIdx.x);
     if ((number | (kRound - 1)) < tiles_m * tiles_n)
         number = (number & ~(kRound - 1)) | (number % kParts) * (kRound / kParts) | (number % kRound) / kParts;
     const int band = number / (kTall * tiles_n), in_band = number - band * kTall * tiles_n;
@@ -383,9 +382,9 @@ template <typename F, int... i> __device__ inline void unrolled(F f, std::intege
 template <int n, typename F> __device__ inline void unrolled(F f) { unrolled(f, std::make_integer_sequence<int, n>()); }
 
 // What a Finish knows of a tile: its group, its first row and the one behind the group's last, its first column; the first of the
-// wavefront's rows and columns in it.
+// wavefront's rows and columns in it; the stretch of k that it sums.
 struct Place {
-    int expert, m0, m_end, n0, wm, wn;
+    int expert, m0, m_end, n0, wm, wn, stretch;
 };
 
 // One tile of kM x kN results; kWavesM x kWavesN wavefronts share it.
@@ -455,7 +454,16 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
     // (of one group only the rows that are there are dealt out: tiles without any, among the others, cost 400 us instead of 275 where 1213 of
     // 2021 rows are, 100003 x 1024 f16)
     if (kForm != WEIGHTS && a.experts == 1) tiles_m = tiles_of<kM>(bound_of(a, 1) - bound_of(a, 0));
-    place_tile<kN>(tiles_m, tiles_n, tile, n0);
+    int number = (int)(blockIdx.y * gridDim.x + blockIdx.x), stretch = 0;
+    if constexpr (Finish::kParts) {
+        // (the launch's third dimension has stretches of k; fewer rows leave room for more of them)
+        const int tiles = tiles_m * tiles_n;
+        if (tiles == 0) return;
+        number += (int)(blockIdx.z * gridDim.y * gridDim.x);
+        stretch = number / tiles;
+        number -= stretch * tiles;
+    }
+    place_tile<kN>(number, tiles_m, tiles_n, tile, n0);
     int expert, m0, m_end, k_begin = 0, k = a.k;
     if (kForm == WEIGHTS) {
         const int tiles = (a.m + kM - 1) / kM;
@@ -470,12 +478,13 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
     const T *q = static_cast<const T *>(a.q);
     const T *p = static_cast<const T *>(a.p) + (int64_t)expert * a.p_stride;
     if constexpr (Finish::kParts) {
-        // (rows: the launch's third dimension has stretches of k)
         static_assert(kForm == ROWS, "k along the rows of Q");
-        const int first = (int)blockIdx.z * finish.k_part;
+        const int part = finish.k_part(m_end);
+        const int64_t first = (int64_t)stretch * part;
+        if (first >= k) return;
         q += first;
-        p += (int64_t)first * a.ldp;
-        k = k - first < finish.k_part ? k - first : finish.k_part;
+        p += first * a.ldp;
+        k = k - (int)first < part ? k - (int)first : part;
     }
     SideQ side_q;
     SideP side_p;
@@ -680,7 +689,7 @@ __device__ inline void Tile<T, kForm, kM, kN, kWavesM, kWavesN, kStep, kAccess>:
         }
         if (t < steps) body(t, zero);
     }
-    finish.template end<Tile>(a, Place{expert, m0, m_end, n0, wm, wn}, acc, stage0, stage1);
+    finish.template end<Tile>(a, Place{expert, m0, m_end, n0, wm, wn, stretch}, acc, stage0, stage1);
 }
 
 // A lane has four consecutive columns of result row lane % 16 of every 16 x 16.  A wavefront takes its tile through its

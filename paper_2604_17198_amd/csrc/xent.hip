@@ -261,11 +261,11 @@ template <typename T> __device__ inline void put_anywhere(T *to, const float (&v
 // Gradients of the rows: sums in 32 bits by stretches of the vocabulary, or, where there is one, the result itself.
 struct RowGradients {
     static constexpr bool kParts = true;
-    unsigned parts() const { return stretches; }
-    unsigned stretches;
-    int k_part;
-    float *sums;                   // [stretches][rows][ld], or NULL
-    int64_t part_stride, ld;
+    unsigned parts() const { return stretches.most; }
+    __device__ int k_part(int live) const { return sums ? stretches.of(live) : stretches.words; }
+    Stretches stretches;
+    float *sums;                   // [stretches][rows that count][ld], or NULL
+    int64_t ld;
     bool first;                    // (the sums hold nothing yet)
     const int32_t *token;
     const float *scale;
@@ -275,7 +275,7 @@ struct RowGradients {
     {
         typedef typename Tile::type T;
         if (sums) {
-            float *const to = sums + (int64_t)blockIdx.z * part_stride;
+            float *const to = sums + (int64_t)at.stretch * at.m_end * ld;
             Tile::each_row(a, at, acc, stage0, stage1, [&](unsigned m, int n, int, float (&v)[8]) {
                 v4f *const p = reinterpret_cast<v4f *>(to + (int64_t)m * ld + n);
                 v4f lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
@@ -324,7 +324,7 @@ struct HeadGradients {
 // row, a wavefront every fourth stretch of them.  (16 rows, 32 stretches of 512 columns: a thread with all stretches of 4 columns took 6 us
 // more a call; with 2 stretches both take the same.)
 constexpr int kSumColumns = 256;
-template <typename T> __global__ void __launch_bounds__(256) xent_row_gradients_kernel(XentArgs a, int stretches, int64_t part_stride, int64_t ld, int chunks)
+template <typename T> __global__ void __launch_bounds__(256) xent_row_gradients_kernel(XentArgs a, Stretches parts, int64_t ld, int chunks)
 {
     constexpr int kWaves = 256 / NACHO_WAVE, kBatch = 8;
     __shared__ v4f share[kWaves][NACHO_WAVE];
@@ -335,6 +335,8 @@ template <typename T> __global__ void __launch_bounds__(256) xent_row_gradients_
     const int c = (int)(number - t * chunks) * kSumColumns + lane * 4;
     v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
     if (slot >= 0) {
+        const int live = a.bounds[1], k_part = parts.of(live), stretches = (parts.words + k_part - 1) / k_part;
+        const int64_t part_stride = live * ld;
         const float *from = a.sums + slot * ld + (c < ld ? c : 0);
         for (int p = wave; p < stretches; p += kBatch * kWaves) {
             v4f next[kBatch];
@@ -476,6 +478,21 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bo
     const int64_t most = by_g < by_copy ? by_g : by_copy, least = most > 256 ? most : 256;
     p.pieces = (vocabulary + least - 1) / least;
     p.words = p.pieces > 1 ? ((vocabulary + p.pieces - 1) / p.pieces + 255) / 256 * 256 : vocabulary;
+    if (p.pieces > 1 && elem == 2 && inner >= 256) {
+        // As many words as fill whole rounds of grad_W's workgroups, if there is room and its rounds and those of g, which go through the
+        // rows and the rows' elements, are shorter together.  (Loss and gradients, bf16, us so and with equal pieces: 3000 x 100000 x 2048
+        // 4735 and 4965, 8192 x 50000 x 1024 3403 and 3665; where they are as long, 4096 x 128000 x 1024, 4260 and 4189.)
+        const int64_t wide = (inner + 255) / 256, tall = (rows + 255) / 256;
+        auto rounds = [&](int64_t words) {
+            const int64_t tiles = (words + 255) / 256;
+            return (tiles * wide + kUnits - 1) / kUnits * rows + (tiles * tall + kUnits - 1) / kUnits * inner;
+        };
+        auto all = [&](int64_t words) { return vocabulary / words * rounds(words) + rounds(vocabulary % words); };
+        int64_t unit = 256;
+        while (unit < 256 * kUnits && unit / 256 * wide % kUnits) unit *= 2;
+        const int64_t words = (p.words + unit - 1) / unit * unit;
+        if (words <= most && all(words) < all(p.words)) p.words = words;
+    }
     p.pieces = (vocabulary + p.words - 1) / p.words;
     p.ldg = padded(p.words);
     // stretches of a piece, where its rows alone are too few tiles for the chip (loss and gradients, us a pass with stretches and without,
@@ -495,7 +512,8 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bo
             for (int64_t n = 1; n * tiles <= 4 * kUnits; ++n) wanted = empty(n) < empty(wanted) ? n : wanted;
         for (int64_t n = two; n >= 1; --n) wanted = empty(n) <= 20 ? n : wanted;
     }
-    const int64_t shortest = large ? 1024 : 256, longest = (p.words + shortest - 1) / shortest;
+    p.shortest = large ? 1024 : 256;
+    const int64_t longest = (p.words + p.shortest - 1) / p.shortest;
     p.stretches = wanted < longest ? wanted : longest;
     if (p.stretches < 1) p.stretches = 1;
     p.k_part = ((p.words + p.stretches - 1) / p.stretches + 127) / 128 * 128;
@@ -545,6 +563,7 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
     const int elem = a.elem;
     by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
+        Stretches stretches = {};
         for (int64_t first = 0; first < a.vocabulary; first += plan.words) {
             const int64_t words = a.vocabulary - first < plan.words ? a.vocabulary - first : plan.words;
             Sides v;
@@ -569,9 +588,12 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
                 p.ldp = v.ldh;
                 p.out = a.grad_x;
                 p.ldo = a.ldgx;
-                const unsigned stretches = (unsigned)((words + plan.k_part - 1) / plan.k_part);
-                const RowGradients f{stretches, (int)plan.k_part, plan.sums ? a.sums : nullptr, a.rows * plan.lds, plan.lds, first == 0, a.token, a.scale, a.inner};
-                rc = by_size<T, ROWS>(p, f, v.access == WORDS && plan.ldg < 0x7fffffff ? WORDS : access_of<ROWS>(p, elem), s);
+                const Access access = v.access == WORDS && plan.ldg < 0x7fffffff ? WORDS : access_of<ROWS>(p, elem);
+                if (first == 0)
+                    stretches = Stretches{(int32_t)plan.stretches, (int32_t)plan.k_part, tall_of(shape_of<T, ROWS>(p, access, plan.stretches)),
+                                          (int32_t)plan.words, (int32_t)plan.shortest, a.rows};
+                const RowGradients f{stretches, plan.sums ? a.sums : nullptr, plan.lds, first == 0, a.token, a.scale, a.inner};
+                rc = by_size<T, ROWS>(p, f, access, s);
                 if (rc != hipSuccess) return;
             }
             if (a.grad_head) {
@@ -598,7 +620,7 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
             if (!plan.sums) b.sums = nullptr;
             const int64_t chunks = (a.inner + kSumColumns - 1) / kSumColumns, all = a.rows * chunks, row = all < (1 << 22) ? all : 1 << 22;
             xent_row_gradients_kernel<T><<<dim3((unsigned)row, (unsigned)((all + row - 1) / row)), 256, 0, s>>>(
-                b, (int)plan.stretches, a.rows * plan.lds, plan.lds, (int)chunks);
+                b, stretches, plan.lds, (int)chunks);
             rc = hipGetLastError();
         }
     });

@@ -155,6 +155,17 @@ def test_rows_that_do_not_count(dtype, label):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sizes,live", [((300, 5000, 300), (1, 40, 255, 256, 299)), ((1100, 3000, 520), (1, 130, 256, 257, 600)), ((70, 9000, 33), (1, 17, 33)),
+                                        ((4200, 40_003, 264), (3, 2500))])
+def test_few_of_many_rows_count(sizes, live, dtype):
+    for n in live:
+        d = problem(n, *sizes, dtype)
+        order = torch.randperm(sizes[0], generator=torch.Generator().manual_seed(n)).cuda()
+        d["label"][order[n:]] = -1
+        check(d, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_no_row_counts(dtype):
     d = problem(5, 40, 300, 64, dtype)
     d["label"].fill_(-100)
