@@ -800,10 +800,15 @@ constexpr int64_t kUnits = 256;        // compute units
 // Floats need four times as many matrix instructions for what is loaded: tiles of 64 x 64, which are as many again.  3000 slots
 // of 7 experts, 777 x 499, us: weights 73 (64 x 128: 95), forward 42 (32 x 128: 45), rows 44 (50); with two steps on their way
 // in registers 54, 43 and 42.  512 x 2048, 32 experts of 64 and 128 slots, us with 32, 64 and 128: rows 51, 52 and 141, 87, 81 and 149.
-enum Shape { TILES_256, TILES_128, TILES_64, TILES_32 };
+// Where a forward product of floats would be half a tile of 64 x 64 a compute unit, or fewer, tiles are of 32 x 32: a stage then takes a
+// wavefront half the time, and four times as many compute units have one.  (us a call with 32 x 32 and without: loss of 21 rows, 1567 x 2275
+// 56 and 76, of 100 rows, 2000 x 4095 87 and 119, of 300 rows, 1300 x 4000 (105 tiles of 64) 95 and 103, of 600 rows, 3000 x 1024 (470) 73
+// and 56; experts in training, 64 tokens, 2 of 4, 2000 x 1000 92 and 113.  With stages of 128 bytes 58, 91, 97 and 62.)
+constexpr int64_t kMostTiny = kUnits / 2;
+enum Shape { TILES_256, TILES_128, TILES_64, TILES_32, TILES_32_32 };
 // Rows and columns of these tiles (of rows shorter than a word: 128 x 128 for the weights, 32 x 128).
 constexpr int tall_of(Shape s) { return s == TILES_256 ? 256 : s == TILES_128 ? 128 : s == TILES_64 ? 64 : 32; }
-constexpr int wide_of(Shape s) { return s == TILES_256 ? 256 : s == TILES_64 ? 64 : 128; }
+constexpr int wide_of(Shape s) { return s == TILES_256 ? 256 : s == TILES_64 ? 64 : s == TILES_32_32 ? 32 : 128; }
 // `parts`: stretches of k that workgroups share a tile's sum by.
 template <typename T, Form kForm> Shape shape_of(const ProductArgs &a, Access access, int64_t parts = 1)
 {
@@ -818,6 +823,7 @@ template <typename T, Form kForm> Shape shape_of(const ProductArgs &a, Access ac
         if (sizeof(T) == 2 && words && each >= 256 && a.n >= 256 && a.slots / 256 * ((a.n + 255) / 256) * parts >= kUnits) return TILES_256;
         const int64_t few = words && sizeof(T) == 2 ? 32 : 64, most = sizeof(T) == 2 ? kUnits / 2 : 2 * kUnits - 1;
         const bool small = each <= few || a.slots / 128 * n128 * parts <= most;
+        if (kForm == FORWARD && sizeof(T) == 4 && (a.slots + 63) / 64 * ((a.n + 63) / 64) <= kMostTiny) return TILES_32_32;
         return !small ? TILES_128 : sizeof(T) == 4 && each > 64 ? TILES_64 : TILES_32;
     }
 }
@@ -831,6 +837,9 @@ template <typename T, Form kForm, typename Finish> hipError_t by_size(const Prod
         if (shape == TILES_256) return run<T, kForm, 256, 256, 2, 4, WORDS>(a, f, s);
     } else if (shape == TILES_64) return words ? run<T, kForm, 64, 64, 2, 2, WORDS>(a, f, s) : run<T, kForm, 64, 64, 2, 2, ANYWHERE>(a, f, s);
     if constexpr (kForm != WEIGHTS) {
+        if constexpr (sizeof(T) == 4 && kForm == FORWARD)
+            if (shape == TILES_32_32)
+                return words ? run<T, kForm, 32, 32, 2, 1, WORDS, 256>(a, f, s) : run<T, kForm, 32, 32, 2, 1, ANYWHERE, 256>(a, f, s);
         if (shape == TILES_32)
             return words ? run<T, kForm, 32, 128, 1, 4, WORDS, 256>(a, f, s) : run<T, kForm, 32, 128, 1, 4, ANYWHERE>(a, f, s);
     }

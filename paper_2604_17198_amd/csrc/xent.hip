@@ -442,8 +442,8 @@ ProductArgs logits_of(const XentArgs &a, const Sides &v, int64_t words)
 // by tiles all the same: 16 rows against 100003 x 999, 66 us by tiles, 86 without LDS.)
 bool few_rows(const XentArgs &a) { return a.rows <= kFewRows && access_of_rows(a) == WORDS; }
 
-// (the rows' access is not known where workspaces are sized: the narrowest tiles there can be)
-int64_t tiles_of_loss(int elem, int64_t vocabulary) { return (vocabulary + (elem == 4 ? 63 : 127)) / (elem == 4 ? 64 : 128); }
+// (the narrowest tiles there can be; of 32 floats there are at most kMostTiny more than of 64)
+int64_t tiles_of_loss(int elem, int64_t vocabulary) { return elem == 4 ? (vocabulary + 63) / 64 + kMostTiny : (vocabulary + 127) / 128; }
 
 hipError_t list_rows(const XentArgs &a, hipStream_t s)
 {

@@ -101,6 +101,12 @@ def test_against_the_definition(sizes, dtype):
     check(problem(seed, *sizes, dtype, weighted=seed % 3 != 0, masked=0.3 if seed % 2 else 0.0), dtype)
 
 
+@pytest.mark.parametrize("sizes", [(17, 1567, 2275), (64, 8192, 12), (64, 8193, 12), (63, 8129, 70), (100, 70, 4096), (33, 31, 5), (500, 1000, 65), (600, 1100, 130)])
+def test_few_tiles_of_floats(sizes):
+    for masked in (0.0, 0.4):
+        check(problem(3, *sizes, torch.float32, masked=masked), torch.float32)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("sizes", [(2048, 8192, 64), (2100, 8200, 72), (4096, 2056, 320), (520, 16_384, 520)])
 def test_large_tiles(sizes, dtype):
