@@ -205,7 +205,9 @@ hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipSt
 // where there is a.g, g.
 constexpr int kFewRows = 16;
 int64_t xent_few_groups(int64_t vocabulary);
-hipError_t launch_xent_few(int dtype, const XentArgs &a, int64_t first, int64_t words, int64_t ldg, hipStream_t s);
+hipError_t launch_xent_few(int dtype, const XentArgs &a, int64_t first, int64_t words, int64_t ldg, bool in_words, hipStream_t s);
+// grad_head of a piece from g and the rows of x.
+hipError_t launch_xent_few_head(int dtype, const XentArgs &a, int64_t first, int64_t words, int64_t ldg, hipStream_t s);
 hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s);
 
 }  // namespace nacho

@@ -438,9 +438,15 @@ ProductArgs logits_of(const XentArgs &a, const Sides &v, int64_t words)
 }
 
 // Few rows of words of 16 bytes go without LDS.  (65536 x 2048 bf16, us a call without LDS and by tiles, a graph's start included: 1 row 58
-// and 79, 16 rows 62 and 79, 48 rows 85 and 85, 64 rows 92 and 84; x 1024: 16 rows 41 and 41, 24 rows 44 and 41.  Rows that start anywhere go
-// by tiles all the same: 16 rows against 100003 x 999, 66 us by tiles, 86 without LDS.)
-bool few_rows(const XentArgs &a) { return a.rows <= kFewRows && access_of_rows(a) == WORDS; }
+// and 79, 16 rows 62 and 79, 48 rows 85 and 85, 64 rows 92 and 84; x 1024: 16 rows 41 and 41, 24 rows 44 and 41.  Rows of 16
+// bits that start anywhere go by tiles all the same: 16 rows against 100003 x 999, 66 us by tiles, 86 without LDS.  Such rows of floats, which
+// memory has no narrower access for, go without as long as the rows of x fit the nearest cache: 16 rows x 20000 x 501 24 us without LDS and 34
+// by tiles, 4 rows x 50622 x 3867 192 and 202, 16 rows x 50622 x 1999 126 and 119.)
+bool few_rows(const XentArgs &a)
+{
+    const Access access = access_of_rows(a);
+    return a.rows <= kFewRows && (access == WORDS || (access == ANYWHERE && a.elem == 4 && a.rows * a.inner <= 1 << 14));
+}
 
 // (the narrowest tiles there can be; of 32 floats there are at most kMostTiny more than of 64)
 int64_t tiles_of_loss(int elem, int64_t vocabulary) { return elem == 4 ? (vocabulary + 63) / 64 + kMostTiny : (vocabulary + 127) / 128; }
@@ -533,7 +539,7 @@ hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipSt
         int64_t parts = 0;
         if (few_rows(a)) {
             parts = xent_few_groups(a.vocabulary);
-            rc = launch_xent_few(dtype, a, 0, a.vocabulary, 0, s);
+            rc = launch_xent_few(dtype, a, 0, a.vocabulary, 0, access_of_rows(a) == WORDS, s);
         } else {
             for (int64_t first = 0; first < a.vocabulary; first += plan.words) {
                 const int64_t words = a.vocabulary - first < plan.words ? a.vocabulary - first : plan.words;
@@ -572,7 +578,7 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
             ProductArgs p = logits_of(a, v, words);
             p.out = a.g;
             p.ldo = plan.ldg;
-            rc = few_rows(a) ? launch_xent_few(dtype, a, first, words, plan.ldg, s)
+            rc = few_rows(a) ? launch_xent_few(dtype, a, first, words, plan.ldg, access_of_rows(a) == WORDS, s)
                              : by_size<T, FORWARD>(p, Gradient{a.slot_label, a.slot_lse, a.factor, a.scale, (int32_t)first}, v.access, s);
             if (rc != hipSuccess) return;
             if (a.grad_x) {
@@ -596,7 +602,10 @@ hipError_t launch_xent_grad(int dtype, const XentArgs &a, const XentPlan &plan, 
                 rc = by_size<T, ROWS>(p, f, access, s);
                 if (rc != hipSuccess) return;
             }
-            if (a.grad_head) {
+            if (a.grad_head && a.rows <= kFewRows) {
+                rc = launch_xent_few_head(dtype, a, first, words, plan.ldg, s);
+                if (rc != hipSuccess) return;
+            } else if (a.grad_head) {
                 p = ProductArgs{};
                 p.bounds = a.bounds;
                 p.token = v.token;

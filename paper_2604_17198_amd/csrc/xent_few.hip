@@ -53,10 +53,10 @@ template <typename Label> __device__ inline int list_rows(const XentArgs &a, Row
     return count;
 }
 
-template <typename T, int kTiles, int kSteps, bool kGradient>
+template <typename T, Access kAccess, int kTiles, int kSteps, bool kGradient>
 __global__ void __launch_bounds__(kThreads) xent_few_kernel(XentArgs a, int first, int words, int64_t ldg)
 {
-    typedef Stretch<T, WORDS, kSteps> Part;
+    typedef Stretch<T, kAccess, kSteps> Part;
     constexpr int kBatch = Part::kBatch, kWords = 16 * kTiles;
     const int lane = lane_id(), slot = lane % 16, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / NACHO_WAVE);
     __shared__ RowList lists[kWaves];
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kThreads) xent_few_kernel(XentArgs a, int firs
     const int tiles = (words + kWords - 1) / kWords, stretches = (a.inner + Part::kLong - 1) / Part::kLong, k = a.inner;
     const T *const head = static_cast<const T *>(a.head) + (int64_t)first * a.ldh;
     struct Loaded {
-        v4u p[kTiles][kBatch], q[kBatch];
+        typename Part::Loaded p[kTiles][kBatch], q[kBatch];
     } one, two;
     for (int tile = (int)blockIdx.x * kWaves + wave; tile < tiles; tile += (int)gridDim.x * kWaves) {
         const T *rows[kTiles];
@@ -180,6 +180,74 @@ __global__ void __launch_bounds__(kThreads) xent_few_kernel(XentArgs a, int firs
     }
 }
 
+// Gradients of the vocabulary's weights: 16 words are one product of g^T with the rows of x, which a wavefront keeps (kAcross columns of them,
+// zeros behind the last) and takes through the words.  Bound by writing: a lane ends with a word of 16 bytes of a row, so results need no LDS.
+// (The tiles of columns that make up such a word take every other four columns.)  Rows that start at multiples of 64 bytes leave by stores that
+// no cache keeps, the 64 bytes that an instruction has of a row at once; other rows' lines would be written in parts.  (Loss and gradients, us a
+// pass so, otherwise, and with the tiles of many rows: 1 row, 65536 x 2048 bf16 220, 231 and 246, 16 rows 238, 253 and 258; 2 rows, 50622 x 3867
+// f32 1255, 782 and 824.  65536 x 2048 bf16 is 268 MB in about 45 us.)
+template <typename T> constexpr int kAcross = sizeof(T) == 4 ? 256 : 128;     // (2 rows, 50622 x 3867 f32: 128 811 us, 256 776; 65536 x 2048 bf16 258 and 261)
+template <typename T, bool kWhole> __global__ void __launch_bounds__(kThreads) xent_few_head_kernel(XentArgs a, int first, int words, int64_t ldg, int chunks, int each)
+{
+    typedef typename Word<T>::type word;
+    constexpr int n = Word<T>::n, kGroup = n / 4, kTiles = kAcross<T> / 16;
+    const int lane = lane_id(), number = (int)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x / NACHO_WAVE);
+    const int c0 = number % chunks * kAcross<T>, tiles = (words + 15) / 16, row0 = lane / 16 * n;
+    const int held = a.rows > 0 ? a.bounds[1] : 0;
+    if (number / chunks >= each) return;
+    const float by = a.scale[1];
+    v4u p[kTiles];
+    word q[2];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) p[i] = v4u{0, 0, 0, 0};
+    auto fetch = [&](word &to, int tile) {
+        const int at = tile * 16 + lane % 16, there = at < words ? at : words - 1;
+#pragma unroll
+        for (int e = 0; e < n; ++e) to[e] = row0 + e < held ? static_cast<const T *>(a.g)[(row0 + e) * ldg + there] : (T)0.0f;
+    };
+    q[0] = q[1] = __builtin_bit_cast(word, p[0]);
+    if (row0 < held) {
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+            if (row0 + e >= held) break;
+            const T *const x = static_cast<const T *>(a.x) + a.token[row0 + e] * a.ldx;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) {
+                const int m = lane % 16, c = c0 + i / kGroup * 16 * kGroup + m / 4 * n + i % kGroup * 4 + m % 4;
+                word v = __builtin_bit_cast(word, p[i]);
+                v[e] = c < a.inner ? x[c] : (T)0.0f;
+                p[i] = __builtin_bit_cast(v4u, v);
+            }
+        }
+        fetch(q[0], number / chunks);
+    }
+    for (int tile = number / chunks; tile < tiles; tile += each) {
+        if (row0 < held && tile + each < tiles) fetch(q[1], tile + each);
+        v4f acc[kTiles];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) acc[i] = matrix_step<T>(p[i], __builtin_bit_cast(v4u, q[0]), v4f{0.0f, 0.0f, 0.0f, 0.0f});
+        const int at = tile * 16 + lane % 16;
+        T *const out = static_cast<T *>(a.grad_head) + (int64_t)(first + at) * a.ldgh;
+        if (at < words) {
+#pragma unroll
+            for (int j = 0; j < kTiles / kGroup; ++j) {
+                const int c = c0 + j * 16 * kGroup + lane / 16 * n;
+                word v;
+#pragma unroll
+                for (int e = 0; e < n; ++e) v[e] = (T)(acc[j * kGroup + e / 4][e % 4] * by);
+                if (kWhole && c + n <= a.inner) __builtin_nontemporal_store(v, reinterpret_cast<word *>(out + c));
+                else if (c + n <= a.inner) __builtin_memcpy(out + c, &v, 16);
+                else {
+#pragma unroll
+                    for (int e = 0; e < n; ++e)
+                        if (c + e < a.inner) out[c + e] = v[e];
+                }
+            }
+        }
+        q[0] = q[1];
+    }
+}
+
 // Words that a wavefront has at a time: 16 as long as 32 would leave a quarter of the compute units without any.  (16 rows bf16, us a call
 // with 16 and with 32: 8000 x 1024 21 and 25, 16000 x 1024 21 and 25, 32000 x 1024 29 and 26, 65536 x 1024 47 and 41, 65536 x 2048 74 and
 // 62, a graph's start included.)
@@ -193,18 +261,41 @@ int64_t xent_few_groups(int64_t vocabulary)
     return groups < 4 * kUnits ? groups : 4 * kUnits;
 }
 
-hipError_t launch_xent_few(int dtype, const XentArgs &a, int64_t first, int64_t words, int64_t ldg, hipStream_t s)
+hipError_t launch_xent_few(int dtype, const XentArgs &a, int64_t first, int64_t words, int64_t ldg, bool in_words, hipStream_t s)
 {
     const unsigned grid = (unsigned)xent_few_groups(words);
     by_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        auto run = [&](auto tiles, auto steps) {
+        auto run = [&](auto access, auto tiles, auto steps) {
+            constexpr Access kAccess = decltype(access)::value;
             constexpr int kTiles = decltype(tiles)::value, kSteps = decltype(steps)::value;
-            if (a.g) xent_few_kernel<T, kTiles, kSteps, true><<<grid, kThreads, 0, s>>>(a, (int)first, (int)words, ldg);
-            else xent_few_kernel<T, kTiles, kSteps, false><<<grid, kThreads, 0, s>>>(a, (int)first, (int)words, ldg);
+            if (a.g) xent_few_kernel<T, kAccess, kTiles, kSteps, true><<<grid, kThreads, 0, s>>>(a, (int)first, (int)words, ldg);
+            else xent_few_kernel<T, kAccess, kTiles, kSteps, false><<<grid, kThreads, 0, s>>>(a, (int)first, (int)words, ldg);
         };
-        if (words_at_a_time(words) == 16) run(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
-        else run(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
+        auto of = [&](auto access) {
+            if (words_at_a_time(words) == 16) run(access, std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
+            else run(access, std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
+        };
+        typedef std::integral_constant<Access, WORDS> Words;
+        typedef std::integral_constant<Access, sizeof(T) == 4 ? ANYWHERE : WORDS> Anywhere;
+        in_words ? of(Words()) : of(Anywhere());
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_xent_few_head(int dtype, const XentArgs &a, int64_t first, int64_t words, int64_t ldg, hipStream_t s)
+{
+    const bool whole = ((uintptr_t)a.grad_head | (uintptr_t)(a.ldgh * a.elem)) % 64 == 0;
+    by_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        // (8 wavefronts a compute unit write as fast as 16 and fetch the rows of x half as often: 1 row, 65536 x 2048 bf16, 220 and 223 us)
+        const int64_t chunks = (a.inner + kAcross<T> - 1) / kAcross<T>, tiles = (words + 15) / 16, most = 8 * kUnits / chunks;
+        const int64_t each = tiles < most ? tiles : most > 1 ? most : 1;
+        auto run = [&](auto streams) {
+            xent_few_head_kernel<T, decltype(streams)::value>
+                <<<(unsigned)((chunks * each + kWaves - 1) / kWaves), kThreads, 0, s>>>(a, (int)first, (int)words, ldg, (int)chunks, (int)each);
+        };
+        whole ? run(std::true_type()) : run(std::false_type());
     });
     return hipGetLastError();
 }
