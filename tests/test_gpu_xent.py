@@ -101,6 +101,16 @@ def test_against_the_definition(sizes, dtype):
     check(problem(seed, *sizes, dtype, weighted=seed % 3 != 0, masked=0.3 if seed % 2 else 0.0), dtype)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sizes", [(16, 1003, 512), (16, 517, 257), (15, 4100, 130), (9, 70, 1024), (1, 33, 2048), (16, 2000, 999), (4, 15, 4096), (16, 40_001, 24)])
+def test_few_rows(sizes, dtype):
+    check(problem(5, *sizes, dtype), dtype)
+    check(problem(6, *sizes, dtype, pad=3), dtype, pad=3)
+    d = problem(7, *sizes, dtype, masked=0.5)
+    d["x"][d["label"] < 0] = float("nan")
+    check(d, dtype)
+
+
 @pytest.mark.parametrize("sizes", [(17, 1567, 2275), (64, 8192, 12), (64, 8193, 12), (63, 8129, 70), (100, 70, 4096), (33, 31, 5), (500, 1000, 65), (600, 1100, 130)])
 def test_few_tiles_of_floats(sizes):
     for masked in (0.0, 0.4):
