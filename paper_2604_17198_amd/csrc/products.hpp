@@ -4,9 +4,10 @@
 //   forward   m: rows of Q, n: rows of P, both run along k        rows    P's columns run along k        weights  both sides' do
 //
 // A workgroup computes a tile of kM x kN results on the matrix units, from tiles of Q and P that pass through LDS.  A side whose
-// rows run along k lies there as rows of k, and a lane reads 16 bytes of its row; a side whose columns run along k lies there as rows
-// of n (or m) for every k, and is transposed by the LDS on the way to the registers (16-bit types), or read an element at a time (floats).  P is the first operand of the matrix instruction, so that a lane ends with four
-// consecutive columns of a result row.  What becomes of the results is the kernel's last argument (a Finish).
+// rows run along k lies there as rows of k, and a lane reads 16 bytes of its row; a side whose columns run along k lies there as
+// rows of n (or m) for every k, and is transposed by the LDS on the way to the registers (16-bit types), or read an element at a
+// time (floats).  P is the first operand of the matrix instruction, so that a lane ends with four consecutive columns of a result
+// row.  What becomes of the results is the kernel's last argument (a Finish).
 //
 // Which group (expert) a tile belongs to is found by its workgroup from the groups' bounds alone (a prefix sum of their tiles
 // over the lanes), so nothing about them is read on the host.

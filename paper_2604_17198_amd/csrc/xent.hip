@@ -403,7 +403,8 @@ Access access_of_rows(const XentArgs &a)
     const bool words = a.ldx < 0x7fffffff && a.ldh < 0x7fffffff && in_words({{a.x, a.ldx}, {a.head, a.ldh}, {a.x, a.inner}}, a.elem);
     return words ? WORDS : a.inner * a.elem < 16 ? TINY : ANYWHERE;
 }
-template <typename T> hipError_t pad(const void *from, int64_t ld, const XentArgs &a, const int32_t *list, const int32_t *held, int64_t rows, void *to, hipStream_t s)
+template <typename T>
+hipError_t pad(const void *from, int64_t ld, const XentArgs &a, const int32_t *list, const int32_t *held, int64_t rows, void *to, hipStream_t s)
 {
     const int64_t groups = (rows + 3) / 4;
     xent_pad_kernel<T><<<(unsigned)(groups < 8 * kUnits ? groups : 8 * kUnits), 256, 0, s>>>(from, ld, a.inner, list, held, rows, to, padded(a.inner));
@@ -480,7 +481,8 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bo
 {
     constexpr int64_t kRoom = 256 << 20;
     XentPlan p;
-    const int64_t by_g = rows > 0 && gradient ? kRoom / (rows * elem) / 256 * 256 : vocabulary, by_copy = pads ? kRoom / (padded(inner) * elem) / 256 * 256 : vocabulary;
+    const int64_t by_g = rows > 0 && gradient ? kRoom / (rows * elem) / 256 * 256 : vocabulary;
+    const int64_t by_copy = pads ? kRoom / (padded(inner) * elem) / 256 * 256 : vocabulary;
     const int64_t most = by_g < by_copy ? by_g : by_copy, least = most > 256 ? most : 256;
     p.pieces = (vocabulary + least - 1) / least;
     p.words = p.pieces > 1 ? ((vocabulary + p.pieces - 1) / p.pieces + 255) / 256 * 256 : vocabulary;

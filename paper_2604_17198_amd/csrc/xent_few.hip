@@ -186,8 +186,10 @@ __global__ void __launch_bounds__(kThreads) xent_few_kernel(XentArgs a, int firs
 // no cache keeps, the 64 bytes that an instruction has of a row at once; other rows' lines would be written in parts.  (Loss and gradients, us a
 // pass so, otherwise, and with the tiles of many rows: 1 row, 65536 x 2048 bf16 220, 231 and 246, 16 rows 238, 253 and 258; 2 rows, 50622 x 3867
 // f32 1255, 782 and 824.  65536 x 2048 bf16 is 268 MB in about 45 us.)
-template <typename T> constexpr int kAcross = sizeof(T) == 4 ? 256 : 128;     // (2 rows, 50622 x 3867 f32: 128 811 us, 256 776; 65536 x 2048 bf16 258 and 261)
-template <typename T, bool kWhole> __global__ void __launch_bounds__(kThreads) xent_few_head_kernel(XentArgs a, int first, int words, int64_t ldg, int chunks, int each)
+// (2 rows, 50622 x 3867 f32: 128 columns 811 us, 256 776; 16 rows, 65536 x 2048 bf16 258 and 261)
+template <typename T> constexpr int kAcross = sizeof(T) == 4 ? 256 : 128;
+template <typename T, bool kWhole>
+__global__ void __launch_bounds__(kThreads) xent_few_head_kernel(XentArgs a, int first, int words, int64_t ldg, int chunks, int each)
 {
     typedef typename Word<T>::type word;
     constexpr int n = Word<T>::n, kGroup = n / 4, kTiles = kAcross<T> / 16;
