@@ -140,6 +140,42 @@ def test_rows_apart(dtype, pad, act):
     check(d, 2, act, True, dtype, pad)
 
 
+# Tiles of 16 rows of the experts that tokens can choose, from 2048 on: a wavefront has one at a time, with all of k.  Rows of words,
+# rows that start anywhere, rows shorter than 16 bytes; one stretch of k and several with a last one that is not whole; experts of more
+# than 16 tokens (2048 choices of 70 experts, 64 of one).
+MANY_ITEMS = [(64, 128, 8, 40, 256, 24), (64, 128, 8, 200, 256, 24), (64, 128, 8, 203, 261, 19), (64, 128, 8, 3, 260, 17), (64, 70, 32, 72, 520, 24),
+              (64, 70, 32, 75, 520, 21), (9, 300, 32, 136, 128, 40), (64, 1, 1, 72, 33_000, 9)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("sizes", MANY_ITEMS)
+def test_many_items(sizes, gated, dtype):
+    tokens, experts, top_k, inner, hidden, outer = sizes
+    assert min(tokens * top_k, experts) * -(-hidden // 16) >= 2048
+    d = problem(sum(sizes), tokens, experts, inner, hidden, outer, dtype, gated=gated, bias=True, residual=gated, keep=not gated)
+    act = ACTS[sum(sizes) % 4]
+    check(d, top_k, act, True, dtype)
+    check(d, top_k, act, False, dtype, pad=8 if inner % 8 == 0 else 3)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("sizes", [(7, 6, 2, 72, 56, 40), (64, 128, 8, 135, 256, 24)])
+@pytest.mark.parametrize("name", ["x", "up", "gate", "down"])
+def test_arrays_that_start_at_an_odd_element(name, sizes, dtype):
+    """16-bit arrays whose first row starts between two words of 4 bytes, which are read element by element."""
+    tokens, experts, top_k, inner, hidden, outer = sizes
+    d = problem(sum(sizes), tokens, experts, inner, hidden, outer, dtype, gated=True)
+    g = on_gpu(d)
+    room = torch.full((g[name].numel() + 2,), float("nan"), dtype=dtype, device="cuda")
+    room[1:-1] = g[name].flatten()
+    g[name] = room[1:-1].view(g[name].shape)
+    assert g[name].data_ptr() % 4 == 2
+    got = nb.nacho_experts_step(g["x"], g["logits"], top_k, g["up"], g["down"], gate=g["gate"], normalise=True)
+    want, off = reference(d, top_k, True, "silu", dtype)
+    assert bool(((got.cpu().double() - want).abs() <= off).all())
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_ties_and_experts_that_are_closed(dtype):
     """Equal logits go to the lowest index; -inf and NaN are never chosen, and a token may choose fewer or none."""
