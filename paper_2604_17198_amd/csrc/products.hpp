@@ -801,15 +801,25 @@ constexpr int64_t kUnits = 256;        // compute units
 // Floats need four times as many matrix instructions for what is loaded: tiles of 64 x 64, which are as many again.  3000 slots
 // of 7 experts, 777 x 499, us: weights 73 (64 x 128: 95), forward 42 (32 x 128: 45), rows 44 (50); with two steps on their way
 // in registers 54, 43 and 42.  512 x 2048, 32 experts of 64 and 128 slots, us with 32, 64 and 128: rows 51, 52 and 141, 87, 81 and 149.
-// Where a forward product of floats would be half a tile of 64 x 64 a compute unit, or fewer, tiles are of 32 x 32: a stage then takes a
-// wavefront half the time, and four times as many compute units have one.  (us a call with 32 x 32 and without: loss of 21 rows, 1567 x 2275
-// 56 and 76, of 100 rows, 2000 x 4095 87 and 119, of 300 rows, 1300 x 4000 (105 tiles of 64) 95 and 103, of 600 rows, 3000 x 1024 (470) 73
-// and 56; experts in training, 64 tokens, 2 of 4, 2000 x 1000 92 and 113.  With stages of 128 bytes 58, 91, 97 and 62.)
-constexpr int64_t kMostTiny = kUnits / 2;
+// Where forward products of floats leave compute units without one of the larger tiles, tiles are of 32 x 32: a stage then takes a
+// wavefront half the time, and more of them are at work.  (us a call with 32 x 32 and without: loss of 21 rows, 1567 x 2275 56 and 76, of
+// 100 rows, 2000 x 4095 87 and 119, of 300 rows, 1300 x 4000 95 and 103, of 600 rows, 3000 x 1024 73 and 56; experts in training, 64 tokens,
+// 2 of 4, 2000 x 1000 92 and 113.  With stages of 128 bytes 58, 91, 97 and 62.)
 enum Shape { TILES_256, TILES_128, TILES_64, TILES_32, TILES_32_32 };
 // Rows and columns of these tiles (of rows shorter than a word: 128 x 128 for the weights, 32 x 128).
 constexpr int tall_of(Shape s) { return s == TILES_256 ? 256 : s == TILES_128 ? 128 : s == TILES_64 ? 64 : 32; }
 constexpr int wide_of(Shape s) { return s == TILES_256 ? 256 : s == TILES_64 ? 64 : s == TILES_32_32 ? 32 : 128; }
+// Whether floats go by tiles of 32 x 32: every expert that can have slots has tiles of its own, and a tile with no more than 16 rows, whose
+// other rows are the last one again, counts half.  (Experts that all have a slot or more, us a launch with 32 x 32 and without, 4096 x 2048: 4 of 4
+// slots 38 and 50, of 24 44 and 50, of 64 63 and 50; 2 of 64 43 and 49; 7 of 8 52 and 55, 8 of 8 (on the line) 65 and 60, 9 of 8 96 and 88, 12 of
+// 8 98 and 96; 4096 x 4096: 7 of 8 98 and 109, 8 of 8 123 and 124, 10 of 8 202 and 181, 16 of 8 230 and 206; 1024 x 1024, 48 of 4 56 and 52; 1000 x
+// 1001, 64 of 8 65 and 57.  Well past the line neither side is ahead: 64 of 4, 2048 x 500 64 and 61, x 1001 121 and 113, x 1024 124 and 142, x 2048
+// 231 and 257, x 4096 438 and 404.)
+inline bool tiny_tiles(int64_t slots, int64_t experts, int64_t n)
+{
+    const int64_t active = slots < experts ? slots : experts;
+    return active == 0 || active * (((slots + active - 1) / active + 15) / 16) * ((n + 31) / 32) <= 4 * kUnits;
+}
 // `parts`: stretches of k that workgroups share a tile's sum by.
 template <typename T, Form kForm> Shape shape_of(const ProductArgs &a, Access access, int64_t parts = 1)
 {
@@ -824,7 +834,7 @@ template <typename T, Form kForm> Shape shape_of(const ProductArgs &a, Access ac
         if (sizeof(T) == 2 && words && each >= 256 && a.n >= 256 && a.slots / 256 * ((a.n + 255) / 256) * parts >= kUnits) return TILES_256;
         const int64_t few = words && sizeof(T) == 2 ? 32 : 64, most = sizeof(T) == 2 ? kUnits / 2 : 2 * kUnits - 1;
         const bool small = each <= few || a.slots / 128 * n128 * parts <= most;
-        if (kForm == FORWARD && sizeof(T) == 4 && (a.slots + 63) / 64 * ((a.n + 63) / 64) <= kMostTiny) return TILES_32_32;
+        if (kForm == FORWARD && sizeof(T) == 4 && tiny_tiles(a.slots, a.experts, a.n)) return TILES_32_32;
         return !small ? TILES_128 : sizeof(T) == 4 && each > 64 ? TILES_64 : TILES_32;
     }
 }

@@ -449,8 +449,12 @@ bool few_rows(const XentArgs &a)
     return a.rows <= kFewRows && (access == WORDS || (access == ANYWHERE && a.elem == 4 && a.rows * a.inner <= 1 << 14));
 }
 
-// (the narrowest tiles there can be; of 32 floats there are at most kMostTiny more than of 64)
-int64_t tiles_of_loss(int elem, int64_t vocabulary) { return elem == 4 ? (vocabulary + 63) / 64 + kMostTiny : (vocabulary + 127) / 128; }
+// (the narrowest tiles there can be)
+int64_t tiles_of_loss(int elem, int64_t rows, int64_t vocabulary)
+{
+    const int64_t wide = elem == 2 ? 128 : tiny_tiles(rows, 1, vocabulary) ? 32 : 64;
+    return (vocabulary + wide - 1) / wide;
+}
 
 hipError_t list_rows(const XentArgs &a, hipStream_t s)
 {
@@ -464,7 +468,7 @@ hipError_t list_rows(const XentArgs &a, hipStream_t s)
 
 int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary)
 {
-    const int64_t few = rows <= kFewRows ? xent_few_groups(vocabulary) : 0, tiles = tiles_of_loss(elem, vocabulary);
+    const int64_t few = rows <= kFewRows ? xent_few_groups(vocabulary) : 0, tiles = tiles_of_loss(elem, rows, vocabulary);
     return (few > tiles ? few : tiles) * rows;
 }
 

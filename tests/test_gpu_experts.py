@@ -266,6 +266,22 @@ def test_the_largest_tiles(counts, inner, outer, dtype):
     check(problem(20, counts, 300, inner, outer, dtype, True), "silu", dtype)
 
 
+# Forward products of floats past the line up to which they go by tiles of 32 x 32: 32 x 128 (few slots an expert, also with empty ones), 64 x 64
+# (72 slots), rows of words and rows that start anywhere; and 8 experts on either side of the line.
+def sixteens(counts, outer):
+    active = min(sum(counts), len(counts))
+    return active * -(-(-(-sum(counts) // active)) // 16) * -(-outer // 32)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("counts,inner,outer,past", [([20] * 10, 72, 2052, True), ([20] * 10, 73, 2051, True), ([0, 40, 3, 0, 61, 33, 1, 22], 268, 4108, True),
+                                                     ([0, 40, 3, 0, 61, 33, 1, 22], 267, 4107, True), ([1, 4, 0, 2] * 16, 41, 701, True), ([70, 80, 66], 64, 3004, True),
+                                                     ([70, 80, 66], 65, 3001, True), ([8] * 8, 136, 4096, False), ([8] * 8, 136, 4100, True), ([8] * 8, 137, 4097, True)])
+def test_many_small_tiles(counts, inner, outer, past, dtype):
+    assert (sixteens(counts, outer) > 1024) == past
+    check(problem(22, counts, 50, inner, outer, dtype, True), "gelu", dtype)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("inner", [64, 128, 192, 256, 264, 320, 136])
 def test_steps_of_the_sum(inner, dtype):
