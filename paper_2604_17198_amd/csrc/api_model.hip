@@ -251,6 +251,13 @@ bool check_xent_arrays(const nacho_xent_layer *l)
     if ((l->n_rows > 0 && !l->label) || !aligned(l->label, (uintptr_t)l->label_bytes) || !aligned(l->weight, 4)) return false;
     return true;
 }
+void carve_counts(Slices *c, XentArgs *a)
+{
+    const int64_t groups = xent_counts(a->rows);
+    if (groups == 0) return;
+    a->counts = c->take<int32_t>(groups);
+    a->most = c->take<float>(groups);
+}
 void carve_copies(Slices *c, const nacho_xent_layer *l, const XentPlan &plan, XentArgs *a)
 {
     const int64_t row = (l->inner + 7) / 8 * 8 * value_bytes(l->dtype);
@@ -266,6 +273,7 @@ size_t carve_xent(void *ws, const nacho_xent_layer *l, const XentPlan &plan, Xen
     a->slot_label = c.take<int32_t>(l->n_rows);
     a->at_label = c.take<float>(l->n_rows);
     a->partial = c.take<float2>(xent_partials((int)value_bytes(l->dtype), l->n_rows, l->vocabulary));
+    carve_counts(&c, a);
     carve_copies(&c, l, plan, a);
     return align_up(c.off, 256);
 }
@@ -281,6 +289,7 @@ size_t carve_xent_grad(void *ws, const nacho_xent_layer *l, const XentPlan &plan
     a->slot_of = c.take<int32_t>(l->n_rows);
     a->g = c.take<char>(l->n_rows * plan.ldg * value_bytes(l->dtype));
     if (sums && plan.sums) a->sums = c.take<float>(plan.stretches * l->n_rows * plan.lds);
+    carve_counts(&c, a);
     carve_copies(&c, l, plan, a);
     return align_up(c.off, 256);
 }

@@ -179,6 +179,9 @@ struct XentArgs {
     int64_t ldgx, ldgh;
     // workspace: the rows that count (slots) and their number
     int32_t *bounds, *token, *slot_label;
+    // of many rows, by workgroups that list them: how many count, and the largest weight (NULL: they need neither)
+    int32_t *counts;
+    float *most;
     // of the loss: [tiles of the vocabulary][rows], and the label's logit by slot
     float2 *partial;
     float *at_label;
@@ -196,6 +199,7 @@ struct XentPlan {
     int64_t pieces, words, ldg, stretches, shortest, k_part, lds;      // (no stretch shorter than `shortest`)
     bool sums;                     // (of the rows' gradients, in 32 bits: `lds` apart, one set a stretch)
 };
+int64_t xent_counts(int64_t rows);     // workgroups that `counts` and `most` are by
 int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary);
 XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bool pads, bool gradient);
 constexpr int64_t kPaddedFrom = 384;   // rows

@@ -21,20 +21,61 @@ namespace {
 
 constexpr int kRowThreads = 1024;
 
+template <typename Label> __device__ inline bool row_counts(const XentArgs &a, int64_t i)
+{
+    const Label label = static_cast<const Label *>(a.label)[i];
+    return label >= 0 && label < (Label)a.vocabulary && (!a.weight || a.weight[i] != 0.0f);
+}
+
+// How many rows count, and the largest weight of one, by workgroups of xent_rows_kernel.
+template <typename Label> __global__ void __launch_bounds__(kRowThreads) xent_count_kernel(XentArgs a, int each)
+{
+    constexpr int kWaves = kRowThreads / NACHO_WAVE;
+    __shared__ int counts[kWaves];
+    __shared__ float share[kWaves];
+    const int tid = (int)threadIdx.x, wave = tid / NACHO_WAVE;
+    const int64_t begin = (int64_t)blockIdx.x * each * kRowThreads, behind = begin + (int64_t)each * kRowThreads, end = behind < a.rows ? behind : a.rows;
+    int count = 0;
+    float most = 0.0f;
+#pragma unroll 4
+    for (int64_t i = begin + tid; i < end; i += kRowThreads) {
+        const bool held = row_counts<Label>(a, i);
+        count += held;
+        if (a.scale && a.weight) most = held ? fmaxf(most, fabsf(a.weight[i])) : most;
+    }
+    count = wave_sum(count);
+    most = wave_all(most, MaxOf());
+    if (lane_id() == 0) {
+        counts[wave] = count;
+        share[wave] = most;
+    }
+    __syncthreads();
+    if (tid != 0) return;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+        count += counts[w];
+        most = fmaxf(most, share[w]);
+    }
+    a.counts[blockIdx.x] = count;
+    a.most[blockIdx.x] = most;
+}
+
 // The list of the rows that count, ascending, and by it their labels (and weights and lse, for the gradient).  Every workgroup has
-// kRowThreads rows and counts those before them itself.  The loss's call clears the results of the other rows.
-template <typename Label> __global__ void __launch_bounds__(kRowThreads) xent_rows_kernel(XentArgs a)
+// `each` x kRowThreads rows, and knows how many count before them from xent_count_kernel or, where there is no a.counts, counts them
+// itself.  The loss's call clears the results of the other rows.
+template <typename Label> __global__ void __launch_bounds__(kRowThreads) xent_rows_kernel(XentArgs a, int each)
 {
     constexpr int kWaves = kRowThreads / NACHO_WAVE;
     __shared__ int counts[kWaves];
     __shared__ float share[kWaves];
     const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid / NACHO_WAVE;
-    const int64_t begin = (int64_t)blockIdx.x * kRowThreads;
-    const Label *labels = static_cast<const Label *>(a.label);
-    auto counts_at = [&](int64_t i) { return labels[i] >= 0 && labels[i] < (Label)a.vocabulary && (!a.weight || a.weight[i] != 0.0f); };
+    const int64_t begin = (int64_t)blockIdx.x * each * kRowThreads;
     int before = 0;
+    if (a.counts) before = tid < (int)blockIdx.x ? a.counts[tid] : 0;
+    else {
 #pragma unroll 4
-    for (int64_t i = tid; i < begin; i += kRowThreads) before += counts_at(i);
+        for (int64_t i = tid; i < begin; i += kRowThreads) before += row_counts<Label>(a, i);
+    }
     before = wave_sum(before);
     if (lane == 0) counts[wave] = before;
     __syncthreads();
@@ -42,35 +83,39 @@ template <typename Label> __global__ void __launch_bounds__(kRowThreads) xent_ro
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) before += counts[w];
     __syncthreads();
-    const int64_t i = begin + tid;
-    const bool held = i < a.rows && counts_at(i);
-    const unsigned long long who = __ballot(held);
-    if (lane == 0) counts[wave] = __popcll((long long)who);
-    __syncthreads();
-    int total = 0;
+    for (int64_t first = begin; first < begin + (int64_t)each * kRowThreads && first < a.rows; first += kRowThreads) {
+        const int64_t i = first + tid;
+        const bool held = i < a.rows && row_counts<Label>(a, i);
+        const unsigned long long who = __ballot(held);
+        if (lane == 0) counts[wave] = __popcll((long long)who);
+        __syncthreads();
+        int slot = before + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0));
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w == wave) before += total;
-        total += counts[w];
-    }
-    const int slot = before + __builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0));
-    if (held) {
-        a.token[slot] = (int32_t)i;
-        a.slot_label[slot] = (int32_t)labels[i];
-        if (a.slot_lse) {
-            a.slot_lse[slot] = a.lse[i];
-            a.factor[slot] = a.weight ? a.weight[i] : 1.0f;
+        for (int w = 0; w < kWaves; ++w) {
+            slot += w < wave ? counts[w] : 0;
+            before += counts[w];
         }
-    } else if (i < a.rows && a.loss) a.loss[i] = a.lse[i] = 0.0f;
-    if (a.slot_of && i < a.rows) a.slot_of[i] = held ? slot : -1;
-    if (blockIdx.x == gridDim.x - 1 && tid == kRowThreads - 1) {
+        __syncthreads();
+        if (held) {
+            a.token[slot] = (int32_t)i;
+            a.slot_label[slot] = (int32_t)static_cast<const Label *>(a.label)[i];
+            if (a.slot_lse) {
+                a.slot_lse[slot] = a.lse[i];
+                a.factor[slot] = a.weight ? a.weight[i] : 1.0f;
+            }
+        } else if (i < a.rows && a.loss) a.loss[i] = a.lse[i] = 0.0f;
+        if (a.slot_of && i < a.rows) a.slot_of[i] = held ? slot : -1;
+    }
+    if (blockIdx.x == gridDim.x - 1 && tid == 0) {
         a.bounds[0] = 0;
-        a.bounds[1] = before + (int)__popcll((long long)who);
+        a.bounds[1] = before;
     }
     if (!a.scale || blockIdx.x != 0) return;
     float most = 0.0f;
-    if (a.weight)
-        for (int64_t j = tid; j < a.rows; j += kRowThreads) most = counts_at(j) ? fmaxf(most, fabsf(a.weight[j])) : most;
+    if (a.counts) most = tid < (int)gridDim.x ? a.most[tid] : 0.0f;
+    else if (a.weight) {
+        for (int64_t j = tid; j < a.rows; j += kRowThreads) most = row_counts<Label>(a, j) ? fmaxf(most, fabsf(a.weight[j])) : most;
+    }
     most = wave_all(most, MaxOf());
     if (lane == 0) share[wave] = most;
     __syncthreads();
@@ -456,15 +501,38 @@ int64_t tiles_of_loss(int elem, int64_t rows, int64_t vocabulary)
     return (vocabulary + wide - 1) / wide;
 }
 
+// How the rows are listed: `groups` workgroups of `each` x kRowThreads rows.  Workgroups that each count all rows before theirs read as many as
+// the square of the rows; from kCountedFrom on a launch of its own counts them first, kRowThreads numbers at most.  (Loss and gradients against
+// 8 x 8, us a pass so and without: 16384 rows 184 and 185, 32768 336 and 344, 131072 1240 and 1327, 16 million 168 and 535 ms.)
+constexpr int64_t kCountedFrom = 1 << 15;
+struct Lists {
+    int64_t groups;
+    int32_t each;
+    explicit Lists(int64_t rows)
+    {
+        const int64_t chunks = rows > 0 ? (rows + kRowThreads - 1) / kRowThreads : 1;
+        each = rows >= kCountedFrom ? (int32_t)((chunks + kRowThreads - 1) / kRowThreads) : 1;
+        groups = (chunks + each - 1) / each;
+    }
+};
+template <typename Label> hipError_t list_rows_of(const XentArgs &a, hipStream_t s)
+{
+    const Lists lists(a.rows);
+    if (a.counts) {
+        xent_count_kernel<Label><<<(unsigned)lists.groups, kRowThreads, 0, s>>>(a, lists.each);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    xent_rows_kernel<Label><<<(unsigned)lists.groups, kRowThreads, 0, s>>>(a, lists.each);
+    return hipGetLastError();
+}
 hipError_t list_rows(const XentArgs &a, hipStream_t s)
 {
-    const int64_t groups = a.rows > 0 ? (a.rows + kRowThreads - 1) / kRowThreads : 1;
-    if (a.label_bytes == 8) xent_rows_kernel<int64_t><<<(unsigned)groups, kRowThreads, 0, s>>>(a);
-    else xent_rows_kernel<int32_t><<<(unsigned)groups, kRowThreads, 0, s>>>(a);
-    return hipGetLastError();
+    return a.label_bytes == 8 ? list_rows_of<int64_t>(a, s) : list_rows_of<int32_t>(a, s);
 }
 
 }  // namespace
+
+int64_t xent_counts(int64_t rows) { return rows >= kCountedFrom ? Lists(rows).groups : 0; }
 
 int64_t xent_partials(int elem, int64_t rows, int64_t vocabulary)
 {

@@ -182,6 +182,55 @@ def test_few_of_many_rows_count(sizes, live, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [32_767, 32_768, 33_793, 1_050_001])
+def test_lists_of_many_rows(rows, dtype):
+    """Rows that are counted before they are listed, a workgroup 1024 of them or more."""
+    d = problem(rows, rows, 5, 8, dtype, masked=0.4, weighted=rows % 2 == 1, label=torch.int32 if rows % 2 else torch.int64)
+    d["label"][2048:9000] = -1
+    d["x"][d["label"] < 0] = float("nan")
+    if rows % 2:
+        d["weight"][20_000:20_050] = 0.0
+        d["weight"][rows - 1] = 3.0                              # (the largest one, in the last workgroup)
+        d["label"][rows - 1] = 2
+    d["x"][rows - 1] = 1.0
+    for last in (False, True):
+        if last:
+            d["label"].fill_(-1)
+            d["label"][rows - 1] = 3
+        loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+        gx, gh = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, weight=d["weight"])
+        want = definition(d, dtype)
+        # (The sum of a million rows' gradients passes the range of f16, whose numbers from 65520 on, the largest one and half a step, are
+        # infinite: the value 67896.7 of 0.6 million rows is, and so may be any that its room brings there.)
+        value, room = want["grad_head"]
+        far = gh.isinf() & (value.abs() + room >= 65520) & (gh.sign() == value.sign()) if dtype is torch.float16 else torch.zeros_like(gh, dtype=torch.bool)
+        close(lse, want["lse"], "lse")
+        close(loss, want["loss"], "loss")
+        close(gx, want["grad_x"], "grad_x")
+        close(torch.where(far, value, gh.double()), want["grad_head"], "grad_head")
+        again = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+        assert torch.equal(again[0], loss) and torch.equal(again[1], lse)
+
+
+def test_the_time_of_listing_grows_as_the_rows():
+    """Four times as many rows take about four times as long, not sixteen times."""
+    times = []
+    for rows in (1 << 22, 1 << 24):
+        x, head = torch.ones((rows, 8), dtype=torch.bfloat16, device="cuda"), torch.ones((8, 8), dtype=torch.bfloat16, device="cuda")
+        label = torch.zeros(rows, dtype=torch.int64, device="cuda")
+        best = float("inf")
+        for _ in range(4):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            nb.nacho_xent(x, head, label)
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end))
+        times.append(best)
+    assert times[1] <= 8 * times[0], times
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_no_row_counts(dtype):
     d = problem(5, 40, 300, 64, dtype)
     d["label"].fill_(-100)
