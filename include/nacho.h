@@ -457,8 +457,10 @@ int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int6
  *   loss[i] = weight[i] (lse[i] - z_i,label[i])
  * Rows whose label lies outside the vocabulary (a negative one: a position that is not
  * to be learned) and rows of weight 0 have loss, lse and gradients 0, whatever they
- * hold; they are not computed.  A row with a NaN or an infinity among its logits has
- * no distribution: NaN.
+ * hold; they are not computed.  A logit of -inf is a probability of 0 (the loss of a
+ * row whose label has it is infinite); a row with a NaN or +inf among its logits, or
+ * with nothing but -inf, has no distribution: NaN.  Gradients are what their formulas
+ * give: an infinite weight times a probability of 0 is a NaN in that column of grad_x.
  * nacho_xent_grad: from the lse of an earlier nacho_xent on the same operands
  *   g_iv      = weight[i] (exp(z_iv - lse[i]) - [v = label[i]]), rounded to the type for
  *               the products (of f16 after multiplication by a power of two, which the

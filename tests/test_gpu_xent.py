@@ -292,6 +292,55 @@ def test_not_a_number_and_infinities():
     assert bool(gx[bad].isnan().all()) and not bool(gx[~bad].isnan().any()) and bool(gh.isnan().all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [5, 16, 50, 300])
+@pytest.mark.parametrize("inner", [32, 33])
+def test_infinite_weights(inner, rows, dtype):
+    """A word whose logits are -inf has probability 0: the others are as without it.  Logits of +inf, or of -inf alone, leave no distribution."""
+    word, column, vocabulary = 7, 4, 200
+    d = problem(14, rows, vocabulary, inner, dtype)
+    d["x"] = d["x"].abs() + 0.125
+    d["label"][d["label"] == word] = 8
+    others = torch.arange(vocabulary, device="cuda") != word
+    without = {**d, "head": d["head"][others], "label": d["label"] - (d["label"] > word).long()}
+    want = definition(without, dtype)
+    d["head"][word, column] = -float("inf")
+    loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+    gx, gh = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, weight=d["weight"])
+    close(loss, want["loss"], "loss")
+    close(lse, want["lse"], "lse")
+    close(gh[others], want["grad_head"], "grad_head")
+    assert bool((gh[word] == 0).all()) and bool(gx[:, column].isnan().all())
+    rest = torch.arange(inner, device="cuda") != column
+    close(gx[:, rest], tuple(t[:, rest] for t in want["grad_x"]), "grad_x")
+    d["label"][0] = word
+    again = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+    assert float(again[0][0]) == float("inf") and torch.equal(again[0][1:], loss[1:]) and torch.equal(again[1], lse)
+    for value, where in ((float("inf"), word), (float("nan"), word), (-float("inf"), slice(None))):
+        head = d["head"].clone()
+        head[where, column] = value
+        loss, lse = nb.nacho_xent(d["x"], head, d["label"], weight=d["weight"])
+        assert bool(loss.isnan().all()) and bool(lse.isnan().all())
+        gx, gh = nb.nacho_xent_grad(d["x"], head, d["label"], lse, weight=d["weight"])
+        assert bool(gx.isnan().all()) and bool(gh.isnan().all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [9, 16, 40])
+def test_values_of_one_row_stay_its_own(rows, dtype):
+    """A NaN, or infinities on both sides, in a row of x reach no other row's results; and all of grad_head."""
+    d = problem(15, rows, 300, 64, dtype)
+    clean = nb.nacho_xent(d["x"], d["head"], d["label"])
+    first = nb.nacho_xent_grad(d["x"], d["head"], d["label"], clean[1], grad_head=False)[0]
+    bad = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    bad[[3, rows - 1]] = True
+    d["x"][3, 5], d["x"][rows - 1, 0] = float("nan"), float("inf")
+    loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"])
+    gx, gh = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse)
+    assert bool(loss[bad].isnan().all()) and bool(lse[bad].isnan().all()) and bool(gx[bad].isnan().all()) and bool(gh.isnan().all())
+    assert torch.equal(loss[~bad], clean[0][~bad]) and torch.equal(lse[~bad], clean[1][~bad]) and torch.equal(gx[~bad], first[~bad])
+
+
 def test_logits_far_apart():
     """Logits of thousands: the softmax is one column."""
     d = problem(8, 20, 130, 16, torch.float32, size=2000.0)
