@@ -961,6 +961,7 @@ def nacho_experts_step(x, logits, top_k, up, down, gate=None, up_bias=None, gate
     if up.dim() != 3 or down.dim() != 3:
         raise ValueError("up, down: [experts, rows, columns] is needed")
     experts, hidden, outer = up.shape[0], up.shape[1], down.shape[1]
+    _need(1 <= top_k <= experts, "top_k: 1 to the number of experts")      # (the descriptor would keep its lowest 32 bits)
     ldl = _matrix(logits, "logits", tokens, experts, dtype, dev)
     if keep is not None:
         _vector_of(keep, "keep", tokens, torch.bool if keep.dtype is torch.bool else torch.uint8, dev)

@@ -30,6 +30,14 @@ def test_step_refuses(calls):  # noqa: F811
     assert out.shape == (3, 20) and out.dtype is torch.float32 and calls[-1] == "nacho_experts_step"
 
 
+@pytest.mark.parametrize("top_k", [0, -1, 6, 2 ** 32 + 2, -2 ** 32 + 2, 2 ** 64 + 1])
+def test_numbers_of_experts_that_there_are_not(calls, top_k):  # noqa: F811
+    """Not one of them is taken for its lowest 32 bits."""
+    with pytest.raises(ValueError):
+        nb.nacho_experts_step(**{**step_args(), "top_k": top_k})
+    assert "nacho_experts_step" not in calls
+
+
 def test_xent_refuses(calls):  # noqa: F811
     z = torch.zeros
     good = dict(x=z(4, 16), head=z(30, 16), label=z(4, dtype=torch.int64))
