@@ -786,8 +786,12 @@ class Kept8:
         self._take(codes, exponent, ldc, lde, device)
 
     def _take(self, codes, exponent, ldc, lde, device):
-        self.codes, self.exponent, self.shape, self.device = codes, exponent, codes.shape, device
+        self._codes, self._exponent, self.shape, self.device = codes, exponent, codes.shape, device
         self.c = _Kept(codes.data_ptr(), ldc, exponent.data_ptr(), lde)
+
+    # (the descriptor holds their addresses: another array would not be the one that calls read)
+    codes = property(lambda self: self._codes)
+    exponent = property(lambda self: self._exponent)
 
     @classmethod
     def empty(cls, rows, cols, device):
@@ -805,7 +809,7 @@ class Kept8:
         if device is not None:
             _need(self.device == device, f"{what}: on {self.device}, expected {device}")
         else:
-            number = self.codes.get_device()
+            number = self._codes.get_device()
             if number == _HOST or number != _current_device():
                 raise ValueError(f"{what}: on {self.device}, and not on the current GPU")
         return C.byref(self.c)

@@ -104,6 +104,14 @@ def test_rows_in_8_bits(calls):  # noqa: F811
     assert [c for c in calls if not c.endswith("_bytes")] == ["nacho_experts_keep8"] + ["nacho_experts_keep8_grad"] * 3 + ["nacho_experts_grad"]
 
 
+def test_arrays_of_kept_rows_stay_those_of_the_descriptor():
+    kept = nb.Kept8(torch.zeros((4, 40), dtype=torch.int8), torch.zeros((4, 2), dtype=torch.uint8))
+    for name in ("codes", "exponent"):
+        with pytest.raises(AttributeError):
+            setattr(kept, name, getattr(kept, name).clone())
+    assert kept.c.code == kept.codes.data_ptr() and kept.c.exponent == kept.exponent.data_ptr()
+
+
 def test_host_tensors_are_refused():
     z = torch.zeros
     kept = nb.Kept8(z((4, 40), dtype=torch.int8), z((4, 2), dtype=torch.uint8))
