@@ -467,8 +467,14 @@ int32_t nacho_distill_grad(const nacho_tensor *teacher, const void *logits, int6
  *               results are divided by: small probabilities do not vanish)
  *   grad_x    = g head, grad_head = g^T x, each NULL where it is not wanted
  * weight then is the factor of the loss times the gradient that arrives at it.  A NaN
- * in a row that counts is one in all of grad_head.  g is made a piece of the vocabulary
- * at a time, and takes 256 MiB at most (more of over 524288 rows of 16 bits).
+ * in a row that counts is one in all of grad_head.
+ * Room: the loss takes 8 bytes for every row and 128 words of the vocabulary (64 of
+ * floats, 32 where a call of floats has few tiles; of up to 16 rows, for at most 1024
+ * parts of it).  The gradients take g of a piece of the vocabulary, 256 MiB or 256 words
+ * of it (which is more of over 524288 rows of 16 bits, 262144 of floats); and, with
+ * grad_x, sums in 32 bits for every stretch of a piece, 256 MiB or rows x inner of them
+ * where that is more (inner in whole eights).  Either call keeps lists of under 40 bytes
+ * a row beside that, and the copies below.
  * Limits: vocabulary, inner < 2^24, and the products of every two of n_rows,
  * vocabulary and inner < 2^42.  Workspaces: nacho_xent_workspace_bytes,
  * nacho_xent_grad_workspace_bytes, of the layer with the arrays that it will have (384

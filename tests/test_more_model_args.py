@@ -185,6 +185,26 @@ def test_sizes_whose_products_pass_64_bits():
     assert lib.nacho_xent_grad(C.byref(xent(n_rows=most, ldx=far)), E, B, 64, None, 0, E + (1 << 45), 1 << 62, None) == BAD
 
 
+@pytest.mark.parametrize("inner", [8, 96, 1024, 5000, 16_384])
+@pytest.mark.parametrize("rows", [1, 16, 17, 300, 511, 4096, 32_767, 32_768, 300_000, 1_100_000])
+@pytest.mark.parametrize("vocabulary", [1, 1000, 32_768, 100_003, 1_000_000])
+@pytest.mark.parametrize("dtype", [nb.F32, nb.BF16])
+def test_workspaces_are_what_the_header_says(rows, vocabulary, inner, dtype):
+    lib = nb.lib()
+    elem, whole = (4 if dtype == nb.F32 else 2), -(-vocabulary // 8) * 8
+    at = xent(n_rows=rows, vocabulary=vocabulary, inner=inner, ldx=inner, ldh=inner, dtype=dtype)
+    rc, loss = size(lib.nacho_xent_workspace_bytes, C.byref(at))
+    narrowest = 128 if elem == 2 else 64 if -(-rows // 16) * -(-vocabulary // 32) > 1024 else 32
+    parts = -(-vocabulary // narrowest)
+    if rows <= 16:
+        parts = max(parts, min(1024, -(-vocabulary // (64 if vocabulary < 24_576 else 128))))      # (four wavefronts of 16 or 32 words)
+    lists = 40 * rows + (1 << 15)
+    assert rc == 0 and 8 * rows * parts <= loss <= 8 * rows * parts + lists
+    rc, grad = size(lib.nacho_xent_grad_workspace_bytes, C.byref(at))
+    g = min(rows * whole * elem, max(256 << 20, rows * 256 * elem))
+    assert rc == 0 and grad <= g + max(256 << 20, rows * inner * 4) + lists
+
+
 @pytest.mark.parametrize("rows", [1, 64, 65, 3000, 100_000])
 @pytest.mark.parametrize("vocabulary", [1, 255, 256, 32_767, 32_768, 200_001])
 @pytest.mark.parametrize("dtype", [nb.F32, nb.BF16])
