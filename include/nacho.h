@@ -607,7 +607,9 @@ int32_t nacho_experts_grad(const nacho_experts_layer *layer, const void *grad_y,
  *   residual [n_tokens x outer], or NULL; out may be residual itself (same leading
  *            dimension)
  * All of one type; sums, gates and the weighted sum are held in 32 bits, out is rounded
- * once.  Weights of experts that no token chose are not read.
+ * once.  Weights of experts that no token chose are not read.  (Arrays of 16 bits should
+ * start at multiples of 4 bytes: where x, up, gate or down starts at an odd element, all
+ * of them are read element by element, two to five times as slowly.)
  * Limits: n_tokens <= 64, n_experts <= 1024, top_k <= min(32, n_experts); inner, hidden,
  * outer < 2^24.  Workspace: nacho_experts_step_workspace_bytes.
  */

@@ -2,7 +2,8 @@
 // their step, and what is written of them for the way back is half of the rows in 16 bits.
 //
 // Bound by the matrix units as the product is without it: 16384 bf16 slots of 32 experts, 1024 x 4096, 257 us a call; with the rows in 16
-// bits 246, with none of them 235.
+// bits 246, with none of them 235.  Floats: 16384 slots of 32 experts, 1024 x 4096, 1326 us, rows kept as floats 1323, not kept 1316; 3000 of 7,
+// 499 x 777, 46, 46 and 44.
 #include "activation.hpp"
 #include "kept.hpp"
 #include "products.hpp"

@@ -205,8 +205,8 @@ XentPlan xent_plan(int elem, int64_t rows, int64_t vocabulary, int64_t inner, bo
 constexpr int64_t kPaddedFrom = 384;   // rows
 bool xent_pads(const XentArgs &a);
 hipError_t launch_xent(int dtype, const XentArgs &a, const XentPlan &plan, hipStream_t s);
-// The logits of up to kFewRows rows of words of 16 bytes (words `first` .. of the vocabulary): statistics by workgroup in a.partial, or,
-// where there is a.g, g.
+// The logits of up to kFewRows rows (words `first` .. of the vocabulary), which are rows of words of 16 bytes, in_words, or rows of four floats or
+// more that start anywhere: statistics by workgroup in a.partial, or, where there is a.g, g.
 constexpr int kFewRows = 16;
 int64_t xent_few_groups(int64_t vocabulary);
 hipError_t launch_xent_few(int dtype, const XentArgs &a, int64_t first, int64_t words, int64_t ldg, bool in_words, hipStream_t s);

@@ -11,8 +11,12 @@
 //
 // Rows that do not count (no label in the vocabulary, weight 0) are left out before the first product: it reads the others by a list.
 //
-// Bound by the matrix units: 4096 x 65536 x 2048 bf16, loss and gradients, 3.9 ms for 4 products of 1.1 TFLOP (1120 TFLOP/s; the loss 915 us
-// a kernel, 1200; the pieces' g 2 x 491, grad_x 2 x 479, grad_W 2 x 561, what joins them 60).  Few rows by the weights: xent_few.hip.
+// g is rounded to the type because the matrix units take it: gradients in bf16 are off by 2.4e-3 (a result's own rounding is 1.7e-3), in f16 by
+// 3.0e-4 (2.1e-4).  Second products for what the rounding leaves would take as long as grad_x and grad_W, 2 ms more than the 3.9 below.
+//
+// Bound by the matrix units: 4096 x 65536 x 2048 bf16, loss and gradients, 3.93 ms a pass for 4 products of 1.1 TFLOP, 1120 TFLOP/s.  (Kernels
+// alone, the least and the median of nine: the loss 909 and 937 us, 1210 TFLOP/s; the pieces' g 2 x 479 and 2 x 496, grad_x 2 x 436 and 2 x 460,
+// grad_W 2 x 543 and 2 x 570; what lists and joins them 74 and 77.)  Few rows by the weights: xent_few.hip.
 #include "xent.hpp"
 
 namespace nacho {

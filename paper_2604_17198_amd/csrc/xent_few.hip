@@ -1,7 +1,7 @@
 // The logits of a few rows against a large vocabulary (see xent.hip): the vocabulary's weights are what is read, once, and the time is
 // that of reading them.  A wavefront takes 16 or 32 words of the vocabulary at a time from memory right into the registers that the
 // matrix units read, and the rows of x the same way from the caches; for the loss it keeps the largest logit of each row and the sum of
-// exponentials under it over all words that it has.  3 rows against 131072 x 2048 bf16: 88 us, 6.1 TB/s (by tiles 119 us).
+// exponentials under it over all words that it has.  3 rows against 131072 x 2048 bf16: 88 us a kernel, 6.1 TB/s (by tiles 119 us).
 #include "xent.hpp"
 
 namespace nacho {
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kThreads) xent_few_kernel(XentArgs a, int firs
                 for (int i = 0; i < kTiles; ++i) acc[i] = matrix_step<T>(of.p[i][b], of.q[b], acc[i]);
         };
         // every wavefront starts somewhere else along k: rows are often a power of two apart, and so would be what is read at a time
-        // (3 rows against 131072 x 2048: 153 us a call without, 136 with)
+        // (3 rows against 131072 x 2048 bf16: 120 us a call without, 95 with; against 131072 x 2000 103 and 103)
         const int turn = tile % stretches;
         auto at = [&](int s) {
             const int t = (s < stretches ? s : stretches - 1) + turn;      // (behind the last stretch it is loaded again: no branch around a load)
