@@ -262,6 +262,24 @@ def test_more_than_2_31_weights():
     assert bool(((got.cpu().double() - want).abs() <= room).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sizes", [(1, 1, 1, 1, 1, 1), (1, 64, 8, 256, 64, 128), (5, 1024, 32, 16, 24, 20), (9, 65, 5, 1025, 257, 129), (64, 6, 6, 72, 130, 33), (64, 128, 8, 40, 256, 24)])
+def test_workspaces_are_enough(sizes, dtype):
+    """A call with a workspace of the bytes that were asked for writes nothing behind it, and gives what one with its own gives."""
+    tokens, experts, top_k, inner, hidden, outer = sizes
+    d = problem(sum(sizes), tokens, experts, inner, hidden, outer, dtype, bias=True, residual=True)
+    asked = []
+    rooms = nb._room_for
+    try:
+        nb._room_for = lambda call, c, ws, device: asked.append(rooms(call, c, None, device)[1]) or rooms(call, c, ws, device)
+        want = run(d, top_k, "silu", True)
+    finally:
+        nb._room_for = rooms
+    room = torch.full((asked[0] + (1 << 16),), 0x5a, dtype=torch.uint8, device="cuda")
+    got = run(d, top_k, "silu", True, ws=room[:asked[0]])
+    assert torch.equal(got, want) and bool((room[asked[0]:] == 0x5a).all())
+
+
 def test_no_token():
     d = problem(9, 1, 6, 64, 48, 72, torch.float32)
     g = on_gpu(d)

@@ -379,6 +379,53 @@ def test_gradients_against_differences():
         assert abs(slope - float((grad.double() * u.double()).sum())) <= third * step ** 2 / 6 + 2 * room / step
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sizes", [(1, 1, 1), (16, 32_768, 1025), (16, 32_769, 1025), (16, 24_575, 64), (17, 16_384, 40), (64, 8192, 12), (64, 8193, 12), (100, 5000, 7),
+                                   (600, 4097, 333), (2100, 8200, 72), (8200, 20_003, 40), (33_000, 70, 16)])
+def test_workspaces_are_enough(sizes, dtype):
+    """Calls with workspaces of the bytes that were asked for write nothing behind them, and give what those with their own give."""
+    d = problem(16, *sizes, dtype, masked=0.1)
+    c = nb._xent_layer(d["x"], d["head"], d["label"], d["weight"])
+    rooms = []
+    for name in ("nacho_xent_workspace_bytes", "nacho_xent_grad_workspace_bytes"):
+        need = nb.C.c_size_t(0)
+        assert getattr(nb.lib(), name)(nb.C.byref(c), nb.C.byref(need)) == 0
+        rooms.append(torch.full((need.value + (1 << 20),), 0x5a, dtype=torch.uint8, device="cuda"))
+    first, second = (room[:-(1 << 20)] for room in rooms)
+    loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"], ws=first)
+    gx, gh = nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, weight=d["weight"], ws=second)
+    assert all(bool((room[-(1 << 20):] == 0x5a).all()) for room in rooms)
+    own = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+    own += nb.nacho_xent_grad(d["x"], d["head"], d["label"], own[1], weight=d["weight"])
+    assert all(torch.equal(a, b) for a, b in zip((loss, lse, gx, gh), own))
+    want = definition(d, dtype)
+    close(loss, want["loss"], "loss")
+    close(lse, want["lse"], "lse")
+
+
+def test_lists_of_many_rows_under_a_captured_graph():
+    d = problem(17, 40_000, 20, 16, torch.float16, masked=0.2)
+
+    def work():
+        loss, lse = nb.nacho_xent(d["x"], d["head"], d["label"], weight=d["weight"])
+        return [loss, lse, *nb.nacho_xent_grad(d["x"], d["head"], d["label"], lse, weight=d["weight"])]
+
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        result = work()
+    for seed in range(4):
+        torch.manual_seed(seed)
+        d["x"].normal_()
+        d["label"].random_(-10, 25)
+        d["weight"].uniform_(0.0, 1.0 + seed)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(result, work()))
+        torch.cuda.synchronize()
+
+
 def test_on_another_stream_and_under_captured_graphs():
     d = problem(11, 400, 3000, 64, torch.bfloat16, masked=0.2)
 
